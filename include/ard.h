@@ -467,6 +467,94 @@ double ard_skew_normal_pdf(double y, double mu, double sigma, double lambda);
 int32_t ard_prune_schedule(int32_t n_epochs, double total, double mean, double var, double lambda,
                            double p_max, double* p_out);
 
+/* ---- layer norm ------------------------------------------------------------ */
+
+/*
+ * Over the D elements of each of R rows: mu = mean(x), r = 1/sqrt(mean((x - mu)^2) + eps),
+ *   Y = (X - mu) r gamma + beta.
+ * dtype: of X, Y, dY, dX.  wdtype: of gamma, beta, dgamma, dbeta; ARD_F32, or dtype.  gamma (= 1) and beta (= 0) may be
+ * NULL.  Rows start at any element, ld* elements apart (at least D).  mean[R] and rstd[R] (fp32) are written by the forward
+ * and read by the backward pass.  Statistics, products and sums are fp32, results are rounded once.
+ * flags: ARD_OUT_COMPACT: the rows written (Y; dX) are compact activations, pad8(D) stored elements, zeros behind D
+ * (then ldy / lddx >= pad8(D)); elements behind D of the rows read are not looked at.
+ * Backward: with q = dY gamma, dX = r (q - mean(q) - xh mean(q xh)), xh = (X - mu) r; dgamma[D] = sum of dY xh and dbeta[D] =
+ * sum of dY over the rows, added in a fixed order; either may be NULL, and with both NULL no workspace is needed.
+ */
+size_t ard_layer_norm_workspace_bytes(int32_t R, int32_t D);
+int32_t ard_layer_norm_fwd(int32_t dtype, int32_t wdtype, int32_t R, int32_t D, const void* X, int64_t ldx,
+                           const void* gamma, const void* beta, float eps, void* Y, int64_t ldy, float* mean, float* rstd,
+                           int32_t flags, void* stream);
+int32_t ard_layer_norm_bwd(int32_t dtype, int32_t wdtype, int32_t R, int32_t D, const void* dY, int64_t lddy, const void* X,
+                           int64_t ldx, const void* gamma, const float* mean, const float* rstd, void* dX, int64_t lddx,
+                           void* dgamma, void* dbeta, int32_t flags, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- gated linear recurrence ------------------------------------------------- */
+
+/*
+ * The cell of an LSTM without its recurrent products, for H channels of B sequences over T steps (sg = the logistic function):
+ *   c_t = sg(f_t) c_{t-1} + (1 - sg(f_t)) v_t,   h_t = sg(o_t) c_t        (o = NULL: h_t = c_t)
+ * f, v, o[t, b, channel] are the preactivations that products left: element (t, b, k) is at t*z_t + b*z_b + k elements, so
+ * the parts of one product's rows, separate tensors and either order of time and batch all serve.  h likewise with h_t, h_b.
+ * c0[B x H] (fp32, NULL: zeros) is the state before the first step, cT[B x H] (fp32, may be NULL) the state after the last;
+ * for T = 1 cT may be c0.  d_lengths[B] (device, may be NULL: all T): sequence b has that many steps (clamped to 0..T);
+ * behind them h is +0.0, the state stands, and what f, v, o hold there has no part in anything.
+ * ckpt (fp32, may be NULL) receives the states before every ard_glr_chunk()-th step, [ceil(T / chunk) x B x H], which the
+ * backward pass needs.  States are fp32 throughout.
+ * flags: 0, or ARD_IN_COMPACT | ARD_OUT_COMPACT: the H channels are the kept units of a compact activation; f, v, o, h, dh and
+ * the gradients have pad8(H) stored channels, zeros behind H (states are [B x H] all the same).
+ * Backward: dh (strides dh_t, dh_b) and dcT (fp32 [B x H], NULL: zeros) are the gradients of h and cT; df, dv, dout (strides
+ * dz_t, dz_b; dout NULL where o is) those of f, v, o, every element written, +0.0 behind a sequence's end; dc0 (fp32
+ * [B x H], may be NULL) that of c0.
+ * The workspace holds what workgroups that share a sequence tell each other; 0 bytes where none do.
+ */
+/* steps between the states of ckpt */
+#define ARD_GLR_CHUNK 16
+int32_t ard_glr_chunk(void);
+size_t ard_glr_workspace_bytes(int32_t dtype, int32_t T, int32_t B, int32_t H);
+int32_t ard_glr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t H, const void* f, const void* v, const void* o, int64_t z_t,
+                    int64_t z_b, const float* c0, const int32_t* d_lengths, void* h, int64_t h_t, int64_t h_b, float* cT,
+                    float* ckpt, int32_t flags, void* ws, size_t ws_bytes, void* stream);
+int32_t ard_glr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t H, const void* f, const void* v, const void* o, int64_t z_t,
+                    int64_t z_b, const int32_t* d_lengths, const float* ckpt, const void* dh, int64_t dh_t, int64_t dh_b,
+                    const float* dcT, void* df, void* dv, void* dout, int64_t dz_t, int64_t dz_b, float* dc0, int32_t flags,
+                    void* ws, size_t ws_bytes, void* stream);
+
+/* ---- AdamW over many tensors --------------------------------------------------- */
+
+/*
+ * One tensor of a step: n elements (0: skipped) of the fp32 parameter p, its gradient g (gdtype), its states m and v, and, if
+ * not NULL, a bf16 copy w of the parameter that the step writes beside it (what products in bf16 read).
+ * bits = 32: m, v are fp32 and m_scale, v_scale NULL.  bits = 8: blocks of ARD_ADAMW_BLOCK neighbouring elements share a scale,
+ * m_scale[nb] and v_scale[nb] (fp32, nb = ceil(n / block)), the largest magnitude of the block's m and the largest v:
+ *   m = int8 codes,  value (c/127) |c/127| m_scale;   v = uint8 codes, value (c/255)^4 v_scale,
+ * even steps in sqrt(|m|) and in the fourth root of v: as fine as 1.6 % at the block's largest and with a range of 1 : 2e-5 in both m
+ * and sqrt(v).  Codes are the nearest, and a v above zero never becomes zero.  (A scale below 2^-126 makes a block of zeros; a
+ * NaN or an infinity makes its whole block stand for NaN.)  All zeros is the state before the first step.
+ */
+#define ARD_ADAMW_BLOCK 256
+typedef struct {
+  int64_t n;
+  float* p;
+  const void* g;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  void* w;
+} ard_adamw_tensor;
+
+/*
+ * AdamW for `count` tensors (a host array, read before the call returns), step = 1, 2, ...:
+ *   g' = *d_grad_scale g (NULL: g),  m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,
+ *   p = (1 - lr wd) p - lr / (1 - b1^step) m / (sqrt(v) / sqrt(1 - b2^step) + eps),
+ * with the new m and v before they are stored.  d_grad_scale (device) is one float for all: a clipping or loss scale that the
+ * host need not know; where it is NaN or infinite the whole step is skipped and nothing is written.
+ * The states' arithmetic is the above in fp32, each operation rounded, so 8-bit codes are the same on every call and machine.
+ */
+int32_t ard_adamw_step(int32_t bits, int32_t gdtype, int32_t count, const ard_adamw_tensor* tensors, double lr, double beta1,
+                       double beta2, double eps, double weight_decay, int64_t step, const float* d_grad_scale, void* stream);
+/* The values that 8-bit states stand for (to store or look at them): m_out[i][n], v_out[i][n] (fp32) of every tensor; of the
+ * tensors' fields n, m, v, m_scale and v_scale are used. */
+int32_t ard_adamw_values(int32_t count, const ard_adamw_tensor* tensors, float* const* m_out, float* const* v_out, void* stream);
+
 /* ---- sizes of compact buffers and grids (host only, nothing is launched) --- */
 
 /* Number of kept units of a ROW / LIST / NONE pattern over `units` units: ceil((units - (b-1)) / dp)

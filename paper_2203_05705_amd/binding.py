@@ -47,10 +47,11 @@ except ImportError as e:   # not built: the names below are looked up in __getat
 
 if _ardcall is not None:
     _ardcall.configure(LIB_PATH, ArdError, torch._C._cuda_getCurrentRawStream)
-    from ._ardcall import (batch, compact_weight, conv_bwd_blocks, conv_bwd_data, conv_bwd_rows, conv_bwd_weight,  # noqa: F401
-                           conv_fwd, conv_fwd_blocks, conv_fwd_rows, conv_select, drop_gemm_bwd_data,
-                           drop_gemm_bwd_weight, drop_gemm_bwd_weight_static, drop_gemm_fwd, lstm_bwd, lstm_fwd,
-                           sens_block_pattern, sens_predict, sens_row_pattern)
+    from ._ardcall import (adamw_step, adamw_values, batch, compact_weight, conv_bwd_blocks, conv_bwd_data,  # noqa: F401
+                           conv_bwd_rows, conv_bwd_weight, conv_fwd, conv_fwd_blocks, conv_fwd_rows, conv_select,
+                           drop_gemm_bwd_data, drop_gemm_bwd_weight, drop_gemm_bwd_weight_static, drop_gemm_fwd, glr_bwd,
+                           glr_fwd, layer_norm_bwd, layer_norm_fwd, lstm_bwd, lstm_fwd, sens_block_pattern, sens_predict,
+                           sens_row_pattern)
 
     class Pattern(_ardcall.PatternBase):
         """Host description of a dropout pattern (keeps the tensors it points to alive):
@@ -129,6 +130,19 @@ _SIGS = {
     "ard_compact_dim": (C.c_int32, [C.c_void_p, C.c_int32]),
     "ard_tile_grid": (C.c_int32, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]),
     "ard_conv_out_size": (C.c_int32, [C.c_int32] * 4),
+    "ard_layer_norm_workspace_bytes": (C.c_size_t, [C.c_int32] * 2),
+    "ard_layer_norm_fwd": (C.c_int32, [C.c_int32] * 4 + [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int64]
+                           + [C.c_void_p] * 2 + [C.c_int32, C.c_void_p]),
+    "ard_layer_norm_bwd": (C.c_int32, [C.c_int32] * 4 + [C.c_void_p, C.c_int64] * 2 + [C.c_void_p] * 4 + [C.c_int64] + [C.c_void_p] * 2
+                           + [C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "ard_glr_chunk": (C.c_int32, []),
+    "ard_glr_workspace_bytes": (C.c_size_t, [C.c_int32] * 4),
+    "ard_glr_fwd": (C.c_int32, [C.c_int32] * 4 + [C.c_void_p] * 3 + [C.c_int64] * 2 + [C.c_void_p] * 3 + [C.c_int64] * 2 + [C.c_void_p] * 2
+                    + [C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "ard_glr_bwd": (C.c_int32, [C.c_int32] * 4 + [C.c_void_p] * 3 + [C.c_int64] * 2 + [C.c_void_p] * 3 + [C.c_int64] * 2 + [C.c_void_p] * 4
+                    + [C.c_int64] * 2 + [C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "ard_adamw_step": (C.c_int32, [C.c_int32] * 3 + [C.c_void_p] + [C.c_double] * 5 + [C.c_int64] + [C.c_void_p] * 2),
+    "ard_adamw_values": (C.c_int32, [C.c_int32] + [C.c_void_p] * 4),
     "ard_debug_set_dry_run": (None, [C.c_int32]),
     "ard_debug_dry_launches": (C.c_int32, [C.c_char_p, C.c_size_t]),
     "ard_debug_dry_instances": (C.c_int32, [C.c_char_p, C.c_size_t]),
@@ -326,6 +340,38 @@ def lstm_status_offset(dtype_code, T, B, I, H, pat=None):
     _, r = _pref(pat)
     off = int(lib().ard_lstm_status_offset(dtype_code, T, B, I, H, r))
     return None if off == (1 << 64) - 1 else off
+
+
+# ---- layer norm, gated linear recurrence, AdamW ---------------------------------------------
+
+ADAMW_BLOCK = 256   # neighbouring elements that share the scales of an 8-bit state
+GLR_CHUNK = 16      # steps between the states that glr_fwd keeps for glr_bwd
+
+
+class CAdamWTensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("w", C.c_void_p)]
+
+
+def adamw_state(params, bits: int = 32):
+    """The states of adamw_step before its first step, as its arguments m, v, m_scale, v_scale: lists of zeros beside
+    `params` (fp32; with bits=8 int8 and uint8 codes and the scales of blocks of ADAMW_BLOCK elements)."""
+    if bits not in (8, 32):
+        raise ValueError(f"states have 32 or 8 bits (got {bits})")
+
+    def zeros(dtype, per=1):
+        return [torch.zeros(p.shape if per == 1 else -(-p.numel() // per), dtype=dtype, device=p.device) for p in params]
+    if bits == 32:
+        return dict(m=zeros(torch.float32), v=zeros(torch.float32), m_scale=None, v_scale=None)
+    return dict(m=zeros(torch.int8), v=zeros(torch.uint8), m_scale=zeros(torch.float32, ADAMW_BLOCK), v_scale=zeros(torch.float32, ADAMW_BLOCK))
+
+
+def layer_norm_workspace_bytes(R: int, D: int) -> int:
+    return int(lib().ard_layer_norm_workspace_bytes(R, D))
+
+
+def glr_workspace_bytes(dtype_code: int, T: int, B: int, H: int) -> int:
+    return int(lib().ard_glr_workspace_bytes(dtype_code, T, B, H))
 
 
 # ---- convolution with dropped input feature maps ---------------------------------------------

@@ -1,0 +1,572 @@
+// Gated linear recurrence: the cell of an LSTM without its recurrent products, so that time can be cut.
+//
+//   F = sigma(f), c_t = F_t c_{t-1} + (1 - F_t) v_t, h_t = sigma(o_t) c_t          (without o: h = c)
+//   dc_t = sigma(o_t) dh_t + e_t, e_{t-1} = F_t dc_t, e_T = dcT
+//   dv = dc (1 - F), df = dc (c_{t-1} - v) F (1 - F), do = dh c sigma(o) (1 - sigma(o)), dc0 = e_0
+//
+// Each step is affine in the state, so a stretch of steps is a pair (P, S): it takes c to P c + S, and stretches
+// compose.  A wavefront takes 16 steps of 64 lanes' channels into registers, makes their pair there, and the wavefronts
+// of a workgroup, which have neighbouring stretches, exchange pairs through LDS: every input is read once and every
+// output written once, which is what bounds these passes.  Where batch and channels alone give too few wavefronts, time
+// is cut into segments for several workgroups; a first pass then makes the segments' pairs (reading f and v, or f, o and
+// dh, once more).  States, pairs and gradients in flight are fp32.  The backward pass starts from the states that the
+// forward pass left before every 16th step, so it needs no second scan for them.
+#include <type_traits>
+
+#include "rows.hpp"
+
+namespace ard {
+
+constexpr int kSteps = ARD_GLR_CHUNK;  // steps of a wavefront's stretch
+constexpr int kMaxWaves = 8;           // stretches a workgroup has at a time
+
+struct Strides {
+  int64_t t, b;
+};
+struct GlrArgs {
+  int T, B, H;      // H: channels that take part
+  int wide;         // channels stored in f, v, o, h and their gradients: H, or pad8(H), zeros behind H
+  int groups;       // workgroups along the channels
+  int seg_steps;    // steps of a segment
+  int segs;
+  const int32_t* len;
+};
+
+// F = sigma(x), I = 1 - F without cancellation: for x >= 0 as exp(-x) F, where 1 - F would lose the digits of a long memory.
+__device__ __forceinline__ void gate_pair(float x, float& F, float& I) {
+  const float e = __builtin_amdgcn_exp2f(x * -1.44269504088896341f);
+  F = __builtin_amdgcn_rcpf(1.0f + e);
+  I = x >= 0.0f ? e * F : 1.0f - F;
+}
+__device__ __forceinline__ float gate(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.44269504088896341f)); }
+
+// what a workgroup works on
+struct GlrPlace {
+  int seg, b;
+  int ch;        // the lane's first channel; lanes behind the last channel read those of the last lane and write nothing
+  bool on;
+  int n;         // of the lane's channels, those that states are kept of (H may end inside a lane's pair)
+  int t0, t1;    // its steps
+  int live;      // steps before the sequence's end, up to T
+};
+template <int VEC> __device__ __forceinline__ GlrPlace glr_place(const GlrArgs& a) {
+  GlrPlace p;
+  int i = blockIdx.x;
+  const int g = i % a.groups;
+  i /= a.groups;
+  p.b = i % a.B, p.seg = i / a.B;
+  const int ch = (g * 64 + (threadIdx.x & 63)) * VEC;
+  p.on = ch < a.wide;
+  p.ch = p.on ? ch : a.wide - VEC;
+  p.n = p.on ? a.H - ch : 0;
+  p.t0 = p.seg * a.seg_steps, p.t1 = imin(a.T - p.t0, a.seg_steps) + p.t0;
+  p.live = a.len ? imin(imax(a.len[p.b], 0), a.T) : a.T;
+  return p;
+}
+
+// pairs of the wavefronts' stretches of a turn, in LDS
+template <int VEC> struct Pairs {
+  float v[2][kMaxWaves][2][VEC][64];  // [turn's parity][stretch][P, S]
+};
+
+// The pairs of `count` stretches (or segments) before this one, applied to c in order.
+template <int VEC> __device__ __forceinline__ void apply(const Pairs<VEC>& s, int turn, int w, float (&c)[VEC]) {
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) c[j] = fmaf(s.v[turn][w][0][j][threadIdx.x & 63], c[j], s.v[turn][w][1][j][threadIdx.x & 63]);
+}
+template <int VEC> __device__ __forceinline__ void leave(Pairs<VEC>& s, int turn, int w, const float (&P)[VEC], const float (&S)[VEC]) {
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) s.v[turn][w][0][j][threadIdx.x & 63] = P[j], s.v[turn][w][1][j][threadIdx.x & 63] = S[j];
+}
+
+// Segment pairs in the workspace: [segment][P, S][B][H].  Composes those of segments [from, from + step * count) in
+// order, dealt to the workgroup's wavefronts in neighbouring shares, and applies them to c (uses parity 0 of the pairs).
+template <int VEC>
+__device__ __forceinline__ void apply_segments(const GlrArgs& a, const GlrPlace& p, const float* seg_pairs, int from, int step, int count,
+                                               Pairs<VEC>& lds, float (&c)[VEC]) {
+  const int waves = blockDim.x >> 6, w = threadIdx.x >> 6;
+  const int lo = (int)((int64_t)count * w / waves), hi = (int)((int64_t)count * (w + 1) / waves);
+  const int64_t plane = (int64_t)a.B * a.H;
+  float P[VEC], S[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
+  for (int i = lo; i < hi; ++i) {
+    const float* at = seg_pairs + (int64_t)(from + step * i) * 2 * plane + (int64_t)p.b * a.H + p.ch;
+    float q[VEC], r[VEC];
+    load_some<VEC>(at, p.n, q);
+    load_some<VEC>(at + plane, p.n, r);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) P[j] *= q[j], S[j] = fmaf(q[j], S[j], r[j]);
+  }
+  leave<VEC>(lds, 0, w, P, S);
+  __syncthreads();
+  for (int k = 0; k < waves; ++k) apply<VEC>(lds, 0, k, c);
+  __syncthreads();
+}
+
+// ---- forward ------------------------------------------------------------------
+// F and (1 - F) v of a stretch's steps, and its pair.  WHOLE: all of its steps are live; else the first `steps` are, and
+// the others leave the state as it is.
+template <bool WHOLE, typename T, int VEC>
+__device__ __forceinline__ void stretch_fwd(const T* f, const T* v, int64_t st, int steps, float (&F)[kSteps][VEC], float (&b)[kSteps][VEC],
+                                            float (&P)[VEC], float (&S)[VEC]) {
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i)
+    if (WHOLE || i < steps) load_run<VEC>(f + i * st, F[i]), load_run<VEC>(v + i * st, b[i]);
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i)
+    if (WHOLE || i < steps) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        float I;
+        gate_pair(F[i][j], F[i][j], I);
+        b[i][j] *= I;
+        P[j] *= F[i][j];
+        S[j] = fmaf(F[i][j], S[j], b[i][j]);
+      }
+    }
+}
+
+template <typename T, int VEC>
+__global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_pairs_kernel(GlrArgs a, const T* f, const T* v, Strides z, float* seg_pairs) {
+  __shared__ Pairs<VEC> lds;
+  const GlrPlace p = glr_place<VEC>(a);
+  const int waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  float tp[VEC], ts[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) tp[j] = 1.0f, ts[j] = 0.0f;
+  int turn = 0;
+  for (int t = p.t0; t < p.t1; t += waves * kSteps, turn ^= 1) {
+    const int tw = t + w * kSteps, steps = imin(p.t1, p.live) - tw;
+    float F[kSteps][VEC], b[kSteps][VEC], P[VEC], S[VEC];
+    const int64_t at = tw * z.t + p.b * z.b + p.ch;
+    if (steps >= kSteps) stretch_fwd<true, T, VEC>(f + at, v + at, z.t, steps, F, b, P, S);
+    else stretch_fwd<false, T, VEC>(f + at, v + at, z.t, steps, F, b, P, S);
+    leave<VEC>(lds, turn, w, P, S);
+    __syncthreads();
+    for (int k = 0; k < waves; ++k) {
+      apply<VEC>(lds, turn, k, ts);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) tp[j] *= lds.v[turn][k][0][j][threadIdx.x & 63];
+    }
+  }
+  if (w == 0) {
+    float* out = seg_pairs + ((int64_t)p.seg * 2 * a.B + p.b) * a.H + p.ch;
+    store_some<VEC>(out, p.n, tp);
+    store_some<VEC>(out + (int64_t)a.B * a.H, p.n, ts);
+  }
+}
+
+// results of a stretch whose state before it is s; steps from `steps` to `stored` lie behind the sequence's end
+template <bool WHOLE, typename T, int VEC, bool GATE>
+__device__ __forceinline__ void stretch_out(T* h, int64_t st, bool on, int steps, int stored, const float (&F)[kSteps][VEC], const float (&b)[kSteps][VEC],
+                                            const float (&g)[kSteps][VEC], float (&s)[VEC]) {
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    if (!WHOLE && i >= stored) break;
+    float y[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) y[j] = 0.0f;
+    if (WHOLE || i < steps) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        s[j] = fmaf(F[i][j], s[j], b[i][j]);
+        y[j] = GATE ? gate(g[i][j]) * s[j] : s[j];
+      }
+    }
+    if (on) store_run<VEC>(h + i * st, y);
+  }
+}
+
+template <typename T, int VEC, bool GATE>
+__global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_kernel(GlrArgs a, const T* f, const T* v, const T* o, Strides z, const float* c0, T* h,
+                                                                 Strides hs, float* cT, float* ckpt, const float* seg_pairs) {
+  __shared__ Pairs<VEC> lds;
+  const GlrPlace p = glr_place<VEC>(a);
+  const int waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t plane = (int64_t)a.B * a.H, state = (int64_t)p.b * a.H + p.ch;
+  float c[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) c[j] = 0.0f;
+  if (c0) load_some<VEC>(c0 + state, p.n, c);
+  if (p.seg) apply_segments<VEC>(a, p, seg_pairs, 0, 1, p.seg, lds, c);
+  int turn = 0;
+  for (int t = p.t0; t < p.t1; t += waves * kSteps, turn ^= 1) {
+    const int tw = t + w * kSteps, steps = imin(p.t1, p.live) - tw;
+    float F[kSteps][VEC], b[kSteps][VEC], g[kSteps][VEC], P[VEC], S[VEC], s[VEC];
+    const int64_t at = tw * z.t + p.b * z.b + p.ch;
+    if (GATE) {
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i)
+        if (i < steps) load_run<VEC>(o + at + i * z.t, g[i]);
+    }
+    if (steps >= kSteps) stretch_fwd<true, T, VEC>(f + at, v + at, z.t, steps, F, b, P, S);
+    else stretch_fwd<false, T, VEC>(f + at, v + at, z.t, steps, F, b, P, S);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) s[j] = c[j];
+    if (waves > 1) {
+      leave<VEC>(lds, turn, w, P, S);
+      __syncthreads();
+      for (int k = 0; k < w; ++k) apply<VEC>(lds, turn, k, s);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) c[j] = s[j];
+      for (int k = w; k < waves; ++k) apply<VEC>(lds, turn, k, c);
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) c[j] = fmaf(P[j], c[j], S[j]);
+    }
+    if (tw < p.t1) {
+      if (ckpt) store_some<VEC>(ckpt + (int64_t)(tw / kSteps) * plane + state, p.n, s);
+      T* out = h + tw * hs.t + p.b * hs.b + p.ch;
+      if (steps >= kSteps) stretch_out<true, T, VEC, GATE>(out, hs.t, p.on, steps, kSteps, F, b, g, s);
+      else stretch_out<false, T, VEC, GATE>(out, hs.t, p.on, steps, p.t1 - tw, F, b, g, s);
+    }
+  }
+  if (cT && w == 0 && p.seg == a.segs - 1) store_some<VEC>(cT + state, p.n, c);
+}
+
+// One step, as generation calls it: a lane's channels of one sequence.  cT may be c0.
+template <typename T, int VEC, bool GATE>
+__global__ __launch_bounds__(64) void glr_step_kernel(GlrArgs a, const T* f, const T* v, const T* o, Strides z, const float* c0, T* h, Strides hs,
+                                                      float* cT, float* ckpt) {
+  const GlrPlace p = glr_place<VEC>(a);
+  if (!p.on) return;
+  const int64_t at = p.b * z.b + p.ch, state = (int64_t)p.b * a.H + p.ch;
+  float c[VEC], x[VEC], u[VEC], g[VEC], y[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) c[j] = y[j] = 0.0f;
+  if (c0) load_some<VEC>(c0 + state, p.n, c);
+  if (ckpt) store_some<VEC>(ckpt + state, p.n, c);
+  if (p.live > 0) {
+    load_run<VEC>(f + at, x);
+    load_run<VEC>(v + at, u);
+    if (GATE) load_run<VEC>(o + at, g);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      float F, I;
+      gate_pair(x[j], F, I);
+      c[j] = fmaf(F, c[j], I * u[j]);
+      y[j] = GATE ? gate(g[j]) * c[j] : c[j];
+    }
+  }
+  store_run<VEC>(h + p.b * hs.b + p.ch, y);
+  if (cT) store_some<VEC>(cT + state, p.n, c);
+}
+
+// ---- backward -----------------------------------------------------------------
+// The adjoint's pair of a stretch takes e behind its last step to e behind the step before its first.
+template <bool WHOLE, typename T, int VEC, bool GATE>
+__device__ __forceinline__ void stretch_adjoint(const T* f, const T* o, const T* dh, int64_t st, int64_t dst, int steps, float (&P)[VEC], float (&S)[VEC]) {
+  float F[kSteps][VEC], q[kSteps][VEC], g[kSteps][VEC];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i)
+    if (WHOLE || i < steps) {
+      load_run<VEC>(f + i * st, F[i]);
+      load_run<VEC>(dh + i * dst, q[i]);
+      if (GATE) load_run<VEC>(o + i * st, g[i]);
+    }
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
+#pragma unroll
+  for (int i = kSteps - 1; i >= 0; --i)
+    if (WHOLE || i < steps) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float x = gate(F[i][j]);
+        S[j] = x * (S[j] + (GATE ? gate(g[i][j]) * q[i][j] : q[i][j]));
+        P[j] *= x;
+      }
+    }
+}
+
+template <typename T, int VEC, bool GATE>
+__global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_pairs_kernel(GlrArgs a, const T* f, const T* o, Strides z, const T* dh, Strides ds,
+                                                                       float* seg_pairs) {
+  __shared__ Pairs<VEC> lds;
+  const GlrPlace p = glr_place<VEC>(a);
+  const int waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  float tp[VEC], ts[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) tp[j] = 1.0f, ts[j] = 0.0f;
+  const int span = waves * kSteps, turns = (p.t1 - p.t0 + span - 1) / span;
+  int turn = 0;
+  for (int t = p.t0 + (turns - 1) * span; t >= p.t0; t -= span, turn ^= 1) {
+    const int tw = t + w * kSteps, steps = imin(p.t1, p.live) - tw;
+    const int64_t at = tw * z.t + p.b * z.b + p.ch, dat = tw * ds.t + p.b * ds.b + p.ch;
+    float P[VEC], S[VEC];
+    if (steps >= kSteps) stretch_adjoint<true, T, VEC, GATE>(f + at, o + at, dh + dat, z.t, ds.t, steps, P, S);
+    else stretch_adjoint<false, T, VEC, GATE>(f + at, o + at, dh + dat, z.t, ds.t, steps, P, S);
+    leave<VEC>(lds, turn, w, P, S);
+    __syncthreads();
+    for (int k = waves - 1; k >= 0; --k) {
+      apply<VEC>(lds, turn, k, ts);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) tp[j] *= lds.v[turn][k][0][j][threadIdx.x & 63];
+    }
+  }
+  if (w == 0) {
+    float* out = seg_pairs + ((int64_t)p.seg * 2 * a.B + p.b) * a.H + p.ch;
+    store_some<VEC>(out, p.n, tp);
+    store_some<VEC>(out + (int64_t)a.B * a.H, p.n, ts);
+  }
+}
+
+// Loads of a stretch, its states again from the one before it, and its adjoint's pair; do is stored on the way (it needs
+// no gradient from later steps).  Leaves F, I = 1 - F, u = c_{t-1} - v and q = sigma(o) dh.
+template <bool WHOLE, typename T, int VEC, bool GATE>
+__device__ __forceinline__ void stretch_back(const T* f, const T* v, const T* o, const T* dh, T* dg, int64_t st, int64_t dst, int64_t gst, bool on, int steps,
+                                             float (&c)[VEC], float (&F)[kSteps][VEC], float (&I)[kSteps][VEC], float (&u)[kSteps][VEC],
+                                             float (&q)[kSteps][VEC], float (&P)[VEC], float (&S)[VEC]) {
+  float g[kSteps][VEC];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i)
+    if (WHOLE || i < steps) {
+      load_run<VEC>(f + i * st, F[i]);
+      load_run<VEC>(v + i * st, u[i]);
+      if (GATE) load_run<VEC>(o + i * st, g[i]);
+      load_run<VEC>(dh + i * dst, q[i]);
+    }
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i)
+    if (WHOLE || i < steps) {
+      float y[VEC];
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        gate_pair(F[i][j], F[i][j], I[i][j]);
+        const float x = u[i][j];
+        u[i][j] = c[j] - x;
+        c[j] = fmaf(F[i][j], c[j], I[i][j] * x);
+        if (GATE) {
+          const float O = gate(g[i][j]);
+          q[i][j] *= O;
+          y[j] = q[i][j] * c[j] * (1.0f - O);
+        }
+      }
+      if (GATE && on) store_run<VEC>(dg + i * gst, y);
+    }
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
+#pragma unroll
+  for (int i = kSteps - 1; i >= 0; --i)
+    if (WHOLE || i < steps) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        S[j] = F[i][j] * (S[j] + q[i][j]);
+        P[j] *= F[i][j];
+      }
+    }
+}
+// df and dv of a stretch, e behind its last step in s; zeros (do's too) for its steps from `steps` to `stored`
+template <bool WHOLE, typename T, int VEC, bool GATE>
+__device__ __forceinline__ void stretch_grads(T* df, T* dv, T* dg, int64_t gst, bool on, int steps, int stored, const float (&F)[kSteps][VEC],
+                                              const float (&I)[kSteps][VEC], const float (&u)[kSteps][VEC], const float (&q)[kSteps][VEC],
+                                              float (&s)[VEC]) {
+#pragma unroll
+  for (int i = kSteps - 1; i >= 0; --i) {
+    if (!WHOLE && i >= stored) continue;
+    float x[VEC], y[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) x[j] = y[j] = 0.0f;
+    if (WHOLE || i < steps) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float dc = q[i][j] + s[j];
+        s[j] = F[i][j] * dc;
+        y[j] = dc * I[i][j];
+        x[j] = y[j] * F[i][j] * u[i][j];
+      }
+    } else if (GATE) {
+      if (on) store_run<VEC>(dg + i * gst, x);
+    }
+    if (on) store_run<VEC>(df + i * gst, x), store_run<VEC>(dv + i * gst, y);
+  }
+}
+
+template <typename T, int VEC, bool GATE>
+__global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_kernel(GlrArgs a, const T* f, const T* v, const T* o, Strides z, const float* ckpt, const T* dh,
+                                                                 Strides ds, const float* dcT, T* df, T* dv, T* dg, Strides gs, float* dc0,
+                                                                 const float* seg_pairs) {
+  __shared__ Pairs<VEC> lds;
+  const GlrPlace p = glr_place<VEC>(a);
+  const int waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t plane = (int64_t)a.B * a.H, state = (int64_t)p.b * a.H + p.ch;
+  float e[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) e[j] = 0.0f;
+  if (dcT) load_some<VEC>(dcT + state, p.n, e);
+  if (p.seg < a.segs - 1) apply_segments<VEC>(a, p, seg_pairs, a.segs - 1, -1, a.segs - 1 - p.seg, lds, e);
+  const int span = waves * kSteps, turns = (p.t1 - p.t0 + span - 1) / span;
+  int turn = 0;
+  for (int t = p.t0 + (turns - 1) * span; t >= p.t0; t -= span, turn ^= 1) {
+    const int tw = t + w * kSteps, steps = imin(p.t1, p.live) - tw;
+    float F[kSteps][VEC], I[kSteps][VEC], u[kSteps][VEC], q[kSteps][VEC], P[VEC], S[VEC], c[VEC], s[VEC];
+    const int64_t at = tw * z.t + p.b * z.b + p.ch, dat = tw * ds.t + p.b * ds.b + p.ch, gat = tw * gs.t + p.b * gs.b + p.ch;
+    if (steps > 0) load_some<VEC>(ckpt + (int64_t)(tw / kSteps) * plane + state, p.n, c);
+    if (steps >= kSteps) stretch_back<true, T, VEC, GATE>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, steps, c, F, I, u, q, P, S);
+    else stretch_back<false, T, VEC, GATE>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, steps, c, F, I, u, q, P, S);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) s[j] = e[j];
+    if (waves > 1) {
+      leave<VEC>(lds, turn, w, P, S);
+      __syncthreads();
+      for (int k = waves - 1; k > w; --k) apply<VEC>(lds, turn, k, s);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) e[j] = s[j];
+      for (int k = w; k >= 0; --k) apply<VEC>(lds, turn, k, e);
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) e[j] = fmaf(P[j], e[j], S[j]);
+    }
+    if (steps >= kSteps) stretch_grads<true, T, VEC, GATE>(df + gat, dv + gat, dg + gat, gs.t, p.on, steps, kSteps, F, I, u, q, s);
+    else stretch_grads<false, T, VEC, GATE>(df + gat, dv + gat, dg + gat, gs.t, p.on, steps, p.t1 - tw, F, I, u, q, s);
+  }
+  if (dc0 && w == 0 && p.seg == 0) store_some<VEC>(dc0 + state, p.n, e);
+}
+
+// ---- host ---------------------------------------------------------------------
+struct GlrPlan {
+  GlrArgs a;
+  int waves;
+};
+// Channels of a lane: 4 bytes of them (one fp32 or two bf16; an odd number of bf16 channels: one), a wavefront's row 256 bytes.
+static int glr_vec(int32_t dtype, int wide) { return dtype == ARD_F32 || wide % 2 ? 1 : 2; }
+static GlrPlan glr_plan(int32_t dtype, int T, int B, int H, int32_t flags, const int32_t* len) {
+  const int wide = flags ? pad8(H) : H, vec = glr_vec(dtype, wide);
+  GlrPlan g{};
+  const int pieces = T / kSteps + (T % kSteps != 0);
+  g.a.T = T, g.a.B = B, g.a.H = H, g.a.wide = wide, g.a.len = len;
+  g.a.groups = ceil_div(wide, 64 * vec);
+  g.waves = imin(pieces, kMaxWaves);
+  const int64_t have = (int64_t)g.a.groups * B * g.waves;  // wavefronts without cutting time
+  const int turns = ceil_div(pieces, g.waves);
+  int segs = 1;
+  if (have < 2048 && turns > 1) segs = imin(turns, (int)(4096 / have));
+  const int per = ceil_div(turns, segs);
+  g.a.segs = ceil_div(turns, per);
+  g.a.seg_steps = per * g.waves * kSteps;
+  return g;
+}
+static size_t glr_ws_bytes(const GlrArgs& a) { return a.segs > 1 ? (size_t)a.segs * 2 * a.B * a.H * sizeof(float) : 0; }
+
+struct GlrCall {
+  GlrPlan g;
+  const void *f, *v, *o;
+  Strides z;
+};
+
+static int32_t glr_check(int32_t dtype, int32_t T, int32_t B, int32_t H, int32_t flags) {
+  if (dtype != ARD_F32 && dtype != ARD_BF16) return fail(ARD_EDTYPE, "unknown dtype %d", dtype);
+  if (T <= 0 || B <= 0 || H <= 0) return fail(ARD_ESHAPE, "T, B and H must be positive (got %d, %d, %d)", T, B, H);
+  if (T > 1 << 30 || H > 1 << 24) return fail(ARD_ESHAPE, "T = %d or H = %d is too large", T, H);
+  if (flags != 0 && flags != (ARD_IN_COMPACT | ARD_OUT_COMPACT)) return fail(ARD_EINVAL, "flags are 0 or ARD_IN_COMPACT | ARD_OUT_COMPACT (got 0x%x)", flags);
+  return ARD_OK;
+}
+static int32_t glr_check_grid(const GlrPlan& g) {  // (HIP counts a grid's threads in 32 bits)
+  if ((int64_t)g.a.groups * g.a.B * g.a.segs * g.waves >= 1 << 26) return fail(ARD_ESHAPE, "B * H is too large (%d, %d)", g.a.B, g.a.H);
+  return ARD_OK;
+}
+
+template <typename T, int VEC, bool GATE>
+static int32_t glr_fwd_t(const GlrCall& c, const float* c0, void* h, Strides hs, float* cT, float* ckpt, float* ws, hipStream_t st) {
+  const GlrArgs& a = c.g.a;
+  const T *f = (const T*)c.f, *v = (const T*)c.v, *o = (const T*)c.o;
+  if (a.T == 1) {
+    ARD_LAUNCH((glr_step_kernel<T, VEC, GATE>), dim3(a.groups * a.B), dim3(64), 0, st, a, f, v, o, c.z, c0, (T*)h, hs, cT, ckpt);
+    ARD_LAUNCH_CHECK("glr_step_kernel");
+    return ARD_OK;
+  }
+  const dim3 block(64 * c.g.waves);
+  if (a.segs > 1) {  // (the last segment's pair is not needed)
+    ARD_LAUNCH((glr_fwd_pairs_kernel<T, VEC>), dim3(a.groups * a.B * (a.segs - 1)), block, 0, st, a, f, v, c.z, ws);
+    ARD_LAUNCH_CHECK("glr_fwd_pairs_kernel");
+  }
+  ARD_LAUNCH((glr_fwd_kernel<T, VEC, GATE>), dim3(a.groups * a.B * a.segs), block, 0, st, a, f, v, o, c.z, c0, (T*)h, hs, cT, ckpt, ws);
+  ARD_LAUNCH_CHECK("glr_fwd_kernel");
+  return ARD_OK;
+}
+
+template <typename T, int VEC, bool GATE>
+static int32_t glr_bwd_t(const GlrCall& c, const float* ckpt, const void* dh, Strides ds, const float* dcT, void* df, void* dv, void* dg, Strides gs,
+                         float* dc0, float* ws, hipStream_t st) {
+  const GlrArgs& a = c.g.a;
+  const T *f = (const T*)c.f, *v = (const T*)c.v, *o = (const T*)c.o;
+  const dim3 block(64 * c.g.waves);
+  if (a.segs > 1) {
+    ARD_LAUNCH((glr_bwd_pairs_kernel<T, VEC, GATE>), dim3(a.groups * a.B * a.segs), block, 0, st, a, f, o, c.z, (const T*)dh, ds, ws);
+    ARD_LAUNCH_CHECK("glr_bwd_pairs_kernel");
+  }
+  ARD_LAUNCH((glr_bwd_kernel<T, VEC, GATE>), dim3(a.groups * a.B * a.segs), block, 0, st, a, f, v, o, c.z, ckpt, (const T*)dh, ds, dcT, (T*)df, (T*)dv,
+             (T*)dg, gs, dc0, ws);
+  ARD_LAUNCH_CHECK("glr_bwd_kernel");
+  return ARD_OK;
+}
+
+template <class F> static int32_t glr_instance(int32_t dtype, int wide, F&& with) {
+  using One = std::integral_constant<int, 1>;
+  if (dtype == ARD_F32) return with(0.0f, One{});
+  return glr_vec(dtype, wide) == 1 ? with((uint16_t)0, One{}) : with((uint16_t)0, std::integral_constant<int, 2>{});
+}
+
+}  // namespace ard
+
+using namespace ard;
+
+extern "C" int32_t ard_glr_chunk(void) { return kSteps; }
+
+extern "C" size_t ard_glr_workspace_bytes(int32_t dtype, int32_t T, int32_t B, int32_t H) {
+  if (dtype < 0 || dtype > ARD_BF16 || T <= 0 || B <= 0 || H <= 0 || T > 1 << 30 || H > 1 << 24) return 0;
+  // (channels may be stored in H or in pad8(H) columns, dealt to different numbers of workgroups)
+  const size_t n = glr_ws_bytes(glr_plan(dtype, T, B, H, 0, nullptr).a), m = glr_ws_bytes(glr_plan(dtype, T, B, H, ARD_IN_COMPACT | ARD_OUT_COMPACT, nullptr).a);
+  return n > m ? n : m;
+}
+
+extern "C" int32_t ard_glr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t H, const void* f, const void* v, const void* o, int64_t z_t, int64_t z_b,
+                               const float* c0, const int32_t* d_lengths, void* h, int64_t h_t, int64_t h_b, float* cT, float* ckpt, int32_t flags,
+                               void* ws, size_t ws_bytes, void* stream) {
+  if (int32_t st = glr_check(dtype, T, B, H, flags)) return st;
+  if (!f || !v || !h) return fail(ARD_EINVAL, "null tensor pointer");
+  if (c0 && cT == c0 && T > 1) return fail(ARD_EINVAL, "cT may take the place of c0 for a single step only");
+  const size_t es = dtype == ARD_F32 ? 4 : 2;
+  if (misaligned(f, es) || misaligned(v, es) || misaligned(o, es) || misaligned(h, es) || misaligned(c0, 4) || misaligned(cT, 4) || misaligned(ckpt, 4) ||
+      misaligned(d_lengths, 4))
+    return fail(ARD_EINVAL, "a tensor does not start at a whole element");
+  const GlrCall c{glr_plan(dtype, T, B, H, flags, d_lengths), f, v, o, {z_t, z_b}};
+  if (int32_t st = glr_check_grid(c.g)) return st;
+  const size_t need = glr_ws_bytes(c.g.a);
+  if (need && (!ws || ws_bytes < need || misaligned(ws, 4))) return fail(ARD_EWORKSPACE, "workspace too small: need %zu bytes, got %zu", need, ws ? ws_bytes : 0);
+  const Strides hs{h_t, h_b};
+  hipStream_t st = (hipStream_t)stream;
+  auto with = [&](auto t, auto vec) {
+    using E = decltype(t);
+    constexpr int N = decltype(vec)::value;
+    return o ? glr_fwd_t<E, N, true>(c, c0, h, hs, cT, ckpt, (float*)ws, st) : glr_fwd_t<E, N, false>(c, c0, h, hs, cT, ckpt, (float*)ws, st);
+  };
+  return glr_instance(dtype, c.g.a.wide, with);
+}
+
+extern "C" int32_t ard_glr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t H, const void* f, const void* v, const void* o, int64_t z_t, int64_t z_b,
+                               const int32_t* d_lengths, const float* ckpt, const void* dh, int64_t dh_t, int64_t dh_b, const float* dcT, void* df,
+                               void* dv, void* dout, int64_t dz_t, int64_t dz_b, float* dc0, int32_t flags, void* ws, size_t ws_bytes, void* stream) {
+  if (int32_t st = glr_check(dtype, T, B, H, flags)) return st;
+  if (!f || !v || !ckpt || !dh || !df || !dv || (o && !dout)) return fail(ARD_EINVAL, "null tensor pointer");
+  if (!o && dout) return fail(ARD_EINVAL, "a gradient of o is asked for, but there is no o");
+  const size_t es = dtype == ARD_F32 ? 4 : 2;
+  if (misaligned(f, es) || misaligned(v, es) || misaligned(o, es) || misaligned(dh, es) || misaligned(df, es) || misaligned(dv, es) || misaligned(dout, es) ||
+      misaligned(ckpt, 4) || misaligned(dcT, 4) || misaligned(dc0, 4) || misaligned(d_lengths, 4))
+    return fail(ARD_EINVAL, "a tensor does not start at a whole element");
+  const GlrCall c{glr_plan(dtype, T, B, H, flags, d_lengths), f, v, o, {z_t, z_b}};
+  if (int32_t st = glr_check_grid(c.g)) return st;
+  const size_t need = glr_ws_bytes(c.g.a);
+  if (need && (!ws || ws_bytes < need || misaligned(ws, 4))) return fail(ARD_EWORKSPACE, "workspace too small: need %zu bytes, got %zu", need, ws ? ws_bytes : 0);
+  const Strides ds{dh_t, dh_b}, gs{dz_t, dz_b};
+  hipStream_t st = (hipStream_t)stream;
+  auto with = [&](auto t, auto vec) {
+    using E = decltype(t);
+    constexpr int N = decltype(vec)::value;
+    return o ? glr_bwd_t<E, N, true>(c, ckpt, dh, ds, dcT, df, dv, dout, gs, dc0, (float*)ws, st)
+             : glr_bwd_t<E, N, false>(c, ckpt, dh, ds, dcT, df, dv, dout, gs, dc0, (float*)ws, st);
+  };
+  return glr_instance(dtype, c.g.a.wide, with);
+}

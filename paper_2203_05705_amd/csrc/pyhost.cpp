@@ -14,15 +14,19 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/full.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <dlfcn.h>
 #include <torch/csrc/Device.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/DynamicTypes.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/Stream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <optional>
 #include <string>
 #include <type_traits>
+#include <vector>
 
 #include "../../include/ard.h"
 
@@ -44,7 +48,9 @@ struct PyRaised {};  // a Python exception is set
   X(ard_drop_gemm_bwd_data) X(ard_drop_gemm_bwd_weight) X(ard_drop_gemm_bwd_weight_static) X(ard_batch_begin)         \
   X(ard_batch_launch) X(ard_batch_abort) X(ard_lstm_workspace_bytes) X(ard_lstm_fwd) X(ard_lstm_bwd)                  \
   X(ard_conv_workspace_bytes) X(ard_conv_out_size) X(ard_fmap_drop_conv) X(ard_conv_fwd_blocks) X(ard_conv_bwd_blocks) \
-  X(ard_sens_regions) X(ard_sens_predict) X(ard_sens_row_pattern) X(ard_sens_block_pattern) X(ard_last_error)
+  X(ard_sens_regions) X(ard_sens_predict) X(ard_sens_row_pattern) X(ard_sens_block_pattern) X(ard_last_error) \
+  X(ard_layer_norm_workspace_bytes) X(ard_layer_norm_fwd) X(ard_layer_norm_bwd) X(ard_glr_workspace_bytes) X(ard_glr_fwd)   \
+  X(ard_glr_bwd) X(ard_adamw_step) X(ard_adamw_values)
 #define DECLARE(name) decltype(&::name) name = nullptr;
 struct Library {
   bool open = false;
@@ -844,6 +850,387 @@ PyObject* sens_block_pattern(const Args& a) {  // pred, balance, m, n, seed, ite
   return d.d;
 }
 
+// ---- norm, recurrence, optimizer ----------------------------------------------------------------
+
+// While one lives, tensors made here belong to the stream the call was given (torch's allocator hands their memory on in
+// that stream's order); without a stream of torch's they belong to the current one, as ever.
+struct OnStream {
+  std::optional<c10::impl::VirtualGuardImpl> impl;
+  std::optional<c10::Stream> before;
+  explicit OnStream(PyObject* o) {
+    if (!o || o == Py_None || !THPStream_Check(o)) return;
+    const THPStream* s = reinterpret_cast<const THPStream*>(o);
+    impl.emplace(static_cast<c10::DeviceType>(s->device_type));
+    before = impl->exchangeStream(c10::Stream::unpack3(s->stream_id, static_cast<c10::DeviceIndex>(s->device_index), static_cast<c10::DeviceType>(s->device_type)));
+  }
+  ~OnStream() {
+    if (before) impl->exchangeStream(*before);
+  }
+};
+
+const at::Tensor& on_device(const at::Tensor& t, at::ScalarType dtype, const char* what) {
+  if (!t.is_cuda()) raise(PyExc_AssertionError, "%s: device-resident tensors only", what);
+  if (t.scalar_type() != dtype) raise(PyExc_TypeError, "%s: dtype %s is wanted, got %s", what, c10::toString(dtype), c10::toString(t.scalar_type()));
+  return t;
+}
+// an optional contiguous tensor of this type and number of elements; NULL where None
+void* optional_tensor(const Args& a, int i, at::ScalarType dtype, int64_t numel, const char* what) {
+  if (!a.given(i)) return nullptr;
+  const at::Tensor& t = on_device(tensor_of(a.v[i], what), dtype, what);
+  if (!t.is_contiguous() || t.numel() != numel) raise(PyExc_ValueError, "%s: %lld contiguous elements are wanted", what, (long long)numel);
+  return t.data_ptr();
+}
+// outputs that the caller gives in a tuple or list; None where the corresponding flag allows
+void outputs_of(PyObject* o, int n, at::Tensor* out) {
+  PyObject* f = PySequence_Fast(o, "a sequence of output tensors is wanted");
+  if (!f) throw PyRaised{};
+  try {
+    if (PySequence_Fast_GET_SIZE(f) != n) raise(PyExc_ValueError, "%d output tensors are wanted, got %zd", n, PySequence_Fast_GET_SIZE(f));
+    for (int i = 0; i < n; ++i)
+      if (PySequence_Fast_GET_ITEM(f, i) != Py_None) out[i] = tensor_of(PySequence_Fast_GET_ITEM(f, i), "out");
+  } catch (...) {
+    Py_DECREF(f);
+    throw;
+  }
+  Py_DECREF(f);
+}
+PyObject* tensors_or_none(const at::Tensor* t, int n) {
+  PyObject* r = PyTuple_New(n);
+  for (int i = 0; i < n; ++i) {
+    PyObject* o = t[i].defined() ? THPVariable_Wrap(t[i]) : give(Py_None);
+    if (!o) {
+      Py_DECREF(r);
+      throw PyRaised{};
+    }
+    PyTuple_SET_ITEM(r, i, o);
+  }
+  return r;
+}
+
+// The rows of a matrix, or of a contiguous tensor of more dimensions, whose last dimension holds D elements, or pad8(D) of a
+// compact activation.
+struct Rows {
+  void* p;
+  int R;
+  int64_t ld;
+};
+Rows rows_of(const at::Tensor& t, int stored, const char* what) {
+  if (t.dim() < 1 || t.size(-1) != stored) raise(PyExc_ValueError, "%s: rows of %d elements are wanted", what, stored);
+  if (t.dim() == 2) {
+    if (t.size(1) > 1 && t.stride(1) != 1) raise(PyExc_AssertionError, "%s: the elements of a row must be neighbours", what);
+    return {t.data_ptr(), dim(t, 0), t.size(0) > 1 ? t.stride(0) : (int64_t)stored};
+  }
+  if (!t.is_contiguous()) raise(PyExc_AssertionError, "%s: a tensor of other than two dimensions must be contiguous", what);
+  const int64_t R = t.numel() / stored;
+  if (R > INT32_MAX) raise(PyExc_OverflowError, "%s: %lld rows are too many", what, (long long)R);
+  return {t.data_ptr(), (int)R, (int64_t)stored};
+}
+void same_rows(const Rows& a, const Rows& b, const char* what) {
+  if (a.R != b.R) raise(PyExc_ValueError, "%s: %d rows are wanted, got %d", what, a.R, b.R);
+}
+// elements of a row that take part, stored elements and flags: all of X's, or the first D of a compact activation
+int norm_width(const Args& a, int iD, const at::Tensor& X, int* stored, int* flags) {
+  if (X.dim() < 1 || X.size(-1) < 1) raise(PyExc_ValueError, "X: rows of at least one element are wanted");
+  *stored = dim(X, (int)X.dim() - 1), *flags = 0;
+  if (!a.given(iD)) return *stored;
+  const int D = as_int(a.v[iD]);
+  *flags = ARD_OUT_COMPACT;
+  if (D < 1 || pad8(D) != *stored) raise(PyExc_ValueError, "X: a compact activation of %d units has pad8(%d) columns, got %d", D, D, *stored);
+  return D;
+}
+const at::Tensor* norm_weight(const Args& a, int i, int D, const char* what) {
+  if (!a.given(i)) return nullptr;
+  const at::Tensor& t = tensor_of(a.v[i], what);
+  on_device(t, t.scalar_type(), what);
+  if (!t.is_contiguous() || t.numel() != D) raise(PyExc_ValueError, "%s: %d contiguous elements are wanted", what, D);
+  return &t;
+}
+
+PyObject* layer_norm_fwd(const Args& a) {  // X, gamma, beta, eps, D, out, stream
+  const at::Tensor& X = tensor_of(a.v[0], "X");
+  const int32_t dt = dtype_code(on_device(X, X.scalar_type(), "X"));
+  int stored, flags;
+  const int D = norm_width(a, 4, X, &stored, &flags);
+  const Rows x = rows_of(X, stored, "X");
+  const at::Tensor *g = norm_weight(a, 1, D, "gamma"), *b = norm_weight(a, 2, D, "beta");
+  if (g && b && g->scalar_type() != b->scalar_type()) raise(PyExc_TypeError, "gamma and beta are of one dtype");
+  const int32_t wt = g ? dtype_code(*g) : b ? dtype_code(*b) : (int32_t)ARD_F32;
+  at::Tensor o[3];
+  {
+    OnStream on(a.v[6]);
+    if (a.given(5)) outputs_of(a.v[5], 3, o);
+    if (!o[0].defined()) o[0] = output(X.sizes(), X.scalar_type(), X.device());
+    for (int i = 1; i < 3; ++i)
+      if (!o[i].defined()) o[i] = output({x.R}, at::kFloat, X.device());
+  }
+  const Rows y = rows_of(on_device(o[0], X.scalar_type(), "out"), stored, "out");
+  same_rows(x, y, "out");
+  for (int i = 1; i < 3; ++i)
+    if (!on_device(o[i], at::kFloat, "out").is_contiguous() || o[i].numel() != x.R) raise(PyExc_ValueError, "out: mean and rstd have an element a row");
+  const float eps = (float)a.real(3, 1e-5);
+  const void *gp = g ? g->data_ptr() : nullptr, *bp = b ? b->data_ptr() : nullptr;
+  float *mean = (float*)o[1].data_ptr(), *rstd = (float*)o[2].data_ptr();
+  void* st = stream_of(a.v[6]);
+  enqueue(lib().ard_layer_norm_fwd, dt, wt, x.R, D, (const void*)x.p, x.ld, gp, bp, eps, y.p, y.ld, mean, rstd, flags, st);
+  return tensors_or_none(o, 3);
+}
+
+PyObject* layer_norm_bwd(const Args& a) {  // dY, X, gamma, mean, rstd, D, out, ws, stream
+  const at::Tensor &dY = tensor_of(a.v[0], "dY"), &X = tensor_of(a.v[1], "X");
+  const int32_t dt = dtype_code(on_device(X, X.scalar_type(), "X"));
+  int stored, flags;
+  const int D = norm_width(a, 5, X, &stored, &flags);
+  const Rows x = rows_of(X, stored, "X"), dy = rows_of(on_device(dY, X.scalar_type(), "dY"), stored, "dY");
+  same_rows(x, dy, "dY");
+  const at::Tensor* g = norm_weight(a, 2, D, "gamma");
+  const int32_t wt = g ? dtype_code(*g) : (int32_t)ARD_F32;
+  if (!a.given(3) || !a.given(4)) raise(PyExc_TypeError, "mean and rstd of the forward pass are wanted");
+  const float *mean = (const float*)optional_tensor(a, 3, at::kFloat, x.R, "mean"), *rstd = (const float*)optional_tensor(a, 4, at::kFloat, x.R, "rstd");
+  at::Tensor o[3];
+  OnStream on(a.v[8]);
+  if (a.given(6)) outputs_of(a.v[6], 3, o);
+  if (!o[0].defined()) o[0] = output(X.sizes(), X.scalar_type(), X.device());
+  // (a norm without weights has no gradients of them unless the caller brings room for them)
+  if (!a.given(6) && g)
+    for (int i = 1; i < 3; ++i) o[i] = output({D}, g->scalar_type(), X.device());
+  const Rows dx = rows_of(on_device(o[0], X.scalar_type(), "out"), stored, "out");
+  same_rows(x, dx, "out");
+  void* grad[2] = {nullptr, nullptr};
+  for (int i = 1; i < 3; ++i)
+    if (o[i].defined()) {
+      if (!on_device(o[i], g ? g->scalar_type() : at::kFloat, "out").is_contiguous() || o[i].numel() != D)
+        raise(PyExc_ValueError, "out: dgamma and dbeta have %d contiguous elements", D);
+      grad[i - 1] = o[i].data_ptr();
+    }
+  Workspace ws(a, 7, X.device(), [&] { return grad[0] || grad[1] ? lib().ard_layer_norm_workspace_bytes(x.R, D) : (size_t)0; });
+  const void* gp = g ? g->data_ptr() : nullptr;
+  void* st = stream_of(a.v[8]);
+  enqueue(lib().ard_layer_norm_bwd, dt, wt, x.R, D, (const void*)dy.p, dy.ld, (const void*)x.p, x.ld, gp, mean, rstd, dx.p, dx.ld, grad[0], grad[1], flags,
+          ws.p, ws.bytes, st);
+  return tensors_or_none(o, 3);
+}
+
+// T, B, H of a recurrence and its stored channels
+struct GlrShape {
+  int T, B, H, stored, flags;
+  int32_t dt;
+  at::ScalarType type;
+  GlrShape(const Args& a, int iH, const at::Tensor& f) {
+    ranked(f, 3, "f");
+    dt = dtype_code(on_device(f, f.scalar_type(), "f")), type = f.scalar_type();
+    T = dim(f, 0), B = dim(f, 1), H = stored = dim(f, 2), flags = 0;
+    if (!a.given(iH)) return;
+    H = as_int(a.v[iH]), flags = ARD_IN_COMPACT | ARD_OUT_COMPACT;
+    if (H < 1 || pad8(H) != stored) raise(PyExc_ValueError, "f: compact channels of %d units are stored in pad8(%d), got %d", H, H, stored);
+  }
+  // strides of [T, B, channels]; `like`: strides that the tensor has to share
+  std::pair<int64_t, int64_t> strides(const at::Tensor& t, const char* what, const std::pair<int64_t, int64_t>* like = nullptr) const {
+    on_device(t, type, what);
+    if (t.dim() != 3 || t.size(0) != T || t.size(1) != B || t.size(2) != stored)
+      raise(PyExc_ValueError, "%s: shape (%d, %d, %d) is wanted", what, T, B, stored);
+    if (stored > 1 && t.stride(2) != 1) raise(PyExc_AssertionError, "%s: the channels of a step must be neighbours", what);
+    // (an axis of one step or sequence is not walked: its stride says nothing)
+    std::pair<int64_t, int64_t> s{T > 1 ? t.stride(0) : like ? like->first : 0, B > 1 ? t.stride(1) : like ? like->second : 0};
+    if (like && s != *like) raise(PyExc_ValueError, "%s: other strides than its companions'", what);
+    return s;
+  }
+};
+// Outputs may not overlap themselves: the axis of the larger stride steps over all that the other spans.
+void spread_out(const GlrShape& s, std::pair<int64_t, int64_t> st, const char* what) {
+  const bool time_outer = st.first >= st.second;
+  const int64_t inner = time_outer ? st.second : st.first, outer = time_outer ? st.first : st.second, n = time_outer ? s.B : s.T, m = time_outer ? s.T : s.B;
+  if ((n > 1 && inner < s.stored) || (m > 1 && outer < (n - 1) * inner + s.stored)) raise(PyExc_ValueError, "%s: its elements overlap", what);
+}
+
+PyObject* glr_fwd(const Args& a) {  // f, v, o, c0, lengths, train, H, out, ws, stream
+  const at::Tensor &f = tensor_of(a.v[0], "f"), &v = tensor_of(a.v[1], "v");
+  const GlrShape s(a, 6, f);
+  const auto zs = s.strides(f, "f");
+  s.strides(v, "v", &zs);
+  const void* op = nullptr;
+  if (a.given(2)) {
+    const at::Tensor& o = tensor_of(a.v[2], "o");
+    s.strides(o, "o", &zs);
+    op = o.data_ptr();
+  }
+  const int64_t n = (int64_t)s.B * s.H;
+  const float* c0 = (const float*)optional_tensor(a, 3, at::kFloat, n, "c0");
+  const int32_t* len = (const int32_t*)optional_tensor(a, 4, at::kInt, s.B, "lengths");
+  const bool train = a.truth(5, true);
+  const int64_t chunks = (s.T + ARD_GLR_CHUNK - 1) / ARD_GLR_CHUNK;
+  at::Tensor out[3];
+  OnStream on(a.v[9]);
+  if (a.given(7)) outputs_of(a.v[7], 3, out);
+  if (!out[0].defined()) out[0] = output({s.T, s.B, s.stored}, s.type, f.device());
+  if (!out[1].defined()) out[1] = output({s.B, s.H}, at::kFloat, f.device());
+  if (!out[2].defined() && train) out[2] = output({chunks, s.B, s.H}, at::kFloat, f.device());
+  const auto hs = s.strides(out[0], "out");
+  spread_out(s, hs, "out");
+  if (!on_device(out[1], at::kFloat, "out").is_contiguous() || out[1].numel() != n) raise(PyExc_ValueError, "out: the state has [B, H] contiguous elements");
+  if (out[2].defined() && (!on_device(out[2], at::kFloat, "out").is_contiguous() || out[2].numel() != chunks * n))
+    raise(PyExc_ValueError, "out: the kept states have [ceil(T / %d), B, H] contiguous elements", ARD_GLR_CHUNK);
+  Workspace ws(a, 8, f.device(), [&] { return lib().ard_glr_workspace_bytes(s.dt, s.T, s.B, s.H); });
+  const void *fp = f.data_ptr(), *vp = v.data_ptr();
+  void* hp = out[0].data_ptr();
+  float *ct = (float*)out[1].data_ptr(), *ck = (float*)ptr(out[2]);
+  void* st = stream_of(a.v[9]);
+  enqueue(lib().ard_glr_fwd, s.dt, s.T, s.B, s.H, fp, vp, op, zs.first, zs.second, c0, len, hp, hs.first, hs.second, ct, ck, s.flags, ws.p, ws.bytes, st);
+  return tensors_or_none(out, 3);
+}
+
+PyObject* glr_bwd(const Args& a) {  // f, v, o, dh, ckpt, dcT, lengths, H, out, ws, stream
+  const at::Tensor &f = tensor_of(a.v[0], "f"), &v = tensor_of(a.v[1], "v"), &dh = tensor_of(a.v[3], "dh");
+  const GlrShape s(a, 7, f);
+  const auto zs = s.strides(f, "f");
+  s.strides(v, "v", &zs);
+  const void* op = nullptr;
+  if (a.given(2)) {
+    const at::Tensor& o = tensor_of(a.v[2], "o");
+    s.strides(o, "o", &zs);
+    op = o.data_ptr();
+  }
+  const auto ds = s.strides(dh, "dh");
+  const int64_t n = (int64_t)s.B * s.H, chunks = (s.T + ARD_GLR_CHUNK - 1) / ARD_GLR_CHUNK;
+  if (!a.given(4)) raise(PyExc_TypeError, "the states that the forward pass kept (train=True) are wanted");
+  const float* ck = (const float*)optional_tensor(a, 4, at::kFloat, chunks * n, "ckpt");
+  const float* dct = (const float*)optional_tensor(a, 5, at::kFloat, n, "dcT");
+  const int32_t* len = (const int32_t*)optional_tensor(a, 6, at::kInt, s.B, "lengths");
+  at::Tensor out[4];
+  OnStream on(a.v[10]);
+  if (a.given(8)) {
+    PyObject* given = a.v[8];
+    const Py_ssize_t k = PySequence_Size(given);
+    if (k < 0) throw PyRaised{};
+    outputs_of(given, k == 3 ? 3 : 4, out);
+  }
+  for (int i = 0; i < 3; ++i)
+    if (!out[i].defined() && (i < 2 || op)) out[i] = output({s.T, s.B, s.stored}, s.type, f.device());
+  if (!out[3].defined()) out[3] = output({s.B, s.H}, at::kFloat, f.device());
+  if (out[2].defined() && !op) raise(PyExc_ValueError, "out: a gradient of o is asked for, but there is no o");
+  const auto gs = s.strides(out[0], "out");
+  spread_out(s, gs, "out");
+  for (int i = 1; i < 3; ++i)
+    if (out[i].defined()) s.strides(out[i], "out", &gs);
+  if (!on_device(out[3], at::kFloat, "out").is_contiguous() || out[3].numel() != n) raise(PyExc_ValueError, "out: the state's gradient has [B, H] contiguous elements");
+  Workspace ws(a, 9, f.device(), [&] { return lib().ard_glr_workspace_bytes(s.dt, s.T, s.B, s.H); });
+  const void *fp = f.data_ptr(), *vp = v.data_ptr(), *hp = dh.data_ptr();
+  void *g0 = out[0].data_ptr(), *g1 = out[1].data_ptr(), *g2 = ptr(out[2]);
+  float* dc0 = (float*)out[3].data_ptr();
+  void* st = stream_of(a.v[10]);
+  enqueue(lib().ard_glr_bwd, s.dt, s.T, s.B, s.H, fp, vp, op, zs.first, zs.second, len, ck, hp, ds.first, ds.second, dct, g0, g1, g2, gs.first, gs.second,
+          dc0, s.flags, ws.p, ws.bytes, st);
+  return tensors_or_none(out, 4);
+}
+
+// A list (or tuple) of tensors, one for each parameter; None: no such list.
+struct TensorList {
+  PyObject* f = nullptr;
+  Py_ssize_t n = 0;
+  const char* what;
+  TensorList(PyObject* o, const char* what_) : what(what_) {
+    if (!o || o == Py_None) return;
+    f = PySequence_Fast(o, "a list of tensors is wanted");
+    if (!f) throw PyRaised{};
+    n = PySequence_Fast_GET_SIZE(f);
+  }
+  ~TensorList() { Py_XDECREF(f); }
+  TensorList(const TensorList&) = delete;
+  // address of the i-th tensor, contiguous, of this type and number of elements
+  void* at(Py_ssize_t i, at::ScalarType dtype, int64_t numel) const {
+    const at::Tensor& t = on_device(tensor_of(PySequence_Fast_GET_ITEM(f, i), what), dtype, what);
+    if (!t.is_contiguous() || t.numel() != numel) raise(PyExc_ValueError, "%s[%zd]: %lld contiguous elements are wanted", what, i, (long long)numel);
+    return t.data_ptr();
+  }
+  void same(Py_ssize_t count) const {
+    if (f && n != count) raise(PyExc_ValueError, "%s: %zd tensors are wanted, got %zd", what, count, n);
+  }
+};
+int64_t adam_blocks(int64_t n) { return (n + ARD_ADAMW_BLOCK - 1) / ARD_ADAMW_BLOCK; }
+
+PyObject* adamw_step(const Args& a) {  // params, grads, m, v, m_scale, v_scale, copies, lr, beta1, beta2, eps, weight_decay, step, grad_scale, stream
+  const TensorList p(a.v[0], "params"), g(a.v[1], "grads"), m(a.v[2], "m"), v(a.v[3], "v"), ms(a.v[4], "m_scale"), vs(a.v[5], "v_scale"), w(a.v[6], "copies");
+  if (!p.f || !g.f || !m.f || !v.f) raise(PyExc_TypeError, "lists of params, grads, m and v are wanted");
+  if (!ms.f != !vs.f) raise(PyExc_ValueError, "8-bit states have scales for m and for v");
+  g.same(p.n), m.same(p.n), v.same(p.n), ms.same(p.n), vs.same(p.n), w.same(p.n);
+  const bool eight = ms.f;
+  int32_t gt = ARD_F32;
+  at::ScalarType gtype = at::kFloat;
+  if (p.n) {
+    const at::Tensor& t = tensor_of(PySequence_Fast_GET_ITEM(g.f, 0), "grads");
+    gt = dtype_code(t), gtype = t.scalar_type();
+  }
+  std::vector<ard_adamw_tensor> tab((size_t)p.n);
+  for (Py_ssize_t i = 0; i < p.n; ++i) {
+    const int64_t n = tensor_of(PySequence_Fast_GET_ITEM(p.f, i), "params").numel();
+    ard_adamw_tensor& t = tab[(size_t)i];
+    t = ard_adamw_tensor{n, (float*)p.at(i, at::kFloat, n), g.at(i, gtype, n), m.at(i, eight ? at::kChar : at::kFloat, n), v.at(i, eight ? at::kByte : at::kFloat, n),
+                         nullptr, nullptr, nullptr};
+    if (eight) t.m_scale = (float*)ms.at(i, at::kFloat, adam_blocks(n)), t.v_scale = (float*)vs.at(i, at::kFloat, adam_blocks(n));
+    if (w.f && PySequence_Fast_GET_ITEM(w.f, i) != Py_None) t.w = w.at(i, at::kBFloat16, n);
+  }
+  const double lr = a.real(7, 1e-3), b1 = a.real(8, 0.9), b2 = a.real(9, 0.999), eps = a.real(10, 1e-8), wd = a.real(11, 0.01);
+  int64_t step = 1;
+  if (a.v[12]) {
+    step = PyLong_AsLongLong(a.v[12]);
+    if (step == -1 && PyErr_Occurred()) throw PyRaised{};
+  }
+  const float* scale = (const float*)optional_tensor(a, 13, at::kFloat, 1, "grad_scale");
+  void* st = stream_of(a.v[14]);
+  if (p.n > INT32_MAX) raise(PyExc_OverflowError, "too many tensors");
+  const ard_adamw_tensor* table = tab.data();
+  enqueue(lib().ard_adamw_step, eight ? 8 : 32, gt, (int)p.n, table, lr, b1, b2, eps, wd, step, scale, st);
+  Py_RETURN_NONE;
+}
+
+PyObject* adamw_values(const Args& a) {  // m, v, m_scale, v_scale, out, stream
+  const TensorList m(a.v[0], "m"), v(a.v[1], "v"), ms(a.v[2], "m_scale"), vs(a.v[3], "v_scale");
+  if (!m.f || !v.f || !ms.f || !vs.f) raise(PyExc_TypeError, "lists of m, v and their scales are wanted");
+  v.same(m.n), ms.same(m.n), vs.same(m.n);
+  std::vector<ard_adamw_tensor> tab((size_t)m.n);
+  std::vector<float*> mo((size_t)m.n), vo((size_t)m.n);
+  PyObject* r = nullptr;
+  OnStream on(a.v[5]);
+  try {
+    if (a.given(4)) {
+      r = give(a.v[4]);
+    } else {
+      r = PyTuple_New(2);
+      for (int k = 0; k < 2; ++k) {
+        PyObject* l = PyList_New(m.n);
+        PyTuple_SET_ITEM(r, k, l);
+        for (Py_ssize_t i = 0; i < m.n; ++i) {
+          const at::Tensor& t = tensor_of(PySequence_Fast_GET_ITEM(m.f, i), "m");
+          PyList_SET_ITEM(l, i, wrap(output(t.sizes(), at::kFloat, t.device())));
+        }
+      }
+    }
+    PyObject* pair = PySequence_Fast(r, "a pair of lists of output tensors is wanted");
+    if (!pair) throw PyRaised{};
+    Py_ssize_t k = PySequence_Fast_GET_SIZE(pair);
+    PyObject* lists[2] = {k == 2 ? PySequence_Fast_GET_ITEM(pair, 0) : nullptr, k == 2 ? PySequence_Fast_GET_ITEM(pair, 1) : nullptr};
+    Py_DECREF(pair);  // (r keeps what the pair holds)
+    if (k != 2) raise(PyExc_ValueError, "a pair of lists of output tensors is wanted");
+    const TensorList om(lists[0], "out"), ov(lists[1], "out");
+    if (!om.f || !ov.f) raise(PyExc_TypeError, "a pair of lists of output tensors is wanted");
+    om.same(m.n), ov.same(m.n);
+    for (Py_ssize_t i = 0; i < m.n; ++i) {
+      const int64_t n = tensor_of(PySequence_Fast_GET_ITEM(m.f, i), "m").numel();
+      tab[(size_t)i] = ard_adamw_tensor{n, nullptr, nullptr, m.at(i, at::kChar, n), v.at(i, at::kByte, n), (float*)ms.at(i, at::kFloat, adam_blocks(n)),
+                                        (float*)vs.at(i, at::kFloat, adam_blocks(n)), nullptr};
+      mo[(size_t)i] = (float*)om.at(i, at::kFloat, n), vo[(size_t)i] = (float*)ov.at(i, at::kFloat, n);
+    }
+    if (m.n > INT32_MAX) raise(PyExc_OverflowError, "too many tensors");
+    const ard_adamw_tensor* table = tab.data();
+    float* const *mp = mo.data(), *const *vp = vo.data();
+    void* st = stream_of(a.v[5]);
+    enqueue(lib().ard_adamw_values, (int)m.n, table, mp, vp, st);
+  } catch (...) {
+    Py_XDECREF(r);
+    throw;
+  }
+  return r;
+}
+
 // ---- grouped launches -------------------------------------------------------------------------
 
 struct BatchObject {
@@ -961,6 +1348,13 @@ CALL(sens_predict, 12, 11, "A", "ksize", "stride", "pad", "x", "y", "k_permille"
 CALL(sens_row_pattern, 8, 7, "sens", "rows", "x", "m", "n", "seed", "iteration", "stream")
 CALL(sens_block_pattern, 7, 6, "pred", "balance", "m", "n", "seed", "iteration", "stream")
 
+CALL(layer_norm_fwd, 7, 1, "X", "gamma", "beta", "eps", "D", "out", "stream")
+CALL(layer_norm_bwd, 9, 5, "dY", "X", "gamma", "mean", "rstd", "D", "out", "ws", "stream")
+CALL(glr_fwd, 10, 2, "f", "v", "o", "c0", "lengths", "train", "H", "out", "ws", "stream")
+CALL(glr_bwd, 11, 5, "f", "v", "o", "dh", "ckpt", "dcT", "lengths", "H", "out", "ws", "stream")
+CALL(adamw_step, 15, 4, "params", "grads", "m", "v", "m_scale", "v_scale", "copies", "lr", "beta1", "beta2", "eps", "weight_decay", "step", "grad_scale", "stream")
+CALL(adamw_values, 6, 4, "m", "v", "m_scale", "v_scale", "out", "stream")
+
 PyObject* py_configure(PyObject*, PyObject* args) {  // library path, ArdError, torch._C._cuda_getCurrentRawStream
   const char* path;
   PyObject *err, *raw;
@@ -1016,6 +1410,25 @@ PyMethodDef methods[] = {
                             "Row-based pattern from the per-band sensitivity sens[N, RB, 1]: dict(mask[N*rows], keep, count)."),
     ENTRY(sens_block_pattern, "sens_block_pattern($module, pred, balance, m, n, seed, iteration, stream=None)\n--\n\n"
                               "Block-based pattern from ard_sens_predict's outputs: dict(sens (balanced), keep), each [N, RB, CB]."),
+    ENTRY(layer_norm_fwd, "layer_norm_fwd($module, X, gamma=None, beta=None, eps=1e-05, D=None, out=None, stream=None)\n--\n\n"
+                          "Layer norm of the rows of X: (Y, mean[R], rstd[R]); out: reuse such a triple (None: a new one).  X: [R, D] with rows any\n"
+                          "distance apart, or contiguous with D last; D: kept units of a compact activation [R, pad8(D)], of which Y is one too."),
+    ENTRY(layer_norm_bwd, "layer_norm_bwd($module, dY, X, gamma, mean, rstd, D=None, out=None, ws=None, stream=None)\n--\n\n"
+                          "Gradients (dX, dgamma, dbeta) of layer_norm_fwd, the latter two in gamma's dtype (None without gamma); out: reuse such a\n"
+                          "triple, where None leaves a weight's gradient out."),
+    ENTRY(glr_fwd, "glr_fwd($module, f, v, o=None, c0=None, lengths=None, train=True, H=None, out=None, ws=None, stream=None)\n--\n\n"
+                   "Gated linear recurrence c = s(f) c + (1 - s(f)) v, h = s(o) c over f, v, o[T, B, H] (views of one strides): (h[T, B, H],\n"
+                   "cT[B, H] fp32, ckpt: the states the backward pass needs, None with train=False); out: reuse such a triple.\n"
+                   "H: kept units of compact tensors [T, B, pad8(H)]; lengths: int32 [B], steps of each sequence."),
+    ENTRY(glr_bwd, "glr_bwd($module, f, v, o, dh, ckpt, dcT=None, lengths=None, H=None, out=None, ws=None, stream=None)\n--\n\n"
+                   "Gradients (df, dv, do, dc0) of glr_fwd (do: None without o); out: the first three or all four, to reuse."),
+    ENTRY(adamw_step, "adamw_step($module, params, grads, m, v, m_scale=None, v_scale=None, copies=None, lr=0.001, beta1=0.9, beta2=0.999, eps=1e-08, "
+                      "weight_decay=0.01, step=1, grad_scale=None, stream=None)\n--\n\n"
+                      "One AdamW step, in place, over lists of tensors: params fp32; grads fp32 or bf16; m, v fp32, or int8 and uint8 codes with\n"
+                      "their scales (adamw_state makes either); copies: bf16 copies of the parameters (or None) that are written too.\n"
+                      "grad_scale: device float that multiplies the gradients; where it is not finite nothing changes."),
+    ENTRY(adamw_values, "adamw_values($module, m, v, m_scale, v_scale, out=None, stream=None)\n--\n\n"
+                        "The fp32 values of 8-bit states: a pair of lists (m, v); out: reuse such a pair."),
     {"configure", py_configure, METH_VARARGS, nullptr},
     {"set_allocator", py_set_allocator, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
