@@ -508,7 +508,7 @@ int32_t ard_layer_norm_bwd(int32_t dtype, int32_t wdtype, int32_t R, int32_t D, 
  * The workspace holds what workgroups that share a sequence tell each other; 0 bytes where none do.
  */
 /* steps between the states of ckpt */
-#define ARD_GLR_CHUNK 16
+#define ARD_GLR_CHUNK 8
 int32_t ard_glr_chunk(void);
 size_t ard_glr_workspace_bytes(int32_t dtype, int32_t T, int32_t B, int32_t H);
 int32_t ard_glr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t H, const void* f, const void* v, const void* o, int64_t z_t,

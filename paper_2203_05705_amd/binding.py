@@ -345,7 +345,7 @@ def lstm_status_offset(dtype_code, T, B, I, H, pat=None):
 # ---- layer norm, gated linear recurrence, AdamW ---------------------------------------------
 
 ADAMW_BLOCK = 256   # neighbouring elements that share the scales of an 8-bit state
-GLR_CHUNK = 16      # steps between the states that glr_fwd keeps for glr_bwd
+GLR_CHUNK = 8       # steps between the states that glr_fwd keeps for glr_bwd
 
 
 class CAdamWTensor(C.Structure):

@@ -5,12 +5,12 @@
 //   dv = dc (1 - F), df = dc (c_{t-1} - v) F (1 - F), do = dh c sigma(o) (1 - sigma(o)), dc0 = e_0
 //
 // Each step is affine in the state, so a stretch of steps is a pair (P, S): it takes c to P c + S, and stretches
-// compose.  A wavefront takes 16 steps of 64 lanes' channels into registers, makes their pair there, and the wavefronts
+// compose.  A wavefront takes 8 steps of 64 lanes' channels into registers, makes their pair there, and the wavefronts
 // of a workgroup, which have neighbouring stretches, exchange pairs through LDS: every input is read once and every
 // output written once, which is what bounds these passes.  Where batch and channels alone give too few wavefronts, time
 // is cut into segments for several workgroups; a first pass then makes the segments' pairs (reading f and v, or f, o and
 // dh, once more).  States, pairs and gradients in flight are fp32.  The backward pass starts from the states that the
-// forward pass left before every 16th step, so it needs no second scan for them.
+// forward pass left before every 8th step, so it needs no second scan for them.
 #include <type_traits>
 
 #include "rows.hpp"
@@ -39,6 +39,9 @@ __device__ __forceinline__ void gate_pair(float x, float& F, float& I) {
   I = x >= 0.0f ? e * F : 1.0f - F;
 }
 __device__ __forceinline__ float gate(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.44269504088896341f)); }
+
+// Loads stay in front of this, in flight together: left to itself the compiler moves them next to their uses.
+__device__ __forceinline__ void all_issued() { __builtin_amdgcn_sched_barrier(0); }
 
 // what a workgroup works on
 struct GlrPlace {
@@ -90,18 +93,31 @@ __device__ __forceinline__ void apply_segments(const GlrArgs& a, const GlrPlace&
   float P[VEC], S[VEC];
 #pragma unroll
   for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
-  for (int i = lo; i < hi; ++i) {
-    const float* at = seg_pairs + (int64_t)(from + step * i) * 2 * plane + (int64_t)p.b * a.H + p.ch;
-    float q[VEC], r[VEC];
-    load_some<VEC>(at, p.n, q);
-    load_some<VEC>(at + plane, p.n, r);
+  for (int i0 = lo; i0 < hi; i0 += 4) {  // (four segments' pairs in flight)
+    float q[4][VEC], r[4][VEC];
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) P[j] *= q[j], S[j] = fmaf(q[j], S[j], r[j]);
+    for (int i = 0; i < 4; ++i) {
+      const float* at = seg_pairs + (int64_t)(from + step * imin(i0 + i, hi - 1)) * 2 * plane + (int64_t)p.b * a.H + p.ch;
+      load_some<VEC>(at, p.n, q[i]);
+      load_some<VEC>(at + plane, p.n, r[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i0 + i < hi) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) P[j] *= q[i][j], S[j] = fmaf(q[i][j], S[j], r[i][j]);
+      }
   }
   leave<VEC>(lds, 0, w, P, S);
   __syncthreads();
   for (int k = 0; k < waves; ++k) apply<VEC>(lds, 0, k, c);
   __syncthreads();
+}
+
+// Results.  CUT: of a launch whose inputs are read a second time, by way of the caches; results are kept from taking their room.
+template <bool CUT, int VEC, typename T> __device__ __forceinline__ void put(T* p, const float (&x)[VEC]) {
+  if constexpr (CUT) store_run_past<VEC>(p, x);
+  else store_run<VEC>(p, x);
 }
 
 // ---- forward ------------------------------------------------------------------
@@ -110,9 +126,11 @@ __device__ __forceinline__ void apply_segments(const GlrArgs& a, const GlrPlace&
 template <bool WHOLE, typename T, int VEC>
 __device__ __forceinline__ void stretch_fwd(const T* f, const T* v, int64_t st, int steps, float (&F)[kSteps][VEC], float (&b)[kSteps][VEC],
                                             float (&P)[VEC], float (&S)[VEC]) {
+  Raw<T, VEC> rf[kSteps], rv[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
-    if (WHOLE || i < steps) load_run<VEC>(f + i * st, F[i]), load_run<VEC>(v + i * st, b[i]);
+    if (WHOLE || i < steps) rf[i] = load_raw<T, VEC>(f + i * st), rv[i] = load_raw<T, VEC>(v + i * st);
+  all_issued();
 #pragma unroll
   for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
 #pragma unroll
@@ -121,8 +139,8 @@ __device__ __forceinline__ void stretch_fwd(const T* f, const T* v, int64_t st, 
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         float I;
-        gate_pair(F[i][j], F[i][j], I);
-        b[i][j] *= I;
+        gate_pair(part_of(rf[i], j), F[i][j], I);
+        b[i][j] = I * part_of(rv[i], j);
         P[j] *= F[i][j];
         S[j] = fmaf(F[i][j], S[j], b[i][j]);
       }
@@ -160,9 +178,9 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_pairs_kernel(GlrArgs a
 }
 
 // results of a stretch whose state before it is s; steps from `steps` to `stored` lie behind the sequence's end
-template <bool WHOLE, typename T, int VEC, bool GATE>
+template <bool WHOLE, typename T, int VEC, bool GATE, bool CUT>
 __device__ __forceinline__ void stretch_out(T* h, int64_t st, bool on, int steps, int stored, const float (&F)[kSteps][VEC], const float (&b)[kSteps][VEC],
-                                            const float (&g)[kSteps][VEC], float (&s)[VEC]) {
+                                            const Raw<T, VEC> (&g)[kSteps], float (&s)[VEC]) {
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     if (!WHOLE && i >= stored) break;
@@ -173,14 +191,14 @@ __device__ __forceinline__ void stretch_out(T* h, int64_t st, bool on, int steps
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         s[j] = fmaf(F[i][j], s[j], b[i][j]);
-        y[j] = GATE ? gate(g[i][j]) * s[j] : s[j];
+        y[j] = GATE ? gate(part_of(g[i], j)) * s[j] : s[j];
       }
     }
-    if (on) store_run<VEC>(h + i * st, y);
+    if (on) put<CUT, VEC>(h + i * st, y);
   }
 }
 
-template <typename T, int VEC, bool GATE>
+template <typename T, int VEC, bool GATE, bool CUT>
 __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_kernel(GlrArgs a, const T* f, const T* v, const T* o, Strides z, const float* c0, T* h,
                                                                  Strides hs, float* cT, float* ckpt, const float* seg_pairs) {
   __shared__ Pairs<VEC> lds;
@@ -191,16 +209,17 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_kernel(GlrArgs a, cons
 #pragma unroll
   for (int j = 0; j < VEC; ++j) c[j] = 0.0f;
   if (c0) load_some<VEC>(c0 + state, p.n, c);
-  if (p.seg) apply_segments<VEC>(a, p, seg_pairs, 0, 1, p.seg, lds, c);
+  if (CUT && p.seg) apply_segments<VEC>(a, p, seg_pairs, 0, 1, p.seg, lds, c);
   int turn = 0;
   for (int t = p.t0; t < p.t1; t += waves * kSteps, turn ^= 1) {
     const int tw = t + w * kSteps, steps = imin(p.t1, p.live) - tw;
-    float F[kSteps][VEC], b[kSteps][VEC], g[kSteps][VEC], P[VEC], S[VEC], s[VEC];
+    float F[kSteps][VEC], b[kSteps][VEC], P[VEC], S[VEC], s[VEC];
+    Raw<T, VEC> g[kSteps];
     const int64_t at = tw * z.t + p.b * z.b + p.ch;
     if (GATE) {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i)
-        if (i < steps) load_run<VEC>(o + at + i * z.t, g[i]);
+        if (i < steps) g[i] = load_raw<T, VEC>(o + at + i * z.t);
     }
     if (steps >= kSteps) stretch_fwd<true, T, VEC>(f + at, v + at, z.t, steps, F, b, P, S);
     else stretch_fwd<false, T, VEC>(f + at, v + at, z.t, steps, F, b, P, S);
@@ -220,8 +239,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_kernel(GlrArgs a, cons
     if (tw < p.t1) {
       if (ckpt) store_some<VEC>(ckpt + (int64_t)(tw / kSteps) * plane + state, p.n, s);
       T* out = h + tw * hs.t + p.b * hs.b + p.ch;
-      if (steps >= kSteps) stretch_out<true, T, VEC, GATE>(out, hs.t, p.on, steps, kSteps, F, b, g, s);
-      else stretch_out<false, T, VEC, GATE>(out, hs.t, p.on, steps, p.t1 - tw, F, b, g, s);
+      if (steps >= kSteps) stretch_out<true, T, VEC, GATE, CUT>(out, hs.t, p.on, steps, kSteps, F, b, g, s);
+      else stretch_out<false, T, VEC, GATE, CUT>(out, hs.t, p.on, steps, p.t1 - tw, F, b, g, s);
     }
   }
   if (cT && w == 0 && p.seg == a.segs - 1) store_some<VEC>(cT + state, p.n, c);
@@ -259,14 +278,15 @@ __global__ __launch_bounds__(64) void glr_step_kernel(GlrArgs a, const T* f, con
 // The adjoint's pair of a stretch takes e behind its last step to e behind the step before its first.
 template <bool WHOLE, typename T, int VEC, bool GATE>
 __device__ __forceinline__ void stretch_adjoint(const T* f, const T* o, const T* dh, int64_t st, int64_t dst, int steps, float (&P)[VEC], float (&S)[VEC]) {
-  float F[kSteps][VEC], q[kSteps][VEC], g[kSteps][VEC];
+  Raw<T, VEC> F[kSteps], q[kSteps], g[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
     if (WHOLE || i < steps) {
-      load_run<VEC>(f + i * st, F[i]);
-      load_run<VEC>(dh + i * dst, q[i]);
-      if (GATE) load_run<VEC>(o + i * st, g[i]);
+      F[i] = load_raw<T, VEC>(f + i * st);
+      q[i] = load_raw<T, VEC>(dh + i * dst);
+      if (GATE) g[i] = load_raw<T, VEC>(o + i * st);
     }
+  all_issued();
 #pragma unroll
   for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
 #pragma unroll
@@ -274,8 +294,8 @@ __device__ __forceinline__ void stretch_adjoint(const T* f, const T* o, const T*
     if (WHOLE || i < steps) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        const float x = gate(F[i][j]);
-        S[j] = x * (S[j] + (GATE ? gate(g[i][j]) * q[i][j] : q[i][j]));
+        const float x = gate(part_of(F[i], j)), d = part_of(q[i], j);
+        S[j] = x * (S[j] + (GATE ? gate(part_of(g[i], j)) * d : d));
         P[j] *= x;
       }
     }
@@ -315,36 +335,38 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_pairs_kernel(GlrArgs a
 
 // Loads of a stretch, its states again from the one before it, and its adjoint's pair; do is stored on the way (it needs
 // no gradient from later steps).  Leaves F, I = 1 - F, u = c_{t-1} - v and q = sigma(o) dh.
-template <bool WHOLE, typename T, int VEC, bool GATE>
+template <bool WHOLE, typename T, int VEC, bool GATE, bool CUT>
 __device__ __forceinline__ void stretch_back(const T* f, const T* v, const T* o, const T* dh, T* dg, int64_t st, int64_t dst, int64_t gst, bool on, int steps,
                                              float (&c)[VEC], float (&F)[kSteps][VEC], float (&I)[kSteps][VEC], float (&u)[kSteps][VEC],
                                              float (&q)[kSteps][VEC], float (&P)[VEC], float (&S)[VEC]) {
-  float g[kSteps][VEC];
+  Raw<T, VEC> rf[kSteps], rv[kSteps], g[kSteps], rd[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
     if (WHOLE || i < steps) {
-      load_run<VEC>(f + i * st, F[i]);
-      load_run<VEC>(v + i * st, u[i]);
-      if (GATE) load_run<VEC>(o + i * st, g[i]);
-      load_run<VEC>(dh + i * dst, q[i]);
+      rf[i] = load_raw<T, VEC>(f + i * st);
+      rv[i] = load_raw<T, VEC>(v + i * st);
+      if (GATE) g[i] = load_raw<T, VEC>(o + i * st);
+      rd[i] = load_raw<T, VEC>(dh + i * dst);
     }
+  all_issued();
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
     if (WHOLE || i < steps) {
       float y[VEC];
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        gate_pair(F[i][j], F[i][j], I[i][j]);
-        const float x = u[i][j];
+        gate_pair(part_of(rf[i], j), F[i][j], I[i][j]);
+        const float x = part_of(rv[i], j);
         u[i][j] = c[j] - x;
         c[j] = fmaf(F[i][j], c[j], I[i][j] * x);
+        q[i][j] = part_of(rd[i], j);
         if (GATE) {
-          const float O = gate(g[i][j]);
+          const float O = gate(part_of(g[i], j));
           q[i][j] *= O;
           y[j] = q[i][j] * c[j] * (1.0f - O);
         }
       }
-      if (GATE && on) store_run<VEC>(dg + i * gst, y);
+      if (GATE && on) put<CUT, VEC>(dg + i * gst, y);
     }
 #pragma unroll
   for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
@@ -359,7 +381,7 @@ __device__ __forceinline__ void stretch_back(const T* f, const T* v, const T* o,
     }
 }
 // df and dv of a stretch, e behind its last step in s; zeros (do's too) for its steps from `steps` to `stored`
-template <bool WHOLE, typename T, int VEC, bool GATE>
+template <bool WHOLE, typename T, int VEC, bool GATE, bool CUT>
 __device__ __forceinline__ void stretch_grads(T* df, T* dv, T* dg, int64_t gst, bool on, int steps, int stored, const float (&F)[kSteps][VEC],
                                               const float (&I)[kSteps][VEC], const float (&u)[kSteps][VEC], const float (&q)[kSteps][VEC],
                                               float (&s)[VEC]) {
@@ -378,13 +400,13 @@ __device__ __forceinline__ void stretch_grads(T* df, T* dv, T* dg, int64_t gst, 
         x[j] = y[j] * F[i][j] * u[i][j];
       }
     } else if (GATE) {
-      if (on) store_run<VEC>(dg + i * gst, x);
+      if (on) put<CUT, VEC>(dg + i * gst, x);
     }
-    if (on) store_run<VEC>(df + i * gst, x), store_run<VEC>(dv + i * gst, y);
+    if (on) put<CUT, VEC>(df + i * gst, x), put<CUT, VEC>(dv + i * gst, y);
   }
 }
 
-template <typename T, int VEC, bool GATE>
+template <typename T, int VEC, bool GATE, bool CUT>
 __global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_kernel(GlrArgs a, const T* f, const T* v, const T* o, Strides z, const float* ckpt, const T* dh,
                                                                  Strides ds, const float* dcT, T* df, T* dv, T* dg, Strides gs, float* dc0,
                                                                  const float* seg_pairs) {
@@ -396,7 +418,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_kernel(GlrArgs a, cons
 #pragma unroll
   for (int j = 0; j < VEC; ++j) e[j] = 0.0f;
   if (dcT) load_some<VEC>(dcT + state, p.n, e);
-  if (p.seg < a.segs - 1) apply_segments<VEC>(a, p, seg_pairs, a.segs - 1, -1, a.segs - 1 - p.seg, lds, e);
+  if (CUT && p.seg < a.segs - 1) apply_segments<VEC>(a, p, seg_pairs, a.segs - 1, -1, a.segs - 1 - p.seg, lds, e);
   const int span = waves * kSteps, turns = (p.t1 - p.t0 + span - 1) / span;
   int turn = 0;
   for (int t = p.t0 + (turns - 1) * span; t >= p.t0; t -= span, turn ^= 1) {
@@ -404,8 +426,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_kernel(GlrArgs a, cons
     float F[kSteps][VEC], I[kSteps][VEC], u[kSteps][VEC], q[kSteps][VEC], P[VEC], S[VEC], c[VEC], s[VEC];
     const int64_t at = tw * z.t + p.b * z.b + p.ch, dat = tw * ds.t + p.b * ds.b + p.ch, gat = tw * gs.t + p.b * gs.b + p.ch;
     if (steps > 0) load_some<VEC>(ckpt + (int64_t)(tw / kSteps) * plane + state, p.n, c);
-    if (steps >= kSteps) stretch_back<true, T, VEC, GATE>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, steps, c, F, I, u, q, P, S);
-    else stretch_back<false, T, VEC, GATE>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, steps, c, F, I, u, q, P, S);
+    if (steps >= kSteps) stretch_back<true, T, VEC, GATE, CUT>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, steps, c, F, I, u, q, P, S);
+    else stretch_back<false, T, VEC, GATE, CUT>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, steps, c, F, I, u, q, P, S);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) s[j] = e[j];
     if (waves > 1) {
@@ -419,8 +441,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_kernel(GlrArgs a, cons
 #pragma unroll
       for (int j = 0; j < VEC; ++j) e[j] = fmaf(P[j], e[j], S[j]);
     }
-    if (steps >= kSteps) stretch_grads<true, T, VEC, GATE>(df + gat, dv + gat, dg + gat, gs.t, p.on, steps, kSteps, F, I, u, q, s);
-    else stretch_grads<false, T, VEC, GATE>(df + gat, dv + gat, dg + gat, gs.t, p.on, steps, p.t1 - tw, F, I, u, q, s);
+    if (steps >= kSteps) stretch_grads<true, T, VEC, GATE, CUT>(df + gat, dv + gat, dg + gat, gs.t, p.on, steps, kSteps, F, I, u, q, s);
+    else stretch_grads<false, T, VEC, GATE, CUT>(df + gat, dv + gat, dg + gat, gs.t, p.on, steps, p.t1 - tw, F, I, u, q, s);
   }
   if (dc0 && w == 0 && p.seg == 0) store_some<VEC>(dc0 + state, p.n, e);
 }
@@ -482,7 +504,9 @@ static int32_t glr_fwd_t(const GlrCall& c, const float* c0, void* h, Strides hs,
     ARD_LAUNCH((glr_fwd_pairs_kernel<T, VEC>), dim3(a.groups * a.B * (a.segs - 1)), block, 0, st, a, f, v, c.z, ws);
     ARD_LAUNCH_CHECK("glr_fwd_pairs_kernel");
   }
-  ARD_LAUNCH((glr_fwd_kernel<T, VEC, GATE>), dim3(a.groups * a.B * a.segs), block, 0, st, a, f, v, o, c.z, c0, (T*)h, hs, cT, ckpt, ws);
+  const dim3 grid(a.groups * a.B * a.segs);
+  if (a.segs > 1) ARD_LAUNCH((glr_fwd_kernel<T, VEC, GATE, true>), grid, block, 0, st, a, f, v, o, c.z, c0, (T*)h, hs, cT, ckpt, ws);
+  else ARD_LAUNCH((glr_fwd_kernel<T, VEC, GATE, false>), grid, block, 0, st, a, f, v, o, c.z, c0, (T*)h, hs, cT, ckpt, nullptr);
   ARD_LAUNCH_CHECK("glr_fwd_kernel");
   return ARD_OK;
 }
@@ -497,8 +521,12 @@ static int32_t glr_bwd_t(const GlrCall& c, const float* ckpt, const void* dh, St
     ARD_LAUNCH((glr_bwd_pairs_kernel<T, VEC, GATE>), dim3(a.groups * a.B * a.segs), block, 0, st, a, f, o, c.z, (const T*)dh, ds, ws);
     ARD_LAUNCH_CHECK("glr_bwd_pairs_kernel");
   }
-  ARD_LAUNCH((glr_bwd_kernel<T, VEC, GATE>), dim3(a.groups * a.B * a.segs), block, 0, st, a, f, v, o, c.z, ckpt, (const T*)dh, ds, dcT, (T*)df, (T*)dv,
-             (T*)dg, gs, dc0, ws);
+  const dim3 grid(a.groups * a.B * a.segs);
+  if (a.segs > 1)
+    ARD_LAUNCH((glr_bwd_kernel<T, VEC, GATE, true>), grid, block, 0, st, a, f, v, o, c.z, ckpt, (const T*)dh, ds, dcT, (T*)df, (T*)dv, (T*)dg, gs, dc0, ws);
+  else
+    ARD_LAUNCH((glr_bwd_kernel<T, VEC, GATE, false>), grid, block, 0, st, a, f, v, o, c.z, ckpt, (const T*)dh, ds, dcT, (T*)df, (T*)dv, (T*)dg, gs, dc0,
+               nullptr);
   ARD_LAUNCH_CHECK("glr_bwd_kernel");
   return ARD_OK;
 }

@@ -66,6 +66,29 @@ template <int N> __device__ __forceinline__ void store_run(uint16_t* p, const fl
     *reinterpret_cast<typename Run<uint16_t, N>::V*>(p) = v;
   }
 }
+// the same past the caches' order of use, for what nothing reads again soon
+template <int N> __device__ __forceinline__ void store_run_past(float* p, const float (&x)[N]) {
+  static_assert(N == 1, "");
+  __builtin_nontemporal_store(x[0], p);
+}
+template <int N> __device__ __forceinline__ void store_run_past(uint16_t* p, const float (&x)[N]) {
+  if constexpr (N == 1) __builtin_nontemporal_store((uint16_t)bf16_pair(x[0], 0.0f), p);
+  else __builtin_nontemporal_store(bf16_pair(x[0], x[1]), reinterpret_cast<typename Run<uint16_t, N>::V*>(p));
+}
+
+// A run of a lane as it lies in memory, to be taken apart where it is used (two bf16 stay one register until then).
+template <typename T, int N> struct Raw;
+template <> struct Raw<float, 1> { float v; };
+template <> struct Raw<uint16_t, 1> { uint16_t v; };
+template <> struct Raw<uint16_t, 2> { uint32_t v; };
+template <typename T, int N> __device__ __forceinline__ Raw<T, N> load_raw(const T* p) {
+  if constexpr (N == 1) return Raw<T, N>{*p};
+  else return Raw<T, N>{*reinterpret_cast<const typename Run<T, N>::V*>(p)};
+}
+__device__ __forceinline__ float part_of(const Raw<float, 1>& r, int) { return r.v; }
+__device__ __forceinline__ float part_of(const Raw<uint16_t, 1>& r, int) { return bf16_bits_to_f32(r.v); }
+__device__ __forceinline__ float part_of(const Raw<uint16_t, 2>& r, int j) { return __uint_as_float(j ? r.v & 0xffff0000u : r.v << 16); }
+
 // the first n of N elements (n >= N: all, one access), the others 0
 template <int N, typename T> __device__ __forceinline__ void load_some(const T* p, int n, float (&x)[N]) {
   if (n >= N) {

@@ -61,11 +61,11 @@ def _check(T, B, H, dtype, gate=True, ragged=False, start=True, seed=0):
                 for b in range(B):
                     x[n[b]:, b] = float("nan") if b % 2 else float("inf")
     h, cT, ckpt = ard.glr_fwd(fd, vd, od, _dev(c0), nd)
-    assert ckpt.shape == (-(-T // 16), B, H)
+    assert ckpt.shape == (-(-T // ard.GLR_CHUNK), B, H)
     grads = ard.glr_bwd(fd, vd, od, dhd, ckpt, _dev(dcT), nd)
     dead = None if n is None else np.broadcast_to(np.arange(T)[:, None, None] >= n[None, :, None], (T, B, H))
     _compare(dtype, (rh, rcT) + rgrads, (h, cT) + grads, dead)
-    assert_parity(ckpt, states[0:T:16], "f32", None, "states kept")
+    assert_parity(ckpt, states[0:T:ard.GLR_CHUNK], "f32", None, "states kept")
     # (without kept states: the same results)
     h2, cT2, none = ard.glr_fwd(fd, vd, od, _dev(c0), nd, train=False)
     assert none is None and np.array_equal(raw_bits(h2), raw_bits(h)) and torch.equal(cT2, cT)
@@ -209,7 +209,7 @@ def test_same_bits_on_every_call_and_in_a_graph():
     f, v, o, dh, c0, dcT = _inputs(T, B, H, "bf16", True, 4)
     fd, vd, od, dhd = (_dev(x, "bf16") for x in (f, v, o, dh))
     c0d, dcTd = _dev(c0), _dev(dcT)
-    out = (torch.empty_like(fd), torch.empty_like(c0d), torch.empty((-(-T // 16), B, H), device="cuda"))
+    out = (torch.empty_like(fd), torch.empty_like(c0d), torch.empty((-(-T // ard.GLR_CHUNK), B, H), device="cuda"))
     grads = tuple(torch.empty_like(fd) for _ in range(3)) + (torch.empty_like(c0d),)
     ws = torch.empty(ard.glr_workspace_bytes(ard.BF16, T, B, H), dtype=torch.uint8, device="cuda")
 
