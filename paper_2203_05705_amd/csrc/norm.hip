@@ -5,10 +5,12 @@
 //
 // Every pass is bound by memory: a row is read once into registers, its mean and then its centred square sum (no
 // difference of large sums) are taken there in fp32, and its result is rounded once, when it is stored.  A row belongs
-// to G threads: a wavefront where its elements fit that one's registers, else a workgroup of 256 or 1024 threads; longer
+// to G threads, 16 elements each: a wavefront, or a workgroup of 128 to 1024 threads; longer
 // rows are read again from the cache.  The backward pass keeps dgamma and dbeta of a thread's columns in registers over
 // all the rows that its workgroup takes, so the sums over rows cost one row of partial sums for each workgroup and a
 // second, small pass that adds them in a fixed order.
+#include <type_traits>
+
 #include "rows.hpp"
 
 namespace ard {
@@ -20,7 +22,7 @@ struct NormRows {
   float eps, d;       // d = D
 };
 
-constexpr int kNormElems = 16;  // elements of a row a thread holds (a wavefront: 1024, 256 threads: 4096, 1024: 16384)
+constexpr int kNormElems = 16;  // elements of a row that a thread holds (a wavefront: 1024, 1024 threads: 16384)
 
 // sum over the G threads of a row; `slot`: LDS of this sum alone (one float for each wavefront)
 template <int G> __device__ __forceinline__ float group_sum(float v, float* slot) {
@@ -44,34 +46,74 @@ template <int N, typename WT> __device__ __forceinline__ void load_weight(const 
   }
 }
 
-template <typename T, typename WT, int G>
+// Where a thread's k-th run of CE elements lies: the run that the row's end cuts lies back from it, so that every access is a
+// whole one inside the row (rows have CE elements at least); its first `skip` elements are other threads', as are all of the
+// runs behind the end.
+template <int CE, int G> struct RunAt {
+  int col, skip;
+  __device__ __forceinline__ RunAt(int k, int lane, int D) {
+    const int c = (k * G + lane) * CE;
+    col = imin(c, D - CE), skip = c - col;
+  }
+};
+template <int CE, typename T> __device__ __forceinline__ void store_own(T* p, int skip, const float (&x)[CE]) {
+  if (skip == 0) {
+    store_run<CE>(p, x);
+  } else if (skip < CE) {
+#pragma unroll
+    for (int j = 1; j < CE; ++j)
+      if (j >= skip) p[j] = ElemTraits<T>::from_f32(x[j]);
+  }
+}
+// zeros behind the D elements of a compact row
+template <typename T> __device__ __forceinline__ void store_padding(const NormRows& a, T* y, int lane) {
+  if (lane < a.wide - a.D) y[a.D + lane] = ElemTraits<T>::from_f32(0.0f);
+}
+
+template <typename T, typename WT, int G, int CE, int NV>
 __global__ __launch_bounds__(G == 64 ? 256 : G) void norm_fwd_kernel(NormRows a, const T* X, const WT* gamma, const WT* beta, T* Y, float* mean,
                                                                      float* rstd) {
-  constexpr int CE = ElemTraits<T>::CE, NV = kNormElems / CE;
   __shared__ float slots[2][G > 64 ? G / 64 : 1];
   constexpr int WAVES = G == 64 ? 4 : 1;
   const int lane = threadIdx.x % G;
-  for (int64_t row = (int64_t)blockIdx.x * WAVES + (G == 64 ? threadIdx.x >> 6 : 0); row < a.R; row += (int64_t)gridDim.x * WAVES) {
-    const T* x = X + row * a.ldx;
+  const int64_t first = (int64_t)blockIdx.x * WAVES + (G == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
+  const int64_t step = (int64_t)gridDim.x * WAVES;
+  // a row is asked for while the one before it is worked on; the weights are held for all
+  typename Run<T, CE>::V rx[NV];
+  typename Run<WT, CE>::V rg[NV], rb[NV];
+  auto ask = [&](int64_t row) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) rx[k] = load_whole<CE>(X + row * a.ldx + RunAt<CE, G>(k, lane, a.D).col);
+  };
+  if (first < a.R) ask(first);
+  if (gamma) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) rg[k] = load_whole<CE>(gamma + RunAt<CE, G>(k, lane, a.D).col);
+  }
+  if (beta) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) rb[k] = load_whole<CE>(beta + RunAt<CE, G>(k, lane, a.D).col);
+  }
+  for (int64_t row = first; row < a.R; row += step) {
     T* y = Y + row * a.ldy;
     float v[NV][CE], s = 0.0f;
 #pragma unroll
+    for (int k = 0; k < NV; ++k) values_of<CE, T>(rx[k], v[k]);
+    if (row + step < a.R) ask(row + step);
+#pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int col = (k * G + lane) * CE;
-      load_some<CE>(x + col, a.D - col, v[k]);
+      const int skip = RunAt<CE, G>(k, lane, a.D).skip;
+#pragma unroll
+      for (int j = 0; j < CE; ++j) s += j >= skip ? v[k][j] : 0.0f;
     }
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-      for (int j = 0; j < CE; ++j) s += v[k][j];
     const float mu = group_sum<G>(s, slots[0]) / a.d;
     float q = 0.0f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int n = a.D - (k * G + lane) * CE;
+      const int skip = RunAt<CE, G>(k, lane, a.D).skip;
 #pragma unroll
       for (int j = 0; j < CE; ++j) {
-        v[k][j] = j < n ? v[k][j] - mu : 0.0f;
+        v[k][j] = j >= skip ? v[k][j] - mu : 0.0f;
         q = fmaf(v[k][j], v[k][j], q);
       }
     }
@@ -79,15 +121,25 @@ __global__ __launch_bounds__(G == 64 ? 256 : G) void norm_fwd_kernel(NormRows a,
     if (lane == 0) mean[row] = mu, rstd[row] = r;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int col = (k * G + lane) * CE, n = a.D - col;
-      if (col >= a.wide) continue;
-      float g[CE], b[CE];
-      load_weight<CE>(gamma, col, n, 1.0f, g);
-      load_weight<CE>(beta, col, n, 0.0f, b);
+      const RunAt<CE, G> at(k, lane, a.D);
+      float w[CE], u[CE];
+      if (gamma) {
+        values_of<CE, WT>(rg[k], w);
+      } else {
 #pragma unroll
-      for (int j = 0; j < CE; ++j) g[j] = j < n ? fmaf(v[k][j] * r, g[j], b[j]) : 0.0f;
-      store_some<CE>(y + col, a.wide - col, g);
+        for (int j = 0; j < CE; ++j) w[j] = 1.0f;
+      }
+      if (beta) {
+        values_of<CE, WT>(rb[k], u);
+      } else {
+#pragma unroll
+        for (int j = 0; j < CE; ++j) u[j] = 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < CE; ++j) w[j] = fmaf(v[k][j] * r, w[j], u[j]);
+      store_own<CE>(y + at.col, at.skip, w);
     }
+    store_padding(a, y, lane);
     // (the next row's first sum is written after every wavefront has passed this row's second barrier, hence has read the
     // first; its second sum after the next row's first barrier: the slots need no barrier of their own)
   }
@@ -137,91 +189,114 @@ struct NormBack {
   int64_t lddy, lddx;
 };
 
-// One row of partial sums [2][D] for each workgroup: dgamma, dbeta of the rows it took.
-template <typename T, typename WT, int G>
-__global__ __launch_bounds__(G == 64 ? 256 : G) void norm_bwd_kernel(NormBack b, const T* dY, const T* X, const WT* gamma, const float* mean,
+// One row of partial sums [2][D] for each workgroup: dgamma, dbeta of the rows it took.  A workgroup of 8 wavefronts (16 for
+// rows of 1024 threads) works on as many rows at a time as it has groups of G threads and adds up their sums in LDS: a partial
+// row for every group would be a third of the traffic of 8192 rows of 1024.
+constexpr int norm_bwd_threads(int G) { return G > 512 ? G : 512; }
+template <typename T, typename WT, int G, int CE, int NV>
+__global__ __launch_bounds__(norm_bwd_threads(G)) void norm_bwd_kernel(NormBack b, const T* dY, const T* X, const WT* gamma, const float* mean,
                                                                      const float* rstd, T* dX, float* part) {
-  constexpr int CE = ElemTraits<T>::CE, NV = kNormElems / CE, WAVES = G == 64 ? 4 : 1;
-  __shared__ float slots[2][2][G > 64 ? G / 64 : 1];
-  __shared__ float sums[G == 64 ? 3 : 1][G == 64 ? 2 * 64 * kNormElems : 1];
-  const int lane = threadIdx.x % G, D = b.a.D;
+  constexpr int GROUPS = norm_bwd_threads(G) / G, N = NV * CE, W = G / 64;  // rows at a time, elements of a thread, wavefronts of a row
+  constexpr bool AHEAD = G < 1024;  // the next row is asked for while one is worked on, and gamma is held (16 wavefronts have no registers for either)
+  __shared__ float slots[2][2][GROUPS][W];
+  __shared__ float sums[GROUPS > 1 ? GROUPS - 1 : 1][GROUPS > 1 ? 2 * G * N : 1];
+  const int lane = threadIdx.x % G, group = __builtin_amdgcn_readfirstlane(threadIdx.x / G), D = b.a.D;
   float g[NV][CE], ag[NV][CE] = {}, ab[NV][CE] = {};
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int col = (k * G + lane) * CE;
-    load_weight<CE>(gamma, col, D - col, 1.0f, g[k]);
-  }
-  int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * WAVES + (G == 64 ? threadIdx.x >> 6 : 0); row < b.a.R; row += (int64_t)gridDim.x * WAVES, turn ^= 1) {
-    const T *x = X + row * b.a.ldx, *dy = dY + row * b.lddy;
-    float v[NV][CE], u[NV][CE];
+  auto weights = [&] {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int col = (k * G + lane) * CE;
-      load_some<CE>(x + col, D - col, v[k]);
-      load_some<CE>(dy + col, D - col, u[k]);
+      if (gamma) {
+        values_of<CE, WT>(load_whole<CE>(gamma + RunAt<CE, G>(k, lane, D).col), g[k]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < CE; ++j) g[k][j] = 1.0f;
+      }
     }
-    const float mu = mean[row], r = rstd[row];
+  };
+  if (AHEAD) weights();
+  const int64_t first = (int64_t)blockIdx.x * GROUPS, step = (int64_t)gridDim.x * GROUPS;
+  typename Run<T, CE>::V nx[NV], ny[NV];
+  float nmu = 0.0f, nr = 0.0f;
+  auto ask = [&](int64_t row) {
+    const T *x = X + row * b.a.ldx, *dy = dY + row * b.lddy;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int col = RunAt<CE, G>(k, lane, D).col;
+      nx[k] = load_whole<CE>(x + col);
+      ny[k] = load_whole<CE>(dy + col);
+    }
+    nmu = mean[row], nr = rstd[row];
+  };
+  if (AHEAD && first + group < b.a.R) ask(first + group);
+  int turn = 0;
+  // (every group takes as many turns, so all meet at the barriers; one without a row of its own in the last turn adds nothing)
+  for (int64_t row0 = first; row0 < b.a.R; row0 += step, turn ^= 1) {
+    const int64_t row = row0 + group;
+    const bool mine = GROUPS == 1 || row < b.a.R;
+    if (!AHEAD) ask(row), weights();
+    float v[NV][CE], u[NV][CE];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) values_of<CE, T>(nx[k], v[k]), values_of<CE, T>(ny[k], u[k]);
+    const float mu = nmu, r = nr;
+    if (AHEAD && row + step < b.a.R) ask(row + step);
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int n = D - (k * G + lane) * CE;
+      const int skip = RunAt<CE, G>(k, lane, D).skip;
 #pragma unroll
       for (int j = 0; j < CE; ++j) {
-        v[k][j] = j < n ? (v[k][j] - mu) * r : 0.0f;
+        v[k][j] = j >= skip && mine ? (v[k][j] - mu) * r : 0.0f;
+        u[k][j] = j >= skip && mine ? u[k][j] : 0.0f;
         ag[k][j] = fmaf(u[k][j], v[k][j], ag[k][j]);
         ab[k][j] += u[k][j];
-        u[k][j] = j < n ? u[k][j] * g[k][j] : 0.0f;
+        u[k][j] *= g[k][j];
         s1 += u[k][j];
         s2 = fmaf(u[k][j], v[k][j], s2);
       }
     }
-    if constexpr (G == 64) {
-      s1 = wave_sum(s1) / b.a.d, s2 = wave_sum(s2) / b.a.d;
-    } else {  // (two sums at one barrier; the next row's go to the other slots, so none is read while it is written)
-      s1 = wave_sum(s1), s2 = wave_sum(s2);
-      if ((threadIdx.x & 63) == 0) slots[turn][0][threadIdx.x >> 6] = s1, slots[turn][1][threadIdx.x >> 6] = s2;
+    s1 = wave_sum(s1), s2 = wave_sum(s2);
+    if constexpr (G > 64) {  // (two sums at one barrier; the next row's go to the other slots, so none is read while it is written)
+      if ((threadIdx.x & 63) == 0) slots[turn][0][group][lane >> 6] = s1, slots[turn][1][group][lane >> 6] = s2;
       __syncthreads();
-      s1 = slots[turn][0][0], s2 = slots[turn][1][0];
+      s1 = slots[turn][0][group][0], s2 = slots[turn][1][group][0];
 #pragma unroll
-      for (int w = 1; w < G / 64; ++w) s1 += slots[turn][0][w], s2 += slots[turn][1][w];
-      s1 /= b.a.d, s2 /= b.a.d;
+      for (int w = 1; w < W; ++w) s1 += slots[turn][0][group][w], s2 += slots[turn][1][group][w];
     }
+    if (!mine) break;  // (the last turn)
+    s1 /= b.a.d, s2 /= b.a.d;
     T* dx = dX + row * b.lddx;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int col = (k * G + lane) * CE, n = D - col;
-      if (col >= b.a.wide) continue;
+      const RunAt<CE, G> at(k, lane, D);
 #pragma unroll
-      for (int j = 0; j < CE; ++j) u[k][j] = j < n ? r * (u[k][j] - s1 - v[k][j] * s2) : 0.0f;
-      store_some<CE>(dx + col, b.a.wide - col, u[k]);
+      for (int j = 0; j < CE; ++j) u[k][j] = r * (u[k][j] - s1 - v[k][j] * s2);
+      store_own<CE>(dx + at.col, at.skip, u[k]);
     }
+    store_padding(b.a, dx, lane);
   }
   if (!part) return;
   float* out = part + (int64_t)blockIdx.x * 2 * D;
-  if constexpr (G == 64) {  // the four wavefronts' sums, added in order
-    const int w = threadIdx.x >> 6;
-    if (w) {
+  if constexpr (GROUPS > 1) {  // the groups' sums, added in order
+    if (group) {
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int j = 0; j < CE; ++j) sums[w - 1][(k * CE + j) * 64 + lane] = ag[k][j], sums[w - 1][(kNormElems + k * CE + j) * 64 + lane] = ab[k][j];
+        for (int j = 0; j < CE; ++j) sums[group - 1][(k * CE + j) * G + lane] = ag[k][j], sums[group - 1][(N + k * CE + j) * G + lane] = ab[k][j];
     }
     __syncthreads();
-    if (w) return;
+    if (group) return;
 #pragma unroll
-    for (int o = 0; o < 3; ++o)
+    for (int o = 0; o < GROUPS - 1; ++o)
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int j = 0; j < CE; ++j) ag[k][j] += sums[o][(k * CE + j) * 64 + lane], ab[k][j] += sums[o][(kNormElems + k * CE + j) * 64 + lane];
+        for (int j = 0; j < CE; ++j) ag[k][j] += sums[o][(k * CE + j) * G + lane], ab[k][j] += sums[o][(N + k * CE + j) * G + lane];
   }
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int col = (k * G + lane) * CE;
-    if (col >= D) continue;
-    store_some<CE>(out + col, D - col, ag[k]);
-    store_some<CE>(out + D + col, D - col, ab[k]);
+    const RunAt<CE, G> at(k, lane, D);
+    store_own<CE>(out + at.col, at.skip, ag[k]);
+    store_own<CE>(out + D + at.col, at.skip, ab[k]);
   }
 }
 
@@ -281,20 +356,24 @@ __global__ __launch_bounds__(64) void norm_bwd_cols_kernel(NormBack b, const T* 
   store_some<CE>(out + b.a.D, n, ab);
 }
 
-// dgamma (columns 0..D-1 of the partial sums) and dbeta (the others): 64 columns a workgroup, P rows dealt to its 16
-// wavefronts, their sums added in order
+// dgamma (columns 0..D-1 of the partial sums) and dbeta (the others): 16 columns a workgroup, the P rows dealt to 64 lanes of
+// it each, whose sums are added in order.  Few columns a workgroup make many workgroups with a few loads in flight a lane:
+// for 512 rows of 2 x 1024 columns 64 columns took 10.8 us, 16 take 3.5.
 template <typename WT>
 __global__ __launch_bounds__(1024) void norm_weight_grad_kernel(int D, int P, const float* part, WT* dgamma, WT* dbeta) {
-  __shared__ float sums[16][64];
-  const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), cols = 2 * (int64_t)D;
+  __shared__ float sums[64][17];
+  const int c = threadIdx.x & 15, at = threadIdx.x >> 4;
+  const int64_t cols = 2 * (int64_t)D, col = (int64_t)blockIdx.x * 16 + c;
   float s = 0.0f;
-  if (col < cols)
-    for (int p = threadIdx.x >> 6; p < P; p += 16) s += part[p * cols + col];
-  sums[threadIdx.x >> 6][threadIdx.x & 63] = s;
+  if (col < cols) {
+#pragma unroll 8
+    for (int p = at; p < P; p += 64) s += part[p * cols + col];
+  }
+  sums[at][c] = s;
   __syncthreads();
-  if (threadIdx.x >= 64 || col >= cols) return;
-#pragma unroll
-  for (int w = 1; w < 16; ++w) s += sums[w][threadIdx.x];
+  if (threadIdx.x >= 16 || col >= cols) return;
+#pragma unroll 8
+  for (int w = 1; w < 64; ++w) s += sums[w][c];
   if (col < D) {
     if (dgamma) dgamma[col] = ElemTraits<WT>::from_f32(s);
   } else if (dbeta) {
@@ -303,15 +382,39 @@ __global__ __launch_bounds__(1024) void norm_weight_grad_kernel(int D, int P, co
 }
 
 // threads a row belongs to; 0: rows too long for registers
-static int norm_group(int wide) { return wide <= 64 * kNormElems ? 64 : wide <= 256 * kNormElems ? 256 : wide <= 1024 * kNormElems ? 1024 : 0; }
+static int norm_group(int D) {
+  for (int g = 64; g <= 1024; g *= 2)
+    if (D <= g * kNormElems) return g;
+  return 0;
+}
 // workgroups of the backward pass, each with a row of partial sums
-static int norm_parts(int R, int wide) {
-  const int g = norm_group(wide);
-  return g == 64 ? imin(R / 4 + (R % 4 != 0), 512) : g == 256 ? imin(R, 512) : g == 1024 ? imin(R, 256) : imin(R, 64);
+#ifndef NPART
+#define NPART 256
+#endif
+static int norm_parts(int R, int D) {
+  const int g = norm_group(D), rows = g ? norm_bwd_threads(g) / g : 1;  // rows a workgroup takes at a time
+  return imin(R / rows + (R % rows != 0), g ? NPART : 64);
+}
+
+// Calls with<threads of a row, elements of a run, runs>: runs of 16 bytes, or of single elements where a row has not more than
+// a wavefront's worth of those (or too few for a run).
+template <typename T, class F> static void norm_instance(int D, F&& with) {
+  constexpr int CE = ElemTraits<T>::CE, NV = kNormElems / CE;
+  using std::integral_constant;
+  if (D <= 64) return with(integral_constant<int, 64>(), integral_constant<int, 1>(), integral_constant<int, 1>());
+  switch (norm_group(D)) {
+    case 64: return with(integral_constant<int, 64>(), integral_constant<int, CE>(), integral_constant<int, NV>());
+    case 128: return with(integral_constant<int, 128>(), integral_constant<int, CE>(), integral_constant<int, NV>());
+    case 256: return with(integral_constant<int, 256>(), integral_constant<int, CE>(), integral_constant<int, NV>());
+    case 512: return with(integral_constant<int, 512>(), integral_constant<int, CE>(), integral_constant<int, NV>());
+    default: return with(integral_constant<int, 1024>(), integral_constant<int, CE>(), integral_constant<int, NV>());
+  }
 }
 
 // (the rows beyond a grid of this size are taken in turns: HIP counts a grid's threads in 32 bits)
 static unsigned norm_grid(int R) { return (unsigned)imin(R, 1 << 20); }
+// workgroups of the forward pass: 16 wavefronts a CU, which then go through their rows
+static unsigned norm_fwd_grid(int R, int G) { return (unsigned)(G == 64 ? imin(R / 4 + (R % 4 != 0), 1024) : imin(R, 1024 * 256 / G)); }
 
 static int32_t norm_check(int32_t dtype, int32_t wdtype, int32_t R, int32_t D, int32_t flags, std::initializer_list<int64_t> lds, std::initializer_list<int64_t> out_lds) {
   if (dtype != ARD_F32 && dtype != ARD_BF16) return fail(ARD_EDTYPE, "unknown dtype %d", dtype);
@@ -332,12 +435,13 @@ static int32_t norm_fwd_t(const NormRows& a, const void* X, const void* gamma, c
   const T* x = (const T*)X;
   const WT *g = (const WT*)gamma, *b = (const WT*)beta;
   T* y = (T*)Y;
-  switch (norm_group(a.wide)) {
-    case 64: ARD_LAUNCH((norm_fwd_kernel<T, WT, 64>), dim3(norm_grid(a.R / 4 + (a.R % 4 != 0))), dim3(256), 0, st, a, x, g, b, y, mean, rstd); break;
-    case 256: ARD_LAUNCH((norm_fwd_kernel<T, WT, 256>), dim3(norm_grid(a.R)), dim3(256), 0, st, a, x, g, b, y, mean, rstd); break;
-    case 1024: ARD_LAUNCH((norm_fwd_kernel<T, WT, 1024>), dim3(norm_grid(a.R)), dim3(1024), 0, st, a, x, g, b, y, mean, rstd); break;
-    default: ARD_LAUNCH((norm_fwd_long_kernel<T, WT>), dim3(norm_grid(a.R)), dim3(1024), 0, st, a, x, g, b, y, mean, rstd);
-  }
+  if (norm_group(a.D))
+    norm_instance<T>(a.D, [&](auto G, auto CE, auto NV) {
+      ARD_LAUNCH((norm_fwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(norm_fwd_grid(a.R, G.value)),
+                 dim3(G.value == 64 ? 256 : G.value), 0, st, a, x, g, b, y, mean, rstd);
+    });
+  else
+    ARD_LAUNCH((norm_fwd_long_kernel<T, WT>), dim3(norm_grid(a.R)), dim3(1024), 0, st, a, x, g, b, y, mean, rstd);
   ARD_LAUNCH_CHECK("norm_fwd_kernel");
   return ARD_OK;
 }
@@ -348,19 +452,19 @@ static int32_t norm_bwd_t(const NormBack& b, const void* dY, const void* X, cons
   const T *dy = (const T*)dY, *x = (const T*)X;
   const WT* g = (const WT*)gamma;
   T* dx = (T*)dX;
-  const int P = norm_parts(b.a.R, b.a.wide), D = b.a.D;
-  switch (norm_group(b.a.wide)) {
-    case 64: ARD_LAUNCH((norm_bwd_kernel<T, WT, 64>), dim3(P), dim3(256), 0, st, b, dy, x, g, mean, rstd, dx, part); break;
-    case 256: ARD_LAUNCH((norm_bwd_kernel<T, WT, 256>), dim3(P), dim3(256), 0, st, b, dy, x, g, mean, rstd, dx, part); break;
-    case 1024: ARD_LAUNCH((norm_bwd_kernel<T, WT, 1024>), dim3(P), dim3(1024), 0, st, b, dy, x, g, mean, rstd, dx, part); break;
-    default:
-      ARD_LAUNCH((norm_bwd_long_kernel<T, WT>), dim3(norm_grid(b.a.R)), dim3(1024), 0, st, b, dy, x, g, mean, rstd, dx);
-      ARD_LAUNCH_CHECK("norm_bwd_long_kernel");
-      if (part) ARD_LAUNCH((norm_bwd_cols_kernel<T>), dim3(ceil_div(D, 64 * ElemTraits<T>::CE), P), dim3(64), 0, st, b, dy, x, mean, rstd, part);
+  const int P = norm_parts(b.a.R, b.a.D), D = b.a.D;
+  if (norm_group(D)) {
+    norm_instance<T>(D, [&](auto G, auto CE, auto NV) {
+      ARD_LAUNCH((norm_bwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(P), dim3(norm_bwd_threads(G.value)), 0, st, b, dy, x, g, mean, rstd, dx, part);
+    });
+  } else {
+    ARD_LAUNCH((norm_bwd_long_kernel<T, WT>), dim3(norm_grid(b.a.R)), dim3(1024), 0, st, b, dy, x, g, mean, rstd, dx);
+    ARD_LAUNCH_CHECK("norm_bwd_long_kernel");
+    if (part) ARD_LAUNCH((norm_bwd_cols_kernel<T>), dim3(ceil_div(D, 64 * ElemTraits<T>::CE), P), dim3(64), 0, st, b, dy, x, mean, rstd, part);
   }
   ARD_LAUNCH_CHECK("norm_bwd_kernel");
   if (!part) return ARD_OK;
-  ARD_LAUNCH((norm_weight_grad_kernel<WT>), dim3((unsigned)((2 * (int64_t)D + 63) / 64)), dim3(1024), 0, st, D, P, part, (WT*)dgamma, (WT*)dbeta);
+  ARD_LAUNCH((norm_weight_grad_kernel<WT>), dim3((unsigned)((2 * (int64_t)D + 15) / 16)), dim3(1024), 0, st, D, P, part, (WT*)dgamma, (WT*)dbeta);
   ARD_LAUNCH_CHECK("norm_weight_grad_kernel");
   return ARD_OK;
 }
@@ -371,8 +475,7 @@ using namespace ard;
 
 extern "C" size_t ard_layer_norm_workspace_bytes(int32_t R, int32_t D) {
   if (R <= 0 || D <= 0 || D > 1 << 30) return 0;
-  // (a row may be stored in D or in pad8(D) columns: whichever needs more partial sums)
-  return (size_t)imax(norm_parts(R, D), norm_parts(R, pad8(D))) * 2 * D * sizeof(float);
+  return (size_t)norm_parts(R, D) * 2 * D * sizeof(float);
 }
 
 extern "C" int32_t ard_layer_norm_fwd(int32_t dtype, int32_t wdtype, int32_t R, int32_t D, const void* X, int64_t ldx, const void* gamma,
@@ -402,7 +505,7 @@ extern "C" int32_t ard_layer_norm_bwd(int32_t dtype, int32_t wdtype, int32_t R, 
   const NormBack b{{R, D, flags & ARD_OUT_COMPACT ? pad8(D) : D, ldx, 0, 0.0f, (float)D}, lddy, lddx};
   float* part = nullptr;
   if (dgamma || dbeta) {
-    const size_t need = (size_t)norm_parts(R, b.a.wide) * 2 * D * sizeof(float);
+    const size_t need = (size_t)norm_parts(R, D) * 2 * D * sizeof(float);
     if (!ws || ws_bytes < need || misaligned(ws, 4)) return fail(ARD_EWORKSPACE, "workspace too small: need %zu bytes, got %zu", need, ws ? ws_bytes : 0);
     part = (float*)ws;
   }

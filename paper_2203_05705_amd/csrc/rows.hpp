@@ -108,6 +108,23 @@ template <int N, typename T> __device__ __forceinline__ void store_some(T* p, in
     if (j < n) p[j] = ElemTraits<T>::from_f32(x[j]);
 }
 
+// A run of N elements as it lies in memory, and its values.
+template <typename T> struct Run<T, 1> { typedef T V; };
+template <int N, typename T> __device__ __forceinline__ typename Run<T, N>::V load_whole(const T* p) {
+  return *reinterpret_cast<const typename Run<T, N>::V*>(p);
+}
+template <int N, typename T> __device__ __forceinline__ void values_of(const typename Run<T, N>::V& v, float (&x)[N]) {
+  if constexpr (N == 1) {
+    x[0] = ElemTraits<T>::to_f32(v);
+  } else if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) x[2 * j] = __uint_as_float(v[j] << 16), x[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = v[j];
+  }
+}
+
 // ---- over a wavefront -----------------------------------------------------------
 // Cross-lane moves in the vector pipe (swaps inside quads, mirrors inside rows of 16, broadcasts of a row's last lane):
 // a sum of 64 lanes in seven instructions, without LDS.  Lane 63 ends with the whole; all lanes get it.
