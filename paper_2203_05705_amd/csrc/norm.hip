@@ -357,23 +357,29 @@ __global__ __launch_bounds__(64) void norm_bwd_cols_kernel(NormBack b, const T* 
 }
 
 // dgamma (columns 0..D-1 of the partial sums) and dbeta (the others): 16 columns a workgroup, the P rows dealt to 64 lanes of
-// it each, whose sums are added in order.  Few columns a workgroup make many workgroups with a few loads in flight a lane:
-// for 512 rows of 2 x 1024 columns 64 columns took 10.8 us, 16 take 3.5.
+// it each; the sums of a wavefront's four lanes of a column, then those of the 16 wavefronts, are added in order.  Few columns
+// a workgroup make many workgroups with a few loads in flight a lane.
 template <typename WT>
 __global__ __launch_bounds__(1024) void norm_weight_grad_kernel(int D, int P, const float* part, WT* dgamma, WT* dbeta) {
-  __shared__ float sums[64][17];
+  __shared__ float sums[16][16];
   const int c = threadIdx.x & 15, at = threadIdx.x >> 4;
   const int64_t cols = 2 * (int64_t)D, col = (int64_t)blockIdx.x * 16 + c;
   float s = 0.0f;
   if (col < cols) {
-#pragma unroll 8
+#pragma unroll 4
     for (int p = at; p < P; p += 64) s += part[p * cols + col];
   }
-  sums[at][c] = s;
+  s += __shfl_xor(s, 16);
+  s += __shfl_xor(s, 32);
+  if ((threadIdx.x & 63) < 16) sums[threadIdx.x >> 6][c] = s;
   __syncthreads();
   if (threadIdx.x >= 16 || col >= cols) return;
-#pragma unroll 8
-  for (int w = 1; w < 64; ++w) s += sums[w][c];
+  float parts[16];
+#pragma unroll
+  for (int w = 0; w < 16; ++w) parts[w] = sums[w][c];
+  s = parts[0];
+#pragma unroll
+  for (int w = 1; w < 16; ++w) s += parts[w];
   if (col < D) {
     if (dgamma) dgamma[col] = ElemTraits<WT>::from_f32(s);
   } else if (dbeta) {
@@ -388,12 +394,9 @@ static int norm_group(int D) {
   return 0;
 }
 // workgroups of the backward pass, each with a row of partial sums
-#ifndef NPART
-#define NPART 256
-#endif
 static int norm_parts(int R, int D) {
   const int g = norm_group(D), rows = g ? norm_bwd_threads(g) / g : 1;  // rows a workgroup takes at a time
-  return imin(R / rows + (R % rows != 0), g ? NPART : 64);
+  return imin(R / rows + (R % rows != 0), g ? 256 : 64);
 }
 
 // Calls with<threads of a row, elements of a run, runs>: runs of 16 bytes, or of single elements where a row has not more than

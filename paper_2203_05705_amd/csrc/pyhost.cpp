@@ -907,6 +907,22 @@ PyObject* tensors_or_none(const at::Tensor* t, int n) {
   return r;
 }
 
+// A workspace for calls that mostly need none: nothing is allocated then.
+struct SeldomWorkspace {
+  at::Tensor own;
+  void* p = nullptr;
+  size_t bytes = 0;
+  template <class F> SeldomWorkspace(const Args& a, int i, c10::Device dev, F&& need) {
+    if (a.given(i)) {
+      const at::Tensor& t = tensor_of(a.v[i], "ws");
+      p = t.data_ptr(), bytes = (size_t)t.numel() * t.element_size();
+    } else if (const size_t n = need()) {
+      own = at::empty({(int64_t)n}, at::TensorOptions().dtype(at::kByte).device(dev));
+      p = own.data_ptr(), bytes = n;
+    }
+  }
+};
+
 // The rows of a matrix, or of a contiguous tensor of more dimensions, whose last dimension holds D elements, or pad8(D) of a
 // compact activation.
 struct Rows {
@@ -1002,7 +1018,7 @@ PyObject* layer_norm_bwd(const Args& a) {  // dY, X, gamma, mean, rstd, D, out, 
         raise(PyExc_ValueError, "out: dgamma and dbeta have %d contiguous elements", D);
       grad[i - 1] = o[i].data_ptr();
     }
-  Workspace ws(a, 7, X.device(), [&] { return grad[0] || grad[1] ? lib().ard_layer_norm_workspace_bytes(x.R, D) : (size_t)0; });
+  SeldomWorkspace ws(a, 7, X.device(), [&] { return grad[0] || grad[1] ? lib().ard_layer_norm_workspace_bytes(x.R, D) : (size_t)0; });
   const void* gp = g ? g->data_ptr() : nullptr;
   void* st = stream_of(a.v[8]);
   enqueue(lib().ard_layer_norm_bwd, dt, wt, x.R, D, (const void*)dy.p, dy.ld, (const void*)x.p, x.ld, gp, mean, rstd, dx.p, dx.ld, grad[0], grad[1], flags,
@@ -1069,7 +1085,7 @@ PyObject* glr_fwd(const Args& a) {  // f, v, o, c0, lengths, train, H, out, ws, 
   if (!on_device(out[1], at::kFloat, "out").is_contiguous() || out[1].numel() != n) raise(PyExc_ValueError, "out: the state has [B, H] contiguous elements");
   if (out[2].defined() && (!on_device(out[2], at::kFloat, "out").is_contiguous() || out[2].numel() != chunks * n))
     raise(PyExc_ValueError, "out: the kept states have [ceil(T / %d), B, H] contiguous elements", ARD_GLR_CHUNK);
-  Workspace ws(a, 8, f.device(), [&] { return lib().ard_glr_workspace_bytes(s.dt, s.T, s.B, s.H); });
+  SeldomWorkspace ws(a, 8, f.device(), [&] { return lib().ard_glr_workspace_bytes(s.dt, s.T, s.B, s.H); });
   const void *fp = f.data_ptr(), *vp = v.data_ptr();
   void* hp = out[0].data_ptr();
   float *ct = (float*)out[1].data_ptr(), *ck = (float*)ptr(out[2]);
@@ -1112,7 +1128,7 @@ PyObject* glr_bwd(const Args& a) {  // f, v, o, dh, ckpt, dcT, lengths, H, out, 
   for (int i = 1; i < 3; ++i)
     if (out[i].defined()) s.strides(out[i], "out", &gs);
   if (!on_device(out[3], at::kFloat, "out").is_contiguous() || out[3].numel() != n) raise(PyExc_ValueError, "out: the state's gradient has [B, H] contiguous elements");
-  Workspace ws(a, 9, f.device(), [&] { return lib().ard_glr_workspace_bytes(s.dt, s.T, s.B, s.H); });
+  SeldomWorkspace ws(a, 9, f.device(), [&] { return lib().ard_glr_workspace_bytes(s.dt, s.T, s.B, s.H); });
   const void *fp = f.data_ptr(), *vp = v.data_ptr(), *hp = dh.data_ptr();
   void *g0 = out[0].data_ptr(), *g1 = out[1].data_ptr(), *g2 = ptr(out[2]);
   float* dc0 = (float*)out[3].data_ptr();
