@@ -5,7 +5,7 @@
 //
 // Every pass is bound by memory: a row is read once into registers, its mean and then its centred square sum (no
 // difference of large sums) are taken there in fp32, and its result is rounded once, when it is stored.  A row belongs
-// to G threads, 16 elements each: a wavefront, or a workgroup of 128 to 1024 threads; longer
+// to G threads, 16 elements each: 16, 32 or 64 lanes of a wavefront, or 128 to 1024 threads of a workgroup; longer
 // rows are read again from the cache.  The backward pass keeps dgamma and dbeta of a thread's columns in registers over
 // all the rows that its workgroup takes, so the sums over rows cost one row of partial sums for each workgroup and a
 // second, small pass that adds them in a fixed order.
@@ -24,11 +24,19 @@ struct NormRows {
 
 constexpr int kNormElems = 16;  // elements of a row that a thread holds (a wavefront: 1024, 1024 threads: 16384)
 
+// sum over the up to 64 lanes of a row that lie in one wavefront (16: a row of the cross-lane moves)
+template <int G> __device__ __forceinline__ float lanes_sum(float v) {
+  static_assert(G == 16 || G == 32 || G >= 64, "");
+  if constexpr (G >= 64) return wave_sum(v);
+  v = row_sum(v);
+  if constexpr (G == 32) v += __shfl_xor(v, 16);
+  return v;
+}
 // sum over the G threads of a row; `slot`: LDS of this sum alone (one float for each wavefront)
 template <int G> __device__ __forceinline__ float group_sum(float v, float* slot) {
-  v = wave_sum(v);
+  v = lanes_sum<G>(v);
   if constexpr (G > 64) {
-    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+    if ((threadIdx.x & 63) == 0) slot[threadIdx.x % G >> 6] = v;
     __syncthreads();
     v = slot[0];
 #pragma unroll
@@ -70,22 +78,24 @@ template <typename T> __device__ __forceinline__ void store_padding(const NormRo
   if (lane < a.wide - a.D) y[a.D + lane] = ElemTraits<T>::from_f32(0.0f);
 }
 
+constexpr int norm_fwd_threads(int G) { return G > 256 ? G : 256; }
+
 template <typename T, typename WT, int G, int CE, int NV>
-__global__ __launch_bounds__(G == 64 ? 256 : G) void norm_fwd_kernel(NormRows a, const T* X, const WT* gamma, const WT* beta, T* Y, float* mean,
-                                                                     float* rstd) {
-  __shared__ float slots[2][G > 64 ? G / 64 : 1];
-  constexpr int WAVES = G == 64 ? 4 : 1;
-  const int lane = threadIdx.x % G;
-  const int64_t first = (int64_t)blockIdx.x * WAVES + (G == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
-  const int64_t step = (int64_t)gridDim.x * WAVES;
+__global__ __launch_bounds__(norm_fwd_threads(G)) void norm_fwd_kernel(NormRows a, const T* X, const WT* gamma, const WT* beta, T* Y, float* mean,
+                                                                      float* rstd) {
+  constexpr int GROUPS = norm_fwd_threads(G) / G;  // rows at a time
+  __shared__ float slots[2][GROUPS][G > 64 ? G / 64 : 1];
+  const int lane = threadIdx.x % G, group = G >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / G) : threadIdx.x / G;
+  const int64_t step = (int64_t)gridDim.x * GROUPS;
   // a row is asked for while the one before it is worked on; the weights are held for all
   typename Run<T, CE>::V rx[NV];
   typename Run<WT, CE>::V rg[NV], rb[NV];
   auto ask = [&](int64_t row) {
+    if (GROUPS > 1) row = row < a.R ? row : a.R - 1;  // (a group without a row of its own reads the last one)
 #pragma unroll
     for (int k = 0; k < NV; ++k) rx[k] = load_whole<CE>(X + row * a.ldx + RunAt<CE, G>(k, lane, a.D).col);
   };
-  if (first < a.R) ask(first);
+  ask((int64_t)blockIdx.x * GROUPS + group);
   if (gamma) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) rg[k] = load_whole<CE>(gamma + RunAt<CE, G>(k, lane, a.D).col);
@@ -94,19 +104,21 @@ __global__ __launch_bounds__(G == 64 ? 256 : G) void norm_fwd_kernel(NormRows a,
 #pragma unroll
     for (int k = 0; k < NV; ++k) rb[k] = load_whole<CE>(beta + RunAt<CE, G>(k, lane, a.D).col);
   }
-  for (int64_t row = first; row < a.R; row += step) {
+  for (int64_t row0 = (int64_t)blockIdx.x * GROUPS; row0 < a.R; row0 += step) {
+    const int64_t row = row0 + group;
+    const bool mine = GROUPS == 1 || row < a.R;
     T* y = Y + row * a.ldy;
     float v[NV][CE], s = 0.0f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) values_of<CE, T>(rx[k], v[k]);
-    if (row + step < a.R) ask(row + step);
+    if (row0 + step < a.R) ask(row + step);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int skip = RunAt<CE, G>(k, lane, a.D).skip;
 #pragma unroll
       for (int j = 0; j < CE; ++j) s += j >= skip ? v[k][j] : 0.0f;
     }
-    const float mu = group_sum<G>(s, slots[0]) / a.d;
+    const float mu = group_sum<G>(s, slots[0][group]) / a.d;
     float q = 0.0f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -117,7 +129,8 @@ __global__ __launch_bounds__(G == 64 ? 256 : G) void norm_fwd_kernel(NormRows a,
         q = fmaf(v[k][j], v[k][j], q);
       }
     }
-    const float r = 1.0f / sqrtf(group_sum<G>(q, slots[1]) / a.d + a.eps);
+    const float r = 1.0f / sqrtf(group_sum<G>(q, slots[1][group]) / a.d + a.eps);
+    if (!mine) break;  // (the last turn)
     if (lane == 0) mean[row] = mu, rstd[row] = r;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -196,11 +209,12 @@ constexpr int norm_bwd_threads(int G) { return G > 512 ? G : 512; }
 template <typename T, typename WT, int G, int CE, int NV>
 __global__ __launch_bounds__(norm_bwd_threads(G)) void norm_bwd_kernel(NormBack b, const T* dY, const T* X, const WT* gamma, const float* mean,
                                                                      const float* rstd, T* dX, float* part) {
-  constexpr int GROUPS = norm_bwd_threads(G) / G, N = NV * CE, W = G / 64;  // rows at a time, elements of a thread, wavefronts of a row
+  constexpr int GROUPS = norm_bwd_threads(G) / G, N = NV * CE, W = G > 64 ? G / 64 : 1;  // rows at a time, elements of a thread, wavefronts of a row
+  constexpr int PARTS = GROUPS / (G < 64 ? 64 / G : 1);  // sums of groups that do not share a wavefront
   constexpr bool AHEAD = G < 1024;  // the next row is asked for while one is worked on, and gamma is held (16 wavefronts have no registers for either)
   __shared__ float slots[2][2][GROUPS][W];
-  __shared__ float sums[GROUPS > 1 ? GROUPS - 1 : 1][GROUPS > 1 ? 2 * G * N : 1];
-  const int lane = threadIdx.x % G, group = __builtin_amdgcn_readfirstlane(threadIdx.x / G), D = b.a.D;
+  __shared__ float sums[PARTS > 1 ? PARTS - 1 : 1][PARTS > 1 ? 2 * G * N : 1];
+  const int lane = threadIdx.x % G, group = G >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / G) : threadIdx.x / G, D = b.a.D;
   float g[NV][CE], ag[NV][CE] = {}, ab[NV][CE] = {};
   auto weights = [&] {
 #pragma unroll
@@ -218,6 +232,7 @@ __global__ __launch_bounds__(norm_bwd_threads(G)) void norm_bwd_kernel(NormBack 
   typename Run<T, CE>::V nx[NV], ny[NV];
   float nmu = 0.0f, nr = 0.0f;
   auto ask = [&](int64_t row) {
+    if (GROUPS > 1) row = row < b.a.R ? row : b.a.R - 1;  // (a group without a row of its own reads the last one)
     const T *x = X + row * b.a.ldx, *dy = dY + row * b.lddy;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -227,7 +242,7 @@ __global__ __launch_bounds__(norm_bwd_threads(G)) void norm_bwd_kernel(NormBack 
     }
     nmu = mean[row], nr = rstd[row];
   };
-  if (AHEAD && first + group < b.a.R) ask(first + group);
+  if (AHEAD) ask(first + group);
   int turn = 0;
   // (every group takes as many turns, so all meet at the barriers; one without a row of its own in the last turn adds nothing)
   for (int64_t row0 = first; row0 < b.a.R; row0 += step, turn ^= 1) {
@@ -238,7 +253,7 @@ __global__ __launch_bounds__(norm_bwd_threads(G)) void norm_bwd_kernel(NormBack 
 #pragma unroll
     for (int k = 0; k < NV; ++k) values_of<CE, T>(nx[k], v[k]), values_of<CE, T>(ny[k], u[k]);
     const float mu = nmu, r = nr;
-    if (AHEAD && row + step < b.a.R) ask(row + step);
+    if (AHEAD && row0 + step < b.a.R) ask(row + step);
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -254,7 +269,7 @@ __global__ __launch_bounds__(norm_bwd_threads(G)) void norm_bwd_kernel(NormBack 
         s2 = fmaf(u[k][j], v[k][j], s2);
       }
     }
-    s1 = wave_sum(s1), s2 = wave_sum(s2);
+    s1 = lanes_sum<G>(s1), s2 = lanes_sum<G>(s2);
     if constexpr (G > 64) {  // (two sums at one barrier; the next row's go to the other slots, so none is read while it is written)
       if ((threadIdx.x & 63) == 0) slots[turn][0][group][lane >> 6] = s1, slots[turn][1][group][lane >> 6] = s2;
       __syncthreads();
@@ -276,17 +291,27 @@ __global__ __launch_bounds__(norm_bwd_threads(G)) void norm_bwd_kernel(NormBack 
   }
   if (!part) return;
   float* out = part + (int64_t)blockIdx.x * 2 * D;
-  if constexpr (GROUPS > 1) {  // the groups' sums, added in order
-    if (group) {
+  if constexpr (G < 64) {  // those of a wavefront's groups, lane to lane
+#pragma unroll
+    for (int o = G; o < 64; o *= 2)
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int j = 0; j < CE; ++j) sums[group - 1][(k * CE + j) * G + lane] = ag[k][j], sums[group - 1][(N + k * CE + j) * G + lane] = ab[k][j];
+        for (int j = 0; j < CE; ++j) ag[k][j] += __shfl_xor(ag[k][j], o), ab[k][j] += __shfl_xor(ab[k][j], o);
+  }
+  if constexpr (PARTS > 1) {  // the groups' sums, added in order
+    const int of = G < 64 ? threadIdx.x >> 6 : group;
+    const bool speaks = G >= 64 || (threadIdx.x & 63) < G;
+    if (of && speaks) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int j = 0; j < CE; ++j) sums[of - 1][(k * CE + j) * G + lane] = ag[k][j], sums[of - 1][(N + k * CE + j) * G + lane] = ab[k][j];
     }
     __syncthreads();
-    if (group) return;
-#pragma unroll
-    for (int o = 0; o < GROUPS - 1; ++o)
+    if (of || !speaks) return;
+#pragma unroll 1
+    for (int o = 0; o < PARTS - 1; ++o)
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -389,7 +414,7 @@ __global__ __launch_bounds__(1024) void norm_weight_grad_kernel(int D, int P, co
 
 // threads a row belongs to; 0: rows too long for registers
 static int norm_group(int D) {
-  for (int g = 64; g <= 1024; g *= 2)
+  for (int g = 16; g <= 1024; g *= 2)
     if (D <= g * kNormElems) return g;
   return 0;
 }
@@ -399,17 +424,16 @@ static int norm_parts(int R, int D) {
   return imin(R / rows + (R % rows != 0), g ? 256 : 64);
 }
 
-// Calls with<threads of a row, elements of a run, runs>: runs of 16 bytes, or of single elements where a row has not more than
-// a wavefront's worth of those (or too few for a run).
+// Calls with<threads of a row, elements of a run, runs>: runs of 16 bytes, or of single elements where a row has too few for one.
 template <typename T, class F> static void norm_instance(int D, F&& with) {
   constexpr int CE = ElemTraits<T>::CE, NV = kNormElems / CE;
   using std::integral_constant;
-  if (D <= 64) return with(integral_constant<int, 64>(), integral_constant<int, 1>(), integral_constant<int, 1>());
+  if (D < CE) return with(integral_constant<int, 16>(), integral_constant<int, 1>(), integral_constant<int, 1>());
   switch (norm_group(D)) {
-    case 64: return with(integral_constant<int, 64>(), integral_constant<int, CE>(), integral_constant<int, NV>());
-    case 128: return with(integral_constant<int, 128>(), integral_constant<int, CE>(), integral_constant<int, NV>());
-    case 256: return with(integral_constant<int, 256>(), integral_constant<int, CE>(), integral_constant<int, NV>());
-    case 512: return with(integral_constant<int, 512>(), integral_constant<int, CE>(), integral_constant<int, NV>());
+#define ARD_NORM_GROUP(G) \
+  case G: return with(integral_constant<int, G>(), integral_constant<int, CE>(), integral_constant<int, NV>());
+    ARD_NORM_GROUP(16) ARD_NORM_GROUP(32) ARD_NORM_GROUP(64) ARD_NORM_GROUP(128) ARD_NORM_GROUP(256) ARD_NORM_GROUP(512)
+#undef ARD_NORM_GROUP
     default: return with(integral_constant<int, 1024>(), integral_constant<int, CE>(), integral_constant<int, NV>());
   }
 }
@@ -417,7 +441,10 @@ template <typename T, class F> static void norm_instance(int D, F&& with) {
 // (the rows beyond a grid of this size are taken in turns: HIP counts a grid's threads in 32 bits)
 static unsigned norm_grid(int R) { return (unsigned)imin(R, 1 << 20); }
 // workgroups of the forward pass: 16 wavefronts a CU, which then go through their rows
-static unsigned norm_fwd_grid(int R, int G) { return (unsigned)(G == 64 ? imin(R / 4 + (R % 4 != 0), 1024) : imin(R, 1024 * 256 / G)); }
+static unsigned norm_fwd_grid(int R, int G) {
+  const int rows = norm_fwd_threads(G) / G;
+  return (unsigned)imin(R / rows + (R % rows != 0), 1024 * 256 / norm_fwd_threads(G));
+}
 
 static int32_t norm_check(int32_t dtype, int32_t wdtype, int32_t R, int32_t D, int32_t flags, std::initializer_list<int64_t> lds, std::initializer_list<int64_t> out_lds) {
   if (dtype != ARD_F32 && dtype != ARD_BF16) return fail(ARD_EDTYPE, "unknown dtype %d", dtype);
@@ -441,7 +468,7 @@ static int32_t norm_fwd_t(const NormRows& a, const void* X, const void* gamma, c
   if (norm_group(a.D))
     norm_instance<T>(a.D, [&](auto G, auto CE, auto NV) {
       ARD_LAUNCH((norm_fwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(norm_fwd_grid(a.R, G.value)),
-                 dim3(G.value == 64 ? 256 : G.value), 0, st, a, x, g, b, y, mean, rstd);
+                 dim3(norm_fwd_threads(G.value)), 0, st, a, x, g, b, y, mean, rstd);
     });
   else
     ARD_LAUNCH((norm_fwd_long_kernel<T, WT>), dim3(norm_grid(a.R)), dim3(1024), 0, st, a, x, g, b, y, mean, rstd);
