@@ -60,6 +60,14 @@ def test_rows_longer_than_registers(R, D, dtype, wdtype):
     _check(R, D, dtype, wdtype, R + D)
 
 
+@pytest.mark.parametrize("R", [1, 2, 31, 33, 255, 511, 512, 513])
+@pytest.mark.parametrize("D", [3, 8, 130, 300, 1000, 2049, 9000])
+def test_few_rows(R, D):
+    """One launch up to 512 rows, two from 513 on."""
+    for dtype, wdtype in DTYPES:
+        _check(R, D, dtype, wdtype, R + D)
+
+
 @pytest.mark.parametrize("R,D", [(4097, 96), (2100, 1536), (300, 6000)])
 def test_more_rows_than_workgroups(R, D):
     _check(R, D, "bf16", "f32", R)
@@ -143,8 +151,9 @@ def test_rows_that_are_constant_or_hold_no_numbers(D):
     assert_parity(db, dY.sum(axis=0), "f32", None, "dbeta")
 
 
-def test_weights_gradients_one_at_a_time_and_none():
-    X, dY, g, b = _inputs(50, 300, "bf16", "f32", 1)
+@pytest.mark.parametrize("rows", [50, 700])
+def test_weights_gradients_one_at_a_time_and_none(rows):
+    X, dY, g, b = _inputs(rows, 300, "bf16", "f32", 1)
     Xd, dYd, gd, bd = from_vals(X, "bf16"), from_vals(dY, "bf16"), from_vals(g, "f32"), from_vals(b, "f32")
     Y, mean, rstd = ard.layer_norm_fwd(Xd, gd, bd)
     full = ard.layer_norm_bwd(dYd, Xd, gd, mean, rstd)

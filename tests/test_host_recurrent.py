@@ -57,18 +57,22 @@ def test_norm_accepts_and_refuses():
 def test_norm_backward_accepts_and_refuses():
     with D.dry_run() as lib:
         heap = D.FakeHeap()
-        assert lib.ard_layer_norm_bwd(*_norm_bwd_args(heap).values()) == 0
-        assert D.launches(lib) == (2, ["norm_bwd_kernel", "norm_weight_grad_kernel"])
-        assert lib.ard_layer_norm_bwd(*_norm_bwd_args(heap, dgamma=None, dbeta=None, ws=None, ws_bytes=0).values()) == 0
-        assert D.launches(lib) == (1, ["norm_bwd_kernel"])
-        for change in (dict(dgamma=None), dict(dbeta=None), dict(gamma=None)):
-            assert lib.ard_layer_norm_bwd(*_norm_bwd_args(heap, **change).values()) == 0 and D.launches(lib)[0] == 2
+        # few rows: one launch and no workspace; more: a second launch for the weights' gradients, if any are asked for
+        for R, kernels in ((4, ["norm_bwd_few_kernel"]), (512, ["norm_bwd_few_kernel"]), (513, ["norm_bwd_kernel", "norm_weight_grad_kernel"])):
+            for change in ({}, dict(dgamma=None), dict(dbeta=None), dict(gamma=None)):
+                assert lib.ard_layer_norm_bwd(*_norm_bwd_args(heap, R=R, **change).values()) == 0
+                assert D.launches(lib) == (len(kernels), kernels)
+            assert lib.ard_layer_norm_bwd(*_norm_bwd_args(heap, R=R, dgamma=None, dbeta=None, ws=None, ws_bytes=0).values()) == 0
+            assert D.launches(lib) == (1, kernels[:1])
+            assert (lib.ard_layer_norm_workspace_bytes(R, 24) > 0) == (R > 512)
+        assert lib.ard_layer_norm_bwd(*_norm_bwd_args(heap, ws=None, ws_bytes=0).values()) == 0
+        D.launches(lib)
         assert lib.ard_layer_norm_bwd(*_norm_bwd_args(heap, D=20000, ldx=20000, lddy=20000, lddx=20000, ws_bytes=1 << 30).values()) == 0
         assert D.launches(lib) == (3, ["norm_bwd_long_kernel", "norm_bwd_cols_kernel", "norm_weight_grad_kernel"])
-        need = lib.ard_layer_norm_workspace_bytes(4, 24)
-        assert need > 0 and lib.ard_layer_norm_bwd(*_norm_bwd_args(heap, ws_bytes=need).values()) == 0
+        need = lib.ard_layer_norm_workspace_bytes(600, 24)
+        assert need > 0 and lib.ard_layer_norm_bwd(*_norm_bwd_args(heap, R=600, ws_bytes=need).values()) == 0
         D.launches(lib)
-        for change, code in ((dict(ws_bytes=need - 1), -4), (dict(ws=None), -4), (dict(lddy=23), -2), (dict(lddx=23), -2), (dict(dY=None), -1), (dict(dX=None), -1),
+        for change, code in ((dict(R=600, ws_bytes=need - 1), -4), (dict(R=600, ws=None), -4), (dict(lddy=23), -2), (dict(lddx=23), -2), (dict(dY=None), -1), (dict(dX=None), -1),
                              (dict(mean=None), -1), (dict(rstd=None), -1), (dict(D=20, lddx=23, flags=ard.OUT_COMPACT), -2), (dict(dX=heap(64) + 1), -1),
                              (dict(dgamma=heap(64) + 2), -1)):
             assert lib.ard_layer_norm_bwd(*_norm_bwd_args(heap, **change).values()) == code, change
@@ -241,7 +245,7 @@ def test_calls_marshal_their_tensors():
 
 def test_calls_refuse():
     bf16 = torch.bfloat16
-    X, w, r, S = fake(30, 24, dtype=bf16), fake(24), fake(30), fake(4, 16)
+    X, w, r, S, many = fake(30, 24, dtype=bf16), fake(24), fake(30), fake(4, 16), fake(600, 24, dtype=bf16)
     f, h, ck = fake(9, 4, 16), fake(9, 4, 16), fake(2, 4, 16)
     p, c8, u8, s = fake(300), fake(300, dtype=torch.int8), fake(300, dtype=torch.uint8), fake(2)
     kw = dict(stream=STREAM)
@@ -260,7 +264,7 @@ def test_calls_refuse():
                 (TypeError, lambda: ard.layer_norm_bwd(X, X, w, None, r, out=(X, w, w), ws=fake_ws(), **kw)),
                 (ValueError, lambda: ard.layer_norm_bwd(fake(29, 24, dtype=bf16), X, w, r, r, out=(X, w, w), ws=fake_ws(), **kw)),
                 (ValueError, lambda: ard.layer_norm_bwd(X, X, w, r, r, out=(X, fake(25), w), ws=fake_ws(), **kw)),
-                (ard.ArdError, lambda: ard.layer_norm_bwd(X, X, w, r, r, out=(X, w, w), ws=fake_ws(16), **kw)),
+                (ard.ArdError, lambda: ard.layer_norm_bwd(many, many, w, fake(600), fake(600), out=(many, w, w), ws=fake_ws(16), **kw)),
                 (ValueError, lambda: ard.glr_fwd(f, fake(8, 4, 16), out=(h, S, ck), **kw)),
                 (ValueError, lambda: ard.glr_fwd(f, f, strided((9, 4, 16), (192, 48, 1)), out=(h, S, ck), **kw)),
                 (TypeError, lambda: ard.glr_fwd(f, fake(9, 4, 16, dtype=bf16), out=(h, S, ck), **kw)),
