@@ -472,8 +472,10 @@ static GlrPlan glr_plan(int32_t dtype, int T, int B, int H, int32_t flags, const
   const int turns = ceil_div(pieces, g.waves);
   int segs = 1;
   // Time is cut below 8 wavefronts a CU, into 16 a CU: with half as many 32768 x 1 x 1024 took 95 us (83 then), 8192 x 4 x 1024 97 (85);
-  // with twice as many 89 and 87, as more pairs are read.
-  if (have < 2048 && turns > 1) segs = imin(turns, (int)(4096 / have));
+  // with twice as many 89 and 87, as more pairs are read.  The second launch is worth four turns of 64 steps where there is
+  // little work (bf16 192 x 8 x 512 forward and backward 9.2 + 12.1 us in one launch, 10.1 + 11.5 in two; 256: 11.7 + 15.6, 10.6 + 11.5),
+  // the second reading eight where there is more (320 x 16 x 1000 18.0 + 23.4, 19.0 + 28.5; 1000: 58 + 87, 47 + 81).
+  if (have < 2048 && turns >= (have <= 512 ? 4 : 8)) segs = imin(turns, (int)(4096 / have));
   const int per = ceil_div(turns, segs);
   g.a.segs = ceil_div(turns, per);
   g.a.seg_steps = per * g.waves * kSteps;
