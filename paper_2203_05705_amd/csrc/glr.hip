@@ -8,14 +8,15 @@
 // compose.  A wavefront takes 8 steps of 64 lanes' channels into registers, makes their pair there, and the wavefronts
 // of a workgroup, which have neighbouring stretches, exchange pairs through LDS: every input is read once and every
 // output written once, and that traffic is what bounds these passes.  8 steps, not 16: half the registers, twice the
-// wavefronts whose loads are in flight (64 x 128 x 1024 bf16 with a gate: forward 16.6 us against 21.7).
+// wavefronts whose loads are in flight (64 x 128 x 1024 bf16 with a gate: forward 16.6 us against 21.7); the forward pass asks for
+// the next turn's steps while it works on one (14.6; the backward pass has no registers for it: 30 -> 33).
 // Where batch and channels alone give too few wavefronts, time is cut into segments for several workgroups; a first pass
 // then makes the segments' pairs (reading f and v, or f, o and dh, once more), and the main pass composes those before
 // its segment.  (One pass would have workgroups wait for others; the second reading comes partly out of the last cache.)
 // States, pairs and gradients in flight are fp32.  The backward pass starts from the states that the forward pass left
 // before every 8th step, so it needs no second scan for them.
 //
-// Measured, bf16 with a gate: 64 x 128 x 1024 forward 16.3 us, backward 23.8 behind it and 30 from memory (4.2, 3.9 TB/s; a large
+// Measured, bf16 with a gate: 64 x 128 x 1024 forward 14.6 us, backward 23.8 behind it and 30 from memory (4.9, 4.0 TB/s; a large
 // copy 4.9); 32768 x 1 x 1024 forward 25 + 49 us; 8192 x 4 x 1024 without one forward 27 + 43, backward 25 + 55; a single
 // step of 128 sequences 2.8 us.
 #include <type_traits>
@@ -128,16 +129,23 @@ template <bool CUT, int VEC, typename T> __device__ __forceinline__ void put(T* 
 }
 
 // ---- forward ------------------------------------------------------------------
+// A stretch's values as they lie in memory; in the place of steps from `steps` on, which nobody looks at, those of the last one
+// before (every register is written on every path, so loads stay in flight behind the branch).
+template <typename T, int VEC> __device__ __forceinline__ void ask(const T* p, int64_t st, int steps, Raw<T, VEC> (&r)[kSteps]) {
+  if (steps >= kSteps) {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) r[i] = load_raw<T, VEC>(p + i * st);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) r[i] = load_raw<T, VEC>(p + (int64_t)imin(i, steps - 1) * st);
+  }
+}
+
 // F and (1 - F) v of a stretch's steps, and its pair.  WHOLE: all of its steps are live; else the first `steps` are, and
 // the others leave the state as it is.
 template <bool WHOLE, typename T, int VEC>
-__device__ __forceinline__ void stretch_fwd(const T* f, const T* v, int64_t st, int steps, float (&F)[kSteps][VEC], float (&b)[kSteps][VEC],
-                                            float (&P)[VEC], float (&S)[VEC]) {
-  Raw<T, VEC> rf[kSteps], rv[kSteps];
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i)
-    if (WHOLE || i < steps) rf[i] = load_raw<T, VEC>(f + i * st), rv[i] = load_raw<T, VEC>(v + i * st);
-  all_issued();
+__device__ __forceinline__ void stretch_fwd(const Raw<T, VEC> (&rf)[kSteps], const Raw<T, VEC> (&rv)[kSteps], int steps, float (&F)[kSteps][VEC],
+                                            float (&b)[kSteps][VEC], float (&P)[VEC], float (&S)[VEC]) {
 #pragma unroll
   for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
 #pragma unroll
@@ -159,16 +167,26 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_pairs_kernel(GlrArgs a
   __shared__ Pairs<VEC> lds;
   const GlrPlace p = glr_place<VEC>(a);
   const int waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t base = p.b * z.b + p.ch;
   float tp[VEC], ts[VEC];
 #pragma unroll
   for (int j = 0; j < VEC; ++j) tp[j] = 1.0f, ts[j] = 0.0f;
+  Raw<T, VEC> rf[kSteps], rv[kSteps];
+  auto ask_all = [&](int tw) {
+    // (a stretch behind the end takes the last step that is stored)
+    const int from = imin(tw, a.T - 1), steps = imax(imin(p.t1, p.live) - tw, 1);
+    const int64_t at = base + from * z.t;
+    ask<T, VEC>(f + at, z.t, steps, rf), ask<T, VEC>(v + at, z.t, steps, rv);
+    all_issued();
+  };
   int turn = 0;
+  ask_all(p.t0 + w * kSteps);
   for (int t = p.t0; t < p.t1; t += waves * kSteps, turn ^= 1) {
     const int tw = t + w * kSteps, steps = imin(p.t1, p.live) - tw;
     float F[kSteps][VEC], b[kSteps][VEC], P[VEC], S[VEC];
-    const int64_t at = tw * z.t + p.b * z.b + p.ch;
-    if (steps >= kSteps) stretch_fwd<true, T, VEC>(f + at, v + at, z.t, steps, F, b, P, S);
-    else stretch_fwd<false, T, VEC>(f + at, v + at, z.t, steps, F, b, P, S);
+    if (steps >= kSteps) stretch_fwd<true, T, VEC>(rf, rv, steps, F, b, P, S);
+    else stretch_fwd<false, T, VEC>(rf, rv, steps, F, b, P, S);
+    if (t + waves * kSteps < p.t1) ask_all(tw + waves * kSteps);  // (the next turn's, in flight meanwhile)
     leave<VEC>(lds, turn, w, P, S);
     __syncthreads();
     for (int k = 0; k < waves; ++k) {
@@ -217,19 +235,28 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_kernel(GlrArgs a, cons
   for (int j = 0; j < VEC; ++j) c[j] = 0.0f;
   if (c0) load_some<VEC>(c0 + state, p.n, c);
   if (CUT && p.seg) apply_segments<VEC>(a, p, seg_pairs, 0, 1, p.seg, lds, c);
+  const int64_t base = p.b * z.b + p.ch;
+  Raw<T, VEC> rf[kSteps], rv[kSteps], rg[kSteps], g[kSteps];
+  auto ask_all = [&](int tw) {
+    // (a stretch behind the end takes the last step that is stored)
+    const int from = imin(tw, a.T - 1), steps = imax(imin(p.t1, p.live) - tw, 1);
+    const int64_t at = base + from * z.t;
+    ask<T, VEC>(f + at, z.t, steps, rf), ask<T, VEC>(v + at, z.t, steps, rv);
+    if (GATE) ask<T, VEC>(o + at, z.t, steps, rg);
+    all_issued();
+  };
   int turn = 0;
+  ask_all(p.t0 + w * kSteps);
   for (int t = p.t0; t < p.t1; t += waves * kSteps, turn ^= 1) {
     const int tw = t + w * kSteps, steps = imin(p.t1, p.live) - tw;
     float F[kSteps][VEC], b[kSteps][VEC], P[VEC], S[VEC], s[VEC];
-    Raw<T, VEC> g[kSteps];
-    const int64_t at = tw * z.t + p.b * z.b + p.ch;
+    if (steps >= kSteps) stretch_fwd<true, T, VEC>(rf, rv, steps, F, b, P, S);
+    else stretch_fwd<false, T, VEC>(rf, rv, steps, F, b, P, S);
     if (GATE) {
 #pragma unroll
-      for (int i = 0; i < kSteps; ++i)
-        if (i < steps) g[i] = load_raw<T, VEC>(o + at + i * z.t);
+      for (int i = 0; i < kSteps; ++i) g[i] = rg[i];
     }
-    if (steps >= kSteps) stretch_fwd<true, T, VEC>(f + at, v + at, z.t, steps, F, b, P, S);
-    else stretch_fwd<false, T, VEC>(f + at, v + at, z.t, steps, F, b, P, S);
+    if (t + waves * kSteps < p.t1) ask_all(tw + waves * kSteps);  // (the next turn's, in flight meanwhile)
 #pragma unroll
     for (int j = 0; j < VEC; ++j) s[j] = c[j];
     if (waves > 1) {
