@@ -15,8 +15,11 @@
 // its segment.  (One pass would have workgroups wait for others; the second reading comes partly out of the last cache.)
 // States, pairs and gradients in flight are fp32.  The backward pass starts from the states that the forward pass left
 // before every 8th step, so it needs no second scan for them.
+// Lanes are counted through the sequences, so few channels a sequence fill wavefronts too: 4000 x 48 x 24 forward 23 us and backward 42
+// against 47 and 64 with whole wavefronts for each sequence, 4000 x 47 x 192 78 and 130 against 93 and 156; where nothing is
+// saved, sequences and addresses by lane cost the backward pass 1 to 5 % (64 x 128 x 1024 30.6 to 31.4 us).
 //
-// Measured, bf16 with a gate: 64 x 128 x 1024 forward 14.6 us, backward 23.8 behind it and 30 from memory (4.9, 4.0 TB/s; a large
+// Measured, bf16 with a gate: 64 x 128 x 1024 forward 14.6 us, backward 24 behind it and 31 from memory (4.9, 3.8 TB/s; a large
 // copy 4.9); 32768 x 1 x 1024 forward 25 + 49 us; 8192 x 4 x 1024 without one forward 27 + 43, backward 25 + 55; a single
 // step of 128 sequences 2.8 us.
 #include <type_traits>
@@ -34,7 +37,9 @@ struct Strides {
 struct GlrArgs {
   int T, B, H;      // H: channels that take part
   int wide;         // channels stored in f, v, o, h and their gradients: H, or pad8(H), zeros behind H
-  int groups;       // workgroups along the channels
+  int per_seq;      // lanes of a sequence
+  int lanes;        // of all sequences
+  int groups;       // wavefronts of 64 lanes that hold them
   int seg_steps;    // steps of a segment
   int segs;
   const int32_t* len;
@@ -46,34 +51,50 @@ __device__ __forceinline__ void gate_pair(float x, float& F, float& I) {
   F = __builtin_amdgcn_rcpf(1.0f + e);
   I = x >= 0.0f ? e * F : 1.0f - F;
 }
+// I again from x and F, by the same operations
+__device__ __forceinline__ float ungate(float x, float F) {
+  const float e = __builtin_amdgcn_exp2f(x * -1.44269504088896341f);
+  return x >= 0.0f ? e * F : 1.0f - F;
+}
 __device__ __forceinline__ float gate(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.44269504088896341f)); }
 
 // Loads stay in front of this, in flight together: left to itself the compiler moves them next to their uses.
 __device__ __forceinline__ void all_issued() { __builtin_amdgcn_sched_barrier(0); }
 
-// what a workgroup works on
+// What a workgroup works on.  Its wavefronts all have the same 64 lanes' channels, counted through the sequences (few channels
+// a sequence still fill the lanes), at different steps.
 struct GlrPlace {
-  int seg, b;
-  int ch;        // the lane's first channel; lanes behind the last channel read those of the last lane and write nothing
+  int seg;
+  int b, ch;        // the lane's sequence and first channel; lanes behind the last one read what that reads and write nothing
   bool on;
-  int n;         // of the lane's channels, those that states are kept of (H may end inside a lane's pair)
-  int t0, t1;    // its steps
-  int live;      // steps before the sequence's end, up to T
+  int n;            // of the lane's channels, those that states are kept of (H may end inside a lane's pair)
+  int t0, t1;       // its steps
+  int live, lo, hi; // steps before the sequence's end, up to T: the lane's, the least and the most of the wavefront
 };
 template <int VEC> __device__ __forceinline__ GlrPlace glr_place(const GlrArgs& a) {
   GlrPlace p;
-  int i = blockIdx.x;
-  const int g = i % a.groups;
-  i /= a.groups;
-  p.b = i % a.B, p.seg = i / a.B;
-  const int ch = (g * 64 + (threadIdx.x & 63)) * VEC;
-  p.on = ch < a.wide;
-  p.ch = p.on ? ch : a.wide - VEC;
-  p.n = p.on ? a.H - ch : 0;
+  p.seg = blockIdx.x / a.groups;
+  const int at = (blockIdx.x - p.seg * a.groups) * 64 + (threadIdx.x & 63), lane = imin(at, a.lanes - 1);
+  p.on = at < a.lanes;
+  p.b = (int)((unsigned)lane / (unsigned)a.per_seq);
+  p.ch = (lane - p.b * a.per_seq) * VEC;
+  p.n = p.on ? a.H - p.ch : 0;
   p.t0 = p.seg * a.seg_steps, p.t1 = imin(a.T - p.t0, a.seg_steps) + p.t0;
-  p.live = a.len ? imin(imax(a.len[p.b], 0), a.T) : a.T;
+  p.live = p.lo = p.hi = a.T;
+  if (a.len) {
+    p.live = imin(imax(a.len[p.b], 0), a.T);
+    p.lo = p.hi = __builtin_amdgcn_readfirstlane(p.live);
+    if (__builtin_amdgcn_readlane(p.b, 0) != __builtin_amdgcn_readlane(p.b, 63))
+      p.lo = a.T - (int)wave_max((uint32_t)(a.T - p.live)), p.hi = (int)wave_max((uint32_t)p.live);
+  }
   return p;
 }
+// Steps of a stretch that begins at t before the ends of its sequences: the lane's own, and the least and the most of the
+// wavefront's, the same for all of it (below 0 and above a stretch's steps as they come).
+struct Steps {
+  int mine, lo, hi;
+  __device__ __forceinline__ Steps(const GlrPlace& p, int t) : mine(imin(p.t1, p.live) - t), lo(imin(p.t1, p.lo) - t), hi(imin(p.t1, p.hi) - t) {}
+};
 
 // pairs of the wavefronts' stretches of a turn, in LDS
 template <int VEC> struct Pairs {
@@ -129,8 +150,8 @@ template <bool CUT, int VEC, typename T> __device__ __forceinline__ void put(T* 
 }
 
 // ---- forward ------------------------------------------------------------------
-// A stretch's values as they lie in memory; in the place of steps from `steps` on, which nobody looks at, those of the last one
-// before (every register is written on every path, so loads stay in flight behind the branch).
+// A stretch's values as they lie in memory; in the place of steps from `steps` (1 at least) on, which nobody looks at, those of the
+// last one before (every register is written on every path, so loads stay in flight behind the branch).
 template <typename T, int VEC> __device__ __forceinline__ void ask(const T* p, int64_t st, int steps, Raw<T, VEC> (&r)[kSteps]) {
   if (steps >= kSteps) {
 #pragma unroll
@@ -141,21 +162,22 @@ template <typename T, int VEC> __device__ __forceinline__ void ask(const T* p, i
   }
 }
 
-// F and (1 - F) v of a stretch's steps, and its pair.  WHOLE: all of its steps are live; else the first `steps` are, and
-// the others leave the state as it is.
+// F and (1 - F) v of a stretch's steps, and its pair.  WHOLE: all of its steps are live in all lanes; else those behind a
+// lane's end leave the state as it is (selected, not multiplied: nothing that lies there takes part).
 template <bool WHOLE, typename T, int VEC>
-__device__ __forceinline__ void stretch_fwd(const Raw<T, VEC> (&rf)[kSteps], const Raw<T, VEC> (&rv)[kSteps], int steps, float (&F)[kSteps][VEC],
+__device__ __forceinline__ void stretch_fwd(const Raw<T, VEC> (&rf)[kSteps], const Raw<T, VEC> (&rv)[kSteps], const Steps& n, float (&F)[kSteps][VEC],
                                             float (&b)[kSteps][VEC], float (&P)[VEC], float (&S)[VEC]) {
 #pragma unroll
   for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
-    if (WHOLE || i < steps) {
+    if (WHOLE || i < n.hi) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         float I;
         gate_pair(part_of(rf[i], j), F[i][j], I);
         b[i][j] = I * part_of(rv[i], j);
+        if (!WHOLE) F[i][j] = i < n.mine ? F[i][j] : 1.0f, b[i][j] = i < n.mine ? b[i][j] : 0.0f;
         P[j] *= F[i][j];
         S[j] = fmaf(F[i][j], S[j], b[i][j]);
       }
@@ -173,8 +195,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_pairs_kernel(GlrArgs a
   for (int j = 0; j < VEC; ++j) tp[j] = 1.0f, ts[j] = 0.0f;
   Raw<T, VEC> rf[kSteps], rv[kSteps];
   auto ask_all = [&](int tw) {
-    // (a stretch behind the end takes the last step that is stored)
-    const int from = imin(tw, a.T - 1), steps = imax(imin(p.t1, p.live) - tw, 1);
+    // (a stretch behind the end takes a step that is stored)
+    const int from = imin(tw, a.T - 1), steps = imax(Steps(p, tw).hi, 1);
     const int64_t at = base + from * z.t;
     ask<T, VEC>(f + at, z.t, steps, rf), ask<T, VEC>(v + at, z.t, steps, rv);
     all_issued();
@@ -182,10 +204,11 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_pairs_kernel(GlrArgs a
   int turn = 0;
   ask_all(p.t0 + w * kSteps);
   for (int t = p.t0; t < p.t1; t += waves * kSteps, turn ^= 1) {
-    const int tw = t + w * kSteps, steps = imin(p.t1, p.live) - tw;
+    const int tw = t + w * kSteps;
+    const Steps n(p, tw);
     float F[kSteps][VEC], b[kSteps][VEC], P[VEC], S[VEC];
-    if (steps >= kSteps) stretch_fwd<true, T, VEC>(rf, rv, steps, F, b, P, S);
-    else stretch_fwd<false, T, VEC>(rf, rv, steps, F, b, P, S);
+    if (n.lo >= kSteps) stretch_fwd<true, T, VEC>(rf, rv, n, F, b, P, S);
+    else stretch_fwd<false, T, VEC>(rf, rv, n, F, b, P, S);
     if (t + waves * kSteps < p.t1) ask_all(tw + waves * kSteps);  // (the next turn's, in flight meanwhile)
     leave<VEC>(lds, turn, w, P, S);
     __syncthreads();
@@ -202,9 +225,9 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_pairs_kernel(GlrArgs a
   }
 }
 
-// results of a stretch whose state before it is s; steps from `steps` to `stored` lie behind the sequence's end
+// results of a stretch whose state before it is s; zeros for those of its `stored` steps that lie behind a lane's end
 template <bool WHOLE, typename T, int VEC, bool GATE, bool CUT>
-__device__ __forceinline__ void stretch_out(T* h, int64_t st, bool on, int steps, int stored, const float (&F)[kSteps][VEC], const float (&b)[kSteps][VEC],
+__device__ __forceinline__ void stretch_out(T* h, int64_t st, bool on, const Steps& n, int stored, const float (&F)[kSteps][VEC], const float (&b)[kSteps][VEC],
                                             const Raw<T, VEC> (&g)[kSteps], float (&s)[VEC]) {
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
@@ -212,11 +235,12 @@ __device__ __forceinline__ void stretch_out(T* h, int64_t st, bool on, int steps
     float y[VEC];
 #pragma unroll
     for (int j = 0; j < VEC; ++j) y[j] = 0.0f;
-    if (WHOLE || i < steps) {
+    if (WHOLE || i < n.hi) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         s[j] = fmaf(F[i][j], s[j], b[i][j]);
         y[j] = GATE ? gate(part_of(g[i], j)) * s[j] : s[j];
+        if (!WHOLE) y[j] = i < n.mine ? y[j] : 0.0f;
       }
     }
     if (on) put<CUT, VEC>(h + i * st, y);
@@ -238,8 +262,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_kernel(GlrArgs a, cons
   const int64_t base = p.b * z.b + p.ch;
   Raw<T, VEC> rf[kSteps], rv[kSteps], rg[kSteps], g[kSteps];
   auto ask_all = [&](int tw) {
-    // (a stretch behind the end takes the last step that is stored)
-    const int from = imin(tw, a.T - 1), steps = imax(imin(p.t1, p.live) - tw, 1);
+    // (a stretch behind the end takes a step that is stored)
+    const int from = imin(tw, a.T - 1), steps = imax(Steps(p, tw).hi, 1);
     const int64_t at = base + from * z.t;
     ask<T, VEC>(f + at, z.t, steps, rf), ask<T, VEC>(v + at, z.t, steps, rv);
     if (GATE) ask<T, VEC>(o + at, z.t, steps, rg);
@@ -248,10 +272,11 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_kernel(GlrArgs a, cons
   int turn = 0;
   ask_all(p.t0 + w * kSteps);
   for (int t = p.t0; t < p.t1; t += waves * kSteps, turn ^= 1) {
-    const int tw = t + w * kSteps, steps = imin(p.t1, p.live) - tw;
+    const int tw = t + w * kSteps;
+    const Steps n(p, tw);
     float F[kSteps][VEC], b[kSteps][VEC], P[VEC], S[VEC], s[VEC];
-    if (steps >= kSteps) stretch_fwd<true, T, VEC>(rf, rv, steps, F, b, P, S);
-    else stretch_fwd<false, T, VEC>(rf, rv, steps, F, b, P, S);
+    if (n.lo >= kSteps) stretch_fwd<true, T, VEC>(rf, rv, n, F, b, P, S);
+    else stretch_fwd<false, T, VEC>(rf, rv, n, F, b, P, S);
     if (GATE) {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) g[i] = rg[i];
@@ -273,8 +298,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_kernel(GlrArgs a, cons
     if (tw < p.t1) {
       if (ckpt) store_some<VEC>(ckpt + (int64_t)(tw / kSteps) * plane + state, p.n, s);
       T* out = h + tw * hs.t + p.b * hs.b + p.ch;
-      if (steps >= kSteps) stretch_out<true, T, VEC, GATE, CUT>(out, hs.t, p.on, steps, kSteps, F, b, g, s);
-      else stretch_out<false, T, VEC, GATE, CUT>(out, hs.t, p.on, steps, p.t1 - tw, F, b, g, s);
+      if (n.lo >= kSteps) stretch_out<true, T, VEC, GATE, CUT>(out, hs.t, p.on, n, kSteps, F, b, g, s);
+      else stretch_out<false, T, VEC, GATE, CUT>(out, hs.t, p.on, n, p.t1 - tw, F, b, g, s);
     }
   }
   if (cT && w == 0 && p.seg == a.segs - 1) store_some<VEC>(cT + state, p.n, c);
@@ -311,11 +336,11 @@ __global__ __launch_bounds__(64) void glr_step_kernel(GlrArgs a, const T* f, con
 // ---- backward -----------------------------------------------------------------
 // The adjoint's pair of a stretch takes e behind its last step to e behind the step before its first.
 template <bool WHOLE, typename T, int VEC, bool GATE>
-__device__ __forceinline__ void stretch_adjoint(const T* f, const T* o, const T* dh, int64_t st, int64_t dst, int steps, float (&P)[VEC], float (&S)[VEC]) {
+__device__ __forceinline__ void stretch_adjoint(const T* f, const T* o, const T* dh, int64_t st, int64_t dst, const Steps& n, float (&P)[VEC], float (&S)[VEC]) {
   Raw<T, VEC> F[kSteps], q[kSteps], g[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
-    if (WHOLE || i < steps) {
+    if (WHOLE || i < n.hi) {
       F[i] = load_raw<T, VEC>(f + i * st);
       q[i] = load_raw<T, VEC>(dh + i * dst);
       if (GATE) g[i] = load_raw<T, VEC>(o + i * st);
@@ -325,11 +350,13 @@ __device__ __forceinline__ void stretch_adjoint(const T* f, const T* o, const T*
   for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
 #pragma unroll
   for (int i = kSteps - 1; i >= 0; --i)
-    if (WHOLE || i < steps) {
+    if (WHOLE || i < n.hi) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        const float x = gate(part_of(F[i], j)), d = part_of(q[i], j);
-        S[j] = x * (S[j] + (GATE ? gate(part_of(g[i], j)) * d : d));
+        float x = gate(part_of(F[i], j)), d = part_of(q[i], j);
+        if (GATE) d *= gate(part_of(g[i], j));
+        if (!WHOLE) x = i < n.mine ? x : 1.0f, d = i < n.mine ? d : 0.0f;
+        S[j] = x * (S[j] + d);
         P[j] *= x;
       }
     }
@@ -347,11 +374,12 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_pairs_kernel(GlrArgs a
   const int span = waves * kSteps, turns = (p.t1 - p.t0 + span - 1) / span;
   int turn = 0;
   for (int t = p.t0 + (turns - 1) * span; t >= p.t0; t -= span, turn ^= 1) {
-    const int tw = t + w * kSteps, steps = imin(p.t1, p.live) - tw;
+    const int tw = t + w * kSteps;
+    const Steps n(p, tw);
     const int64_t at = tw * z.t + p.b * z.b + p.ch, dat = tw * ds.t + p.b * ds.b + p.ch;
     float P[VEC], S[VEC];
-    if (steps >= kSteps) stretch_adjoint<true, T, VEC, GATE>(f + at, o + at, dh + dat, z.t, ds.t, steps, P, S);
-    else stretch_adjoint<false, T, VEC, GATE>(f + at, o + at, dh + dat, z.t, ds.t, steps, P, S);
+    if (n.lo >= kSteps) stretch_adjoint<true, T, VEC, GATE>(f + at, o + at, dh + dat, z.t, ds.t, n, P, S);
+    else stretch_adjoint<false, T, VEC, GATE>(f + at, o + at, dh + dat, z.t, ds.t, n, P, S);
     leave<VEC>(lds, turn, w, P, S);
     __syncthreads();
     for (int k = waves - 1; k >= 0; --k) {
@@ -368,15 +396,16 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_pairs_kernel(GlrArgs a
 }
 
 // Loads of a stretch, its states again from the one before it, and its adjoint's pair; do is stored on the way (it needs
-// no gradient from later steps).  Leaves F, I = 1 - F, u = c_{t-1} - v and q = sigma(o) dh.
+// no gradient from later steps).  Leaves F, u = c_{t-1} - v, q = sigma(o) dh, and f as it was
+// read: 1 - F is made again where it is wanted, as holding it would cost a workgroup of the two that a CU has registers for.
 template <bool WHOLE, typename T, int VEC, bool GATE, bool CUT>
-__device__ __forceinline__ void stretch_back(const T* f, const T* v, const T* o, const T* dh, T* dg, int64_t st, int64_t dst, int64_t gst, bool on, int steps,
-                                             float (&c)[VEC], float (&F)[kSteps][VEC], float (&I)[kSteps][VEC], float (&u)[kSteps][VEC],
+__device__ __forceinline__ void stretch_back(const T* f, const T* v, const T* o, const T* dh, T* dg, int64_t st, int64_t dst, int64_t gst, bool on, const Steps& n,
+                                             float (&c)[VEC], Raw<T, VEC> (&rf)[kSteps], float (&F)[kSteps][VEC], float (&u)[kSteps][VEC],
                                              float (&q)[kSteps][VEC], float (&P)[VEC], float (&S)[VEC]) {
-  Raw<T, VEC> rf[kSteps], rv[kSteps], g[kSteps], rd[kSteps];
+  Raw<T, VEC> rv[kSteps], g[kSteps], rd[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
-    if (WHOLE || i < steps) {
+    if (WHOLE || i < n.hi) {
       rf[i] = load_raw<T, VEC>(f + i * st);
       rv[i] = load_raw<T, VEC>(v + i * st);
       if (GATE) g[i] = load_raw<T, VEC>(o + i * st);
@@ -385,20 +414,24 @@ __device__ __forceinline__ void stretch_back(const T* f, const T* v, const T* o,
   all_issued();
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
-    if (WHOLE || i < steps) {
+    if (WHOLE || i < n.hi) {
       float y[VEC];
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        gate_pair(part_of(rf[i], j), F[i][j], I[i][j]);
+        const bool live = WHOLE || i < n.mine;
+        float I;
+        gate_pair(part_of(rf[i], j), F[i][j], I);
         const float x = part_of(rv[i], j);
         u[i][j] = c[j] - x;
-        c[j] = fmaf(F[i][j], c[j], I[i][j] * x);
+        const float next = fmaf(F[i][j], c[j], I * x);
+        c[j] = live ? next : c[j];
         q[i][j] = part_of(rd[i], j);
         if (GATE) {
           const float O = gate(part_of(g[i], j));
           q[i][j] *= O;
-          y[j] = q[i][j] * c[j] * (1.0f - O);
+          y[j] = live ? q[i][j] * c[j] * (1.0f - O) : 0.0f;
         }
+        if (!live) F[i][j] = 1.0f, q[i][j] = 0.0f;
       }
       if (GATE && on) put<CUT, VEC>(dg + i * gst, y);
     }
@@ -406,7 +439,7 @@ __device__ __forceinline__ void stretch_back(const T* f, const T* v, const T* o,
   for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
 #pragma unroll
   for (int i = kSteps - 1; i >= 0; --i)
-    if (WHOLE || i < steps) {
+    if (WHOLE || i < n.hi) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         S[j] = F[i][j] * (S[j] + q[i][j]);
@@ -414,10 +447,10 @@ __device__ __forceinline__ void stretch_back(const T* f, const T* v, const T* o,
       }
     }
 }
-// df and dv of a stretch, e behind its last step in s; zeros (do's too) for its steps from `steps` to `stored`
+// df and dv of a stretch, e behind its last step in s; zeros (do's too) for those of its `stored` steps behind a lane's end
 template <bool WHOLE, typename T, int VEC, bool GATE, bool CUT>
-__device__ __forceinline__ void stretch_grads(T* df, T* dv, T* dg, int64_t gst, bool on, int steps, int stored, const float (&F)[kSteps][VEC],
-                                              const float (&I)[kSteps][VEC], const float (&u)[kSteps][VEC], const float (&q)[kSteps][VEC],
+__device__ __forceinline__ void stretch_grads(T* df, T* dv, T* dg, int64_t gst, bool on, const Steps& n, int stored, const Raw<T, VEC> (&rf)[kSteps],
+                                              const float (&F)[kSteps][VEC], const float (&u)[kSteps][VEC], const float (&q)[kSteps][VEC],
                                               float (&s)[VEC]) {
 #pragma unroll
   for (int i = kSteps - 1; i >= 0; --i) {
@@ -425,13 +458,14 @@ __device__ __forceinline__ void stretch_grads(T* df, T* dv, T* dg, int64_t gst, 
     float x[VEC], y[VEC];
 #pragma unroll
     for (int j = 0; j < VEC; ++j) x[j] = y[j] = 0.0f;
-    if (WHOLE || i < steps) {
+    if (WHOLE || i < n.hi) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const float dc = q[i][j] + s[j];
         s[j] = F[i][j] * dc;
-        y[j] = dc * I[i][j];
+        y[j] = dc * ungate(part_of(rf[i], j), F[i][j]);
         x[j] = y[j] * F[i][j] * u[i][j];
+        if (!WHOLE) x[j] = i < n.mine ? x[j] : 0.0f, y[j] = i < n.mine ? y[j] : 0.0f;
       }
     } else if (GATE) {
       if (on) put<CUT, VEC>(dg + i * gst, x);
@@ -441,7 +475,7 @@ __device__ __forceinline__ void stretch_grads(T* df, T* dv, T* dg, int64_t gst, 
 }
 
 template <typename T, int VEC, bool GATE, bool CUT>
-__global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_kernel(GlrArgs a, const T* f, const T* v, const T* o, Strides z, const float* ckpt, const T* dh,
+__global__ __launch_bounds__(64 * kMaxWaves, 4) void glr_bwd_kernel(GlrArgs a, const T* f, const T* v, const T* o, Strides z, const float* ckpt, const T* dh,
                                                                  Strides ds, const float* dcT, T* df, T* dv, T* dg, Strides gs, float* dc0,
                                                                  const float* seg_pairs) {
   __shared__ Pairs<VEC> lds;
@@ -456,12 +490,14 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_kernel(GlrArgs a, cons
   const int span = waves * kSteps, turns = (p.t1 - p.t0 + span - 1) / span;
   int turn = 0;
   for (int t = p.t0 + (turns - 1) * span; t >= p.t0; t -= span, turn ^= 1) {
-    const int tw = t + w * kSteps, steps = imin(p.t1, p.live) - tw;
-    float F[kSteps][VEC], I[kSteps][VEC], u[kSteps][VEC], q[kSteps][VEC], P[VEC], S[VEC], c[VEC], s[VEC];
+    const int tw = t + w * kSteps;
+    const Steps n(p, tw);
+    float F[kSteps][VEC], u[kSteps][VEC], q[kSteps][VEC], P[VEC], S[VEC], c[VEC], s[VEC];
+    Raw<T, VEC> rf[kSteps];
     const int64_t at = tw * z.t + p.b * z.b + p.ch, dat = tw * ds.t + p.b * ds.b + p.ch, gat = tw * gs.t + p.b * gs.b + p.ch;
-    if (steps > 0) load_some<VEC>(ckpt + (int64_t)(tw / kSteps) * plane + state, p.n, c);
-    if (steps >= kSteps) stretch_back<true, T, VEC, GATE, CUT>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, steps, c, F, I, u, q, P, S);
-    else stretch_back<false, T, VEC, GATE, CUT>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, steps, c, F, I, u, q, P, S);
+    if (n.hi > 0) load_some<VEC>(ckpt + (int64_t)(tw / kSteps) * plane + state, p.n, c);
+    if (n.lo >= kSteps) stretch_back<true, T, VEC, GATE, CUT>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, n, c, rf, F, u, q, P, S);
+    else stretch_back<false, T, VEC, GATE, CUT>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, n, c, rf, F, u, q, P, S);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) s[j] = e[j];
     if (waves > 1) {
@@ -475,8 +511,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_kernel(GlrArgs a, cons
 #pragma unroll
       for (int j = 0; j < VEC; ++j) e[j] = fmaf(P[j], e[j], S[j]);
     }
-    if (steps >= kSteps) stretch_grads<true, T, VEC, GATE, CUT>(df + gat, dv + gat, dg + gat, gs.t, p.on, steps, kSteps, F, I, u, q, s);
-    else stretch_grads<false, T, VEC, GATE, CUT>(df + gat, dv + gat, dg + gat, gs.t, p.on, steps, p.t1 - tw, F, I, u, q, s);
+    if (n.lo >= kSteps) stretch_grads<true, T, VEC, GATE, CUT>(df + gat, dv + gat, dg + gat, gs.t, p.on, n, kSteps, rf, F, u, q, s);
+    else stretch_grads<false, T, VEC, GATE, CUT>(df + gat, dv + gat, dg + gat, gs.t, p.on, n, p.t1 - tw, rf, F, u, q, s);
   }
   if (dc0 && w == 0 && p.seg == 0) store_some<VEC>(dc0 + state, p.n, e);
 }
@@ -490,12 +526,14 @@ struct GlrPlan {
 static int glr_vec(int32_t dtype, int wide) { return dtype == ARD_F32 || wide % 2 ? 1 : 2; }
 static GlrPlan glr_plan(int32_t dtype, int T, int B, int H, int32_t flags, const int32_t* len) {
   const int wide = flags ? pad8(H) : H, vec = glr_vec(dtype, wide);
+  const int64_t lanes = (int64_t)B * (wide / vec);
   GlrPlan g{};
   const int pieces = T / kSteps + (T % kSteps != 0);
   g.a.T = T, g.a.B = B, g.a.H = H, g.a.wide = wide, g.a.len = len;
-  g.a.groups = ceil_div(wide, 64 * vec);
+  g.a.per_seq = wide / vec, g.a.lanes = (int)lanes, g.a.groups = (int)((lanes + 63) / 64);
+  if (lanes > INT32_MAX - 64) return g;  // (refused: no wavefronts)
   g.waves = imin(pieces, kMaxWaves);
-  const int64_t have = (int64_t)g.a.groups * B * g.waves;  // wavefronts without cutting time
+  const int64_t have = (int64_t)g.a.groups * g.waves;  // wavefronts without cutting time
   const int turns = ceil_div(pieces, g.waves);
   int segs = 1;
   // Time is cut below 8 wavefronts a CU, into 16 a CU: with half as many 32768 x 1 x 1024 took 95 us (83 then), 8192 x 4 x 1024 97 (85);
@@ -524,27 +562,34 @@ static int32_t glr_check(int32_t dtype, int32_t T, int32_t B, int32_t H, int32_t
   return ARD_OK;
 }
 static int32_t glr_check_grid(const GlrPlan& g) {  // (HIP counts a grid's threads in 32 bits)
-  if ((int64_t)g.a.groups * g.a.B * g.a.segs * g.waves >= 1 << 26) return fail(ARD_ESHAPE, "B * H is too large (%d, %d)", g.a.B, g.a.H);
+  if (!g.waves || (int64_t)g.a.groups * g.a.segs * g.waves >= 1 << 26) return fail(ARD_ESHAPE, "B * H is too large (%d, %d)", g.a.B, g.a.H);
   return ARD_OK;
 }
+
+// The one shape of all these launches: every wavefront's worth of lanes, segment by segment (what glr_place takes apart; a
+// workgroup of a segment that does not exist would read behind the segments' pairs).
+static dim3 glr_grid(const GlrArgs& a, int segs) { return dim3((unsigned)a.groups * (unsigned)segs); }
+
+// (a dry run's log says the grid, the lanes' wavefronts and the segments)
+#define ARD_GLR_LAUNCH(name, kernel, grid, ...) ARD_LAUNCH_NAMED(launch_instance(name, (int)(grid).x, a.groups, a.segs), kernel, grid, __VA_ARGS__)
 
 template <typename T, int VEC, bool GATE>
 static int32_t glr_fwd_t(const GlrCall& c, const float* c0, void* h, Strides hs, float* cT, float* ckpt, float* ws, hipStream_t st) {
   const GlrArgs& a = c.g.a;
   const T *f = (const T*)c.f, *v = (const T*)c.v, *o = (const T*)c.o;
   if (a.T == 1) {
-    ARD_LAUNCH((glr_step_kernel<T, VEC, GATE>), dim3(a.groups * a.B), dim3(64), 0, st, a, f, v, o, c.z, c0, (T*)h, hs, cT, ckpt);
+    ARD_GLR_LAUNCH("glr_step_kernel", (glr_step_kernel<T, VEC, GATE>), glr_grid(a, 1), dim3(64), 0, st, a, f, v, o, c.z, c0, (T*)h, hs, cT, ckpt);
     ARD_LAUNCH_CHECK("glr_step_kernel");
     return ARD_OK;
   }
   const dim3 block(64 * c.g.waves);
   if (a.segs > 1) {  // (the last segment's pair is not needed)
-    ARD_LAUNCH((glr_fwd_pairs_kernel<T, VEC>), dim3(a.groups * a.B * (a.segs - 1)), block, 0, st, a, f, v, c.z, ws);
+    ARD_GLR_LAUNCH("glr_fwd_pairs_kernel", (glr_fwd_pairs_kernel<T, VEC>), glr_grid(a, a.segs - 1), block, 0, st, a, f, v, c.z, ws);
     ARD_LAUNCH_CHECK("glr_fwd_pairs_kernel");
   }
-  const dim3 grid(a.groups * a.B * a.segs);
-  if (a.segs > 1) ARD_LAUNCH((glr_fwd_kernel<T, VEC, GATE, true>), grid, block, 0, st, a, f, v, o, c.z, c0, (T*)h, hs, cT, ckpt, ws);
-  else ARD_LAUNCH((glr_fwd_kernel<T, VEC, GATE, false>), grid, block, 0, st, a, f, v, o, c.z, c0, (T*)h, hs, cT, ckpt, nullptr);
+  const dim3 grid = glr_grid(a, a.segs);
+  if (a.segs > 1) ARD_GLR_LAUNCH("glr_fwd_kernel", (glr_fwd_kernel<T, VEC, GATE, true>), grid, block, 0, st, a, f, v, o, c.z, c0, (T*)h, hs, cT, ckpt, ws);
+  else ARD_GLR_LAUNCH("glr_fwd_kernel", (glr_fwd_kernel<T, VEC, GATE, false>), grid, block, 0, st, a, f, v, o, c.z, c0, (T*)h, hs, cT, ckpt, nullptr);
   ARD_LAUNCH_CHECK("glr_fwd_kernel");
   return ARD_OK;
 }
@@ -556,15 +601,16 @@ static int32_t glr_bwd_t(const GlrCall& c, const float* ckpt, const void* dh, St
   const T *f = (const T*)c.f, *v = (const T*)c.v, *o = (const T*)c.o;
   const dim3 block(64 * c.g.waves);
   if (a.segs > 1) {
-    ARD_LAUNCH((glr_bwd_pairs_kernel<T, VEC, GATE>), dim3(a.groups * a.B * a.segs), block, 0, st, a, f, o, c.z, (const T*)dh, ds, ws);
+    ARD_GLR_LAUNCH("glr_bwd_pairs_kernel", (glr_bwd_pairs_kernel<T, VEC, GATE>), glr_grid(a, a.segs), block, 0, st, a, f, o, c.z, (const T*)dh, ds, ws);
     ARD_LAUNCH_CHECK("glr_bwd_pairs_kernel");
   }
-  const dim3 grid(a.groups * a.B * a.segs);
+  const dim3 grid = glr_grid(a, a.segs);
   if (a.segs > 1)
-    ARD_LAUNCH((glr_bwd_kernel<T, VEC, GATE, true>), grid, block, 0, st, a, f, v, o, c.z, ckpt, (const T*)dh, ds, dcT, (T*)df, (T*)dv, (T*)dg, gs, dc0, ws);
+    ARD_GLR_LAUNCH("glr_bwd_kernel", (glr_bwd_kernel<T, VEC, GATE, true>), grid, block, 0, st, a, f, v, o, c.z, ckpt, (const T*)dh, ds, dcT, (T*)df, (T*)dv,
+                   (T*)dg, gs, dc0, ws);
   else
-    ARD_LAUNCH((glr_bwd_kernel<T, VEC, GATE, false>), grid, block, 0, st, a, f, v, o, c.z, ckpt, (const T*)dh, ds, dcT, (T*)df, (T*)dv, (T*)dg, gs, dc0,
-               nullptr);
+    ARD_GLR_LAUNCH("glr_bwd_kernel", (glr_bwd_kernel<T, VEC, GATE, false>), grid, block, 0, st, a, f, v, o, c.z, ckpt, (const T*)dh, ds, dcT, (T*)df, (T*)dv,
+                   (T*)dg, gs, dc0, nullptr);
   ARD_LAUNCH_CHECK("glr_bwd_kernel");
   return ARD_OK;
 }

@@ -99,6 +99,15 @@ def test_sequences_of_unequal_length(T, B, H, gate, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gate", [True, False])
+@pytest.mark.parametrize("T,B,H", [(1, 70, 1), (9, 200, 2), (20, 33, 5), (65, 50, 22), (130, 9, 37), (600, 48, 22), (300, 130, 3)])
+def test_several_sequences_in_a_wavefront(T, B, H, gate, dtype):
+    """Few channels a sequence: neighbouring lanes belong to sequences of different lengths."""
+    _check(T, B, H, dtype, gate=gate, ragged=True, seed=T + B)
+    _check(T, B, H, dtype, gate=gate, ragged=False, seed=T + B + 1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,B,H,ragged", [(1000, 1, 10, False), (4099, 1, 130, False), (2500, 3, 64, True), (20000, 1, 3, False)])
 def test_time_cut_over_workgroups(T, B, H, ragged, dtype):
     assert ard.glr_workspace_bytes(ard.F32 if dtype == "f32" else ard.BF16, T, B, H) > 0
