@@ -520,19 +520,26 @@ __global__ __launch_bounds__(64 * kMaxWaves, 4) void glr_bwd_kernel(GlrArgs a, c
 // ---- host ---------------------------------------------------------------------
 struct GlrPlan {
   GlrArgs a;
-  int waves;
+  int waves, vec;
 };
-// Channels of a lane: 4 bytes of them (one fp32 or two bf16; an odd number of bf16 channels: one), a wavefront's row 256 bytes.
-static int glr_vec(int32_t dtype, int wide) { return dtype == ARD_F32 || wide % 2 ? 1 : 2; }
 static GlrPlan glr_plan(int32_t dtype, int T, int B, int H, int32_t flags, const int32_t* len) {
-  const int wide = flags ? pad8(H) : H, vec = glr_vec(dtype, wide);
-  const int64_t lanes = (int64_t)B * (wide / vec);
+  const int wide = flags ? pad8(H) : H, pieces = T / kSteps + (T % kSteps != 0), waves = imin(pieces, kMaxWaves);
+  const auto groups_of = [&](int vec) { return ((int64_t)B * (wide / vec) + 63) / 64; };
   GlrPlan g{};
-  const int pieces = T / kSteps + (T % kSteps != 0);
+  g.vec = 1;
+  if (dtype == ARD_BF16 && wide % 2 == 0) {
+    // Two channels a lane, 256 bytes a wavefront's row, as one's 128 fetch less well (64 x 128 x 1024 forward and backward 14.4 + 31.0 us,
+    // 14.5 + 34.5 with one; 4000 x 47 x 192 78 + 130, 90 + 154).  One where that leaves fewer than 8 stretches a CU, as a lane's two come one
+    // after the other (130 x 8 x 512 8.2 + 10.9, 6.8 + 8.6 with one; 1000 x 8 x 512, which has 16, 13.3 + 17.7, 13.5 + 18.7), and
+    // where one fills the CUs with wavefronts and two would not (224 x 16 x 1024 11.9 + 17.5, 9.4 + 15.0; 4000: 147 + 263, 129 + 229).
+    const int64_t two = groups_of(2);
+    g.vec = two * pieces <= 2048 || (two * waves < 2048 && groups_of(1) * waves >= 2048) ? 1 : 2;
+  }
+  const int64_t lanes = (int64_t)B * (wide / g.vec);
   g.a.T = T, g.a.B = B, g.a.H = H, g.a.wide = wide, g.a.len = len;
-  g.a.per_seq = wide / vec, g.a.lanes = (int)lanes, g.a.groups = (int)((lanes + 63) / 64);
   if (lanes > INT32_MAX - 64) return g;  // (refused: no wavefronts)
-  g.waves = imin(pieces, kMaxWaves);
+  g.waves = waves;
+  g.a.per_seq = wide / g.vec, g.a.lanes = (int)lanes, g.a.groups = (int)groups_of(g.vec);
   const int64_t have = (int64_t)g.a.groups * g.waves;  // wavefronts without cutting time
   const int turns = ceil_div(pieces, g.waves);
   int segs = 1;
@@ -615,10 +622,10 @@ static int32_t glr_bwd_t(const GlrCall& c, const float* ckpt, const void* dh, St
   return ARD_OK;
 }
 
-template <class F> static int32_t glr_instance(int32_t dtype, int wide, F&& with) {
+template <class F> static int32_t glr_instance(int32_t dtype, int vec, F&& with) {
   using One = std::integral_constant<int, 1>;
   if (dtype == ARD_F32) return with(0.0f, One{});
-  return glr_vec(dtype, wide) == 1 ? with((uint16_t)0, One{}) : with((uint16_t)0, std::integral_constant<int, 2>{});
+  return vec == 1 ? with((uint16_t)0, One{}) : with((uint16_t)0, std::integral_constant<int, 2>{});
 }
 
 }  // namespace ard
@@ -655,7 +662,7 @@ extern "C" int32_t ard_glr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t H, c
     constexpr int N = decltype(vec)::value;
     return o ? glr_fwd_t<E, N, true>(c, c0, h, hs, cT, ckpt, (float*)ws, st) : glr_fwd_t<E, N, false>(c, c0, h, hs, cT, ckpt, (float*)ws, st);
   };
-  return glr_instance(dtype, c.g.a.wide, with);
+  return glr_instance(dtype, c.g.vec, with);
 }
 
 extern "C" int32_t ard_glr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t H, const void* f, const void* v, const void* o, int64_t z_t, int64_t z_b,
@@ -680,5 +687,5 @@ extern "C" int32_t ard_glr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t H, c
     return o ? glr_bwd_t<E, N, true>(c, ckpt, dh, ds, dcT, df, dv, dout, gs, dc0, (float*)ws, st)
              : glr_bwd_t<E, N, false>(c, ckpt, dh, ds, dcT, df, dv, dout, gs, dc0, (float*)ws, st);
   };
-  return glr_instance(dtype, c.g.a.wide, with);
+  return glr_instance(dtype, c.g.vec, with);
 }
