@@ -5,7 +5,7 @@
 //
 // Every pass is bound by memory: a row is read once into registers, its mean and then its centred square sum (no
 // difference of large sums) are taken there in fp32, and its result is rounded once, when it is stored.  A row belongs
-// to G threads, 16 elements each: 16, 32 or 64 lanes of a wavefront, or 128 to 1024 threads of a workgroup; longer
+// to G threads, 16 elements each (8 to 24 in bf16): 16, 32 or 64 lanes of a wavefront, or 128 to 1024 threads of a workgroup; longer
 // rows are read again from the cache.  The backward pass keeps dgamma and dbeta of a thread's columns in registers over
 // all the rows that its workgroup takes, so the sums over rows cost one row of partial sums for each workgroup and a
 // second, small pass that adds them in a fixed order.
@@ -13,6 +13,7 @@
 // Measured, bf16: 16384 x 4096 forward 47 us (5.7 TB/s from and to memory and the last cache; a large copy 4.9), backward 79 + 5 (5.1);
 // 8192 x 1024 8.4, 11.3 + 3.8; 1027 x 1501 (rows at odd addresses) 4.8, 7.6 + 3.4; 100000 x 128 13, 22 together.  The next row in
 // flight, kept whole accesses and fewer partial sums made the backward pass of 16384 x 4096 136 -> 84 us.
+#include <algorithm>
 #include <type_traits>
 
 #include "rows.hpp"
@@ -26,7 +27,6 @@ struct NormRows {
   float eps, d;       // d = D
 };
 
-constexpr int kNormElems = 16;  // elements of a row that a thread holds (a wavefront: 1024, 1024 threads: 16384)
 
 // sum over the up to 64 lanes of a row that lie in one wavefront (16: a row of the cross-lane moves)
 template <int G> __device__ __forceinline__ float lanes_sum(float v) {
@@ -209,11 +209,11 @@ struct NormBack {
 // One row of partial sums [2][D] for each workgroup: dgamma, dbeta of the rows it took.  A workgroup of 8 wavefronts (16 for
 // rows of 1024 threads) works on as many rows at a time as it has groups of G threads and adds up their sums in LDS: a partial
 // row for every group would be a third of the traffic of 8192 rows of 1024.
-constexpr int norm_bwd_threads(int G) { return G > 512 ? G : 512; }
+constexpr int norm_bwd_threads(int G, int NV) { return G > 512 || NV == 1 ? 1024 : 512; }
 template <typename T, typename WT, int G, int CE, int NV>
-__global__ __launch_bounds__(norm_bwd_threads(G)) void norm_bwd_kernel(NormBack b, const T* dY, const T* X, const WT* gamma, const float* mean,
+__global__ __launch_bounds__(norm_bwd_threads(G, NV)) void norm_bwd_kernel(NormBack b, const T* dY, const T* X, const WT* gamma, const float* mean,
                                                                      const float* rstd, T* dX, float* part) {
-  constexpr int GROUPS = norm_bwd_threads(G) / G, N = NV * CE, W = G > 64 ? G / 64 : 1;  // rows at a time, elements of a thread, wavefronts of a row
+  constexpr int GROUPS = norm_bwd_threads(G, NV) / G, N = NV * CE, W = G > 64 ? G / 64 : 1;  // rows at a time, elements of a thread, wavefronts of a row
   constexpr int PARTS = GROUPS / (G < 64 ? 64 / G : 1);  // sums of groups that do not share a wavefront
   constexpr bool AHEAD = G < 1024;  // the next row is asked for while one is worked on, and gamma is held (16 wavefronts have no registers for either)
   __shared__ float slots[2][2][GROUPS][W];
@@ -332,10 +332,11 @@ __global__ __launch_bounds__(norm_bwd_threads(G)) void norm_bwd_kernel(NormBack 
 // Few rows: one launch in place of two.  The first `row_blocks` workgroups take a row a group, the others 16 runs of columns
 // each, whose sums over the rows they make from the inputs themselves (which the caches hold): dealt to threads / 16 lanes,
 // added in order.  128 x 1000 bf16 takes 4.2 us of calls in a row (the host's time), 6.7 in two launches.
+constexpr int norm_few_threads(int G) { return G > 512 ? G : 512; }
 template <typename T, typename WT, int G, int CE, int NV>
-__global__ __launch_bounds__(norm_bwd_threads(G)) void norm_bwd_few_kernel(NormBack b, const T* dY, const T* X, const WT* gamma, const float* mean,
+__global__ __launch_bounds__(norm_few_threads(G)) void norm_bwd_few_kernel(NormBack b, const T* dY, const T* X, const WT* gamma, const float* mean,
                                                                          const float* rstd, T* dX, WT* dgamma, WT* dbeta, int row_blocks) {
-  constexpr int THREADS = norm_bwd_threads(G), GROUPS = THREADS / G, W = G > 64 ? G / 64 : 1;
+  constexpr int THREADS = norm_few_threads(G), GROUPS = THREADS / G, W = G > 64 ? G / 64 : 1;
   __shared__ float slots[2][GROUPS][W];
   __shared__ float sums[THREADS / 64][16][2 * CE];
   const int D = b.a.D, R = b.a.R;
@@ -501,42 +502,66 @@ __global__ __launch_bounds__(1024) void norm_weight_grad_kernel(int D, int P, co
   }
 }
 
-// threads a row belongs to; 0: rows too long for registers
-static int norm_group(int D) {
-  for (int g = 16; g <= 1024; g *= 2)
-    if (D <= g * kNormElems) return g;
-  return 0;
+// How a row is dealt: `threads`, each with `runs` runs of 16 bytes (a row too short for one: of single elements).  No threads: rows
+// too long for registers.
+struct NormShape {
+  int threads, runs;
+};
+// 16 elements a thread.  bf16, whose lanes hold fewer bytes, also 24 in place of twice the threads (forward + backward, 2^25 elements in rows of
+// 1100: 29.5 + 45.5 us, 36.6 + 61.4 as 16 of 128 threads; 2100: 31 + 47, 37 + 64; 9000: 28 + 49, 38 + 64; at the other end of the range,
+// 1400 and 6000, 28 + 44, 28 + 42 and 29 + 47, 28 + 45), and 8 of the shortest rows (72: 39 + 49, 54 + 73).  fp32 lost nothing there (1100 and 2100:
+// 5.0 TB/s and more).
+template <typename T> static NormShape norm_shape(int D) {
+  constexpr int CE = ElemTraits<T>::CE;
+  const int runs = (D + CE - 1) / CE;
+  if (D < CE || (CE == 8 && runs <= 16)) return {16, 1};
+  for (int g = 16; g <= 1024; g *= 2) {
+    if (runs <= g * 16 / CE) return {g, 16 / CE};
+    if (CE == 8 && g < 1024 && runs <= g * 3) return {g, 3};
+  }
+  return {0, 0};
 }
 // workgroups of the backward pass, each with a row of partial sums
-static int norm_parts(int R, int D) {
-  const int g = norm_group(D), rows = g ? norm_bwd_threads(g) / g : 1;  // rows a workgroup takes at a time
-  return imin(R / rows + (R % rows != 0), g ? 256 : 64);
+template <typename T> static int norm_parts(int R, int D) {
+  const NormShape s = norm_shape<T>(D);
+  const int rows = s.threads ? norm_bwd_threads(s.threads, s.runs) / s.threads : 1;  // rows a workgroup takes at a time
+  return imin(R / rows + (R % rows != 0), s.threads ? 256 : 64);
 }
 
 // Few rows take one launch: up to 512, bf16 or fp32, 100 to 8192 elements, it was faster throughout (512 x 1000 bf16 5.6 us against
 // 6.8, 512 x 8192 10.0 against 16.0); at 1024 rows of 1000 it was not (10.4 against 7.5).
-static bool norm_few(int R, int D) { return R <= 512 && norm_group(D); }
+static bool norm_few(int R, int D) { return R <= 512 && D <= 16384; }
 
-// Calls with<threads of a row, elements of a run, runs>: runs of 16 bytes, or of single elements where a row has too few for one.
+// (one answer for all types, whose partial rows are not equally many)
+static size_t norm_ws_bytes(int R, int D) {
+  return norm_few(R, D) ? 0 : (size_t)std::max(norm_parts<float>(R, D), norm_parts<uint16_t>(R, D)) * 2 * D * sizeof(float);
+}
+
+// Calls with<threads of a row, elements of a run, runs>.
 template <typename T, class F> static void norm_instance(int D, F&& with) {
-  constexpr int CE = ElemTraits<T>::CE, NV = kNormElems / CE;
+  constexpr int CE = ElemTraits<T>::CE;
   using std::integral_constant;
   if (D < CE) return with(integral_constant<int, 16>(), integral_constant<int, 1>(), integral_constant<int, 1>());
-  switch (norm_group(D)) {
-#define ARD_NORM_GROUP(G) \
-  case G: return with(integral_constant<int, G>(), integral_constant<int, CE>(), integral_constant<int, NV>());
-    ARD_NORM_GROUP(16) ARD_NORM_GROUP(32) ARD_NORM_GROUP(64) ARD_NORM_GROUP(128) ARD_NORM_GROUP(256) ARD_NORM_GROUP(512)
-#undef ARD_NORM_GROUP
-    default: return with(integral_constant<int, 1024>(), integral_constant<int, CE>(), integral_constant<int, NV>());
+  const NormShape s = norm_shape<T>(D);
+#define ARD_NORM_SHAPE(G, NV) \
+  if (s.threads == G && s.runs == NV) return with(integral_constant<int, G>(), integral_constant<int, CE>(), integral_constant<int, NV>());
+#define ARD_NORM_SHAPES(NV) ARD_NORM_SHAPE(16, NV) ARD_NORM_SHAPE(32, NV) ARD_NORM_SHAPE(64, NV) ARD_NORM_SHAPE(128, NV) ARD_NORM_SHAPE(256, NV) ARD_NORM_SHAPE(512, NV)
+  ARD_NORM_SHAPES(16 / CE)
+  ARD_NORM_SHAPE(1024, 16 / CE)
+  if constexpr (CE == 8) {
+    ARD_NORM_SHAPE(16, 1)
+    ARD_NORM_SHAPES(3)
   }
+#undef ARD_NORM_SHAPES
+#undef ARD_NORM_SHAPE
 }
 
 // (the rows beyond a grid of this size are taken in turns: HIP counts a grid's threads in 32 bits)
 static unsigned norm_grid(int R) { return (unsigned)imin(R, 1 << 20); }
 // workgroups of the forward pass: 16 wavefronts a CU, which then go through their rows
-static unsigned norm_fwd_grid(int R, int G) {
+static unsigned norm_fwd_grid(int R, int G, int NV) {
   const int rows = norm_fwd_threads(G) / G;
-  return (unsigned)imin(R / rows + (R % rows != 0), 1024 * 256 / norm_fwd_threads(G));
+  return (unsigned)imin(R / rows + (R % rows != 0), (NV == 1 ? 2048 : 1024) * 256 / norm_fwd_threads(G));
 }
 
 static int32_t norm_check(int32_t dtype, int32_t wdtype, int32_t R, int32_t D, int32_t flags, std::initializer_list<int64_t> lds, std::initializer_list<int64_t> out_lds) {
@@ -558,9 +583,9 @@ static int32_t norm_fwd_t(const NormRows& a, const void* X, const void* gamma, c
   const T* x = (const T*)X;
   const WT *g = (const WT*)gamma, *b = (const WT*)beta;
   T* y = (T*)Y;
-  if (norm_group(a.D))
+  if (norm_shape<T>(a.D).threads)
     norm_instance<T>(a.D, [&](auto G, auto CE, auto NV) {
-      ARD_LAUNCH((norm_fwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(norm_fwd_grid(a.R, G.value)),
+      ARD_LAUNCH((norm_fwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(norm_fwd_grid(a.R, G.value, NV.value)),
                  dim3(norm_fwd_threads(G.value)), 0, st, a, x, g, b, y, mean, rstd);
     });
   else
@@ -575,20 +600,20 @@ static int32_t norm_bwd_t(const NormBack& b, const void* dY, const void* X, cons
   const T *dy = (const T*)dY, *x = (const T*)X;
   const WT* g = (const WT*)gamma;
   T* dx = (T*)dX;
-  const int P = norm_parts(b.a.R, b.a.D), D = b.a.D;
+  const int P = norm_parts<T>(b.a.R, b.a.D), D = b.a.D;
   if (norm_few(b.a.R, D)) {
     norm_instance<T>(D, [&](auto G, auto CE, auto NV) {
-      constexpr int rows = norm_bwd_threads(G.value) / G.value;
+      constexpr int rows = norm_few_threads(G.value) / G.value;
       const int row_blocks = ceil_div(b.a.R, rows), col_blocks = dgamma || dbeta ? ceil_div(D, 16 * CE.value) : 0;
-      ARD_LAUNCH((norm_bwd_few_kernel<T, WT, G.value, CE.value, NV.value>), dim3(row_blocks + col_blocks), dim3(norm_bwd_threads(G.value)), 0, st, b, dy, x, g,
+      ARD_LAUNCH((norm_bwd_few_kernel<T, WT, G.value, CE.value, NV.value>), dim3(row_blocks + col_blocks), dim3(norm_few_threads(G.value)), 0, st, b, dy, x, g,
                  mean, rstd, dx, (WT*)dgamma, (WT*)dbeta, row_blocks);
     });
     ARD_LAUNCH_CHECK("norm_bwd_few_kernel");
     return ARD_OK;
   }
-  if (norm_group(D)) {
+  if (norm_shape<T>(D).threads) {
     norm_instance<T>(D, [&](auto G, auto CE, auto NV) {
-      ARD_LAUNCH((norm_bwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(P), dim3(norm_bwd_threads(G.value)), 0, st, b, dy, x, g, mean, rstd, dx, part);
+      ARD_LAUNCH((norm_bwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(P), dim3(norm_bwd_threads(G.value, NV.value)), 0, st, b, dy, x, g, mean, rstd, dx, part);
     });
   } else {
     ARD_LAUNCH((norm_bwd_long_kernel<T, WT>), dim3(norm_grid(b.a.R)), dim3(1024), 0, st, b, dy, x, g, mean, rstd, dx);
@@ -608,7 +633,7 @@ using namespace ard;
 
 extern "C" size_t ard_layer_norm_workspace_bytes(int32_t R, int32_t D) {
   if (R <= 0 || D <= 0 || D > 1 << 30) return 0;
-  return norm_few(R, D) ? 0 : (size_t)norm_parts(R, D) * 2 * D * sizeof(float);
+  return norm_ws_bytes(R, D);
 }
 
 extern "C" int32_t ard_layer_norm_fwd(int32_t dtype, int32_t wdtype, int32_t R, int32_t D, const void* X, int64_t ldx, const void* gamma,
@@ -638,7 +663,7 @@ extern "C" int32_t ard_layer_norm_bwd(int32_t dtype, int32_t wdtype, int32_t R, 
   const NormBack b{{R, D, flags & ARD_OUT_COMPACT ? pad8(D) : D, ldx, 0, 0.0f, (float)D}, lddy, lddx};
   float* part = nullptr;
   if ((dgamma || dbeta) && !norm_few(R, D)) {
-    const size_t need = (size_t)norm_parts(R, D) * 2 * D * sizeof(float);
+    const size_t need = norm_ws_bytes(R, D);
     if (!ws || ws_bytes < need || misaligned(ws, 4)) return fail(ARD_EWORKSPACE, "workspace too small: need %zu bytes, got %zu", need, ws ? ws_bytes : 0);
     part = (float*)ws;
   }

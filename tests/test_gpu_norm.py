@@ -74,6 +74,13 @@ def test_more_rows_than_workgroups(R, D):
     _check(R, D, "f32", "f32", R)
 
 
+@pytest.mark.parametrize("D", [8, 127, 128, 129, 257, 384, 385, 520, 768, 769, 1026, 1535, 1537, 2100, 3071, 3080, 4100, 6144, 6145, 8200, 12288, 12290, 16383])
+def test_rows_on_both_sides_of_every_number_of_runs(D):
+    for R in (3, 520, 1030):
+        _check(R, D, "bf16", "f32", R + D)
+    _check(700, D, "bf16", "bf16", D)
+
+
 @pytest.mark.parametrize("gamma,beta", [(False, False), (True, False), (False, True)])
 @pytest.mark.parametrize("D", [33, 2048, 18000])
 def test_without_weights(gamma, beta, D):
