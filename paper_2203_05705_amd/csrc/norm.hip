@@ -11,7 +11,7 @@
 // second, small pass that adds them in a fixed order.
 //
 // Measured, bf16: 16384 x 4096 forward 47 us (5.7 TB/s from and to memory and the last cache; a large copy 4.9), backward 79 + 5 (5.1);
-// 8192 x 1024 8.4, 11.3 + 3.8; 1027 x 1501 (rows at odd addresses) 4.8, 7.6 + 3.4; 100000 x 128 13, 22 together.  The next row in
+// 8192 x 1024 8.6, 11.5 + 3.8; 1027 x 1501 (rows at odd addresses) 4.8, 7.6 + 3.4; 100000 x 128 10, 18 together.  The next row in
 // flight, kept whole accesses and fewer partial sums made the backward pass of 16384 x 4096 136 -> 84 us.
 #include <algorithm>
 #include <type_traits>
@@ -509,21 +509,22 @@ struct NormShape {
 };
 // 16 elements a thread.  bf16, whose lanes hold fewer bytes, also 24 in place of twice the threads (forward + backward, 2^25 elements in rows of
 // 1100: 29.5 + 45.5 us, 36.6 + 61.4 as 16 of 128 threads; 2100: 31 + 47, 37 + 64; 9000: 28 + 49, 38 + 64; at the other end of the range,
-// 1400 and 6000, 28 + 44, 28 + 42 and 29 + 47, 28 + 45), and 8 of the shortest rows (72: 39 + 49, 54 + 73).  fp32 lost nothing there (1100 and 2100:
-// 5.0 TB/s and more).
-template <typename T> static NormShape norm_shape(int D) {
+// 1400 and 6000, 28 + 44, 28 + 42 and 29 + 47, 28 + 45), if that leaves two rows a group to the backward pass's 256 workgroups
+// (8000 x 600 6.1 + 12.7, 6.6 + 11.9; 2000 x 300 4.7 + 10.7, 4.7 + 8.8) or the alternative is 1024 threads (300 x 9000 6.0 + 8.1, 7.1 + 12.2), and 8 of the shortest rows (466033 x 72: 39 + 49, 54 + 73; 2500 x 100 5.2 + 8.5, 4.7 + 8.9).
+// fp32 lost nothing there (1100 and 2100: 5.0 TB/s and more).
+template <typename T> static NormShape norm_shape(int R, int D) {
   constexpr int CE = ElemTraits<T>::CE;
   const int runs = (D + CE - 1) / CE;
   if (D < CE || (CE == 8 && runs <= 16)) return {16, 1};
   for (int g = 16; g <= 1024; g *= 2) {
     if (runs <= g * 16 / CE) return {g, 16 / CE};
-    if (CE == 8 && g < 1024 && runs <= g * 3) return {g, 3};
+    if (CE == 8 && g < 1024 && runs <= g * 3 && (g == 512 || (int64_t)R * g >= 1 << 18)) return {g, 3};
   }
   return {0, 0};
 }
 // workgroups of the backward pass, each with a row of partial sums
 template <typename T> static int norm_parts(int R, int D) {
-  const NormShape s = norm_shape<T>(D);
+  const NormShape s = norm_shape<T>(R, D);
   const int rows = s.threads ? norm_bwd_threads(s.threads, s.runs) / s.threads : 1;  // rows a workgroup takes at a time
   return imin(R / rows + (R % rows != 0), s.threads ? 256 : 64);
 }
@@ -538,11 +539,11 @@ static size_t norm_ws_bytes(int R, int D) {
 }
 
 // Calls with<threads of a row, elements of a run, runs>.
-template <typename T, class F> static void norm_instance(int D, F&& with) {
+template <typename T, class F> static void norm_instance(int R, int D, F&& with) {
   constexpr int CE = ElemTraits<T>::CE;
   using std::integral_constant;
   if (D < CE) return with(integral_constant<int, 16>(), integral_constant<int, 1>(), integral_constant<int, 1>());
-  const NormShape s = norm_shape<T>(D);
+  const NormShape s = norm_shape<T>(R, D);
 #define ARD_NORM_SHAPE(G, NV) \
   if (s.threads == G && s.runs == NV) return with(integral_constant<int, G>(), integral_constant<int, CE>(), integral_constant<int, NV>());
 #define ARD_NORM_SHAPES(NV) ARD_NORM_SHAPE(16, NV) ARD_NORM_SHAPE(32, NV) ARD_NORM_SHAPE(64, NV) ARD_NORM_SHAPE(128, NV) ARD_NORM_SHAPE(256, NV) ARD_NORM_SHAPE(512, NV)
@@ -583,8 +584,8 @@ static int32_t norm_fwd_t(const NormRows& a, const void* X, const void* gamma, c
   const T* x = (const T*)X;
   const WT *g = (const WT*)gamma, *b = (const WT*)beta;
   T* y = (T*)Y;
-  if (norm_shape<T>(a.D).threads)
-    norm_instance<T>(a.D, [&](auto G, auto CE, auto NV) {
+  if (norm_shape<T>(a.R, a.D).threads)
+    norm_instance<T>(a.R, a.D, [&](auto G, auto CE, auto NV) {
       ARD_LAUNCH((norm_fwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(norm_fwd_grid(a.R, G.value, NV.value)),
                  dim3(norm_fwd_threads(G.value)), 0, st, a, x, g, b, y, mean, rstd);
     });
@@ -602,7 +603,7 @@ static int32_t norm_bwd_t(const NormBack& b, const void* dY, const void* X, cons
   T* dx = (T*)dX;
   const int P = norm_parts<T>(b.a.R, b.a.D), D = b.a.D;
   if (norm_few(b.a.R, D)) {
-    norm_instance<T>(D, [&](auto G, auto CE, auto NV) {
+    norm_instance<T>(b.a.R, D, [&](auto G, auto CE, auto NV) {
       constexpr int rows = norm_few_threads(G.value) / G.value;
       const int row_blocks = ceil_div(b.a.R, rows), col_blocks = dgamma || dbeta ? ceil_div(D, 16 * CE.value) : 0;
       ARD_LAUNCH((norm_bwd_few_kernel<T, WT, G.value, CE.value, NV.value>), dim3(row_blocks + col_blocks), dim3(norm_few_threads(G.value)), 0, st, b, dy, x, g,
@@ -611,8 +612,8 @@ static int32_t norm_bwd_t(const NormBack& b, const void* dY, const void* X, cons
     ARD_LAUNCH_CHECK("norm_bwd_few_kernel");
     return ARD_OK;
   }
-  if (norm_shape<T>(D).threads) {
-    norm_instance<T>(D, [&](auto G, auto CE, auto NV) {
+  if (norm_shape<T>(b.a.R, D).threads) {
+    norm_instance<T>(b.a.R, D, [&](auto G, auto CE, auto NV) {
       ARD_LAUNCH((norm_bwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(P), dim3(norm_bwd_threads(G.value, NV.value)), 0, st, b, dy, x, g, mean, rstd, dx, part);
     });
   } else {

@@ -81,6 +81,12 @@ def test_rows_on_both_sides_of_every_number_of_runs(D):
     _check(700, D, "bf16", "bf16", D)
 
 
+@pytest.mark.parametrize("R,D", [(20001, 270), (8200, 600), (4099, 1101), (2051, 2177), (1027, 4353), (520, 8705)])
+def test_enough_rows_for_more_elements_a_thread(R, D):
+    _check(R, D, "bf16", "f32", R)
+    _check(R, D, "bf16", "bf16", D)
+
+
 @pytest.mark.parametrize("gamma,beta", [(False, False), (True, False), (False, True)])
 @pytest.mark.parametrize("D", [33, 2048, 18000])
 def test_without_weights(gamma, beta, D):
