@@ -20,7 +20,7 @@
 // saved, sequences and addresses by lane cost the backward pass 1 to 5 % (64 x 128 x 1024 30.6 to 31.4 us).
 //
 // Measured, bf16 with a gate: 64 x 128 x 1024 forward 14.6 us, backward 24 behind it and 31 from memory (4.9, 3.8 TB/s; a large
-// copy 4.9); 32768 x 1 x 1024 forward 25 + 49 us; 8192 x 4 x 1024 without one forward 27 + 43, backward 25 + 55; a single
+// copy 4.9); 32768 x 1 x 1024 forward 24 + 49 us; 8192 x 4 x 1024 without one forward 27 + 41, backward 24 + 57; a single
 // step of 128 sequences 2.8 us.
 #include <type_traits>
 
