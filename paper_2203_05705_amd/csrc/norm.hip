@@ -5,7 +5,7 @@
 //
 // Every pass is bound by memory: a row is read once into registers, its mean and then its centred square sum (no
 // difference of large sums) are taken there in fp32, and its result is rounded once, when it is stored.  A row belongs
-// to G threads, 16 elements each (8 to 24 in bf16): 16, 32 or 64 lanes of a wavefront, or 128 to 1024 threads of a workgroup; longer
+// to G threads, 16 elements each (up to 24 in bf16, a run of 16 bytes of short rows): 8 to 64 lanes of a wavefront, or 128 to 1024 threads of a workgroup; longer
 // rows are read again from the cache.  The backward pass keeps dgamma and dbeta of a thread's columns in registers over
 // all the rows that its workgroup takes, so the sums over rows cost one row of partial sums for each workgroup and a
 // second, small pass that adds them in a fixed order.
@@ -28,10 +28,11 @@ struct NormRows {
 };
 
 
-// sum over the up to 64 lanes of a row that lie in one wavefront (16: a row of the cross-lane moves)
+// sum over the up to 64 lanes of a row that lie in one wavefront (16: a row of the cross-lane moves, 8: half of one)
 template <int G> __device__ __forceinline__ float lanes_sum(float v) {
-  static_assert(G == 16 || G == 32 || G >= 64, "");
+  static_assert(G == 8 || G == 16 || G == 32 || G >= 64, "");
   if constexpr (G >= 64) return wave_sum(v);
+  if constexpr (G == 8) return half_row_sum(v);
   v = row_sum(v);
   if constexpr (G == 32) v += __shfl_xor(v, 16);
   return v;
@@ -209,11 +210,11 @@ struct NormBack {
 // One row of partial sums [2][D] for each workgroup: dgamma, dbeta of the rows it took.  A workgroup of 8 wavefronts (16 for
 // rows of 1024 threads) works on as many rows at a time as it has groups of G threads and adds up their sums in LDS: a partial
 // row for every group would be a third of the traffic of 8192 rows of 1024.
-constexpr int norm_bwd_threads(int G, int NV) { return G > 512 || NV == 1 ? 1024 : 512; }
+constexpr int norm_bwd_threads(int G, int N) { return G > 512 || N <= 8 ? 1024 : 512; }
 template <typename T, typename WT, int G, int CE, int NV>
-__global__ __launch_bounds__(norm_bwd_threads(G, NV)) void norm_bwd_kernel(NormBack b, const T* dY, const T* X, const WT* gamma, const float* mean,
+__global__ __launch_bounds__(norm_bwd_threads(G, NV * CE)) void norm_bwd_kernel(NormBack b, const T* dY, const T* X, const WT* gamma, const float* mean,
                                                                      const float* rstd, T* dX, float* part) {
-  constexpr int GROUPS = norm_bwd_threads(G, NV) / G, N = NV * CE, W = G > 64 ? G / 64 : 1;  // rows at a time, elements of a thread, wavefronts of a row
+  constexpr int GROUPS = norm_bwd_threads(G, NV * CE) / G, N = NV * CE, W = G > 64 ? G / 64 : 1;  // rows at a time, elements of a thread, wavefronts of a row
   constexpr int PARTS = GROUPS / (G < 64 ? 64 / G : 1);  // sums of groups that do not share a wavefront
   constexpr bool AHEAD = G < 1024;  // the next row is asked for while one is worked on, and gamma is held (16 wavefronts have no registers for either)
   __shared__ float slots[2][2][GROUPS][W];
@@ -515,7 +516,9 @@ struct NormShape {
 template <typename T> static NormShape norm_shape(int R, int D) {
   constexpr int CE = ElemTraits<T>::CE;
   const int runs = (D + CE - 1) / CE;
-  if (D < CE || (CE == 8 && runs <= 16)) return {16, 1};
+  if (runs <= 8 || D < CE) return {8, 1};
+  if (runs <= 16) return {16, 1};
+  if (CE == 4 && runs <= 32) return {16, 2};
   for (int g = 16; g <= 1024; g *= 2) {
     if (runs <= g * 16 / CE) return {g, 16 / CE};
     if (CE == 8 && g < 1024 && runs <= g * 3 && (g == 512 || (int64_t)R * g >= 1 << 18)) return {g, 3};
@@ -525,7 +528,7 @@ template <typename T> static NormShape norm_shape(int R, int D) {
 // workgroups of the backward pass, each with a row of partial sums
 template <typename T> static int norm_parts(int R, int D) {
   const NormShape s = norm_shape<T>(R, D);
-  const int rows = s.threads ? norm_bwd_threads(s.threads, s.runs) / s.threads : 1;  // rows a workgroup takes at a time
+  const int rows = s.threads ? norm_bwd_threads(s.threads, s.runs * ElemTraits<T>::CE) / s.threads : 1;  // rows a workgroup takes at a time
   return imin(R / rows + (R % rows != 0), s.threads ? 256 : 64);
 }
 
@@ -542,16 +545,19 @@ static size_t norm_ws_bytes(int R, int D) {
 template <typename T, class F> static void norm_instance(int R, int D, F&& with) {
   constexpr int CE = ElemTraits<T>::CE;
   using std::integral_constant;
-  if (D < CE) return with(integral_constant<int, 16>(), integral_constant<int, 1>(), integral_constant<int, 1>());
+  if (D < CE) return with(integral_constant<int, 8>(), integral_constant<int, 1>(), integral_constant<int, 1>());
   const NormShape s = norm_shape<T>(R, D);
 #define ARD_NORM_SHAPE(G, NV) \
   if (s.threads == G && s.runs == NV) return with(integral_constant<int, G>(), integral_constant<int, CE>(), integral_constant<int, NV>());
 #define ARD_NORM_SHAPES(NV) ARD_NORM_SHAPE(16, NV) ARD_NORM_SHAPE(32, NV) ARD_NORM_SHAPE(64, NV) ARD_NORM_SHAPE(128, NV) ARD_NORM_SHAPE(256, NV) ARD_NORM_SHAPE(512, NV)
+  ARD_NORM_SHAPE(8, 1)
+  ARD_NORM_SHAPE(16, 1)
   ARD_NORM_SHAPES(16 / CE)
   ARD_NORM_SHAPE(1024, 16 / CE)
   if constexpr (CE == 8) {
-    ARD_NORM_SHAPE(16, 1)
     ARD_NORM_SHAPES(3)
+  } else {
+    ARD_NORM_SHAPE(16, 2)
   }
 #undef ARD_NORM_SHAPES
 #undef ARD_NORM_SHAPE
@@ -560,9 +566,9 @@ template <typename T, class F> static void norm_instance(int R, int D, F&& with)
 // (the rows beyond a grid of this size are taken in turns: HIP counts a grid's threads in 32 bits)
 static unsigned norm_grid(int R) { return (unsigned)imin(R, 1 << 20); }
 // workgroups of the forward pass: 16 wavefronts a CU, which then go through their rows
-static unsigned norm_fwd_grid(int R, int G, int NV) {
+static unsigned norm_fwd_grid(int R, int G, int N) {
   const int rows = norm_fwd_threads(G) / G;
-  return (unsigned)imin(R / rows + (R % rows != 0), (NV == 1 ? 2048 : 1024) * 256 / norm_fwd_threads(G));
+  return (unsigned)imin(R / rows + (R % rows != 0), (N <= 8 ? 2048 : 1024) * 256 / norm_fwd_threads(G));
 }
 
 static int32_t norm_check(int32_t dtype, int32_t wdtype, int32_t R, int32_t D, int32_t flags, std::initializer_list<int64_t> lds, std::initializer_list<int64_t> out_lds) {
@@ -586,7 +592,7 @@ static int32_t norm_fwd_t(const NormRows& a, const void* X, const void* gamma, c
   T* y = (T*)Y;
   if (norm_shape<T>(a.R, a.D).threads)
     norm_instance<T>(a.R, a.D, [&](auto G, auto CE, auto NV) {
-      ARD_LAUNCH((norm_fwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(norm_fwd_grid(a.R, G.value, NV.value)),
+      ARD_LAUNCH((norm_fwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(norm_fwd_grid(a.R, G.value, NV.value * CE.value)),
                  dim3(norm_fwd_threads(G.value)), 0, st, a, x, g, b, y, mean, rstd);
     });
   else
@@ -614,7 +620,7 @@ static int32_t norm_bwd_t(const NormBack& b, const void* dY, const void* X, cons
   }
   if (norm_shape<T>(b.a.R, D).threads) {
     norm_instance<T>(b.a.R, D, [&](auto G, auto CE, auto NV) {
-      ARD_LAUNCH((norm_bwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(P), dim3(norm_bwd_threads(G.value, NV.value)), 0, st, b, dy, x, g, mean, rstd, dx, part);
+      ARD_LAUNCH((norm_bwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(P), dim3(norm_bwd_threads(G.value, NV.value * CE.value)), 0, st, b, dy, x, g, mean, rstd, dx, part);
     });
   } else {
     ARD_LAUNCH((norm_bwd_long_kernel<T, WT>), dim3(norm_grid(b.a.R)), dim3(1024), 0, st, b, dy, x, g, mean, rstd, dx);

@@ -131,10 +131,14 @@ template <int N, typename T> __device__ __forceinline__ void values_of(const typ
 template <int CTRL, int ROWS> __device__ __forceinline__ float dpp_or_zero(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, false));
 }
-__device__ __forceinline__ float row_sum(float v) {  // over 16 neighbouring lanes, in all of them
+__device__ __forceinline__ float half_row_sum(float v) {  // over 8 neighbouring lanes, in all of them
   v += dpp_or_zero<0xB1, 0xf>(v);
   v += dpp_or_zero<0x4E, 0xf>(v);
   v += dpp_or_zero<0x141, 0xf>(v);
+  return v;
+}
+__device__ __forceinline__ float row_sum(float v) {  // over 16
+  v = half_row_sum(v);
   v += dpp_or_zero<0x140, 0xf>(v);
   return v;
 }
