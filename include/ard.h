@@ -479,6 +479,8 @@ int32_t ard_prune_schedule(int32_t n_epochs, double total, double mean, double v
  * (then ldy / lddx >= pad8(D)); elements behind D of the rows read are not looked at.
  * Backward: with q = dY gamma, dX = r (q - mean(q) - xh mean(q xh)), xh = (X - mu) r; dgamma[D] = sum of dY xh and dbeta[D] =
  * sum of dY over the rows, added in a fixed order; either may be NULL, and with both NULL no workspace is needed.
+ * In place: Y may lie where X does, dX where dY or X does (the same address and leading dimension); the results are the same bits.
+ * Otherwise no output may overlap an input or another output.
  */
 size_t ard_layer_norm_workspace_bytes(int32_t R, int32_t D);
 int32_t ard_layer_norm_fwd(int32_t dtype, int32_t wdtype, int32_t R, int32_t D, const void* X, int64_t ldx,

@@ -339,7 +339,8 @@ __global__ __launch_bounds__(norm_bwd_threads(G, NV * CE)) void norm_bwd_kernel(
 
 // Few rows: one launch in place of two.  The first `row_blocks` workgroups take a row a group, the others 16 runs of columns
 // each, whose sums over the rows they make from the inputs themselves (which the caches hold): dealt to threads / 16 lanes,
-// added in order.  128 x 1000 bf16 takes 4.2 us of calls in a row (the host's time), 6.7 in two launches.
+// added in order.  128 x 1000 bf16 takes 4.2 us of calls in a row (the host's time), 6.7 in two launches.  Where dX takes the place of an
+// input the two kinds of workgroups are two launches, sums first.
 constexpr int norm_few_threads(int G) { return G > 512 ? G : 512; }
 template <typename T, typename WT, int G, int CE, int NV>
 __global__ __launch_bounds__(norm_few_threads(G)) void norm_bwd_few_kernel(NormBack b, const T* dY, const T* X, const WT* gamma, const float* mean,
@@ -608,9 +609,11 @@ static int32_t norm_fwd_t(const NormRows& a, const void* X, const void* gamma, c
   return ARD_OK;
 }
 
+// in_place: dX lies where dY or X does.  A row's threads have read it before they store it, so only the sums over rows, where they
+// are made from the inputs once more, have to be made before dX is stored: a launch of their own then.
 template <typename T, typename WT>
 static int32_t norm_bwd_t(const NormBack& b, const void* dY, const void* X, const void* gamma, const float* mean, const float* rstd, void* dX,
-                          void* dgamma, void* dbeta, float* part, hipStream_t st) {
+                          void* dgamma, void* dbeta, float* part, bool in_place, hipStream_t st) {
   const T *dy = (const T*)dY, *x = (const T*)X;
   const WT* g = (const WT*)gamma;
   T* dx = (T*)dX;
@@ -619,8 +622,12 @@ static int32_t norm_bwd_t(const NormBack& b, const void* dY, const void* X, cons
     norm_instance<T>(b.a.R, D, [&](auto G, auto CE, auto NV) {
       constexpr int rows = norm_few_threads(G.value) / G.value;
       const int row_blocks = ceil_div(b.a.R, rows), col_blocks = dgamma || dbeta ? ceil_div(D, 16 * CE.value) : 0;
-      ARD_LAUNCH((norm_bwd_few_kernel<T, WT, G.value, CE.value, NV.value>), dim3(row_blocks + col_blocks), dim3(norm_few_threads(G.value)), 0, st, b, dy, x, g,
-                 mean, rstd, dx, (WT*)dgamma, (WT*)dbeta, row_blocks);
+      auto launch = [&](int of_rows, int of_cols) {
+        ARD_LAUNCH((norm_bwd_few_kernel<T, WT, G.value, CE.value, NV.value>), dim3(of_rows + of_cols), dim3(norm_few_threads(G.value)), 0, st, b, dy, x, g,
+                   mean, rstd, dx, (WT*)dgamma, (WT*)dbeta, of_rows);
+      };
+      if (in_place && col_blocks) launch(0, col_blocks), launch(row_blocks, 0);
+      else launch(row_blocks, col_blocks);
     });
     ARD_LAUNCH_CHECK("norm_bwd_few_kernel");
     return ARD_OK;
@@ -630,9 +637,11 @@ static int32_t norm_bwd_t(const NormBack& b, const void* dY, const void* X, cons
       ARD_LAUNCH((norm_bwd_kernel<T, WT, G.value, CE.value, NV.value>), dim3(P), dim3(norm_bwd_threads(G.value, NV.value * CE.value)), 0, st, b, dy, x, g, mean, rstd, dx, part);
     });
   } else {
+    auto sums = [&] { ARD_LAUNCH((norm_bwd_cols_kernel<T>), dim3(ceil_div(D, 64 * ElemTraits<T>::CE), P), dim3(64), 0, st, b, dy, x, mean, rstd, part); };
+    if (part && in_place) sums();
     ARD_LAUNCH((norm_bwd_long_kernel<T, WT>), dim3(norm_grid(b.a.R)), dim3(1024), 0, st, b, dy, x, g, mean, rstd, dx);
     ARD_LAUNCH_CHECK("norm_bwd_long_kernel");
-    if (part) ARD_LAUNCH((norm_bwd_cols_kernel<T>), dim3(ceil_div(D, 64 * ElemTraits<T>::CE), P), dim3(64), 0, st, b, dy, x, mean, rstd, part);
+    if (part && !in_place) sums();
   }
   ARD_LAUNCH_CHECK("norm_bwd_kernel");
   if (!part) return ARD_OK;
@@ -658,6 +667,7 @@ extern "C" int32_t ard_layer_norm_fwd(int32_t dtype, int32_t wdtype, int32_t R, 
   const size_t es = dtype == ARD_F32 ? 4 : 2, ws = wdtype == ARD_F32 ? 4 : 2;
   if (misaligned(X, es) || misaligned(Y, es) || misaligned(gamma, ws) || misaligned(beta, ws) || misaligned(mean, 4) || misaligned(rstd, 4))
     return fail(ARD_EINVAL, "a tensor does not start at a whole element");
+  if (R > 1 && X == Y && ldx != ldy) return fail(ARD_EINVAL, "Y in the place of X has its leading dimension");
   const NormRows a{R, D, flags & ARD_OUT_COMPACT ? pad8(D) : D, ldx, ldy, eps, (float)D};
   hipStream_t st = (hipStream_t)stream;
   if (dtype == ARD_F32) return norm_fwd_t<float, float>(a, X, gamma, beta, Y, mean, rstd, st);
@@ -675,6 +685,8 @@ extern "C" int32_t ard_layer_norm_bwd(int32_t dtype, int32_t wdtype, int32_t R, 
       misaligned(mean, 4) || misaligned(rstd, 4))
     return fail(ARD_EINVAL, "a tensor does not start at a whole element");
   const NormBack b{{R, D, flags & ARD_OUT_COMPACT ? pad8(D) : D, ldx, 0, 0.0f, (float)D}, lddy, lddx};
+  const bool in_place = dX == dY || dX == X;
+  if (R > 1 && ((dX == dY && lddx != lddy) || (dX == X && lddx != ldx))) return fail(ARD_EINVAL, "dX in the place of an input has its leading dimension");
   float* part = nullptr;
   if ((dgamma || dbeta) && !norm_few(R, D)) {
     const size_t need = norm_ws_bytes(R, D);
@@ -682,7 +694,7 @@ extern "C" int32_t ard_layer_norm_bwd(int32_t dtype, int32_t wdtype, int32_t R, 
     part = (float*)ws;
   }
   hipStream_t st = (hipStream_t)stream;
-  if (dtype == ARD_F32) return norm_bwd_t<float, float>(b, dY, X, gamma, mean, rstd, dX, dgamma, dbeta, part, st);
-  if (wdtype == ARD_F32) return norm_bwd_t<uint16_t, float>(b, dY, X, gamma, mean, rstd, dX, dgamma, dbeta, part, st);
-  return norm_bwd_t<uint16_t, uint16_t>(b, dY, X, gamma, mean, rstd, dX, dgamma, dbeta, part, st);
+  if (dtype == ARD_F32) return norm_bwd_t<float, float>(b, dY, X, gamma, mean, rstd, dX, dgamma, dbeta, part, in_place, st);
+  if (wdtype == ARD_F32) return norm_bwd_t<uint16_t, float>(b, dY, X, gamma, mean, rstd, dX, dgamma, dbeta, part, in_place, st);
+  return norm_bwd_t<uint16_t, uint16_t>(b, dY, X, gamma, mean, rstd, dX, dgamma, dbeta, part, in_place, st);
 }

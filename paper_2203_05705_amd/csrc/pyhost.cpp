@@ -1427,11 +1427,11 @@ PyMethodDef methods[] = {
     ENTRY(sens_block_pattern, "sens_block_pattern($module, pred, balance, m, n, seed, iteration, stream=None)\n--\n\n"
                               "Block-based pattern from ard_sens_predict's outputs: dict(sens (balanced), keep), each [N, RB, CB]."),
     ENTRY(layer_norm_fwd, "layer_norm_fwd($module, X, gamma=None, beta=None, eps=1e-05, D=None, out=None, stream=None)\n--\n\n"
-                          "Layer norm of the rows of X: (Y, mean[R], rstd[R]); out: reuse such a triple (None: a new one).  X: [R, D] with rows any\n"
+                          "Layer norm of the rows of X: (Y, mean[R], rstd[R]); out: reuse such a triple (None: a new one; Y may be X).  X: [R, D] with rows any\n"
                           "distance apart, or contiguous with D last; D: kept units of a compact activation [R, pad8(D)], of which Y is one too."),
     ENTRY(layer_norm_bwd, "layer_norm_bwd($module, dY, X, gamma, mean, rstd, D=None, out=None, ws=None, stream=None)\n--\n\n"
                           "Gradients (dX, dgamma, dbeta) of layer_norm_fwd, the latter two in gamma's dtype (None without gamma); out: reuse such a\n"
-                          "triple, where None leaves a weight's gradient out."),
+                          "triple, where None leaves a weight's gradient out (dX may be dY or X)."),
     ENTRY(glr_fwd, "glr_fwd($module, f, v, o=None, c0=None, lengths=None, train=True, H=None, out=None, ws=None, stream=None)\n--\n\n"
                    "Gated linear recurrence c = s(f) c + (1 - s(f)) v, h = s(o) c over f, v, o[T, B, H] (views of one strides): (h[T, B, H],\n"
                    "cT[B, H] fp32, ckpt: the states the backward pass needs, None with train=False); out: reuse such a triple.\n"

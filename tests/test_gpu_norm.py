@@ -187,6 +187,23 @@ def test_weights_gradients_one_at_a_time_and_none(rows):
             assert got[i] is None or torch.equal(got[i], full[i])
 
 
+@pytest.mark.parametrize("dtype,wdtype", DTYPES)
+@pytest.mark.parametrize("R,D", [(1, 1), (40, 7), (70, 60), (130, 1000), (512, 2100), (513, 70), (1030, 1501), (700, 16384), (3, 17000), (130, 20001)])
+def test_results_in_the_place_of_inputs(R, D, dtype, wdtype):
+    """Y over X, dX over dY and over X: the bits of a call with results elsewhere."""
+    X, dY, g, b = _inputs(R, D, dtype, wdtype, R + D)
+    Xd, dYd, gd, bd = from_vals(X, dtype), from_vals(dY, dtype), from_vals(g, wdtype), from_vals(b, wdtype)
+    Y, mean, rstd = ard.layer_norm_fwd(Xd, gd, bd)
+    want = ard.layer_norm_bwd(dYd, Xd, gd, mean, rstd)
+    over = Xd.clone()
+    got = ard.layer_norm_fwd(over, gd, bd, out=(over, None, None))
+    assert got[0] is over and all(torch.equal(p, q) for p, q in zip(got, (Y, mean, rstd)))
+    for place in range(2):
+        x, dy = Xd.clone(), dYd.clone()
+        got = ard.layer_norm_bwd(dy, x, gd, mean, rstd, out=((dy, x)[place], torch.empty_like(gd), torch.empty_like(gd)))
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
 def test_same_bits_on_every_call_and_in_a_graph():
     X, dY, g, b = _inputs(2000, 1100, "bf16", "f32", 2)
     Xd, dYd, gd, bd = from_vals(X, "bf16"), from_vals(dY, "bf16"), from_vals(g, "f32"), from_vals(b, "f32")

@@ -80,6 +80,29 @@ def test_norm_backward_accepts_and_refuses():
         assert lib.ard_layer_norm_workspace_bytes(0, 5) == 0 and lib.ard_layer_norm_workspace_bytes(5, -1) == 0
 
 
+def test_norm_backward_in_the_place_of_an_input_makes_its_sums_over_rows_first():
+    """Sums over rows that are made from the inputs once more may not meet a dX that is stored meanwhile or before."""
+    with D.dry_run() as lib:
+        heap = D.FakeHeap()
+        for place in ("dY", "X"):
+            for R, n, kernels in ((4, 24, ["norm_bwd_few_kernel"] * 2), (512, 24, ["norm_bwd_few_kernel"] * 2), (513, 24, ["norm_bwd_kernel", "norm_weight_grad_kernel"]),
+                                  (4, 20000, ["norm_bwd_cols_kernel", "norm_bwd_long_kernel", "norm_weight_grad_kernel"])):
+                a = _norm_bwd_args(heap, R=R, D=n, ldx=n, lddy=n, lddx=n, ws_bytes=1 << 30)
+                a["dX"] = a[place]
+                assert lib.ard_layer_norm_bwd(*a.values()) == 0 and D.launches(lib) == (len(kernels), kernels)
+                a.update(dgamma=None, dbeta=None)
+                assert lib.ard_layer_norm_bwd(*a.values()) == 0 and D.launches(lib)[0] == 1
+                a["lddx"] = n + 8   # rows that lie elsewhere than the input's, over each other
+                assert lib.ard_layer_norm_bwd(*a.values()) == -1 and D.launches(lib)[0] == 0
+                a["R"] = 1
+                assert lib.ard_layer_norm_bwd(*a.values()) == 0 and D.launches(lib)[0] == 1
+        a = _norm_args(heap)
+        a["Y"] = a["X"]
+        assert lib.ard_layer_norm_fwd(*a.values()) == 0 and D.launches(lib)[0] == 1
+        a["ldy"] = 32
+        assert lib.ard_layer_norm_fwd(*a.values()) == -1 and D.launches(lib)[0] == 0
+
+
 @pytest.mark.parametrize("dtype", [ard.F32, ard.BF16])
 def test_norm_takes_rows_of_every_length(dtype):
     with D.dry_run() as lib:
