@@ -367,6 +367,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_pairs_kernel(GlrArgs a
                                                                        float* seg_pairs) {
   __shared__ Pairs<VEC> lds;
   const GlrPlace p = glr_place<VEC>(a);
+  if (p.seg == 0) return;  // (nothing lies before it: its pair is not needed)
   const int waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   float tp[VEC], ts[VEC];
 #pragma unroll
@@ -607,7 +608,7 @@ static int32_t glr_bwd_t(const GlrCall& c, const float* ckpt, const void* dh, St
   const GlrArgs& a = c.g.a;
   const T *f = (const T*)c.f, *v = (const T*)c.v, *o = (const T*)c.o;
   const dim3 block(64 * c.g.waves);
-  if (a.segs > 1) {
+  if (a.segs > 1) {  // (the first segment's pair is not needed: its workgroups end at once)
     ARD_GLR_LAUNCH("glr_bwd_pairs_kernel", (glr_bwd_pairs_kernel<T, VEC, GATE>), glr_grid(a, a.segs), block, 0, st, a, f, o, c.z, (const T*)dh, ds, ws);
     ARD_LAUNCH_CHECK("glr_bwd_pairs_kernel");
   }

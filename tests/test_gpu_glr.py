@@ -115,6 +115,23 @@ def test_time_cut_over_workgroups(T, B, H, ragged, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_cut_time_makes_the_pairs_that_are_read(dtype):
+    """Of the segments' pairs in the workspace, [segment][P, S][B][H], the forward pass leaves the last out and the backward pass the first."""
+    T, B, H = 2500, 3, 64
+    f, v, o, dh, c0, dcT = _inputs(T, B, H, dtype, True, 9)
+    fd, vd, od, dhd = (_dev(x, dtype) for x in (f, v, o, dh))
+    n = ard.glr_workspace_bytes(ard.F32 if dtype == "f32" else ard.BF16, T, B, H) // 4
+    segs, none = n // (2 * B * H), 12345.0
+    ws = torch.full((segs, 2 * B * H), none, device="cuda")
+    assert segs > 2 and ws.numel() == n
+    _, _, ckpt = ard.glr_fwd(fd, vd, od, _dev(c0), ws=ws)
+    assert not (ws[:-1] == none).any() and (ws[-1] == none).all()
+    ws.fill_(none)
+    ard.glr_bwd(fd, vd, od, dhd, ckpt, _dev(dcT), ws=ws)
+    assert not (ws[1:] == none).any() and (ws[0] == none).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("H", [1, 6, 171, 500, 683])
 @pytest.mark.parametrize("T", [1, 35])
 def test_kept_units_of_a_row_pattern(T, H, dtype):
