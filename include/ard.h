@@ -506,7 +506,8 @@ int32_t ard_layer_norm_bwd(int32_t dtype, int32_t wdtype, int32_t R, int32_t D, 
  * the gradients have pad8(H) stored channels, zeros behind H (states are [B x H] all the same).
  * Backward: dh (strides dh_t, dh_b) and dcT (fp32 [B x H], NULL: zeros) are the gradients of h and cT; df, dv, dout (strides
  * dz_t, dz_b; dout NULL where o is) those of f, v, o, every element written, +0.0 behind a sequence's end; dc0 (fp32
- * [B x H], may be NULL) that of c0.
+ * [B x H], may be NULL) that of c0, which may be dcT.  The gradients may lie where f, v and o do, or h where f or v does (the same addresses
+ * and strides).  Otherwise no output may overlap an input or another output.
  * The workspace holds what workgroups that share a sequence tell each other; 0 bytes where none do.
  */
 /* steps between the states of ckpt */

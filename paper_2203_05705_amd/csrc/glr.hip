@@ -364,10 +364,18 @@ __device__ __forceinline__ void stretch_adjoint(const T* f, const T* o, const T*
 
 template <typename T, int VEC, bool GATE>
 __global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_pairs_kernel(GlrArgs a, const T* f, const T* o, Strides z, const T* dh, Strides ds,
-                                                                       float* seg_pairs) {
+                                                                       const float* dcT, float* seg_pairs) {
   __shared__ Pairs<VEC> lds;
   const GlrPlace p = glr_place<VEC>(a);
-  if (p.seg == 0) return;  // (nothing lies before it: its pair is not needed)
+  if (p.seg == 0) {  // (nothing lies before it: its pair is not needed)
+    if (dcT && threadIdx.x < 64) {  // the place of its P keeps a gradient that dc0 will be stored over
+      float e[VEC];
+      const int64_t state = (int64_t)p.b * a.H + p.ch;
+      load_some<VEC>(dcT + state, p.n, e);
+      store_some<VEC>(seg_pairs + state, p.n, e);
+    }
+    return;
+  }
   const int waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   float tp[VEC], ts[VEC];
 #pragma unroll
@@ -608,9 +616,13 @@ static int32_t glr_bwd_t(const GlrCall& c, const float* ckpt, const void* dh, St
   const GlrArgs& a = c.g.a;
   const T *f = (const T*)c.f, *v = (const T*)c.v, *o = (const T*)c.o;
   const dim3 block(64 * c.g.waves);
-  if (a.segs > 1) {  // (the first segment's pair is not needed: its workgroups end at once)
-    ARD_GLR_LAUNCH("glr_bwd_pairs_kernel", (glr_bwd_pairs_kernel<T, VEC, GATE>), glr_grid(a, a.segs), block, 0, st, a, f, o, c.z, (const T*)dh, ds, ws);
+  if (a.segs > 1) {
+    // Every segment's workgroups of the main launch begin with dcT; the first segment's store dc0.  Where the two are one, dcT is kept for them by the
+    // first segment's workgroups of this launch, which make no pair.
+    const float* keep = dcT && dcT == dc0 ? dcT : nullptr;
+    ARD_GLR_LAUNCH("glr_bwd_pairs_kernel", (glr_bwd_pairs_kernel<T, VEC, GATE>), glr_grid(a, a.segs), block, 0, st, a, f, o, c.z, (const T*)dh, ds, keep, ws);
     ARD_LAUNCH_CHECK("glr_bwd_pairs_kernel");
+    if (keep) dcT = ws;
   }
   const dim3 grid = glr_grid(a, a.segs);
   if (a.segs > 1)

@@ -1437,7 +1437,7 @@ PyMethodDef methods[] = {
                    "cT[B, H] fp32, ckpt: the states the backward pass needs, None with train=False); out: reuse such a triple.\n"
                    "H: kept units of compact tensors [T, B, pad8(H)]; lengths: int32 [B], steps of each sequence."),
     ENTRY(glr_bwd, "glr_bwd($module, f, v, o, dh, ckpt, dcT=None, lengths=None, H=None, out=None, ws=None, stream=None)\n--\n\n"
-                   "Gradients (df, dv, do, dc0) of glr_fwd (do: None without o); out: the first three or all four, to reuse."),
+                   "Gradients (df, dv, do, dc0) of glr_fwd (do: None without o); out: the first three or all four, to reuse (dc0 may be dcT)."),
     ENTRY(adamw_step, "adamw_step($module, params, grads, m, v, m_scale=None, v_scale=None, copies=None, lr=0.001, beta1=0.9, beta2=0.999, eps=1e-08, "
                       "weight_decay=0.01, step=1, grad_scale=None, stream=None)\n--\n\n"
                       "One AdamW step, in place, over lists of tensors: params fp32; grads fp32 or bf16; m, v fp32, or int8 and uint8 codes with\n"

@@ -132,6 +132,27 @@ def test_cut_time_makes_the_pairs_that_are_read(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,B,H", [(1, 3, 20), (40, 20, 70), (2500, 3, 64), (4099, 2, 37), (20000, 1, 130)])
+def test_gradients_in_the_place_of_what_they_are_made_from(T, B, H, dtype):
+    """dc0 over dcT, and df, dv, do over f, v, o as well: the bits of a call with results elsewhere, time cut or not."""
+    f, v, o, dh, c0, dcT = _inputs(T, B, H, dtype, True, T)
+    fd, vd, od, dhd = (_dev(x, dtype) for x in (f, v, o, dh))
+    n = torch.from_numpy(_lengths(T, B, T)).cuda() if B > 2 else None
+    h, cT, ckpt = ard.glr_fwd(fd, vd, od, _dev(c0), n)
+    want = ard.glr_bwd(fd, vd, od, dhd, ckpt, _dev(dcT), n)
+    e = _dev(dcT)
+    got = ard.glr_bwd(fd, vd, od, dhd, ckpt, e, n, out=(None, None, None, e))
+    assert got[3] is e and all(torch.equal(p, q) for p, q in zip(got, want))
+    e, place = _dev(dcT), [t.clone() for t in (fd, vd, od)]
+    got = ard.glr_bwd(*place, dhd, ckpt, e, n, out=(*place, e))
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    place = [t.clone() for t in (fd, vd)]
+    for out in place:
+        a, b = (out, vd) if out is place[0] else (fd, out)
+        assert torch.equal(ard.glr_fwd(a, b, od, _dev(c0), n, out=(out, None, None))[0], h)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("H", [1, 6, 171, 500, 683])
 @pytest.mark.parametrize("T", [1, 35])
 def test_kept_units_of_a_row_pattern(T, H, dtype):
