@@ -1208,7 +1208,10 @@ PyObject* adamw_values(const Args& a) {  // m, v, m_scale, v_scale, out, stream
   OnStream on(a.v[5]);
   try {
     if (a.given(4)) {
-      r = give(a.v[4]);
+      // (the list or tuple itself; of anything else a list of its items, which keeps them)
+      r = PySequence_Fast(a.v[4], "a pair of lists of output tensors is wanted");
+      if (!r) throw PyRaised{};
+      if (PySequence_Fast_GET_SIZE(r) != 2) raise(PyExc_ValueError, "a pair of lists of output tensors is wanted");
     } else {
       r = PyTuple_New(2);
       for (int k = 0; k < 2; ++k) {
@@ -1220,13 +1223,7 @@ PyObject* adamw_values(const Args& a) {  // m, v, m_scale, v_scale, out, stream
         }
       }
     }
-    PyObject* pair = PySequence_Fast(r, "a pair of lists of output tensors is wanted");
-    if (!pair) throw PyRaised{};
-    Py_ssize_t k = PySequence_Fast_GET_SIZE(pair);
-    PyObject* lists[2] = {k == 2 ? PySequence_Fast_GET_ITEM(pair, 0) : nullptr, k == 2 ? PySequence_Fast_GET_ITEM(pair, 1) : nullptr};
-    Py_DECREF(pair);  // (r keeps what the pair holds)
-    if (k != 2) raise(PyExc_ValueError, "a pair of lists of output tensors is wanted");
-    const TensorList om(lists[0], "out"), ov(lists[1], "out");
+    const TensorList om(PySequence_Fast_GET_ITEM(r, 0), "out"), ov(PySequence_Fast_GET_ITEM(r, 1), "out");
     if (!om.f || !ov.f) raise(PyExc_TypeError, "a pair of lists of output tensors is wanted");
     om.same(m.n), ov.same(m.n);
     for (Py_ssize_t i = 0; i < m.n; ++i) {

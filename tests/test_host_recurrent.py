@@ -286,6 +286,25 @@ def test_calls_marshal_their_tensors():
         assert ard.adamw_values([c8], [u8], [s], [s], out=([p], [m]), stream=STREAM)[0][0] is p
 
 
+def test_values_go_into_any_pair_of_lists():
+    """A pair that is made item by item has no other owner than the call."""
+    c8, u8 = fake(300, dtype=torch.int8), fake(300, dtype=torch.uint8)
+    m, v = fake(300), fake(300)
+    with D.dry_run() as lib:
+        for out in (([m], [v]), [[m], (v,)], map(list, ((m,), (v,))), ([t] for t in (m, v)), (map(lambda t: t, [m]), iter([v]))):
+            kept = out if isinstance(out, (list, tuple)) else None
+            got = ard.adamw_values([c8], [u8], [fake(2)], [fake(2)], out=out, stream=STREAM)
+            assert kept is None or got is kept
+            if kept is None:
+                junk = [[i] for i in range(100)]   # (takes the memory of lists that were let go)
+                assert len(got) == 2 and got[0][0] is m and got[1][0] is v and len(junk) == 100
+            assert D.launches(lib) == (1, ["adamw_values_kernel"])
+        for bad in (iter([[m]]), map(list, ((m,), (v,), (m,))), 3):
+            with pytest.raises((TypeError, ValueError)):
+                ard.adamw_values([c8], [u8], [fake(2)], [fake(2)], out=bad, stream=STREAM)
+        assert D.launches(lib)[0] == 0
+
+
 def test_calls_refuse():
     bf16 = torch.bfloat16
     X, w, r, S, many = fake(30, 24, dtype=bf16), fake(24), fake(30), fake(4, 16), fake(600, 24, dtype=bf16)
