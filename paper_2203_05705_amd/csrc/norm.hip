@@ -169,7 +169,9 @@ __global__ __launch_bounds__(norm_fwd_threads(G)) void norm_fwd_kernel(NormRows 
   }
 }
 
-// rows too long for the registers of a workgroup: read three times, the second and third time from the cache
+// Rows too long for the registers of a workgroup: read three times, the second and third time from the cache.  A run's elements are added
+// up before their sum joins the thread's: one by one, 32768 squares of a thread (rows of 2^25 bf16 elements) came out
+// 1e-5 too large, each being ever less beside the growing sum.
 template <typename T, typename WT>
 __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(NormRows a, const T* X, const WT* gamma, const WT* beta, T* Y, float* mean, float* rstd) {
   constexpr int CE = ElemTraits<T>::CE;
@@ -180,18 +182,22 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(NormRows a, const T
     float s = 0.0f, v[CE];
     for (int64_t col = threadIdx.x * CE; col < a.D; col += 1024 * CE) {
       load_some<CE>(x + col, (int)(a.D - col), v);
+      float of_run = 0.0f;
   #pragma unroll
-      for (int j = 0; j < CE; ++j) s += v[j];
+      for (int j = 0; j < CE; ++j) of_run += v[j];
+      s += of_run;
     }
     const float mu = group_sum<1024>(s, slots[0]) / a.d;
     float q = 0.0f;
     for (int64_t col = threadIdx.x * CE; col < a.D; col += 1024 * CE) {
       load_some<CE>(x + col, (int)(a.D - col), v);
+      float of_run = 0.0f;
   #pragma unroll
       for (int j = 0; j < CE; ++j) {
         const float d = j < a.D - col ? v[j] - mu : 0.0f;
-        q = fmaf(d, d, q);
+        of_run = fmaf(d, d, of_run);
       }
+      q += of_run;
     }
     const float r = 1.0f / sqrtf(group_sum<1024>(q, slots[1]) / a.d + a.eps);
     if (threadIdx.x == 0) mean[row] = mu, rstd[row] = r;
@@ -440,12 +446,14 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(NormBack b, const T
       load_some<CE>(x + col, n, v);
       load_some<CE>(dy + col, n, u);
       load_weight<CE>(gamma, (int)col, n, 1.0f, g);
+      float of_run1 = 0.0f, of_run2 = 0.0f;
   #pragma unroll
       for (int j = 0; j < CE; ++j) {
         const float q = j < n ? u[j] * g[j] : 0.0f;
-        s1 += q;
-        s2 = fmaf(q, j < n ? (v[j] - mu) * r : 0.0f, s2);
+        of_run1 += q;
+        of_run2 = fmaf(q, j < n ? (v[j] - mu) * r : 0.0f, of_run2);
       }
+      s1 += of_run1, s2 += of_run2;
     }
     s1 = group_sum<1024>(s1, slots[0]) / b.a.d, s2 = group_sum<1024>(s2, slots[1]) / b.a.d;
     T* dx = dX + row * b.lddx;

@@ -258,6 +258,28 @@ def test_rows_beyond_32_bit_offsets():
     assert_parity(dX.contiguous(), N.layer_norm_bwd(dY, X, g, rmean, rrstd)[0], "bf16", None, "dX")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sums_of_very_long_rows(dtype):
+    """A row of 2^25 elements.  A thread adds the sums of 2^13 (fp32) or 2^12 (bf16) runs, each with at most half an ulp of the growing sum, to
+    either side: 2^6 halves of 2^-24, a thousandth of that once 1024 threads are added up, and 22 more roundings on the way there: 1.3e-6, of
+    which the root halves the square sum's share.  2e-6 of each result; the mean's against the spread."""
+    D = 1 << 25
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    X, dY = (torch.randn((1, D), generator=gen, device="cuda").to(torch.float32 if dtype == "f32" else torch.bfloat16) for _ in range(2))
+    dY += X   # (so that the mean of q xh is about 1)
+    Y, mean, rstd = ard.layer_norm_fwd(X)
+    dX, _, _ = ard.layer_norm_bwd(dY, X, None, mean, rstd)
+    x, dy = to_host(X), to_host(dY)
+    rY, rmean, rrstd = N.layer_norm_fwd(x)
+    assert abs(to_host(mean)[0] - rmean[0]) * rrstd[0] <= 2e-6 and abs(to_host(rstd)[0] / rrstd[0] - 1) <= 2e-6
+    rdX = N.layer_norm_bwd(dy, x, None, rmean, rrstd)[0]
+    assert_parity(Y, rY, dtype, None, "Y")
+    assert_parity(dX, rdX, dtype, None, "dX")
+    if dtype == "f32":   # the kernel's mean of q xh, read off its result along xh
+        xh = (x[0] - rmean[0]) * rrstd[0]
+        assert abs((to_host(dX)[0] - rdX[0]) @ xh) / D <= 4e-6
+
+
 def test_gradient_against_differences_of_the_forward_pass():
     """Along random directions: the change of sum(dY Y) in the oracle's 64 bits beside the kernel's gradients."""
     R, D = 5, 90
