@@ -495,7 +495,7 @@ template <typename WT>
 __global__ __launch_bounds__(1024) void norm_weight_grad_kernel(int D, int P, const float* part, WT* dgamma, WT* dbeta) {
   __shared__ float sums[16][16];
   const int c = threadIdx.x & 15, at = threadIdx.x >> 4;
-  const int64_t cols = 2 * (int64_t)D, col = (int64_t)blockIdx.x * 16 + c;
+  const int64_t cols = 2 * (int64_t)D, col = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 16 + c;
   float s = 0.0f;
   if (col < cols) {
 #pragma unroll 4
@@ -653,7 +653,9 @@ static int32_t norm_bwd_t(const NormBack& b, const void* dY, const void* X, cons
   }
   ARD_LAUNCH_CHECK("norm_bwd_kernel");
   if (!part) return ARD_OK;
-  ARD_LAUNCH((norm_weight_grad_kernel<WT>), dim3((unsigned)((2 * (int64_t)D + 15) / 16)), dim3(1024), 0, st, D, P, part, (WT*)dgamma, (WT*)dbeta);
+  const int blocks = (int)((2 * (int64_t)D + 15) / 16), planes = ceil_div(blocks, 1 << 20);  // (HIP counts a grid's threads along an axis in 32 bits)
+  ARD_LAUNCH_NAMED(launch_instance("norm_weight_grad_kernel", ceil_div(blocks, planes), planes, 1024), (norm_weight_grad_kernel<WT>),
+                   dim3(ceil_div(blocks, planes), planes), dim3(1024), 0, st, D, P, part, (WT*)dgamma, (WT*)dbeta);
   ARD_LAUNCH_CHECK("norm_weight_grad_kernel");
   return ARD_OK;
 }

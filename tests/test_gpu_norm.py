@@ -280,6 +280,23 @@ def test_sums_of_very_long_rows(dtype):
         assert abs((to_host(dX)[0] - rdX[0]) @ xh) / D <= 4e-6
 
 
+def test_rows_of_more_columns_than_a_grid_has_threads_for():
+    """2 x (2^25 + 24): the weights' gradients, 128 threads for each of their columns, at both ends and on both sides of the grid's limit."""
+    R, D = 2, (1 << 25) + 24
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    X, dY = (torch.randn((R, D), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    g = 1 + 0.3 * torch.randn(D, generator=gen, device="cuda")
+    Y, mean, rstd = ard.layer_norm_fwd(X, g)
+    dX, dg, db = ard.layer_norm_bwd(dY, X, g, mean, rstd)
+    x, dy, w = (to_host(t) for t in (X, dY, g))
+    rY, rmean, rrstd = N.layer_norm_fwd(x, w)
+    rdX, rdg, rdb = N.layer_norm_bwd(dy, x, w, rmean, rrstd)
+    assert_parity(Y, rY, "bf16", None, "Y")
+    assert_parity(dX, rdX, "bf16", None, "dX")
+    assert_parity(dg, rdg, "f32", None, "dgamma")
+    assert_parity(db, rdb, "f32", None, "dbeta")
+
+
 def test_gradient_against_differences_of_the_forward_pass():
     """Along random directions: the change of sum(dY Y) in the oracle's 64 bits beside the kernel's gradients."""
     R, D = 5, 90

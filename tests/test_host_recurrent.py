@@ -114,6 +114,18 @@ def test_norm_takes_rows_of_every_length(dtype):
             assert name == (["norm_fwd_kernel"] if n <= 16384 else ["norm_fwd_long_kernel"]), n
 
 
+def test_norm_gradients_of_the_longest_rows_have_a_grid():
+    """HIP counts the threads along an axis of a grid in 32 bits; 16 of dgamma's and dbeta's columns a workgroup of 1024."""
+    with D.dry_run() as lib:
+        heap = D.FakeHeap()
+        for n in (16385, (1 << 25) - 9, 1 << 25, (1 << 25) + 24, (1 << 29) + 5, 1 << 30):
+            ws = lib.ard_layer_norm_workspace_bytes(2, n)
+            a = _norm_bwd_args(heap, R=2, D=n, ldx=n, lddy=n, lddx=n, ws_bytes=ws)
+            assert lib.ard_layer_norm_bwd(*a.values()) == 0
+            x, y, threads = (int(v) for v in next(i for i in D.instances(lib) if i.startswith("norm_weight_grad_kernel")).split("<")[1][:-1].split(","))
+            assert x * threads < 1 << 32 and 2 * n <= x * y * 16 < 2 * n + 16 * (y + 1), n
+
+
 # ---- gated linear recurrence -------------------------------------------------------------------
 
 def _glr_args(heap, **change):
