@@ -501,7 +501,8 @@ int32_t ard_layer_norm_bwd(int32_t dtype, int32_t wdtype, int32_t R, int32_t D, 
  * for T = 1 cT may be c0.  d_lengths[B] (device, may be NULL: all T): sequence b has that many steps (clamped to 0..T);
  * behind them h is +0.0, the state stands, and what f, v, o hold there has no part in anything.
  * ckpt (fp32, may be NULL) receives the states before every ard_glr_chunk()-th step, [ceil(T / chunk) x B x H], which the
- * backward pass needs.  States are fp32 throughout.
+ * backward pass needs.  States are stored in fp32; in flight over more than 8 steps they are fp64, so a long memory's are off by what one
+ * gate is: sg(f) and 1 - sg(f) both by some |f| 2^-24 + 4 ulp of themselves.
  * flags: 0, or ARD_IN_COMPACT | ARD_OUT_COMPACT: the H channels are the kept units of a compact activation; f, v, o, h, dh and
  * the gradients have pad8(H) stored channels, zeros behind H (states are [B x H] all the same).
  * Backward: dh (strides dh_t, dh_b) and dcT (fp32 [B x H], NULL: zeros) are the gradients of h and cT; df, dv, dout (strides

@@ -13,7 +13,10 @@
 // Where batch and channels alone give too few wavefronts, time is cut into segments for several workgroups; a first pass
 // then makes the segments' pairs (reading f and v, or f, o and dh, once more), and the main pass composes those before
 // its segment.  (One pass would have workgroups wait for others; the second reading comes partly out of the last cache.)
-// States, pairs and gradients in flight are fp32.  The backward pass starts from the states that the forward pass left
+// A state in flight and the pairs that move it over 8 steps and more are fp64, everything inside a stretch fp32.  F of a long memory is so near 1
+// that what rounding takes, from F or from a state that hardly moves, is the same at every step of a steady gate and adds up (in fp32
+// what is left of a state after 32768 steps at f = 12 came out 1.8e-3 of itself off, 1e-7 so): P comes from 1 - P, a sum of positive terms with
+// digits of its own.  The card's fp64 multiply-add takes no longer than its fp32 one; the reads from LDS cost 0 to 4 % of a pass.  The backward pass starts from the states that the forward pass left
 // before every 8th step, so it needs no second scan for them.
 // Lanes are counted through the sequences, so few channels a sequence fill wavefronts too: 4000 x 48 x 24 forward 23 us and backward 42
 // against 47 and 64 with whole wavefronts for each sequence, 4000 x 47 x 192 78 and 130 against 93 and 156; where nothing is
@@ -45,16 +48,11 @@ struct GlrArgs {
   const int32_t* len;
 };
 
-// F = sigma(x), I = 1 - F without cancellation: for x >= 0 as exp(-x) F, where 1 - F would lose the digits of a long memory.
-__device__ __forceinline__ void gate_pair(float x, float& F, float& I) {
-  const float e = __builtin_amdgcn_exp2f(x * -1.44269504088896341f);
+// F = sigma(x), I = 1 - F from e = exp(-x), without cancellation: for x >= 0 as e F, where 1 - F would lose the digits of a long memory.
+__device__ __forceinline__ float shut(float x) { return __builtin_amdgcn_exp2f(x * -1.44269504088896341f); }
+__device__ __forceinline__ void gate_pair(float e, float& F, float& I) {
   F = __builtin_amdgcn_rcpf(1.0f + e);
-  I = x >= 0.0f ? e * F : 1.0f - F;
-}
-// I again from x and F, by the same operations
-__device__ __forceinline__ float ungate(float x, float F) {
-  const float e = __builtin_amdgcn_exp2f(x * -1.44269504088896341f);
-  return x >= 0.0f ? e * F : 1.0f - F;
+  I = e <= 1.0f ? e * F : 1.0f - F;
 }
 __device__ __forceinline__ float gate(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.44269504088896341f)); }
 
@@ -96,32 +94,76 @@ struct Steps {
   __device__ __forceinline__ Steps(const GlrPlace& p, int t) : mine(imin(p.t1, p.live) - t), lo(imin(p.t1, p.lo) - t), hi(imin(p.t1, p.hi) - t) {}
 };
 
-// pairs of the wavefronts' stretches of a turn, in LDS
-template <int VEC> struct Pairs {
-  float v[2][kMaxWaves][2][VEC][64];  // [turn's parity][stretch][P, S]
+// A stretch (or segment) of steps: takes c to P c + S.
+template <int VEC> struct Pair {
+  double P[VEC], S[VEC];
+};
+// The same as it is made from the steps of a stretch, in fp32: Q = 1 - P beside P, each with its own digits.  (S is the caller's.)
+template <int VEC> struct Steps8 {
+  float P[VEC], Q[VEC], S[VEC];
+  __device__ __forceinline__ Steps8() {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) P[j] = 1.0f, Q[j] = S[j] = 0.0f;
+  }
+  // one more step of gate F, I = 1 - F, before those that it has or behind them
+  __device__ __forceinline__ void times(int j, float F, float I) {
+    Q[j] = fmaf(I, P[j], Q[j]);
+    P[j] *= F;
+  }
+  __device__ __forceinline__ double whole(int j) const { return P[j] >= 0.5f ? 1.0 - (double)Q[j] : (double)P[j]; }
 };
 
-// The pairs of `count` stretches (or segments) before this one, applied to c in order.
-template <int VEC> __device__ __forceinline__ void apply(const Pairs<VEC>& s, int turn, int w, float (&c)[VEC]) {
+// pairs of the wavefronts' stretches of a turn, in LDS
+template <int VEC> struct Pairs {
+  double v[2][kMaxWaves][2][VEC][64];  // [turn's parity][stretch][P, S]
+  double c[2][VEC][64];                // [turn's parity]: the state behind the turn before it
+};
+// One wavefront moves the state over a whole turn and leaves it for the others' next one: written behind a turn's barrier, read behind the next one's, in
+// the place that was read behind the barrier before.  (Where each did it for itself, 1000 x 16 x 1024 took 36.2 + 64.0 us, 34.9 + 62.0 so.)
+template <int VEC> __device__ __forceinline__ void hand_on(Pairs<VEC>& s, int turn, const double (&c)[VEC]) {
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) c[j] = fmaf(s.v[turn][w][0][j][threadIdx.x & 63], c[j], s.v[turn][w][1][j][threadIdx.x & 63]);
+  for (int j = 0; j < VEC; ++j) s.c[turn][j][threadIdx.x & 63] = c[j];
 }
-template <int VEC> __device__ __forceinline__ void leave(Pairs<VEC>& s, int turn, int w, const float (&P)[VEC], const float (&S)[VEC]) {
+template <int VEC> __device__ __forceinline__ void take(const Pairs<VEC>& s, int turn, double (&c)[VEC]) {
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) s.v[turn][w][0][j][threadIdx.x & 63] = P[j], s.v[turn][w][1][j][threadIdx.x & 63] = S[j];
+  for (int j = 0; j < VEC; ++j) c[j] = s.c[turn][j][threadIdx.x & 63];
 }
 
-// Segment pairs in the workspace: [segment][P, S][B][H].  Composes those of segments [from, from + step * count) in
-// order, dealt to the workgroup's wavefronts in neighbouring shares, and applies them to c (uses parity 0 of the pairs).
+template <int VEC> __device__ __forceinline__ void apply(const Pairs<VEC>& s, int turn, int w, double (&c)[VEC]) {
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) c[j] = fma(s.v[turn][w][0][j][threadIdx.x & 63], c[j], s.v[turn][w][1][j][threadIdx.x & 63]);
+}
+template <int VEC> __device__ __forceinline__ void leave(Pairs<VEC>& s, int turn, int w, const Steps8<VEC>& m) {
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) s.v[turn][w][0][j][threadIdx.x & 63] = m.whole(j), s.v[turn][w][1][j][threadIdx.x & 63] = m.S[j];
+}
+// `all` and then the pair of a stretch, as one
+template <int VEC> __device__ __forceinline__ void join(const Pairs<VEC>& s, int turn, int w, Pair<VEC>& all) {
+  apply<VEC>(s, turn, w, all.S);
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) all.P[j] *= s.v[turn][w][0][j][threadIdx.x & 63];
+}
+
+// Segment pairs in the workspace, fp32: [segment][A, S][B][H], A = P, or -(1 - P) with its sign set where P is 1/2 or more.
+template <int VEC> __device__ __forceinline__ void leave_segment(const GlrArgs& a, const GlrPlace& p, float* seg_pairs, const Pair<VEC>& m) {
+  float A[VEC], S[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) A[j] = m.P[j] >= 0.5 ? -(float)(1.0 - m.P[j]) : (float)m.P[j], S[j] = (float)m.S[j];
+  float* out = seg_pairs + ((int64_t)p.seg * 2 * a.B + p.b) * a.H + p.ch;
+  store_some<VEC>(out, p.n, A);
+  store_some<VEC>(out + (int64_t)a.B * a.H, p.n, S);
+}
+// Composes those of segments [from, from + step * count) in order, dealt to the workgroup's wavefronts in neighbouring shares, and
+// applies them to c (uses parity 0 of the pairs).
 template <int VEC>
 __device__ __forceinline__ void apply_segments(const GlrArgs& a, const GlrPlace& p, const float* seg_pairs, int from, int step, int count,
-                                               Pairs<VEC>& lds, float (&c)[VEC]) {
+                                               Pairs<VEC>& lds, double (&c)[VEC]) {
   const int waves = blockDim.x >> 6, w = threadIdx.x >> 6;
   const int lo = (int)((int64_t)count * w / waves), hi = (int)((int64_t)count * (w + 1) / waves);
   const int64_t plane = (int64_t)a.B * a.H;
-  float P[VEC], S[VEC];
+  Pair<VEC> m;
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
+  for (int j = 0; j < VEC; ++j) m.P[j] = 1.0, m.S[j] = 0.0;
   for (int i0 = lo; i0 < hi; i0 += 4) {  // (four segments' pairs in flight)
     float q[4][VEC], r[4][VEC];
 #pragma unroll
@@ -134,10 +176,14 @@ __device__ __forceinline__ void apply_segments(const GlrArgs& a, const GlrPlace&
     for (int i = 0; i < 4; ++i)
       if (i0 + i < hi) {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) P[j] *= q[i][j], S[j] = fmaf(q[i][j], S[j], r[i][j]);
+        for (int j = 0; j < VEC; ++j) {
+          const double P = (__float_as_int(q[i][j]) < 0 ? 1.0 : 0.0) + (double)q[i][j];
+          m.P[j] *= P, m.S[j] = fma(P, m.S[j], (double)r[i][j]);
+        }
       }
   }
-  leave<VEC>(lds, 0, w, P, S);
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) lds.v[0][w][0][j][threadIdx.x & 63] = m.P[j], lds.v[0][w][1][j][threadIdx.x & 63] = m.S[j];
   __syncthreads();
   for (int k = 0; k < waves; ++k) apply<VEC>(lds, 0, k, c);
   __syncthreads();
@@ -166,20 +212,18 @@ template <typename T, int VEC> __device__ __forceinline__ void ask(const T* p, i
 // lane's end leave the state as it is (selected, not multiplied: nothing that lies there takes part).
 template <bool WHOLE, typename T, int VEC>
 __device__ __forceinline__ void stretch_fwd(const Raw<T, VEC> (&rf)[kSteps], const Raw<T, VEC> (&rv)[kSteps], const Steps& n, float (&F)[kSteps][VEC],
-                                            float (&b)[kSteps][VEC], float (&P)[VEC], float (&S)[VEC]) {
-#pragma unroll
-  for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
+                                            float (&b)[kSteps][VEC], Steps8<VEC>& m) {
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
     if (WHOLE || i < n.hi) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         float I;
-        gate_pair(part_of(rf[i], j), F[i][j], I);
+        gate_pair(shut(part_of(rf[i], j)), F[i][j], I);
         b[i][j] = I * part_of(rv[i], j);
-        if (!WHOLE) F[i][j] = i < n.mine ? F[i][j] : 1.0f, b[i][j] = i < n.mine ? b[i][j] : 0.0f;
-        P[j] *= F[i][j];
-        S[j] = fmaf(F[i][j], S[j], b[i][j]);
+        if (!WHOLE) F[i][j] = i < n.mine ? F[i][j] : 1.0f, b[i][j] = i < n.mine ? b[i][j] : 0.0f, I = i < n.mine ? I : 0.0f;
+        m.times(j, F[i][j], I);
+        m.S[j] = fmaf(F[i][j], m.S[j], b[i][j]);
       }
     }
 }
@@ -190,9 +234,9 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_pairs_kernel(GlrArgs a
   const GlrPlace p = glr_place<VEC>(a);
   const int waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t base = p.b * z.b + p.ch;
-  float tp[VEC], ts[VEC];
+  Pair<VEC> all;
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) tp[j] = 1.0f, ts[j] = 0.0f;
+  for (int j = 0; j < VEC; ++j) all.P[j] = 1.0, all.S[j] = 0.0;
   Raw<T, VEC> rf[kSteps], rv[kSteps];
   auto ask_all = [&](int tw) {
     // (a stretch behind the end takes a step that is stored)
@@ -206,23 +250,17 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_pairs_kernel(GlrArgs a
   for (int t = p.t0; t < p.t1; t += waves * kSteps, turn ^= 1) {
     const int tw = t + w * kSteps;
     const Steps n(p, tw);
-    float F[kSteps][VEC], b[kSteps][VEC], P[VEC], S[VEC];
-    if (n.lo >= kSteps) stretch_fwd<true, T, VEC>(rf, rv, n, F, b, P, S);
-    else stretch_fwd<false, T, VEC>(rf, rv, n, F, b, P, S);
+    float F[kSteps][VEC], b[kSteps][VEC];
+    Steps8<VEC> m;
+    if (n.lo >= kSteps) stretch_fwd<true, T, VEC>(rf, rv, n, F, b, m);
+    else stretch_fwd<false, T, VEC>(rf, rv, n, F, b, m);
     if (t + waves * kSteps < p.t1) ask_all(tw + waves * kSteps);  // (the next turn's, in flight meanwhile)
-    leave<VEC>(lds, turn, w, P, S);
+    leave<VEC>(lds, turn, w, m);
     __syncthreads();
-    for (int k = 0; k < waves; ++k) {
-      apply<VEC>(lds, turn, k, ts);
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) tp[j] *= lds.v[turn][k][0][j][threadIdx.x & 63];
-    }
+    if (w == 0)
+      for (int k = 0; k < waves; ++k) join<VEC>(lds, turn, k, all);
   }
-  if (w == 0) {
-    float* out = seg_pairs + ((int64_t)p.seg * 2 * a.B + p.b) * a.H + p.ch;
-    store_some<VEC>(out, p.n, tp);
-    store_some<VEC>(out + (int64_t)a.B * a.H, p.n, ts);
-  }
+  if (w == 0) leave_segment<VEC>(a, p, seg_pairs, all);
 }
 
 // results of a stretch whose state before it is s; zeros for those of its `stored` steps that lie behind a lane's end
@@ -254,10 +292,13 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_kernel(GlrArgs a, cons
   const GlrPlace p = glr_place<VEC>(a);
   const int waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t plane = (int64_t)a.B * a.H, state = (int64_t)p.b * a.H + p.ch;
-  float c[VEC];
+  double c[VEC];
+  {
+    float start[VEC] = {};
+    if (c0) load_some<VEC>(c0 + state, p.n, start);
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) c[j] = 0.0f;
-  if (c0) load_some<VEC>(c0 + state, p.n, c);
+    for (int j = 0; j < VEC; ++j) c[j] = start[j];
+  }
   if (CUT && p.seg) apply_segments<VEC>(a, p, seg_pairs, 0, 1, p.seg, lds, c);
   const int64_t base = p.b * z.b + p.ch;
   Raw<T, VEC> rf[kSteps], rv[kSteps], rg[kSteps], g[kSteps];
@@ -274,26 +315,31 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_kernel(GlrArgs a, cons
   for (int t = p.t0; t < p.t1; t += waves * kSteps, turn ^= 1) {
     const int tw = t + w * kSteps;
     const Steps n(p, tw);
-    float F[kSteps][VEC], b[kSteps][VEC], P[VEC], S[VEC], s[VEC];
-    if (n.lo >= kSteps) stretch_fwd<true, T, VEC>(rf, rv, n, F, b, P, S);
-    else stretch_fwd<false, T, VEC>(rf, rv, n, F, b, P, S);
+    float F[kSteps][VEC], b[kSteps][VEC], s[VEC];
+    Steps8<VEC> m;
+    if (n.lo >= kSteps) stretch_fwd<true, T, VEC>(rf, rv, n, F, b, m);
+    else stretch_fwd<false, T, VEC>(rf, rv, n, F, b, m);
     if (GATE) {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) g[i] = rg[i];
     }
     if (t + waves * kSteps < p.t1) ask_all(tw + waves * kSteps);  // (the next turn's, in flight meanwhile)
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) s[j] = c[j];
     if (waves > 1) {
-      leave<VEC>(lds, turn, w, P, S);
+      leave<VEC>(lds, turn, w, m);
       __syncthreads();
-      for (int k = 0; k < w; ++k) apply<VEC>(lds, turn, k, s);
+      if (w && t > p.t0) take<VEC>(lds, turn, c);
+#pragma unroll 2
+      for (int k = 0; k < w; ++k) apply<VEC>(lds, turn, k, c);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) c[j] = s[j];
-      for (int k = w; k < waves; ++k) apply<VEC>(lds, turn, k, c);
+      for (int j = 0; j < VEC; ++j) s[j] = (float)c[j];
+      if (w == 0) {
+#pragma unroll 2
+        for (int k = 0; k < waves; ++k) apply<VEC>(lds, turn, k, c);
+        hand_on<VEC>(lds, turn ^ 1, c);
+      }
     } else {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) c[j] = fmaf(P[j], c[j], S[j]);
+      for (int j = 0; j < VEC; ++j) s[j] = (float)c[j], c[j] = fma(m.whole(j), c[j], (double)m.S[j]);
     }
     if (tw < p.t1) {
       if (ckpt) store_some<VEC>(ckpt + (int64_t)(tw / kSteps) * plane + state, p.n, s);
@@ -302,7 +348,12 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_kernel(GlrArgs a, cons
       else stretch_out<false, T, VEC, GATE, CUT>(out, hs.t, p.on, n, p.t1 - tw, F, b, g, s);
     }
   }
-  if (cT && w == 0 && p.seg == a.segs - 1) store_some<VEC>(cT + state, p.n, c);
+  if (cT && w == 0 && p.seg == a.segs - 1) {
+    float end[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) end[j] = (float)c[j];
+    store_some<VEC>(cT + state, p.n, end);
+  }
 }
 
 // One step, as generation calls it: a lane's channels of one sequence.  cT may be c0.
@@ -324,8 +375,9 @@ __global__ __launch_bounds__(64) void glr_step_kernel(GlrArgs a, const T* f, con
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
       float F, I;
-      gate_pair(x[j], F, I);
-      c[j] = fmaf(F, c[j], I * u[j]);
+      const float e = shut(x[j]);
+      gate_pair(e, F, I);
+      c[j] = (float)fma(e <= 1.0f ? 1.0 - (double)I : (double)F, (double)c[j], (double)I * u[j]);
       y[j] = GATE ? gate(g[j]) * c[j] : c[j];
     }
   }
@@ -336,7 +388,7 @@ __global__ __launch_bounds__(64) void glr_step_kernel(GlrArgs a, const T* f, con
 // ---- backward -----------------------------------------------------------------
 // The adjoint's pair of a stretch takes e behind its last step to e behind the step before its first.
 template <bool WHOLE, typename T, int VEC, bool GATE>
-__device__ __forceinline__ void stretch_adjoint(const T* f, const T* o, const T* dh, int64_t st, int64_t dst, const Steps& n, float (&P)[VEC], float (&S)[VEC]) {
+__device__ __forceinline__ void stretch_adjoint(const T* f, const T* o, const T* dh, int64_t st, int64_t dst, const Steps& n, Steps8<VEC>& m) {
   Raw<T, VEC> F[kSteps], q[kSteps], g[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
@@ -347,17 +399,16 @@ __device__ __forceinline__ void stretch_adjoint(const T* f, const T* o, const T*
     }
   all_issued();
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
-#pragma unroll
   for (int i = kSteps - 1; i >= 0; --i)
     if (WHOLE || i < n.hi) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        float x = gate(part_of(F[i], j)), d = part_of(q[i], j);
+        float x, I, d = part_of(q[i], j);
+        gate_pair(shut(part_of(F[i], j)), x, I);
         if (GATE) d *= gate(part_of(g[i], j));
-        if (!WHOLE) x = i < n.mine ? x : 1.0f, d = i < n.mine ? d : 0.0f;
-        S[j] = x * (S[j] + d);
-        P[j] *= x;
+        if (!WHOLE) x = i < n.mine ? x : 1.0f, d = i < n.mine ? d : 0.0f, I = i < n.mine ? I : 0.0f;
+        m.S[j] = x * (m.S[j] + d);
+        m.times(j, x, I);
       }
     }
 }
@@ -377,41 +428,33 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_pairs_kernel(GlrArgs a
     return;
   }
   const int waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  float tp[VEC], ts[VEC];
+  Pair<VEC> all;
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) tp[j] = 1.0f, ts[j] = 0.0f;
+  for (int j = 0; j < VEC; ++j) all.P[j] = 1.0, all.S[j] = 0.0;
   const int span = waves * kSteps, turns = (p.t1 - p.t0 + span - 1) / span;
   int turn = 0;
   for (int t = p.t0 + (turns - 1) * span; t >= p.t0; t -= span, turn ^= 1) {
     const int tw = t + w * kSteps;
     const Steps n(p, tw);
     const int64_t at = tw * z.t + p.b * z.b + p.ch, dat = tw * ds.t + p.b * ds.b + p.ch;
-    float P[VEC], S[VEC];
-    if (n.lo >= kSteps) stretch_adjoint<true, T, VEC, GATE>(f + at, o + at, dh + dat, z.t, ds.t, n, P, S);
-    else stretch_adjoint<false, T, VEC, GATE>(f + at, o + at, dh + dat, z.t, ds.t, n, P, S);
-    leave<VEC>(lds, turn, w, P, S);
+    Steps8<VEC> m;
+    if (n.lo >= kSteps) stretch_adjoint<true, T, VEC, GATE>(f + at, o + at, dh + dat, z.t, ds.t, n, m);
+    else stretch_adjoint<false, T, VEC, GATE>(f + at, o + at, dh + dat, z.t, ds.t, n, m);
+    leave<VEC>(lds, turn, w, m);
     __syncthreads();
-    for (int k = waves - 1; k >= 0; --k) {
-      apply<VEC>(lds, turn, k, ts);
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) tp[j] *= lds.v[turn][k][0][j][threadIdx.x & 63];
-    }
+    if (w == 0)
+      for (int k = waves - 1; k >= 0; --k) join<VEC>(lds, turn, k, all);
   }
-  if (w == 0) {
-    float* out = seg_pairs + ((int64_t)p.seg * 2 * a.B + p.b) * a.H + p.ch;
-    store_some<VEC>(out, p.n, tp);
-    store_some<VEC>(out + (int64_t)a.B * a.H, p.n, ts);
-  }
+  if (w == 0) leave_segment<VEC>(a, p, seg_pairs, all);
 }
 
 // Loads of a stretch, its states again from the one before it, and its adjoint's pair; do is stored on the way (it needs
-// no gradient from later steps).  Leaves F, u = c_{t-1} - v, q = sigma(o) dh, and f as it was
-// read: 1 - F is made again where it is wanted, as holding it would cost a workgroup of the two that a CU has registers for.
+// no gradient from later steps).  Leaves ex = exp(-f) (F and 1 - F are made from it again where they are wanted, as holding them would cost a
+// workgroup of the two that a CU has registers for), u = c_{t-1} - v, and q = sigma(o) dh.
 template <bool WHOLE, typename T, int VEC, bool GATE, bool CUT>
 __device__ __forceinline__ void stretch_back(const T* f, const T* v, const T* o, const T* dh, T* dg, int64_t st, int64_t dst, int64_t gst, bool on, const Steps& n,
-                                             float (&c)[VEC], Raw<T, VEC> (&rf)[kSteps], float (&F)[kSteps][VEC], float (&u)[kSteps][VEC],
-                                             float (&q)[kSteps][VEC], float (&P)[VEC], float (&S)[VEC]) {
-  Raw<T, VEC> rv[kSteps], g[kSteps], rd[kSteps];
+                                             float (&c)[VEC], float (&ex)[kSteps][VEC], float (&u)[kSteps][VEC], float (&q)[kSteps][VEC], Steps8<VEC>& m) {
+  Raw<T, VEC> rf[kSteps], rv[kSteps], g[kSteps], rd[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
     if (WHOLE || i < n.hi) {
@@ -428,11 +471,13 @@ __device__ __forceinline__ void stretch_back(const T* f, const T* v, const T* o,
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const bool live = WHOLE || i < n.mine;
-        float I;
-        gate_pair(part_of(rf[i], j), F[i][j], I);
+        float F, I;
+        ex[i][j] = shut(part_of(rf[i], j));
+        if (!live) ex[i][j] = 0.0f;
+        gate_pair(ex[i][j], F, I);
         const float x = part_of(rv[i], j);
         u[i][j] = c[j] - x;
-        const float next = fmaf(F[i][j], c[j], I * x);
+        const float next = fmaf(F, c[j], I * x);
         c[j] = live ? next : c[j];
         q[i][j] = part_of(rd[i], j);
         if (GATE) {
@@ -440,26 +485,17 @@ __device__ __forceinline__ void stretch_back(const T* f, const T* v, const T* o,
           q[i][j] *= O;
           y[j] = live ? q[i][j] * c[j] * (1.0f - O) : 0.0f;
         }
-        if (!live) F[i][j] = 1.0f, q[i][j] = 0.0f;
+        if (!live) q[i][j] = 0.0f;
+        m.times(j, F, I);
+        m.S[j] = fmaf(m.P[j], q[i][j], m.S[j]);
       }
       if (GATE && on) put<CUT, VEC>(dg + i * gst, y);
-    }
-#pragma unroll
-  for (int j = 0; j < VEC; ++j) P[j] = 1.0f, S[j] = 0.0f;
-#pragma unroll
-  for (int i = kSteps - 1; i >= 0; --i)
-    if (WHOLE || i < n.hi) {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        S[j] = F[i][j] * (S[j] + q[i][j]);
-        P[j] *= F[i][j];
-      }
     }
 }
 // df and dv of a stretch, e behind its last step in s; zeros (do's too) for those of its `stored` steps behind a lane's end
 template <bool WHOLE, typename T, int VEC, bool GATE, bool CUT>
-__device__ __forceinline__ void stretch_grads(T* df, T* dv, T* dg, int64_t gst, bool on, const Steps& n, int stored, const Raw<T, VEC> (&rf)[kSteps],
-                                              const float (&F)[kSteps][VEC], const float (&u)[kSteps][VEC], const float (&q)[kSteps][VEC],
+__device__ __forceinline__ void stretch_grads(T* df, T* dv, T* dg, int64_t gst, bool on, const Steps& n, int stored, const float (&ex)[kSteps][VEC],
+                                              const float (&u)[kSteps][VEC], const float (&q)[kSteps][VEC],
                                               float (&s)[VEC]) {
 #pragma unroll
   for (int i = kSteps - 1; i >= 0; --i) {
@@ -471,9 +507,11 @@ __device__ __forceinline__ void stretch_grads(T* df, T* dv, T* dg, int64_t gst, 
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         const float dc = q[i][j] + s[j];
-        s[j] = F[i][j] * dc;
-        y[j] = dc * ungate(part_of(rf[i], j), F[i][j]);
-        x[j] = y[j] * F[i][j] * u[i][j];
+        float F, I;
+        gate_pair(ex[i][j], F, I);
+        s[j] = F * dc;
+        y[j] = dc * I;
+        x[j] = y[j] * F * u[i][j];
         if (!WHOLE) x[j] = i < n.mine ? x[j] : 0.0f, y[j] = i < n.mine ? y[j] : 0.0f;
       }
     } else if (GATE) {
@@ -491,39 +529,52 @@ __global__ __launch_bounds__(64 * kMaxWaves, 4) void glr_bwd_kernel(GlrArgs a, c
   const GlrPlace p = glr_place<VEC>(a);
   const int waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t plane = (int64_t)a.B * a.H, state = (int64_t)p.b * a.H + p.ch;
-  float e[VEC];
+  double e[VEC];
+  {
+    float end[VEC] = {};
+    if (dcT) load_some<VEC>(dcT + state, p.n, end);
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) e[j] = 0.0f;
-  if (dcT) load_some<VEC>(dcT + state, p.n, e);
+    for (int j = 0; j < VEC; ++j) e[j] = end[j];
+  }
   if (CUT && p.seg < a.segs - 1) apply_segments<VEC>(a, p, seg_pairs, a.segs - 1, -1, a.segs - 1 - p.seg, lds, e);
   const int span = waves * kSteps, turns = (p.t1 - p.t0 + span - 1) / span;
   int turn = 0;
   for (int t = p.t0 + (turns - 1) * span; t >= p.t0; t -= span, turn ^= 1) {
     const int tw = t + w * kSteps;
     const Steps n(p, tw);
-    float F[kSteps][VEC], u[kSteps][VEC], q[kSteps][VEC], P[VEC], S[VEC], c[VEC], s[VEC];
-    Raw<T, VEC> rf[kSteps];
+    float ex[kSteps][VEC], u[kSteps][VEC], q[kSteps][VEC], c[VEC], s[VEC];
+    Steps8<VEC> m;
     const int64_t at = tw * z.t + p.b * z.b + p.ch, dat = tw * ds.t + p.b * ds.b + p.ch, gat = tw * gs.t + p.b * gs.b + p.ch;
     if (n.hi > 0) load_some<VEC>(ckpt + (int64_t)(tw / kSteps) * plane + state, p.n, c);
-    if (n.lo >= kSteps) stretch_back<true, T, VEC, GATE, CUT>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, n, c, rf, F, u, q, P, S);
-    else stretch_back<false, T, VEC, GATE, CUT>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, n, c, rf, F, u, q, P, S);
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) s[j] = e[j];
+    if (n.lo >= kSteps) stretch_back<true, T, VEC, GATE, CUT>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, n, c, ex, u, q, m);
+    else stretch_back<false, T, VEC, GATE, CUT>(f + at, v + at, o + at, dh + dat, dg + gat, z.t, ds.t, gs.t, p.on, n, c, ex, u, q, m);
     if (waves > 1) {
-      leave<VEC>(lds, turn, w, P, S);
+      leave<VEC>(lds, turn, w, m);
       __syncthreads();
-      for (int k = waves - 1; k > w; --k) apply<VEC>(lds, turn, k, s);
+      const bool last = w == waves - 1;
+      if (!last && t + span < p.t1) take<VEC>(lds, turn, e);
+#pragma unroll 2
+      for (int k = waves - 1; k > w; --k) apply<VEC>(lds, turn, k, e);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) e[j] = s[j];
-      for (int k = w; k >= 0; --k) apply<VEC>(lds, turn, k, e);
+      for (int j = 0; j < VEC; ++j) s[j] = (float)e[j];
+      if (last) {
+#pragma unroll 2
+        for (int k = waves - 1; k >= 0; --k) apply<VEC>(lds, turn, k, e);
+        hand_on<VEC>(lds, turn ^ 1, e);
+      }
     } else {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) e[j] = fmaf(P[j], e[j], S[j]);
+      for (int j = 0; j < VEC; ++j) s[j] = (float)e[j], e[j] = fma(m.whole(j), e[j], (double)m.S[j]);
     }
-    if (n.lo >= kSteps) stretch_grads<true, T, VEC, GATE, CUT>(df + gat, dv + gat, dg + gat, gs.t, p.on, n, kSteps, rf, F, u, q, s);
-    else stretch_grads<false, T, VEC, GATE, CUT>(df + gat, dv + gat, dg + gat, gs.t, p.on, n, p.t1 - tw, rf, F, u, q, s);
+    if (n.lo >= kSteps) stretch_grads<true, T, VEC, GATE, CUT>(df + gat, dv + gat, dg + gat, gs.t, p.on, n, kSteps, ex, u, q, s);
+    else stretch_grads<false, T, VEC, GATE, CUT>(df + gat, dv + gat, dg + gat, gs.t, p.on, n, p.t1 - tw, ex, u, q, s);
   }
-  if (dc0 && w == 0 && p.seg == 0) store_some<VEC>(dc0 + state, p.n, e);
+  if (dc0 && w == waves - 1 && p.seg == 0) {
+    float start[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) start[j] = (float)e[j];
+    store_some<VEC>(dc0 + state, p.n, start);
+  }
 }
 
 // ---- host ---------------------------------------------------------------------

@@ -220,6 +220,60 @@ def test_gates_at_the_ends_of_their_range(dtype):
     assert torch.equal(cT[:, 0], _dev(c0)[:, 0]) and torch.equal(cT[:, 1], vd[-1, :, 1].float())
 
 
+@pytest.mark.parametrize("dtype,T,B,H", [("f32", 8192, 64, 256), ("f32", 32768, 1, 60), ("bf16", 32768, 64, 512), ("bf16", 32768, 2, 62), ("f32", 24, 3, 60)])
+def test_long_memories_of_steady_gates(dtype, T, B, H):
+    """Gates and inputs that stay as they are, where roundings of one sign would add up, against the closed form
+    c_T = v + (c0 - v) F^T, e_0 = F^T e_T + dh F (1 - F^T) / (1 - F).  A state is rounded once in 8 steps, half an ulp to either side: 6 deviations
+    of their sum; the gate's argument costs |f| 2^-24 of 1 - F and its operations 4 ulp."""
+    code, dt = (ard.F32, torch.float32) if dtype == "f32" else (ard.BF16, torch.bfloat16)
+    assert (ard.glr_workspace_bytes(code, T, B, H) > 0) == (T > 64 and B < 10)   # (time cut, and not)
+    k = np.arange(H)
+    f, v, c0 = np.array([8.0, 9, 10, 11, 12, 14])[k % 6], np.array([1.0, 0, -0.5])[k % 3], np.array([0.0, 1, 2, -1])[k % 4]
+    dh, dcT = np.array([0.0, 1, -0.5])[k % 3], np.array([1.0, 0, 2, -1])[k % 4]
+    fd, vd, dhd = (_dev(x, dtype).expand(T, B, H) for x in (f, v, dh))
+    c0d, dcTd = (_dev(x).expand(B, H).contiguous() for x in (c0, dcT))
+    h, cT, ckpt = ard.glr_fwd(fd, vd, None, c0d)
+    df, dv, _, dc0 = ard.glr_bwd(fd, vd, None, dhd, ckpt, dcTd)
+    I = L.sigmoid(-f)
+    FT = np.exp(T * np.log1p(-I))
+    rc, re = v + (c0 - v) * FT, FT * dcT + dh * (1 - I) * -np.expm1(T * np.log1p(-I)) / I
+    tol = 2.0 ** -24 * (6 * np.sqrt(T / 8 / 3) + f + 4)
+    bound_c, bound_e = tol * (np.abs(v) + np.abs(c0 - v)), tol * (np.abs(dcT) + np.abs(dh) * np.minimum(T, 1 / I))
+    assert (np.abs(to_host(cT) - rc) <= bound_c).all()
+    assert (np.abs(to_host(dc0) - re) <= bound_e).all()
+    round_off = 1e-6 if dtype == "f32" else 2.0 ** -8
+    assert (np.abs(to_host(h[-1]) - rc) <= bound_c + round_off * np.abs(rc)).all()
+    dc = re / (1 - I)   # of the first step
+    assert (np.abs(to_host(dv[0]) - dc * I) <= (bound_e + round_off * np.abs(dc) + tol * np.abs(dc)) * I).all()
+    want = dc * (c0 - v) * I * (1 - I)
+    assert (np.abs(to_host(df[0]) - want) <= bound_e * np.abs(c0 - v) * I + (round_off + tol) * np.abs(want)).all()
+
+
+def test_long_memories_step_by_step():
+    """The same by single steps, the state in its place: a rounding each."""
+    T, B, H = 4096, 2, 60
+    k = np.arange(H)
+    f, v, c0 = np.array([8.0, 9, 10, 11, 12, 14])[k % 6], np.array([1.0, 0, -0.5])[k % 3], np.array([0.0, 1, 2, -1])[k % 4]
+    fd, vd, c = _dev(f).expand(1, B, H), _dev(v).expand(1, B, H), _dev(c0).expand(B, H).contiguous()
+    out = (torch.empty((1, B, H), device="cuda"), c, None)
+    for _ in range(T):
+        ard.glr_fwd(fd, vd, None, c, train=False, out=out)
+    want = v + (c0 - v) * np.exp(T * np.log1p(-L.sigmoid(-f)))
+    assert (np.abs(to_host(c) - want) <= 2.0 ** -24 * (6 * np.sqrt(T / 3) + f + 4) * (np.abs(v) + np.abs(c0 - v))).all()
+
+
+@pytest.mark.parametrize("T", [1, 7, 40, 300, 5000])
+def test_an_infinite_state_stays_one(T):
+    f, v = (torch.full((T, 2, 8), x, device="cuda") for x in (3.0, 0.5))
+    f[..., 4:] = float("inf")
+    c0 = torch.zeros(2, 8, device="cuda")
+    c0[0, ::2], c0[1, 1::2] = float("inf"), -float("inf")
+    h, cT, _ = ard.glr_fwd(f, v, None, c0)
+    inf = torch.isinf(c0)
+    assert torch.equal(cT[inf], c0[inf]) and torch.isfinite(cT[~inf]).all()
+    assert torch.equal(h[:, inf], c0[inf].expand(T, -1)) and torch.isfinite(h[:, ~inf]).all()
+
+
 def test_a_nan_stays_in_its_channel():
     T, B, H = 300, 2, 70
     f, v, o, dh, c0, dcT = _inputs(T, B, H, "f32", True, 2)
