@@ -481,9 +481,10 @@ __device__ __forceinline__ void stretch_back(const T* f, const T* v, const T* o,
         c[j] = live ? next : c[j];
         q[i][j] = part_of(rd[i], j);
         if (GATE) {
-          const float O = gate(part_of(g[i], j));
+          float O, N;
+          gate_pair(shut(part_of(g[i], j)), O, N);
           q[i][j] *= O;
-          y[j] = live ? q[i][j] * c[j] * (1.0f - O) : 0.0f;
+          y[j] = live ? q[i][j] * c[j] * N : 0.0f;
         }
         if (!live) q[i][j] = 0.0f;
         m.times(j, F, I);

@@ -274,6 +274,29 @@ def test_an_infinite_state_stays_one(T):
     assert torch.equal(h[:, inf], c0[inf].expand(T, -1)) and torch.isfinite(h[:, ~inf]).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 30, 700])
+def test_gradients_of_gates_that_are_almost_open_or_shut(T, dtype):
+    """df and do of f and o from -20 to 20, each element beside itself: 1 - s(x) of an x past 8 is smaller than the rounding of s(x).
+    fp32: two gates' arguments, (|f| + |o|) 2^-24, some ten operations of 2^-24 and the state's 1e-6; bf16: its rounding, 2^-8 too."""
+    B, H = 2, 41
+    rng = np.random.default_rng(T)
+    x = np.linspace(-20, 20, H)
+    o = stored(np.broadcast_to(x, (T, B, H)), dtype)
+    f = stored(np.broadcast_to(x[::-1], (T, B, H)), dtype)
+    v, dh = (stored(0.5 + rng.random((T, B, H)), dtype) for _ in range(2))   # (positive: no element of a gradient is small by cancellation)
+    c0 = stored(2.0 + rng.random((B, H)), "f32")
+    h, cT, ckpt = ard.glr_fwd(_dev(f, dtype), _dev(v, dtype), _dev(o, dtype), _dev(c0))
+    df, dv, do, dc0 = ard.glr_bwd(_dev(f, dtype), _dev(v, dtype), _dev(o, dtype), _dev(dh, dtype), ckpt)
+    rh, rcT, states = L.glr_fwd(f, v, o, c0)
+    rdf, rdv, rdo, rdc0 = L.glr_bwd(f, v, o, states, dh)
+    tol = (40 + 10) * 2.0 ** -24 + 1e-6 + (2.0 ** -8 if dtype == "bf16" else 0)
+    for what, got, ref in (("h", h, rh), ("dv", dv, rdv), ("do", do, rdo)):
+        assert (np.abs(to_host(got) - ref) <= tol * np.abs(ref)).all(), what
+    # (c_{t-1} - v of df does cancel: against its terms)
+    assert (np.abs(to_host(df) - rdf) <= tol * np.abs(rdv) * L.sigmoid(f) * (states[:T] + v)).all()
+
+
 def test_a_nan_stays_in_its_channel():
     T, B, H = 300, 2, 70
     f, v, o, dh, c0, dcT = _inputs(T, B, H, "f32", True, 2)
