@@ -50,7 +50,9 @@ __device__ __forceinline__ void adam_states(const AdamConsts& k, float g, float&
   v = v * k.b2 + (g * g) * k.omb2;
 }
 __device__ __forceinline__ float adam_param(const AdamConsts& k, float p, float m, float v) {
-  const float root = fmaf(__builtin_amdgcn_sqrtf(v), k.r2, k.eps);
+  // (the root's instruction takes what is below the smallest normal number for 0: such a v is scaled up before it)
+  const bool tiny = v < 0x1p-100f;
+  const float root = fmaf(__builtin_amdgcn_sqrtf(tiny ? v * 0x1p64f : v), tiny ? k.r2 * 0x1p-32f : k.r2, k.eps);
   return fmaf(-k.lr * m, __builtin_amdgcn_rcpf(root), p * k.keep);
 }
 

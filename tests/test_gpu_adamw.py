@@ -135,6 +135,28 @@ def test_first_and_late_steps(t, bits):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_second_moments_below_the_smallest_normal_number(bits):
+    """Gradients of some 1e-19 and an eps that is smaller still: each step within 1e-6 of the formula on the states in 32 bits."""
+    n, eps, t = 4096, 1e-32, 1000
+    rng = np.random.default_rng(4)
+    v = (10.0 ** rng.uniform(-44, -34, n)).astype(np.float32)
+    m = (np.sqrt(v.astype(np.float64)) * rng.uniform(0.1, 1, n)).astype(np.float32)
+    g = np.where(np.arange(n) % 2, 0, 1e-20 * rng.standard_normal(n)).astype(np.float32)
+    p, gd = torch.zeros(n, device="cuda"), from_vals(g, "f32")
+    if bits == 8:
+        (mc, mt), (vc, vt) = A.encode_m(m), A.encode_v(v)
+        m, v = A.decode_m(mc, mt), A.decode_v(vc, vt)
+        state = [[torch.from_numpy(a).cuda()] for a in (mc, vc, mt, vt)]
+    else:
+        state = [[torch.from_numpy(a).cuda()] for a in (m.copy(), v.copy())] + [None, None]
+    ard.adamw_step([p], [gd], *state, lr=1e-3, eps=eps, weight_decay=0.0, step=t)
+    m, v = (x.astype(np.float64) for x in A.states_f32(g, m, v, 0.9, 0.999))
+    assert np.count_nonzero((v > 0) & (v < 2.0 ** -126)) > n // 10
+    want = -1e-3 / (1 - 0.9 ** t) * m / (np.sqrt(v) / np.sqrt(1 - 0.999 ** t) + eps)
+    assert (np.abs(to_host(p) - want) <= 1e-6 * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_a_scale_that_the_host_does_not_know(bits):
     for scale in (0.25, 0.0, 3.0):
         _check([_case(n, bits, "bf16", n) for n in (10, 3001)], bits, "bf16", scale=scale)
