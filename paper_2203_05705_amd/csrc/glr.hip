@@ -137,18 +137,30 @@ template <int VEC> __device__ __forceinline__ void leave(Pairs<VEC>& s, int turn
 #pragma unroll
   for (int j = 0; j < VEC; ++j) s.v[turn][w][0][j][threadIdx.x & 63] = m.whole(j), s.v[turn][w][1][j][threadIdx.x & 63] = m.S[j];
 }
-// `all` and then the pair of a stretch, as one
-template <int VEC> __device__ __forceinline__ void join(const Pairs<VEC>& s, int turn, int w, Pair<VEC>& all) {
-  apply<VEC>(s, turn, w, all.S);
-#pragma unroll
-  for (int j = 0; j < VEC; ++j) all.P[j] *= s.v[turn][w][0][j][threadIdx.x & 63];
+// Pairs of many stretches, as a first pass makes them: a wavefront joins its own, which follow each other, and the first one the wavefronts'.
+template <int VEC> __device__ __forceinline__ void join(Pair<VEC>& all, int j, double P, double S) {
+  all.P[j] *= P, all.S[j] = fma(P, all.S[j], S);
 }
-
-// Segment pairs in the workspace, fp32: [segment][A, S][B][H], A = P, or -(1 - P) with its sign set where P is 1/2 or more.
-template <int VEC> __device__ __forceinline__ void leave_segment(const GlrArgs& a, const GlrPlace& p, float* seg_pairs, const Pair<VEC>& m) {
+template <int VEC> __device__ __forceinline__ void none(Pair<VEC>& all) {
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) all.P[j] = 1.0, all.S[j] = 0.0;
+}
+// Segment pairs in the workspace, fp32: [segment][A, S][B][H], A = P, or -(1 - P) with its sign set where P is 1/2 or more.  `all`: the
+// wavefront's own; the workgroup's are joined from wavefront `from` on in steps of 1 or -1.
+template <int VEC>
+__device__ __forceinline__ void leave_segment(const GlrArgs& a, const GlrPlace& p, float* seg_pairs, Pair<VEC>& all, int from, int step, Pairs<VEC>& lds) {
+  const int waves = blockDim.x >> 6, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) lds.v[0][w][0][j][threadIdx.x & 63] = all.P[j], lds.v[0][w][1][j][threadIdx.x & 63] = all.S[j];
+  __syncthreads();
+  if (w) return;
+  none(all);
+  for (int k = 0; k < waves; ++k)
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) join(all, j, lds.v[0][from + step * k][0][j][threadIdx.x & 63], lds.v[0][from + step * k][1][j][threadIdx.x & 63]);
   float A[VEC], S[VEC];
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) A[j] = m.P[j] >= 0.5 ? -(float)(1.0 - m.P[j]) : (float)m.P[j], S[j] = (float)m.S[j];
+  for (int j = 0; j < VEC; ++j) A[j] = all.P[j] >= 0.5 ? -(float)(1.0 - all.P[j]) : (float)all.P[j], S[j] = (float)all.S[j];
   float* out = seg_pairs + ((int64_t)p.seg * 2 * a.B + p.b) * a.H + p.ch;
   store_some<VEC>(out, p.n, A);
   store_some<VEC>(out + (int64_t)a.B * a.H, p.n, S);
@@ -162,8 +174,7 @@ __device__ __forceinline__ void apply_segments(const GlrArgs& a, const GlrPlace&
   const int lo = (int)((int64_t)count * w / waves), hi = (int)((int64_t)count * (w + 1) / waves);
   const int64_t plane = (int64_t)a.B * a.H;
   Pair<VEC> m;
-#pragma unroll
-  for (int j = 0; j < VEC; ++j) m.P[j] = 1.0, m.S[j] = 0.0;
+  none(m);
   for (int i0 = lo; i0 < hi; i0 += 4) {  // (four segments' pairs in flight)
     float q[4][VEC], r[4][VEC];
 #pragma unroll
@@ -178,7 +189,7 @@ __device__ __forceinline__ void apply_segments(const GlrArgs& a, const GlrPlace&
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
           const double P = (__float_as_int(q[i][j]) < 0 ? 1.0 : 0.0) + (double)q[i][j];
-          m.P[j] *= P, m.S[j] = fma(P, m.S[j], (double)r[i][j]);
+          join(m, j, P, (double)r[i][j]);
         }
       }
   }
@@ -235,8 +246,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_pairs_kernel(GlrArgs a
   const int waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t base = p.b * z.b + p.ch;
   Pair<VEC> all;
-#pragma unroll
-  for (int j = 0; j < VEC; ++j) all.P[j] = 1.0, all.S[j] = 0.0;
+  none(all);
   Raw<T, VEC> rf[kSteps], rv[kSteps];
   auto ask_all = [&](int tw) {
     // (a stretch behind the end takes a step that is stored)
@@ -245,22 +255,20 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_fwd_pairs_kernel(GlrArgs a
     ask<T, VEC>(f + at, z.t, steps, rf), ask<T, VEC>(v + at, z.t, steps, rv);
     all_issued();
   };
-  int turn = 0;
-  ask_all(p.t0 + w * kSteps);
-  for (int t = p.t0; t < p.t1; t += waves * kSteps, turn ^= 1) {
-    const int tw = t + w * kSteps;
+  const int turns = (p.t1 - p.t0 + waves * kSteps - 1) / (waves * kSteps), first = p.t0 + w * turns * kSteps;
+  ask_all(first);
+  for (int i = 0; i < turns; ++i) {
+    const int tw = first + i * kSteps;
     const Steps n(p, tw);
     float F[kSteps][VEC], b[kSteps][VEC];
     Steps8<VEC> m;
     if (n.lo >= kSteps) stretch_fwd<true, T, VEC>(rf, rv, n, F, b, m);
     else stretch_fwd<false, T, VEC>(rf, rv, n, F, b, m);
-    if (t + waves * kSteps < p.t1) ask_all(tw + waves * kSteps);  // (the next turn's, in flight meanwhile)
-    leave<VEC>(lds, turn, w, m);
-    __syncthreads();
-    if (w == 0)
-      for (int k = 0; k < waves; ++k) join<VEC>(lds, turn, k, all);
+    if (i + 1 < turns) ask_all(tw + kSteps);  // (the next stretch's, in flight meanwhile)
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) join(all, j, m.whole(j), (double)m.S[j]);
   }
-  if (w == 0) leave_segment<VEC>(a, p, seg_pairs, all);
+  leave_segment<VEC>(a, p, seg_pairs, all, 0, 1, lds);
 }
 
 // results of a stretch whose state before it is s; zeros for those of its `stored` steps that lie behind a lane's end
@@ -398,19 +406,23 @@ __device__ __forceinline__ void stretch_adjoint(const T* f, const T* o, const T*
       if (GATE) g[i] = load_raw<T, VEC>(o + i * st);
     }
   all_issued();
+  float E[VEC] = {};  // 1 / P - 1, the (1 + e) multiplied less 1 (nobody looks at one past 1)
 #pragma unroll
   for (int i = kSteps - 1; i >= 0; --i)
     if (WHOLE || i < n.hi) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        float x, I, d = part_of(q[i], j);
-        gate_pair(shut(part_of(F[i], j)), x, I);
+        float e = shut(part_of(F[i], j)), d = part_of(q[i], j);
         if (GATE) d *= gate(part_of(g[i], j));
-        if (!WHOLE) x = i < n.mine ? x : 1.0f, d = i < n.mine ? d : 0.0f, I = i < n.mine ? I : 0.0f;
+        if (!WHOLE) e = i < n.mine ? e : 0.0f, d = i < n.mine ? d : 0.0f;
+        const float x = __builtin_amdgcn_rcpf(1.0f + e);
         m.S[j] = x * (m.S[j] + d);
-        m.times(j, x, I);
+        m.P[j] *= x;
+        E[j] = fmaf(e, E[j], e + E[j]);
       }
     }
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) m.Q[j] = E[j] * __builtin_amdgcn_rcpf(1.0f + E[j]);
 }
 
 template <typename T, int VEC, bool GATE>
@@ -418,34 +430,33 @@ __global__ __launch_bounds__(64 * kMaxWaves) void glr_bwd_pairs_kernel(GlrArgs a
                                                                        const float* dcT, float* seg_pairs) {
   __shared__ Pairs<VEC> lds;
   const GlrPlace p = glr_place<VEC>(a);
-  if (p.seg == 0) {  // (nothing lies before it: its pair is not needed)
-    if (dcT && threadIdx.x < 64) {  // the place of its P keeps a gradient that dc0 will be stored over
+  if (p.seg == 0) {  // nothing lies before it: its pair is not needed, and its place keeps a gradient that dc0 will be stored over
+    if (dcT && threadIdx.x < 64) {
       float e[VEC];
       const int64_t state = (int64_t)p.b * a.H + p.ch;
       load_some<VEC>(dcT + state, p.n, e);
       store_some<VEC>(seg_pairs + state, p.n, e);
     }
-    return;
+    // Of many segments it is read all the same, for the last cache: alone without its inputs there it would be what the main launch waits for
+    // (8192 x 4 x 1024 without a gate, 16 segments, 24 + 65 us in place of 24 + 57; 4608 x 24 x 256, 10, 31 + 81 and 32 + 71).  Of few that costs more than it
+    // gives (1000 x 16 x 1000, 4, 21 + 51 us in place of 17 + 51; with 7 or 8 both take as long).
+    if (a.segs < 8) return;
   }
   const int waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Pair<VEC> all;
-#pragma unroll
-  for (int j = 0; j < VEC; ++j) all.P[j] = 1.0, all.S[j] = 0.0;
-  const int span = waves * kSteps, turns = (p.t1 - p.t0 + span - 1) / span;
-  int turn = 0;
-  for (int t = p.t0 + (turns - 1) * span; t >= p.t0; t -= span, turn ^= 1) {
-    const int tw = t + w * kSteps;
+  none(all);
+  const int turns = (p.t1 - p.t0 + waves * kSteps - 1) / (waves * kSteps), first = p.t0 + w * turns * kSteps;
+  for (int i = turns - 1; i >= 0; --i) {
+    const int tw = first + i * kSteps;
     const Steps n(p, tw);
     const int64_t at = tw * z.t + p.b * z.b + p.ch, dat = tw * ds.t + p.b * ds.b + p.ch;
     Steps8<VEC> m;
     if (n.lo >= kSteps) stretch_adjoint<true, T, VEC, GATE>(f + at, o + at, dh + dat, z.t, ds.t, n, m);
     else stretch_adjoint<false, T, VEC, GATE>(f + at, o + at, dh + dat, z.t, ds.t, n, m);
-    leave<VEC>(lds, turn, w, m);
-    __syncthreads();
-    if (w == 0)
-      for (int k = waves - 1; k >= 0; --k) join<VEC>(lds, turn, k, all);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) join(all, j, m.whole(j), (double)m.S[j]);
   }
-  if (w == 0) leave_segment<VEC>(a, p, seg_pairs, all);
+  if (p.seg) leave_segment<VEC>(a, p, seg_pairs, all, waves - 1, -1, lds);
 }
 
 // Loads of a stretch, its states again from the one before it, and its adjoint's pair; do is stored on the way (it needs
