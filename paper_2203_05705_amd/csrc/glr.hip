@@ -196,8 +196,12 @@ __device__ __forceinline__ void apply_segments(const GlrArgs& a, const GlrPlace&
 #pragma unroll
   for (int j = 0; j < VEC; ++j) lds.v[0][w][0][j][threadIdx.x & 63] = m.P[j], lds.v[0][w][1][j][threadIdx.x & 63] = m.S[j];
   __syncthreads();
-  for (int k = 0; k < waves; ++k) apply<VEC>(lds, 0, k, c);
+  if (w == 0) {
+    for (int k = 0; k < waves; ++k) apply<VEC>(lds, 0, k, c);
+    hand_on<VEC>(lds, 0, c);
+  }
   __syncthreads();
+  take<VEC>(lds, 0, c);
 }
 
 // Results.  CUT: of a launch whose inputs are read a second time, by way of the caches; results are kept from taking their room.
