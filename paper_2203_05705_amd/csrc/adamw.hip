@@ -4,7 +4,7 @@
 //   with lr' = lr / (1 - b1^t) and r2 = 1 / sqrt(1 - b2^t)
 //
 // Bound by memory: a parameter costs 28 bytes with 32-bit states and fp32 gradients, 14 with 8-bit states and bf16
-// gradients (16 with a bf16 copy): 67M parameters of the latter kind take 207 us, 5.2 TB/s, and 16.8M of the former 90 us, 5.2 TB/s.  A wavefront takes a block of 256 neighbouring elements, four a lane in 16-byte accesses; that is also
+// gradients (16 with a bf16 copy): 67M parameters of the latter kind take 208 us, 5.2 TB/s, and 16.8M of the former 93 us, 5.0 TB/s.  A wavefront takes a block of 256 neighbouring elements, four a lane in 16-byte accesses; that is also
 // the block that shares the scales of an 8-bit state, so its largest m and v are maxima over a wavefront's registers and
 // the state is read, updated and written in one pass.  The tensors' table travels in the kernel's arguments.
 #include <math.h>

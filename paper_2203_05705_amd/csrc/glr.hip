@@ -9,22 +9,22 @@
 // of a workgroup, which have neighbouring stretches, exchange pairs through LDS: every input is read once and every
 // output written once, and that traffic is what bounds these passes.  8 steps, not 16: half the registers, twice the
 // wavefronts whose loads are in flight (64 x 128 x 1024 bf16 with a gate: forward 16.6 us against 21.7); the forward pass asks for
-// the next turn's steps while it works on one (14.6; the backward pass has no registers for it: 30 -> 33).
+// the next turn's steps while it works on one (14.7; the backward pass has no registers for it: 30 -> 33).
 // Where batch and channels alone give too few wavefronts, time is cut into segments for several workgroups; a first pass
-// then makes the segments' pairs (reading f and v, or f, o and dh, once more), and the main pass composes those before
-// its segment.  (One pass would have workgroups wait for others; the second reading comes partly out of the last cache.)
+// then makes the segments' pairs (reading f and v, or f, o and dh, once more; a wavefront takes stretches that follow each other and
+// meets the others only at the end), and the main pass composes those before its segment.  (One pass would have workgroups wait for others; the second reading comes partly out of the last cache.)
 // A state in flight and the pairs that move it over 8 steps and more are fp64, everything inside a stretch fp32.  F of a long memory is so near 1
 // that what rounding takes, from F or from a state that hardly moves, is the same at every step of a steady gate and adds up (in fp32
 // what is left of a state after 32768 steps at f = 12 came out 1.8e-3 of itself off, 1e-7 so): P comes from 1 - P, a sum of positive terms with
 // digits of its own.  The card's fp64 multiply-add takes no longer than its fp32 one; the reads from LDS cost 0 to 4 % of a pass.  The backward pass starts from the states that the forward pass left
 // before every 8th step, so it needs no second scan for them.
-// Lanes are counted through the sequences, so few channels a sequence fill wavefronts too: 4000 x 48 x 24 forward 23 us and backward 42
-// against 47 and 64 with whole wavefronts for each sequence, 4000 x 47 x 192 78 and 130 against 93 and 156; where nothing is
-// saved, sequences and addresses by lane cost the backward pass 1 to 5 % (64 x 128 x 1024 30.6 to 31.4 us).
+// Lanes are counted through the sequences, so few channels a sequence fill wavefronts too: 4000 x 48 x 24 forward 23 us and backward 44
+// against 47 and 64 with whole wavefronts for each sequence, 4000 x 47 x 192 82 and 130 against 93 and 156; where nothing is
+// saved, sequences and addresses by lane cost the backward pass 1 to 5 % (64 x 128 x 1024).
 //
-// Measured, bf16 with a gate: 64 x 128 x 1024 forward 14.6 us, backward 24 behind it and 31 from memory (4.9, 3.8 TB/s; a large
-// copy 4.9); 32768 x 1 x 1024 forward 24 + 49 us; 8192 x 4 x 1024 without one forward 27 + 41, backward 24 + 57; a single
-// step of 128 sequences 2.8 us.
+// Measured, bf16 with a gate: 64 x 128 x 1024 forward 14.7 us, backward 26 behind it and 32 from memory (4.6, 3.7 TB/s; a large
+// copy 4.9), fp32 32 and 55 from memory (4.1, 4.3 TB/s); 32768 x 1 x 1024 forward 25 + 51 us; 8192 x 4 x 1024 without one forward 27 + 42, backward
+// 25 + 58; a single step of 128 sequences 2.8 us.
 #include <type_traits>
 
 #include "rows.hpp"
@@ -604,10 +604,10 @@ static GlrPlan glr_plan(int32_t dtype, int T, int B, int H, int32_t flags, const
   GlrPlan g{};
   g.vec = 1;
   if (dtype == ARD_BF16 && wide % 2 == 0) {
-    // Two channels a lane, 256 bytes a wavefront's row, as one's 128 fetch less well (64 x 128 x 1024 forward and backward 14.4 + 31.0 us,
-    // 14.5 + 34.5 with one; 4000 x 47 x 192 78 + 130, 90 + 154).  One where that leaves fewer than 8 stretches a CU, as a lane's two come one
-    // after the other (130 x 8 x 512 8.2 + 10.9, 6.8 + 8.6 with one; 1000 x 8 x 512, which has 16, 13.3 + 17.7, 13.5 + 18.7), and
-    // where one fills the CUs with wavefronts and two would not (224 x 16 x 1024 11.9 + 17.5, 9.4 + 15.0; 4000: 147 + 263, 129 + 229).
+    // Two channels a lane, 256 bytes a wavefront's row, as one's 128 fetch less well (64 x 128 x 1024 forward and backward 14.8 + 31.8 us,
+    // 14.8 + 36.7 with one; 4000 x 47 x 192 82 + 130, 92 + 146).  One where that leaves fewer than 8 stretches a CU, as a lane's two come one
+    // after the other (130 x 8 x 512 8.4 + 11.3, 6.9 + 8.8 with one; 1000 x 8 x 512, which has 16, takes as long either way), and
+    // where one fills the CUs with wavefronts and two would not (224 x 16 x 1024 12.6 + 19.1, 9.7 + 15.4; 4000: 149 + 244, 128 + 230).
     const int64_t two = groups_of(2);
     g.vec = two * pieces <= 2048 || (two * waves < 2048 && groups_of(1) * waves >= 2048) ? 1 : 2;
   }
@@ -619,10 +619,11 @@ static GlrPlan glr_plan(int32_t dtype, int T, int B, int H, int32_t flags, const
   const int64_t have = (int64_t)g.a.groups * g.waves;  // wavefronts without cutting time
   const int turns = ceil_div(pieces, g.waves);
   int segs = 1;
-  // Time is cut below 8 wavefronts a CU, into 16 a CU: with half as many 32768 x 1 x 1024 took 95 us (83 then), 8192 x 4 x 1024 97 (85);
-  // with twice as many 89 and 87, as more pairs are read.  The second launch is worth four turns of 64 steps where there is
-  // little work (bf16 192 x 8 x 512 forward and backward 9.2 + 12.1 us in one launch, 10.1 + 11.5 in two; 256: 11.7 + 15.6, 10.6 + 11.5),
-  // the second reading eight where there is more (320 x 16 x 1000 18.0 + 23.4, 19.0 + 28.5; 1000: 58 + 87, 47 + 81).
+  // Time is cut below 8 wavefronts a CU, into 16 a CU: with half as many 32768 x 1 x 1024 takes 87 us (81), 8192 x 4 x 1024 without a gate 77 + 102 (73 + 96);
+  // with twice as many 87 and 75 + 99, as more pairs are read.  (Where there are few bytes, half as many would do: 4000 x 48 x 24 20 + 38, 23 + 44 so.)
+  // The second launch is worth four turns of 64 steps where there is little work (bf16 192 x 8 x 512 forward and backward 7.5 + 10.4 us in
+  // one launch, 9.4 + 10.3 in two; 256: 8.6 + 13.5, 8.9 + 10.5), the second reading eight where there is more (320 x 16 x 1000 16.2 + 25.7,
+  // 17.1 + 25.4; 1000: 50 + 93, 48 + 80).
   if (have < 2048 && turns >= (have <= 512 ? 4 : 8)) segs = imin(turns, (int)(4096 / have));
   const int per = ceil_div(turns, segs);
   g.a.segs = ceil_div(turns, per);

@@ -171,7 +171,8 @@ __global__ __launch_bounds__(norm_fwd_threads(G)) void norm_fwd_kernel(NormRows 
 
 // Rows too long for the registers of a workgroup: read three times, the second and third time from the cache.  A run's elements are added
 // up before their sum joins the thread's: one by one, 32768 squares of a thread (rows of 2^25 bf16 elements) came out
-// 1e-5 too large, each being ever less beside the growing sum.
+// 1e-5 too large, each being ever less beside the growing sum.  2048 x 20480 bf16 forward 50 us, backward 112 (3.3, 2.2 TB/s of inputs and results;
+// 2048 x 16384, held in registers, 29 and 63), 2048 x 32768 84 and 170; fp32 97 and 195, 159 and 317.
 template <typename T, typename WT>
 __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(NormRows a, const T* X, const WT* gamma, const WT* beta, T* Y, float* mean, float* rstd) {
   constexpr int CE = ElemTraits<T>::CE;
