@@ -523,6 +523,77 @@ int32_t ard_glr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t H, const void* 
                     const float* dcT, void* df, void* dv, void* dout, int64_t dz_t, int64_t dz_b, float* dc0, int32_t flags,
                     void* ws, size_t ws_bytes, void* stream);
 
+/* ---- gated delta rule ----------------------------------------------------------- */
+
+/*
+ * A recurrence whose state of a head is a matrix S[Dk x Dv], for B sequences of T steps (sg = the logistic function, |x| the length):
+ *   a = sg(f), w = sg(b), kh = k / sqrt(|k|^2 + eps), qh = q / sqrt(|q|^2 + eps)
+ *   S_t = a_t S_{t-1} + w_t kh_t (v_t - a_t S_{t-1}^T kh_t)^T,    o_t = scale S_t^T qh_t
+ * q, k have Hk heads of Dk elements, v and o H heads of Dv, f and b one element for each of H heads; H is a multiple of Hk, and head h reads
+ * the queries and keys of head h / (H / Hk).  All five are what a product left: element i of head h at step t of sequence n is at
+ * p + t*t + n*b + h*D + i elements (ard_steps: the parts of one product's rows, separate tensors and either order of time and batch all serve).
+ * S0[B x H x Dk x Dv] (fp32, NULL: zeros) is the state before the first step, ST (may be NULL) the one behind the last; ST may be S0.
+ * d_lengths[B] (device, may be NULL: all T): sequence n has that many steps (clamped to 0..T); behind them o is +0.0, the state
+ * stands, and what the inputs hold there has no part in anything.
+ * ckpt (fp32, may be NULL) receives the states before every ard_gdr_chunk()-th step, [ceil(T / chunk) x B x H x Dk x Dv], which the
+ * backward pass needs.  States, sums and gates are fp32, sums of log(a) fp64; results are rounded once.
+ * Backward: d_o and dST (fp32, NULL: zeros) are the gradients of o and ST; grads[5] those of q, k, v, f, b (the heads that share a query or key
+ * added up), every element written, +0.0 behind a sequence's end; dS0 (fp32, may be NULL) that of S0, which may be dST.
+ * in, grads: five ard_steps on the host, in the order q, k, v, f, b.  Otherwise no output may overlap an input or another output.
+ * Dk and Dv are at most ARD_GDR_MAX (else ARD_EUNSUPPORTED).
+ */
+#define ARD_GDR_CHUNK 64 /* steps between the states of ckpt */
+#define ARD_GDR_MAX 128
+typedef struct {
+  void* p;
+  int64_t t, b; /* elements from step to step and from sequence to sequence */
+} ard_steps;
+int32_t ard_gdr_chunk(void);
+size_t ard_gdr_workspace_bytes(int32_t dtype, int32_t T, int32_t B, int32_t Hk, int32_t H, int32_t Dk, int32_t Dv, int32_t backward);
+int32_t ard_gdr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, int32_t H, int32_t Dk, int32_t Dv, const ard_steps* in, float scale, float eps,
+                    const float* S0, const int32_t* d_lengths, const ard_steps* o, float* ST, float* ckpt, void* ws, size_t ws_bytes, void* stream);
+int32_t ard_gdr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, int32_t H, int32_t Dk, int32_t Dv, const ard_steps* in, float scale, float eps,
+                    const int32_t* d_lengths, const float* ckpt, const ard_steps* d_o, const float* dST, const ard_steps* grads, float* dS0,
+                    void* ws, size_t ws_bytes, void* stream);
+
+/* ---- embedding -------------------------------------------------------------- */
+
+/*
+ * R tokens into rows of D elements: Y[r] = scale * E[id_r], +0.0 where id_r is outside 0 .. V-1 (padding).
+ * E[V x D] is the table, ld* elements from row to row (at least D), rows start at any element.  dtype: of Y and dY; wdtype: of E and dE, ARD_F32
+ * or dtype.  Products and sums are fp32, results are rounded once.
+ * Backward: dE[v] = beta dE[v] + scale * (sum of dY[r] over the r with id_r = v, in ascending r, of frequent tokens in pieces of a fixed size: the
+ * same bits on every call).  beta = 0: every row is written, +0.0 where no token met it; beta = 1: rows that no token met are neither read nor
+ * written (the table that is the output product's weight too has its gradient added).  No output may overlap an input.
+ */
+size_t ard_embed_workspace_bytes(int32_t R, int32_t V, int32_t D);   /* of the backward pass */
+int32_t ard_embed_fwd(int32_t dtype, int32_t wdtype, int32_t R, int32_t V, int32_t D, const int32_t* d_ids, const void* E, int64_t lde, float scale,
+                      void* Y, int64_t ldy, void* stream);
+int32_t ard_embed_bwd(int32_t dtype, int32_t wdtype, int32_t R, int32_t V, int32_t D, const int32_t* d_ids, const void* dY, int64_t lddy, float scale,
+                      float beta, void* dE, int64_t lddE, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- distillation ------------------------------------------------------------- */
+
+/*
+ * Loss of R rows of V logits Z against a teacher's K largest logits t[R x K] of the elements d_ids[R x K], and labels d_labels[R] (or NULL):
+ *   p = softmax(t / T) over the row's entries, qT = softmax(z / T), q = softmax(z) over all V,
+ *   loss[r] = alpha T^2 sum_k p_k (log p_k - log qT[id_k]) + (1 - alpha) (-log q[label]),       T = temperature > 0, alpha from 0 to 1
+ *   dZ = dloss[r] (alpha T (qT - the p at their elements) + (1 - alpha) (q - 1 at the label)).
+ * An id outside 0 .. V-1 or a teacher's logit of -infinity is an entry that has no part; a label outside 0 .. V-1 is a row without one; what a row has
+ * no entries or label for is left out of its sums, as is all of a row whose logits are all -infinity.  A logit of -infinity (masked) has no share.
+ * An element may be named more than once: its entries' shares are added.  K = 0 or alpha = 0 is the labels' cross entropy (times 1 - alpha), t and d_ids may then
+ * be NULL.  dtype: of Z and dZ, rows ldz and lddz elements apart (at least V), which start at any element; tdtype: of t, ARD_F32 or dtype.
+ * stats[R x 3] (fp32): the largest logit and the sums of the exponentials at T and at 1, what ard_distill_bwd reads.  Statistics and sums are fp32.
+ * ard_distill_fwd with dZ (may be NULL) makes the gradient of dloss[R] (d_dloss, fp32; NULL: 1) in the same reading of Z.  dZ may lie where Z does (the same address
+ * and leading dimension); otherwise no output may overlap an input.  K is at most 1024 (else ARD_EUNSUPPORTED).
+ */
+int32_t ard_distill_fwd(int32_t dtype, int32_t tdtype, int32_t R, int32_t V, int32_t K, const void* Z, int64_t ldz, const int32_t* d_ids, const void* t,
+                        const int32_t* d_labels, float temperature, float alpha, const float* d_dloss, float* loss, float* stats, void* dZ,
+                        int64_t lddz, void* stream);
+int32_t ard_distill_bwd(int32_t dtype, int32_t tdtype, int32_t R, int32_t V, int32_t K, const void* Z, int64_t ldz, const int32_t* d_ids, const void* t,
+                        const int32_t* d_labels, float temperature, float alpha, const float* stats, const float* d_dloss, void* dZ, int64_t lddz,
+                        void* stream);
+
 /* ---- AdamW over many tensors --------------------------------------------------- */
 
 /*

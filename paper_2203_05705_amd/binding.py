@@ -48,9 +48,9 @@ except ImportError as e:   # not built: the names below are looked up in __getat
 if _ardcall is not None:
     _ardcall.configure(LIB_PATH, ArdError, torch._C._cuda_getCurrentRawStream)
     from ._ardcall import (adamw_step, adamw_values, batch, compact_weight, conv_bwd_blocks, conv_bwd_data,  # noqa: F401
-                           conv_bwd_rows, conv_bwd_weight, conv_fwd, conv_fwd_blocks, conv_fwd_rows, conv_select,
-                           drop_gemm_bwd_data, drop_gemm_bwd_weight, drop_gemm_bwd_weight_static, drop_gemm_fwd, glr_bwd,
-                           glr_fwd, layer_norm_bwd, layer_norm_fwd, lstm_bwd, lstm_fwd, sens_block_pattern, sens_predict,
+                           conv_bwd_rows, conv_bwd_weight, conv_fwd, conv_fwd_blocks, conv_fwd_rows, conv_select, distill_bwd, distill_fwd,
+                           drop_gemm_bwd_data, drop_gemm_bwd_weight, drop_gemm_bwd_weight_static, drop_gemm_fwd, embed_bwd,
+                           embed_fwd, gdr_bwd, gdr_fwd, glr_bwd, glr_fwd, layer_norm_bwd, layer_norm_fwd, lstm_bwd, lstm_fwd, sens_block_pattern, sens_predict,
                            sens_row_pattern)
 
     class Pattern(_ardcall.PatternBase):
@@ -126,6 +126,15 @@ _SIGS = {
     "ard_skew_normal_params": (C.c_int32, [C.c_double] * 3 + [C.c_void_p] * 2),
     "ard_skew_normal_pdf": (C.c_double, [C.c_double] * 4),
     "ard_prune_schedule": (C.c_int32, [C.c_int32] + [C.c_double] * 5 + [C.c_void_p]),
+    "ard_embed_workspace_bytes": (C.c_size_t, [C.c_int32] * 3),
+    "ard_embed_fwd": (C.c_int32, [C.c_int32] * 5 + [C.c_void_p] * 2 + [C.c_int64, C.c_float, C.c_void_p, C.c_int64, C.c_void_p]),
+    "ard_embed_bwd": (C.c_int32, [C.c_int32] * 5 + [C.c_void_p] * 2 + [C.c_int64, C.c_float, C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "ard_distill_fwd": (C.c_int32, [C.c_int32] * 5 + [C.c_void_p, C.c_int64] + [C.c_void_p] * 3 + [C.c_float] * 2 + [C.c_void_p] * 4 + [C.c_int64, C.c_void_p]),
+    "ard_distill_bwd": (C.c_int32, [C.c_int32] * 5 + [C.c_void_p, C.c_int64] + [C.c_void_p] * 3 + [C.c_float] * 2 + [C.c_void_p] * 3 + [C.c_int64, C.c_void_p]),
+    "ard_gdr_chunk": (C.c_int32, []),
+    "ard_gdr_workspace_bytes": (C.c_size_t, [C.c_int32] * 8),
+    "ard_gdr_fwd": (C.c_int32, [C.c_int32] * 7 + [C.c_void_p, C.c_float, C.c_float] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]),
+    "ard_gdr_bwd": (C.c_int32, [C.c_int32] * 7 + [C.c_void_p, C.c_float, C.c_float] + [C.c_void_p] * 7 + [C.c_size_t, C.c_void_p]),
     "ard_kept_count": (C.c_int32, [C.c_void_p, C.c_int32]),
     "ard_compact_dim": (C.c_int32, [C.c_void_p, C.c_int32]),
     "ard_tile_grid": (C.c_int32, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]),
@@ -342,15 +351,20 @@ def lstm_status_offset(dtype_code, T, B, I, H, pat=None):
     return None if off == (1 << 64) - 1 else off
 
 
-# ---- layer norm, gated linear recurrence, AdamW ---------------------------------------------
+# ---- layer norm, recurrences, embedding, AdamW ---------------------------------------------
 
 ADAMW_BLOCK = 256   # neighbouring elements that share the scales of an 8-bit state
+GDR_CHUNK = 64      # steps between the states that gdr_fwd keeps for gdr_bwd
 GLR_CHUNK = 8       # steps between the states that glr_fwd keeps for glr_bwd
 
 
 class CAdamWTensor(C.Structure):
     _fields_ = [("n", C.c_int64), ("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
                 ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("w", C.c_void_p)]
+
+
+class CSteps(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("t", C.c_int64), ("b", C.c_int64)]
 
 
 def adamw_state(params, bits: int = 32):
@@ -368,6 +382,14 @@ def adamw_state(params, bits: int = 32):
 
 def layer_norm_workspace_bytes(R: int, D: int) -> int:
     return int(lib().ard_layer_norm_workspace_bytes(R, D))
+
+
+def embed_workspace_bytes(R: int, V: int, D: int) -> int:
+    return int(lib().ard_embed_workspace_bytes(R, V, D))
+
+
+def gdr_workspace_bytes(dtype_code: int, T: int, B: int, Hk: int, H: int, Dk: int, Dv: int, backward: bool = False) -> int:
+    return int(lib().ard_gdr_workspace_bytes(dtype_code, T, B, Hk, H, Dk, Dv, int(backward)))
 
 
 def glr_workspace_bytes(dtype_code: int, T: int, B: int, H: int) -> int:

@@ -1,0 +1,912 @@
+// Gated delta rule: a recurrence whose state of a head is a matrix.
+//   S_t = a_t S_{t-1} + w_t kh_t (v_t - a_t S_{t-1}^T kh_t)^T,  o_t = scale S_t^T qh_t
+//
+// Few steps (a generation step above all) go one by one: a lane holds a column of S.  More steps are taken in chunks of 64.  With
+// G_i the sum of log(a) inside the chunk up to step i, Gamma_ij = exp(G_i - G_j), K and Q the unit keys and queries by rows, S the state before the chunk:
+//   A_ij = w_i Gamma_ij K_i.K_j (j < i),  P_ij = scale Gamma_ij Q_i.K_j (j <= i),  M = (I + A)^-1
+//   X_i = w_i (v_i - exp(G_i) S^T K_i),  U = M X                  (the rows that the steps write beside their keys)
+//   o_i = scale exp(G_i) S^T Q_i + sum_j P_ij U_j,   S' = exp(G_last) S + sum_j exp(G_last - G_j) K_j U_j^T
+// All factors are at most 1 and every G_i - G_j comes from fp64 sums, so no decay loses digits, however fast.
+//
+// A first launch, over all chunks at once, makes what does not depend on the states: A, P, M (blocks of 16 by substitution, the rest by
+// fp32 matrix instructions), written as operands of the second.  The second walks the chunks; a wavefront holds 16 or 32 columns of S in registers and
+// needs no other's: everything a chunk does to a column is a chain of products in its own registers (gdr.hpp).
+#include <type_traits>
+
+#include "gdr.hpp"
+
+namespace ard {
+
+// ---- step by step ---------------------------------------------------------------
+// A lane holds a column of S, a wavefront 64 of a head's; keys and queries reach the lanes through LDS.
+template <typename T, int DK>
+__global__ __launch_bounds__(64) void gdr_steps_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt) {
+  __shared__ float kq[2][DK];
+  const int slices = (a.Dv + 63) / 64, lane = threadIdx.x;
+  const int unit = blockIdx.x / slices, col = (blockIdx.x - unit * slices) * 64 + lane, n = unit / a.H, h = unit - n * a.H, hk = h / a.group;
+  const bool on = col < a.Dv;
+  const int64_t state = (int64_t)unit * a.Dk * a.Dv + col, plane = (int64_t)a.B * a.H * a.Dk * a.Dv;
+  float S[DK];
+#pragma unroll
+  for (int i = 0; i < DK; ++i) S[i] = S0 && on && i < a.Dk ? S0[state + (int64_t)i * a.Dv] : 0.0f;
+  const int live = live_steps(a, n);
+  for (int t = 0; t < a.T; ++t) {
+    if (ckpt && t % kChunk == 0 && on) {
+#pragma unroll
+      for (int i = 0; i < DK; ++i)
+        if (i < a.Dk) ckpt[(t / kChunk) * plane + state + (int64_t)i * a.Dv] = S[i];
+    }
+    T* out = (T*)o.p + t * o.t + n * o.b + h * a.Dv + col;
+    if (t >= live) {
+      if (on) *out = ElemTraits<T>::from_f32(0.0f);
+      continue;
+    }
+    const T* kp = (const T*)a.k.p + t * a.k.t + n * a.k.b + hk * a.Dk;
+    const T* qp = (const T*)a.q.p + t * a.q.t + n * a.q.b + hk * a.Dk;
+    float kx[DK / 64], qx[DK / 64], ks = 0.0f, qs = 0.0f;
+#pragma unroll
+    for (int i = 0; i < DK / 64; ++i) {
+      const int c = lane + 64 * i;
+      kx[i] = c < a.Dk ? ElemTraits<T>::to_f32(kp[c]) : 0.0f, qx[i] = c < a.Dk ? ElemTraits<T>::to_f32(qp[c]) : 0.0f;
+      ks = fmaf(kx[i], kx[i], ks), qs = fmaf(qx[i], qx[i], qs);
+    }
+    const float al = logistic(ElemTraits<T>::to_f32(((const T*)a.f.p)[t * a.f.t + n * a.f.b + h]));
+    const float w = logistic(ElemTraits<T>::to_f32(((const T*)a.b.p)[t * a.b.t + n * a.b.b + h]));
+    const float v = on ? ElemTraits<T>::to_f32(((const T*)a.v.p)[t * a.v.t + n * a.v.b + h * a.Dv + col]) : 0.0f;
+    const float rk = 1.0f / sqrtf(wave_sum(ks) + a.eps), rq = a.scale / sqrtf(wave_sum(qs) + a.eps);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < DK / 64; ++i) kq[0][lane + 64 * i] = kx[i] * rk, kq[1][lane + 64 * i] = qx[i] * rq;
+    __syncthreads();
+    float p[4] = {}, y[4] = {};
+#pragma unroll
+    for (int i = 0; i < DK; ++i) p[i & 3] = fmaf(kq[0][i], S[i], p[i & 3]);
+    const float e = w * (v - al * ((p[0] + p[1]) + (p[2] + p[3])));
+#pragma unroll
+    for (int i = 0; i < DK; ++i) {
+      S[i] = fmaf(kq[0][i], e, al * S[i]);
+      y[i & 3] = fmaf(kq[1][i], S[i], y[i & 3]);
+    }
+    if (on) *out = ElemTraits<T>::from_f32((y[0] + y[1]) + (y[2] + y[3]));
+  }
+  if (ST && on) {
+#pragma unroll
+    for (int i = 0; i < DK; ++i)
+      if (i < a.Dk) ST[state + (int64_t)i * a.Dv] = S[i];
+  }
+}
+
+// ---- what does not depend on the states -------------------------------------------
+template <int DK> struct PrepShared {
+  union {
+    struct {
+      float k[kChunk][DK + 4], q[kChunk][DK + 4];
+    };
+    struct {
+      float A[kChunk][kChunk + 4], M[kChunk][kChunk + 4], P[kChunk][kChunk + 4];
+    };
+  };
+  double G[kChunk];
+  float w[kChunk], rk[kChunk], rq[kChunk];
+};
+
+// 8 values of row `row` of a matrix in LDS, columns kb * 32 + {4 g + 0..3, 16 + 4 g + 0..3}
+template <int N, int LD> __device__ __forceinline__ Parts<N> row_parts(const float (*m)[LD], int row, int kb, int g) {
+  const f32x4 lo = *reinterpret_cast<const f32x4*>(&m[row][kb * 32 + 4 * g]), hi = *reinterpret_cast<const f32x4*>(&m[row][kb * 32 + 16 + 4 * g]);
+  return parts_of<N>(lo, hi);
+}
+// the same of the transpose: of column `col`, rows in that order
+template <int N, int LD> __device__ __forceinline__ Parts<N> col_parts(const float (*m)[LD], int col, int kb, int g) {
+  float x[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = m[kb * 32 + 4 * g + (j & 3) + 16 * (j >> 2)][col];
+  return parts_of<N>(x);
+}
+
+template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void gdr_prep_kernel(GdrArgs a) {
+  constexpr int IN = GdrType<T>::IN, OUT = GdrType<T>::OUT, KB = DK / 32;
+  __shared__ PrepShared<DK> sh;
+  const int unit = blockIdx.x, chunk = unit / (a.B * a.Hk), n = (unit - chunk * a.B * a.Hk) / a.Hk, hk = unit % a.Hk;
+  const int t0 = chunk * kChunk, live = imin(live_steps(a, n) - t0, kChunk);
+  if (live <= 0) return;  // (nobody reads this chunk's operands)
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  {
+    const int row = threadIdx.x >> 2, part = threadIdx.x & 3;
+    const int64_t t = t0 + row;
+    const T *kp = (const T*)a.k.p + t * a.k.t + n * a.k.b + hk * a.Dk, *qp = (const T*)a.q.p + t * a.q.t + n * a.q.b + hk * a.Dk;
+    float ks = 0.0f, qs = 0.0f;
+#pragma unroll
+    for (int i = 0; i < KB; ++i) {
+      const int at = (part + 4 * i) * 8;
+      float x[8] = {}, y[8] = {};
+      if (row < live) load_some<8>(kp + at, a.Dk - at, x), load_some<8>(qp + at, a.Dk - at, y);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) ks = fmaf(x[j], x[j], ks), qs = fmaf(y[j], y[j], qs), sh.k[row][at + j] = x[j], sh.q[row][at + j] = y[j];
+    }
+    ks += __shfl_xor(ks, 1), qs += __shfl_xor(qs, 1);
+    ks += __shfl_xor(ks, 2), qs += __shfl_xor(qs, 2);
+    if (part == 0) sh.rk[row] = row < live ? 1.0f / sqrtf(ks + a.eps) : 0.0f, sh.rq[row] = row < live ? 1.0f / sqrtf(qs + a.eps) : 0.0f;
+  }
+  __syncthreads();
+  f32x4 kk[4] = {}, qk[4] = {};
+  {
+    u32x4 *kf = a.kf + (int64_t)unit * 4 * KB * IN * 64, *qf = a.qf + (int64_t)unit * 4 * KB * IN * 64;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const Parts<IN> ka = row_parts<IN>(sh.k, w * 16 + c, kb, g), qa = row_parts<IN>(sh.q, w * 16 + c, kb, g);
+      store_parts(kf, w * KB + kb, ka);
+      store_parts(qf, w * KB + kb, qa);
+#pragma unroll
+      for (int ct = 0; ct < 4; ++ct)
+        if (ct <= w) {
+          const Parts<IN> b = row_parts<IN>(sh.k, ct * 16 + c, kb, g);
+          mul_add(ka, b, kk[ct]);
+          mul_add(qa, b, qk[ct]);
+        }
+    }
+    u32x4 *ktf = a.ktf + (int64_t)unit * (DK / 16) * 2 * IN * 64, *qtf = a.qtf + (int64_t)unit * (DK / 16) * 2 * IN * 64;
+    for (int i = w; i < DK / 8; i += 4) {
+      store_parts(ktf, i, col_parts<IN>(sh.k, (i >> 1) * 16 + c, i & 1, g));
+      if (BWD) store_parts(qtf, i, col_parts<IN>(sh.q, (i >> 1) * 16 + c, i & 1, g));
+    }
+  }
+  for (int s = 0; s < a.group; ++s) {
+    const int h = hk * a.group + s;
+    const int64_t out = ((int64_t)chunk * a.B + n) * a.H + h;
+    __syncthreads();  // keys and queries, or the head before, have been read
+    if (w == 0) {
+      const int64_t t = t0 + lane;
+      double G = 0.0;
+      float wr = 0.0f;
+      if (lane < live) {
+        const float f = ElemTraits<T>::to_f32(((const T*)a.f.p)[t * a.f.t + n * a.f.b + h]);
+        wr = logistic(ElemTraits<T>::to_f32(((const T*)a.b.p)[t * a.b.t + n * a.b.b + h]));
+        // log(sg(f)); below -1e4 its exponential is 0 as well, and sums stay finite
+        const float l = fminf(f, 0.0f) - log1pf(expf(-fabsf(f)));
+        G = (double)(l < -1e4f ? -1e4f : l);
+      }
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const double before = __shfl_up(G, d);
+        if (lane >= d) G += before;
+      }
+      sh.G[lane] = G, sh.w[lane] = wr;
+      const double last = __shfl(G, 63);
+      Steps64& st = a.steps[out];
+      const float rk = sh.rk[lane], rq = sh.rq[lane], since = expf((float)G), still = expf((float)(last - G));
+      st.G[lane] = G, st.since[lane] = since, st.still[lane] = still, st.w[lane] = wr, st.rk[lane] = rk, st.rq[lane] = rq;
+      st.ka[lane] = rk * since, st.qa[lane] = a.scale * rq * since, st.ke[lane] = rk * still;
+      if (lane == 63) st.whole = since;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct) {
+      const int j = ct * 16 + c;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = w * 16 + 4 * g + r;
+        float A = 0.0f, P = 0.0f;
+        if (j <= i) {
+          const float fade = expf((float)(sh.G[i] - sh.G[j])) * sh.rk[j];
+          A = j < i ? sh.w[i] * sh.rk[i] * fade * kk[ct][r] : 0.0f;
+          P = a.scale * sh.rq[i] * fade * qk[ct][r];
+        }
+        sh.A[i][j] = A, sh.P[i][j] = P, sh.M[i][j] = 0.0f;
+      }
+    }
+    __syncthreads();
+    {  // the diagonal blocks' inverses, a column a lane
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float s0 = i == c ? 1.0f : 0.0f, s1 = 0.0f;
+#pragma unroll
+        for (int j = 0; j < i; ++j) {
+          const float m = sh.A[w * 16 + i][w * 16 + j];
+          if (j & 1) s1 = fmaf(-m, x[j], s1);
+          else s0 = fmaf(-m, x[j], s0);
+        }
+        x[i] = s0 + s1;
+        if (g == 0) sh.M[w * 16 + i][w * 16 + c] = x[i];
+      }
+    }
+#pragma unroll
+    for (int d = 1; d < 4; ++d) {  // the blocks d below: M_rc = -M_rr sum_m A_rm M_mc
+      __syncthreads();
+      if (w + d < 4) {
+        const int rb = w + d, cb = w;
+        f32x4 s = {}, y = {};
+#pragma unroll
+        for (int m = 0; m < d; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            s = __builtin_amdgcn_mfma_f32_16x16x4f32(sh.A[rb * 16 + c][(cb + m) * 16 + 4 * e + g], sh.M[(cb + m) * 16 + 4 * e + g][cb * 16 + c], s, 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y = __builtin_amdgcn_mfma_f32_16x16x4f32(sh.M[rb * 16 + c][rb * 16 + 4 * g + e], -s[e], y, 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sh.M[rb * 16 + 4 * g + e][cb * 16 + c] = y[e];
+      }
+    }
+    __syncthreads();
+    constexpr int PP = BWD ? 3 : OUT;
+    u32x4 *mf = a.mf + out * 6 * 3 * 64, *pf = a.pf + out * 6 * OUT * 64, *mtf = a.mtf + out * 6 * 3 * 64, *ptf = a.ptf + out * 6 * PP * 64;
+    for (int i = w; i < 6; i += 4) {
+      const int rt = i < 2 ? i : 1 + i / 2, kb = i < 2 ? 0 : i & 1;  // (lower_frag's)
+      store_parts(mf, i, row_parts<3>(sh.M, rt * 16 + c, kb, g));
+      if (!BWD) store_parts(pf, i, row_parts<OUT>(sh.P, rt * 16 + c, kb, g));
+      if (BWD) {
+        const int ut = i < 4 ? i / 2 : i - 2, ub = i < 4 ? i & 1 : 1;  // (upper_frag's)
+        store_parts(mtf, i, col_parts<3>(sh.M, ut * 16 + c, ub, g));
+        store_parts(ptf, i, col_parts<PP>(sh.P, ut * 16 + c, ub, g));
+      }
+    }
+  }
+}
+
+// ---- a wavefront's columns ----------------------------------------------------------
+template <int NT> struct Columns {
+  int unit, n, h, hk, first;  // first: the lane's first column; NT = 2: the next one is its other
+  bool on;
+  __device__ __forceinline__ Columns(const GdrArgs& a, int index, int slices) {
+    const int g16 = threadIdx.x & 15;
+    unit = index / slices, first = (index - unit * slices) * 16 * NT + g16 * NT;
+    n = unit / a.H, h = unit - n * a.H, hk = h / a.group;
+  }
+};
+// rows 16 rt + 4 g + r of a matrix of fp32 rows `ld` apart, the lane's columns; rows and columns outside are 0
+template <int NT, int TILES> __device__ __forceinline__ void load_state(const float* p, int rows, int ld, int first, f32x4 (&S)[TILES][NT]) {
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int rt = 0; rt < TILES; ++rt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int i = rt * 16 + 4 * g + r;
+      float x[NT] = {};
+      if (i < rows) load_some<NT>(p + (int64_t)i * ld + first, ld - first, x);
+#pragma unroll
+      for (int e = 0; e < NT; ++e) S[rt][e][r] = x[e];
+    }
+}
+template <int NT, int TILES> __device__ __forceinline__ void store_state(float* p, int rows, int ld, int first, const f32x4 (&S)[TILES][NT]) {
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int rt = 0; rt < TILES; ++rt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int i = rt * 16 + 4 * g + r;
+      float x[NT];
+#pragma unroll
+      for (int e = 0; e < NT; ++e) x[e] = S[rt][e][r];
+      if (i < rows && first < ld) store_some<NT>(p + (int64_t)i * ld + first, ld - first, x);
+    }
+}
+// the same of a chunk's steps in a tensor of the caller's, of which `live` count (the others are 0 / are written as 0 up to `steps`)
+template <int NT, typename T> __device__ __forceinline__ void load_chunk(const T* p, int64_t step, int live, int wide, int first, f32x4 (&S)[4][NT]) {
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int i = rt * 16 + 4 * g + r;
+      float x[NT] = {};
+      if (i < live) load_some<NT>(p + i * step + first, wide - first, x);
+#pragma unroll
+      for (int e = 0; e < NT; ++e) S[rt][e][r] = x[e];
+    }
+}
+template <int NT, typename T> __device__ __forceinline__ void store_chunk(T* p, int64_t step, int live, int steps, int wide, int first, const f32x4 (&S)[4][NT]) {
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int i = rt * 16 + 4 * g + r;
+      float x[NT];
+#pragma unroll
+      for (int e = 0; e < NT; ++e) x[e] = i < live ? S[rt][e][r] : 0.0f;
+      if (i < steps && first < wide) store_some<NT>(p + i * step + first, wide - first, x);
+    }
+}
+__device__ __forceinline__ f32x4 row_weights(const float* w, int rt) { return *reinterpret_cast<const f32x4*>(w + rt * 16 + 4 * ((threadIdx.x & 63) >> 4)); }
+
+// U of a chunk: the state's columns as parts, Sp; v: the values; leaves U in x
+template <int IN, int DK, int NT>
+__device__ __forceinline__ void written_rows(const GdrArgs& a, int64_t ku, int64_t hu, const Parts<3> (&Sp)[DK / 32][NT], const f32x4 (&v)[4][NT], f32x4 (&u)[4][NT]) {
+  constexpr int KB = DK / 32;
+  const u32x4 *kf = a.kf + ku * 4 * KB * IN * 64, *mf = a.mf + hu * 6 * 3 * 64;
+  const Steps64& st = a.steps[hu];
+  f32x4 x[4][NT];
+#pragma unroll
+  for (int rt = 0; rt < 4; ++rt) {
+    f32x4 y[NT] = {};
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const Parts<IN> k = load_parts<IN>(kf, rt * KB + kb);
+#pragma unroll
+      for (int e = 0; e < NT; ++e) mul_add(k, Sp[kb][e], y[e]);
+    }
+    const f32x4 ka = row_weights(st.ka, rt), wr = row_weights(st.w, rt);
+#pragma unroll
+    for (int e = 0; e < NT; ++e) x[rt][e] = wr * (v[rt][e] - ka * y[e]);
+  }
+  Parts<3> xp[2][NT];
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+    for (int e = 0; e < NT; ++e) xp[kb][e] = parts_of<3>(x[2 * kb][e], x[2 * kb + 1][e]);
+#pragma unroll
+  for (int rt = 0; rt < 4; ++rt) {
+#pragma unroll
+    for (int e = 0; e < NT; ++e) u[rt][e] = f32x4{};
+#pragma unroll
+    for (int kb = 0; kb <= rt / 2; ++kb) {
+      const Parts<3> m = load_parts<3>(mf, lower_frag(rt, kb));
+#pragma unroll
+      for (int e = 0; e < NT; ++e) mul_add(m, xp[kb][e], u[rt][e]);
+    }
+  }
+}
+// S += (operands of DK rows x 64 steps) x (y, weighed by rows)
+template <int IN, int DK, int NT> __device__ __forceinline__ void add_outer(const u32x4* f, const float* weights, float sign, const f32x4 (&y)[4][NT], f32x4 (&S)[DK / 16][NT]) {
+  Parts<3> p[2][NT];
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    const f32x4 lo = sign * row_weights(weights, 2 * kb), hi = sign * row_weights(weights, 2 * kb + 1);
+#pragma unroll
+    for (int e = 0; e < NT; ++e) p[kb][e] = parts_of<3>(lo * y[2 * kb][e], hi * y[2 * kb + 1][e]);
+  }
+#pragma unroll
+  for (int rt = 0; rt < DK / 16; ++rt)
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const Parts<IN> k = load_parts<IN>(f, rt * 2 + kb);
+#pragma unroll
+      for (int e = 0; e < NT; ++e) mul_add(k, p[kb][e], S[rt][e]);
+    }
+}
+
+template <typename T, int DK, int NT>
+__global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt, int slices, int waves) {
+  constexpr int IN = GdrType<T>::IN, OUT = GdrType<T>::OUT, KB = DK / 32;
+  const int index = __builtin_amdgcn_readfirstlane(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6));
+  if (index >= waves) return;
+  const Columns<NT> at(a, index, slices);
+  const int64_t matrix = (int64_t)a.Dk * a.Dv, plane = (int64_t)a.B * a.H * matrix;
+  f32x4 S[DK / 16][NT] = {};
+  if (S0) load_state<NT, DK / 16>(S0 + at.unit * matrix, a.Dk, a.Dv, at.first, S);
+  const int all = live_steps(a, at.n);
+  for (int chunk = 0; chunk < a.chunks; ++chunk) {
+    if (ckpt) store_state<NT, DK / 16>(ckpt + chunk * plane + at.unit * matrix, a.Dk, a.Dv, at.first, S);
+    const int t0 = chunk * kChunk, steps = imin(a.T - t0, kChunk), live = imin(all - t0, steps);
+    T* out = (T*)o.p + t0 * o.t + at.n * o.b + at.h * a.Dv;
+    f32x4 y[4][NT] = {}, u[4][NT];
+    if (live <= 0) {
+      store_chunk<NT>(out, o.t, 0, steps, a.Dv, at.first, y);
+      continue;
+    }
+    const int64_t ku = ((int64_t)chunk * a.B + at.n) * a.Hk + at.hk, hu = ((int64_t)chunk * a.B + at.n) * a.H + at.h;
+    load_chunk<NT>((const T*)a.v.p + t0 * a.v.t + at.n * a.v.b + at.h * a.Dv, a.v.t, live, a.Dv, at.first, u);
+    const Steps64& st = a.steps[hu];
+    Parts<3> Sp[KB][NT];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < NT; ++e) Sp[kb][e] = parts_of<3>(S[2 * kb][e], S[2 * kb + 1][e]);
+    const u32x4* qf = a.qf + ku * 4 * KB * IN * 64;
+#pragma unroll
+    for (int rt = 0; rt < 4; ++rt) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const Parts<IN> q = load_parts<IN>(qf, rt * KB + kb);
+#pragma unroll
+        for (int e = 0; e < NT; ++e) mul_add(q, leading<OUT>(Sp[kb][e]), y[rt][e]);
+      }
+      const f32x4 qa = row_weights(st.qa, rt);
+#pragma unroll
+      for (int e = 0; e < NT; ++e) y[rt][e] *= qa;
+    }
+    {
+      f32x4 v[4][NT];
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+        for (int e = 0; e < NT; ++e) v[rt][e] = u[rt][e];
+      written_rows<IN, DK, NT>(a, ku, hu, Sp, v, u);
+    }
+    const u32x4* pf = a.pf + hu * 6 * OUT * 64;
+    Parts<OUT> up[2][NT];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < NT; ++e) up[kb][e] = parts_of<OUT>(u[2 * kb][e], u[2 * kb + 1][e]);
+#pragma unroll
+    for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+      for (int kb = 0; kb <= rt / 2; ++kb) {
+        const Parts<OUT> p = load_parts<OUT>(pf, lower_frag(rt, kb));
+#pragma unroll
+        for (int e = 0; e < NT; ++e) mul_add(p, up[kb][e], y[rt][e]);
+      }
+    store_chunk<NT>(out, o.t, live, steps, a.Dv, at.first, y);
+    const float whole = st.whole;
+#pragma unroll
+    for (int rt = 0; rt < DK / 16; ++rt)
+#pragma unroll
+      for (int e = 0; e < NT; ++e) S[rt][e] *= whole;
+    add_outer<IN, DK, NT>(a.ktf + ku * (DK / 8) * IN * 64, st.ke, 1.0f, u, S);
+  }
+  if (ST) store_state<NT, DK / 16>(ST + at.unit * matrix, a.Dk, a.Dv, at.first, S);
+}
+
+// ---- backward -----------------------------------------------------------------------
+// With dS' the gradient of the state behind a chunk, E = dX U^T, F = dO U^T:
+//   dX = M^T (P^T dO + still K dS'),  dV = w dX,  dS = exp(G_last) dS' + scale Q^T (since dO) - K^T (since w dX)
+//   dA = -E (j < i),  dP = F (j <= i), and with N_ij = -E_ij w_i Gamma_ij, R_ij = F_ij scale Gamma_ij:
+//   dQ_i = scale since_i S dO_i + sum_j R_ij K_j
+//   dK_i = [sum_j N_ij K_j - w_i since_i S dX_i] + [sum_j N_ji K_j + sum_j R_ji Q_j + still_i dS' U_i]      = dK+ + dK-
+//   dw_i / w_i = E_ii  (dX_i . X_i less what A's own w_i takes back; no division by a small w)
+//   d log(a_t) = the sum over i >= t of Q_i.dQ_i + K_i.dK+_i - K_i.dK-_i, and of what G_last moves: sum_i still_i K_i.dS' U_i + exp(G_last) <S, dS'>
+// Three launches after the first: U of every chunk from the states kept; the chunks from the last to the first, which leaves dX and dS' of each; and
+// all other gradients, every chunk for itself.
+
+// U of every chunk
+template <typename T, int DK, int NT> __global__ __launch_bounds__(256) void gdr_rows_kernel(GdrArgs a, const float* ckpt, int slices, int waves) {
+  constexpr int IN = GdrType<T>::IN, KB = DK / 32;
+  const int index = __builtin_amdgcn_readfirstlane(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6));
+  const int chunk = index / waves;
+  if (chunk >= a.chunks) return;
+  const Columns<NT> at(a, index - chunk * waves, slices);
+  const int t0 = chunk * kChunk, live = imin(live_steps(a, at.n) - t0, kChunk);
+  if (live <= 0) return;
+  const int64_t ku = ((int64_t)chunk * a.B + at.n) * a.Hk + at.hk, hu = ((int64_t)chunk * a.B + at.n) * a.H + at.h;
+  f32x4 S[DK / 16][NT], v[4][NT], u[4][NT];
+  load_state<NT, DK / 16>(ckpt + hu * a.Dk * a.Dv, a.Dk, a.Dv, at.first, S);
+  load_chunk<NT>((const T*)a.v.p + t0 * a.v.t + at.n * a.v.b + at.h * a.Dv, a.v.t, live, a.Dv, at.first, v);
+  Parts<3> Sp[KB][NT];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int e = 0; e < NT; ++e) Sp[kb][e] = parts_of<3>(S[2 * kb][e], S[2 * kb + 1][e]);
+  written_rows<IN, DK, NT>(a, ku, hu, Sp, v, u);
+  store_chunk<NT>(a.u + hu * kChunk * a.dvp, a.dvp, kChunk, kChunk, a.dvp, at.first, u);
+}
+
+template <typename T, int DK, int NT>
+__global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o, const float* dST, ard_steps dv, float* dS0, int slices, int waves) {
+  constexpr int IN = GdrType<T>::IN, KB = DK / 32;
+  const int index = __builtin_amdgcn_readfirstlane(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6));
+  if (index >= waves) return;
+  const Columns<NT> at(a, index, slices);
+  const int64_t matrix = (int64_t)a.Dk * a.Dv;
+  f32x4 S[DK / 16][NT] = {};
+  if (dST) load_state<NT, DK / 16>(dST + at.unit * matrix, a.Dk, a.Dv, at.first, S);
+  const int all = live_steps(a, at.n);
+  for (int chunk = a.chunks - 1; chunk >= 0; --chunk) {
+    const int t0 = chunk * kChunk, steps = imin(a.T - t0, kChunk), live = imin(all - t0, steps);
+    const int64_t ku = ((int64_t)chunk * a.B + at.n) * a.Hk + at.hk, hu = ((int64_t)chunk * a.B + at.n) * a.H + at.h;
+    T* out = (T*)dv.p + t0 * dv.t + at.n * dv.b + at.h * a.Dv;
+    f32x4 y[4][NT] = {}, x[4][NT];
+    if (live <= 0) {
+      store_chunk<NT>(out, dv.t, 0, steps, a.Dv, at.first, y);
+      continue;
+    }
+    load_chunk<NT>((const T*)d_o.p + t0 * d_o.t + at.n * d_o.b + at.h * a.Dv, d_o.t, live, a.Dv, at.first, x);
+    store_state<NT, DK / 16>(a.ds + hu * DK * a.dvp, DK, a.dvp, at.first, S);
+    const Steps64& st = a.steps[hu];
+    const u32x4 *kf = a.kf + ku * 4 * KB * IN * 64, *ptf = a.ptf + hu * 6 * 3 * 64, *mtf = a.mtf + hu * 6 * 3 * 64;
+    {
+      Parts<3> Sp[KB][NT];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < NT; ++e) Sp[kb][e] = parts_of<3>(S[2 * kb][e], S[2 * kb + 1][e]);
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const Parts<IN> k = load_parts<IN>(kf, rt * KB + kb);
+#pragma unroll
+          for (int e = 0; e < NT; ++e) mul_add(k, Sp[kb][e], y[rt][e]);
+        }
+        const f32x4 ke = row_weights(st.ke, rt);
+#pragma unroll
+        for (int e = 0; e < NT; ++e) y[rt][e] *= ke;
+      }
+    }
+    {
+      Parts<IN> p[2][NT];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < NT; ++e) p[kb][e] = parts_of<IN>(x[2 * kb][e], x[2 * kb + 1][e]);
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+        for (int kb = rt / 2; kb < 2; ++kb) {
+          const Parts<3> m = load_parts<3>(ptf, upper_frag(rt, kb));
+#pragma unroll
+          for (int e = 0; e < NT; ++e) mul_add(m, p[kb][e], y[rt][e]);
+        }
+    }
+    const float whole = st.whole;
+#pragma unroll
+    for (int rt = 0; rt < DK / 16; ++rt)
+#pragma unroll
+      for (int e = 0; e < NT; ++e) S[rt][e] *= whole;
+    add_outer<IN, DK, NT>(a.qtf + ku * (DK / 8) * IN * 64, st.qa, 1.0f, x, S);
+    {
+      Parts<3> p[2][NT];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < NT; ++e) p[kb][e] = parts_of<3>(y[2 * kb][e], y[2 * kb + 1][e]);
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) {
+#pragma unroll
+        for (int e = 0; e < NT; ++e) x[rt][e] = f32x4{};
+#pragma unroll
+        for (int kb = rt / 2; kb < 2; ++kb) {
+          const Parts<3> m = load_parts<3>(mtf, upper_frag(rt, kb));
+#pragma unroll
+          for (int e = 0; e < NT; ++e) mul_add(m, p[kb][e], x[rt][e]);
+        }
+      }
+    }
+    store_chunk<NT>(a.dx + hu * kChunk * a.dvp, a.dvp, kChunk, kChunk, a.dvp, at.first, x);
+#pragma unroll
+    for (int rt = 0; rt < 4; ++rt) {
+      const f32x4 wr = row_weights(st.w, rt);
+#pragma unroll
+      for (int e = 0; e < NT; ++e) x[rt][e] *= wr;
+    }
+    store_chunk<NT>(out, dv.t, live, steps, a.Dv, at.first, x);
+    add_outer<IN, DK, NT>(a.ktf + ku * (DK / 8) * IN * 64, st.ka, -1.0f, x, S);
+  }
+  if (dS0) store_state<NT, DK / 16>(dS0 + at.unit * matrix, a.Dk, a.Dv, at.first, S);
+}
+
+// 8 neighbouring fp32 values of a workspace row as parts
+template <int N> __device__ __forceinline__ Parts<N> run_parts(const float* p) {
+  float x[8];
+  load_run<8>(p, x);
+  return parts_of<N>(x);
+}
+__device__ __forceinline__ float over_rows(float x) {  // the sum over the lanes that share a column
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// The gradients of queries, keys and gates of a chunk and a key head: wavefront w has the 16 steps from 16 w on, as columns.
+template <typename T, int DK, int DV>
+__global__ __launch_bounds__(256) void gdr_grads_kernel(GdrArgs a, ard_steps d_o, const float* ckpt, ard_steps dq, ard_steps dk, ard_steps df, ard_steps db) {
+  constexpr int IN = GdrType<T>::IN, N = GdrType<T>::OUT, VB = DV / 32, RT = DK / 16;
+  __shared__ double dG[kChunk];
+  __shared__ float ends[4];
+  const int unit = blockIdx.x, chunk = unit / (a.B * a.Hk), n = (unit - chunk * a.B * a.Hk) / a.Hk, hk = unit % a.Hk;
+  const int t0 = chunk * kChunk, steps = imin(a.T - t0, kChunk), live = imin(live_steps(a, n) - t0, steps);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, mine = w * 16 + c;
+  T *dqp = (T*)dq.p + (int64_t)(t0 + mine) * dq.t + n * dq.b + hk * a.Dk, *dkp = (T*)dk.p + (int64_t)(t0 + mine) * dk.t + n * dk.b + hk * a.Dk;
+  f32x4 sumq[RT] = {}, sumk[RT] = {};
+  if (live > 0) {
+    const T *kp = (const T*)a.k.p + (int64_t)(t0 + mine) * a.k.t + n * a.k.b + hk * a.Dk, *qp = (const T*)a.q.p + (int64_t)(t0 + mine) * a.q.t + n * a.q.b + hk * a.Dk;
+    const u32x4 *ktf = a.ktf + (int64_t)unit * (DK / 8) * IN * 64, *qtf = a.qtf + (int64_t)unit * (DK / 8) * IN * 64;
+    for (int s = 0; s < a.group; ++s) {
+      const int h = hk * a.group + s;
+      const int64_t hu = ((int64_t)chunk * a.B + n) * a.H + h;
+      const Steps64& st = a.steps[hu];
+      const float *u = a.u + hu * kChunk * a.dvp, *dx = a.dx + hu * kChunk * a.dvp, *ds = a.ds + hu * DK * a.dvp, *S = ckpt + hu * a.Dk * a.Dv;
+      const T* dop = (const T*)d_o.p + t0 * d_o.t + n * d_o.b + h * a.Dv;
+      const auto of_do = [&](int row, int kb) {
+        float x[8] = {};
+        const int at = kb * 32 + 8 * g;
+        if (row < live) load_some<8>(dop + row * d_o.t + at, a.Dv - at, x);
+        return parts_of<IN>(x);
+      };
+      Parts<N> ub[VB], xb[VB];
+      Parts<IN> ob[VB];
+#pragma unroll
+      for (int kb = 0; kb < VB; ++kb) {
+        ub[kb] = run_parts<N>(u + mine * a.dvp + kb * 32 + 8 * g);
+        xb[kb] = run_parts<N>(dx + mine * a.dvp + kb * 32 + 8 * g);
+        ob[kb] = of_do(mine, kb);
+      }
+      const double Gm = st.G[mine];
+      const float wm = st.w[mine];
+      float dw = 0.0f;
+      // by pairs of row tiles: what the wavefront's steps take from the keys and queries of others, ready as operands
+      Parts<N> below[2], belowq[2], above[2], aboveq[2];  // N_ij K_i and R_ij Q_i of later rows i; N_ij K_j and R_ij K_j of earlier rows j
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        f32x4 lo[2] = {}, loq[2] = {}, up[2] = {}, upq[2] = {};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int rt = 2 * kb + half;
+          const f32x4 rk = row_weights(st.rk, rt);
+          float fade[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) fade[r] = expf(-(float)fabs(st.G[rt * 16 + 4 * g + r] - Gm));
+          if (rt >= w) {
+            f32x4 E = {}, F = {};
+#pragma unroll
+            for (int vb = 0; vb < VB; ++vb) {
+              mul_add(run_parts<N>(dx + (rt * 16 + c) * a.dvp + vb * 32 + 8 * g), ub[vb], E);
+              mul_add(of_do(rt * 16 + c, vb), ub[vb], F);
+            }
+            const f32x4 wr = row_weights(st.w, rt), rq = row_weights(st.rq, rt);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int i = rt * 16 + 4 * g + r;
+              if (i == mine) dw = E[r];
+              lo[half][r] = i > mine ? -E[r] * wr[r] * fade[r] * rk[r] : 0.0f;
+              loq[half][r] = i >= mine ? F[r] * a.scale * fade[r] * rq[r] : 0.0f;
+            }
+          }
+          if (rt <= w) {
+            f32x4 E = {}, F = {};
+#pragma unroll
+            for (int vb = 0; vb < VB; ++vb) {
+              const Parts<N> x = run_parts<N>(u + (rt * 16 + c) * a.dvp + vb * 32 + 8 * g);
+              mul_add(x, xb[vb], E);
+              mul_add(x, ob[vb], F);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int j = rt * 16 + 4 * g + r;
+              up[half][r] = j < mine ? -E[r] * wm * fade[r] * rk[r] : 0.0f;
+              upq[half][r] = j <= mine ? F[r] * a.scale * fade[r] * rk[r] : 0.0f;
+            }
+          }
+        }
+        below[kb] = parts_of<N>(lo[0], lo[1]), belowq[kb] = parts_of<N>(loq[0], loq[1]);
+        above[kb] = parts_of<N>(up[0], up[1]), aboveq[kb] = parts_of<N>(upq[0], upq[1]);
+      }
+      const float since = st.since[mine], still = st.still[mine], rkm = st.rk[mine], rqm = st.rq[mine];
+      float moved = 0.0f, into = 0.0f, both = 0.0f;
+#pragma unroll 1
+      for (int rt = 0; rt < RT; ++rt) {
+        f32x4 sq = {}, sx = {}, su = {};
+        const int row = rt * 16 + c;
+#pragma unroll
+        for (int vb = 0; vb < VB; ++vb) {
+          const int at = vb * 32 + 8 * g;
+          float x[8] = {}, y[8];
+          if (row < a.Dk) load_some<8>(S + (int64_t)row * a.Dv + at, a.Dv - at, x);
+          load_run<8>(ds + (int64_t)row * a.dvp + at, y);
+          const Parts<N> xs = parts_of<N>(x), ys = parts_of<N>(y);
+          mul_add(xs, ob[vb], sq);
+          mul_add(xs, xb[vb], sx);
+          mul_add(ys, ub[vb], su);
+          if (rt % 4 == w)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) both = fmaf(x[j], y[j], both);
+        }
+        f32x4 tq = sq * (a.scale * since), tp = sx * (-wm * since), te = su * still, tm = {};
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const Parts<IN> k = load_parts<IN>(ktf, rt * 2 + kb), q = load_parts<IN>(qtf, rt * 2 + kb);
+          if (2 * kb + 1 >= w) mul_add(k, below[kb], tm), mul_add(q, belowq[kb], tm);
+          if (2 * kb <= w) mul_add(k, above[kb], tp), mul_add(k, aboveq[kb], tq);
+        }
+        float kx[4] = {}, qx[4] = {};
+        const int at = rt * 16 + 4 * g;
+        if (mine < live) load_some<4>(kp + at, a.Dk - at, kx), load_some<4>(qp + at, a.Dk - at, qx);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          into = fmaf(kx[r] * rkm, te[r], into);
+          moved = fmaf(qx[r] * rqm, tq[r], fmaf(kx[r] * rkm, tp[r] - tm[r], moved));
+        }
+        tm += te;
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+          if (i == rt) sumq[i] += tq, sumk[i] += tp + tm;
+      }
+      dw = over_rows(dw), moved = over_rows(moved), into = over_rows(into);
+      both = wave_sum(both);
+      if (g == 0) dG[mine] = (double)moved - (double)into;
+      into = row_sum(into);
+      if (lane == 0) ends[w] = into + both * st.whole;
+      __syncthreads();
+      if (w == 0) {
+        double x = dG[63 - lane];
+        if (lane == 0) x += ((double)ends[0] + ends[1]) + ((double)ends[2] + ends[3]);
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+          const double before = __shfl_up(x, d);
+          if (lane >= d) x += before;
+        }
+        const int i = 63 - lane;
+        const int64_t t = t0 + i;
+        float grad = 0.0f;
+        if (i < live) grad = (float)x * logistic(-ElemTraits<T>::to_f32(((const T*)a.f.p)[t * a.f.t + n * a.f.b + h]));
+        if (i < steps) ((T*)df.p)[t * df.t + n * df.b + h] = ElemTraits<T>::from_f32(grad);
+      }
+      if (g == 0 && mine < steps) {
+        const int64_t t = t0 + mine;
+        float grad = 0.0f;
+        if (mine < live) grad = dw * logistic(-ElemTraits<T>::to_f32(((const T*)a.b.p)[t * a.b.t + n * a.b.b + h]));
+        ((T*)db.p)[t * db.t + n * db.b + h] = ElemTraits<T>::from_f32(grad);
+      }
+      __syncthreads();
+    }
+    // through the division by the length
+    float kd = 0.0f, qd = 0.0f;
+    const float rkm = a.steps[((int64_t)chunk * a.B + n) * a.H + hk * a.group].rk[mine], rqm = a.steps[((int64_t)chunk * a.B + n) * a.H + hk * a.group].rq[mine];
+    f32x4 kh[RT], qh[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float kx[4] = {}, qx[4] = {};
+      const int at = rt * 16 + 4 * g;
+      if (mine < live) load_some<4>(kp + at, a.Dk - at, kx), load_some<4>(qp + at, a.Dk - at, qx);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        kh[rt][r] = kx[r] * rkm, qh[rt][r] = qx[r] * rqm;
+        kd = fmaf(kh[rt][r], sumk[rt][r], kd), qd = fmaf(qh[rt][r], sumq[rt][r], qd);
+      }
+    }
+    kd = over_rows(kd), qd = over_rows(qd);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) sumk[rt] = rkm * (sumk[rt] - kh[rt] * kd), sumq[rt] = rqm * (sumq[rt] - qh[rt] * qd);
+  } else if ((int)threadIdx.x < steps) {
+    const int64_t t = t0 + threadIdx.x;
+    for (int s = 0; s < a.group; ++s) {
+      const int h = hk * a.group + s;
+      ((T*)df.p)[t * df.t + n * df.b + h] = ElemTraits<T>::from_f32(0.0f);
+      ((T*)db.p)[t * db.t + n * db.b + h] = ElemTraits<T>::from_f32(0.0f);
+    }
+  }
+  if (mine >= steps) return;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int at = rt * 16 + 4 * g;
+    float x[4], y[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] = mine < live ? sumq[rt][r] : 0.0f, y[r] = mine < live ? sumk[rt][r] : 0.0f;
+    store_some<4>(dqp + at, a.Dk - at, x);
+    store_some<4>(dkp + at, a.Dk - at, y);
+  }
+}
+
+// ---- host ---------------------------------------------------------------------------
+struct GdrPlan {
+  GdrArgs a;
+  int dk, nt, slices, waves;  // padded key size; columns of a wavefront / 16, their number in a head, and all of them
+  size_t bytes;
+};
+// The workspace's parts, one behind the other; `base` may be NULL, when only the size is asked for.
+static GdrPlan gdr_plan(int32_t dtype, int T, int B, int Hk, int H, int Dk, int Dv, bool backward, void* base) {
+  GdrPlan p{};
+  GdrArgs& a = p.a;
+  a.T = T, a.B = B, a.Hk = Hk, a.H = H, a.Dk = Dk, a.Dv = Dv, a.group = H / Hk, a.chunks = ceil_div(T, kChunk);
+  p.dk = Dk <= 64 ? 64 : 128;
+  p.nt = 1;
+  p.slices = ceil_div(Dv, 16 * p.nt);
+  p.waves = B * H * p.slices;
+  a.dvp = Dv <= 64 ? 64 : 128;
+  const size_t in = dtype == ARD_F32 ? 3 : 1, out = dtype == ARD_F32 ? 3 : 2, ku = (size_t)a.chunks * B * Hk, hu = (size_t)a.chunks * B * H;
+  size_t at = 0;
+  const auto take = [&](auto*& ptr, size_t n) {
+    ptr = (std::decay_t<decltype(ptr)>)((char*)base + at);
+    at = align_up(at + n, 256);
+  };
+  const size_t rows = (size_t)4 * (p.dk / 32) * in * 1024, cols = (size_t)(p.dk / 8) * in * 1024;
+  take(a.steps, hu * sizeof(Steps64));
+  take(a.kf, ku * rows), take(a.qf, ku * rows), take(a.ktf, ku * cols);
+  take(a.mf, hu * 6 * 3 * 1024);
+  if (backward) {
+    take(a.qtf, ku * cols), take(a.mtf, hu * 6 * 3 * 1024), take(a.ptf, hu * 6 * 3 * 1024);
+    take(a.u, hu * kChunk * a.dvp * 4), take(a.dx, hu * kChunk * a.dvp * 4), take(a.ds, hu * p.dk * a.dvp * 4);
+  } else {
+    take(a.pf, hu * 6 * out * 1024);
+  }
+  p.bytes = at;
+  return p;
+}
+
+// Up to this many steps go one by one.
+constexpr int kFewSteps = 4;
+
+static int32_t gdr_check(int32_t dtype, int32_t T, int32_t B, int32_t Hk, int32_t H, int32_t Dk, int32_t Dv) {
+  if (dtype != ARD_F32 && dtype != ARD_BF16) return fail(ARD_EDTYPE, "unknown dtype %d", dtype);
+  if (T <= 0 || B <= 0 || Hk <= 0 || H <= 0 || Dk <= 0 || Dv <= 0)
+    return fail(ARD_ESHAPE, "T, B, Hk, H, Dk and Dv must be positive (got %d, %d, %d, %d, %d, %d)", T, B, Hk, H, Dk, Dv);
+  if (H % Hk) return fail(ARD_ESHAPE, "H = %d is no multiple of Hk = %d", H, Hk);
+  if (Dk > ARD_GDR_MAX || Dv > ARD_GDR_MAX) return fail(ARD_EUNSUPPORTED, "Dk = %d and Dv = %d may be %d at most", Dk, Dv, ARD_GDR_MAX);
+  // (HIP counts a grid's threads in 32 bits)
+  if (T > 1 << 30 || (int64_t)B * H > 1 << 20 || (int64_t)ceil_div(T, kChunk) * B * H > 1 << 21) return fail(ARD_ESHAPE, "T = %d, B = %d, H = %d are too large", T, B, H);
+  return ARD_OK;
+}
+static int32_t gdr_tensors(int32_t dtype, const ard_steps* s, int n, const char* what) {
+  if (!s) return fail(ARD_EINVAL, "%s: null pointer", what);
+  for (int i = 0; i < n; ++i) {
+    if (!s[i].p) return fail(ARD_EINVAL, "%s: null tensor pointer", what);
+    if (misaligned(s[i].p, dtype == ARD_F32 ? 4 : 2)) return fail(ARD_EINVAL, "%s: a tensor does not start at a whole element", what);
+  }
+  return ARD_OK;
+}
+static int32_t gdr_numbers(float scale, float eps) {
+  if (!(eps > 0.0f && eps < INFINITY)) return fail(ARD_EINVAL, "eps must be positive and finite (got %g)", eps);
+  if (!(scale > -INFINITY && scale < INFINITY)) return fail(ARD_EINVAL, "scale must be finite (got %g)", scale);
+  return ARD_OK;
+}
+
+template <class F> static int32_t gdr_instance(int32_t dtype, int dk, F&& with) {
+  using Wide = std::integral_constant<int, 128>;
+  using Narrow = std::integral_constant<int, 64>;
+  if (dtype == ARD_F32) return dk == 64 ? with(0.0f, Narrow{}) : with(0.0f, Wide{});
+  return dk == 64 ? with((uint16_t)0, Narrow{}) : with((uint16_t)0, Wide{});
+}
+
+}  // namespace ard
+
+using namespace ard;
+
+extern "C" int32_t ard_gdr_chunk(void) { return kChunk; }
+
+extern "C" size_t ard_gdr_workspace_bytes(int32_t dtype, int32_t T, int32_t B, int32_t Hk, int32_t H, int32_t Dk, int32_t Dv, int32_t backward) {
+  if (gdr_check(dtype, T, B, Hk, H, Dk, Dv) != ARD_OK || (!backward && T <= kFewSteps)) return 0;
+  return gdr_plan(dtype, T, B, Hk, H, Dk, Dv, backward != 0, nullptr).bytes;
+}
+
+extern "C" int32_t ard_gdr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, int32_t H, int32_t Dk, int32_t Dv, const ard_steps* in, float scale, float eps,
+                               const float* S0, const int32_t* d_lengths, const ard_steps* o, float* ST, float* ckpt, void* ws, size_t ws_bytes, void* stream) {
+  if (int32_t st = gdr_check(dtype, T, B, Hk, H, Dk, Dv)) return st;
+  if (int32_t st = gdr_tensors(dtype, in, 5, "inputs")) return st;
+  if (int32_t st = gdr_tensors(dtype, o, 1, "o")) return st;
+  if (int32_t st = gdr_numbers(scale, eps)) return st;
+  if (misaligned(S0, 4) || misaligned(ST, 4) || misaligned(ckpt, 4) || misaligned(d_lengths, 4)) return fail(ARD_EINVAL, "a tensor does not start at a whole element");
+  const bool few = T <= kFewSteps;
+  GdrPlan p = gdr_plan(dtype, T, B, Hk, H, Dk, Dv, false, ws);
+  if (!few && (!ws || ws_bytes < p.bytes || misaligned(ws, 16))) return fail(ARD_EWORKSPACE, "workspace too small: need %zu bytes, got %zu", p.bytes, ws ? ws_bytes : 0);
+  GdrArgs& a = p.a;
+  a.q = in[0], a.k = in[1], a.v = in[2], a.f = in[3], a.b = in[4], a.scale = scale, a.eps = eps, a.len = d_lengths;
+  hipStream_t st = (hipStream_t)stream;
+  return gdr_instance(dtype, p.dk, [&](auto t, auto dk) {
+    using E = decltype(t);
+    constexpr int DK = decltype(dk)::value;
+    if (few) {
+      ARD_LAUNCH_NAMED("gdr_steps_kernel", (gdr_steps_kernel<E, DK>), dim3(B * H * ceil_div(Dv, 64)), dim3(64), 0, st, a, S0, *o, ST, ckpt);
+      ARD_LAUNCH_CHECK("gdr_steps_kernel");
+      return (int32_t)ARD_OK;
+    }
+    ARD_LAUNCH_NAMED("gdr_prep_kernel", (gdr_prep_kernel<E, DK, false>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a);
+    ARD_LAUNCH_CHECK("gdr_prep_kernel");
+    ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, 1>), dim3(ceil_div(p.waves, 4)), dim3(256), 0, st, a, S0, *o, ST, ckpt, p.slices, p.waves);
+    ARD_LAUNCH_CHECK("gdr_fwd_kernel");
+    return (int32_t)ARD_OK;
+  });
+}
+
+extern "C" int32_t ard_gdr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, int32_t H, int32_t Dk, int32_t Dv, const ard_steps* in, float scale, float eps,
+                               const int32_t* d_lengths, const float* ckpt, const ard_steps* d_o, const float* dST, const ard_steps* grads, float* dS0,
+                               void* ws, size_t ws_bytes, void* stream) {
+  if (int32_t st = gdr_check(dtype, T, B, Hk, H, Dk, Dv)) return st;
+  if (int32_t st = gdr_tensors(dtype, in, 5, "inputs")) return st;
+  if (int32_t st = gdr_tensors(dtype, d_o, 1, "the gradient of o")) return st;
+  if (int32_t st = gdr_tensors(dtype, grads, 5, "gradients")) return st;
+  if (int32_t st = gdr_numbers(scale, eps)) return st;
+  if (!ckpt) return fail(ARD_EINVAL, "null tensor pointer");
+  if (misaligned(ckpt, 4) || misaligned(dST, 4) || misaligned(dS0, 4) || misaligned(d_lengths, 4)) return fail(ARD_EINVAL, "a tensor does not start at a whole element");
+  GdrPlan p = gdr_plan(dtype, T, B, Hk, H, Dk, Dv, true, ws);
+  if (!ws || ws_bytes < p.bytes || misaligned(ws, 16)) return fail(ARD_EWORKSPACE, "workspace too small: need %zu bytes, got %zu", p.bytes, ws ? ws_bytes : 0);
+  GdrArgs& a = p.a;
+  a.q = in[0], a.k = in[1], a.v = in[2], a.f = in[3], a.b = in[4], a.scale = scale, a.eps = eps, a.len = d_lengths;
+  hipStream_t st = (hipStream_t)stream;
+  // dX and U are read in whole operands of 32 columns: the wavefronts of the padded columns write them as zeros
+  const int slices = a.dvp / (16 * p.nt), waves = B * H * slices;
+  return gdr_instance(dtype, p.dk, [&](auto t, auto dk) {
+    using E = decltype(t);
+    constexpr int DK = decltype(dk)::value;
+    ARD_LAUNCH_NAMED("gdr_prep_kernel", (gdr_prep_kernel<E, DK, true>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a);
+    ARD_LAUNCH_CHECK("gdr_prep_kernel");
+    ARD_LAUNCH_NAMED("gdr_rows_kernel", (gdr_rows_kernel<E, DK, 1>), dim3((unsigned)(((int64_t)a.chunks * waves + 3) / 4)), dim3(256), 0, st, a, ckpt, slices, waves);
+    ARD_LAUNCH_CHECK("gdr_rows_kernel");
+    ARD_LAUNCH_NAMED("gdr_back_kernel", (gdr_back_kernel<E, DK, 1>), dim3(ceil_div(waves, 4)), dim3(256), 0, st, a, *d_o, dST, grads[2], dS0, slices, waves);
+    ARD_LAUNCH_CHECK("gdr_back_kernel");
+    if (a.dvp == 64)
+      ARD_LAUNCH_NAMED("gdr_grads_kernel", (gdr_grads_kernel<E, DK, 64>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a, *d_o, ckpt, grads[0], grads[1], grads[3], grads[4]);
+    else
+      ARD_LAUNCH_NAMED("gdr_grads_kernel", (gdr_grads_kernel<E, DK, 128>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a, *d_o, ckpt, grads[0], grads[1], grads[3], grads[4]);
+    ARD_LAUNCH_CHECK("gdr_grads_kernel");
+    return (int32_t)ARD_OK;
+  });
+}

@@ -1,0 +1,113 @@
+// What the passes of the gated delta rule share: products of fp32 values on the bf16 matrix instructions, and the workspace.
+//
+// An fp32 value is the sum of three bf16 values (8 bits of its 24 each), so a product of two is the sum of the six products of parts that
+// reach its 24 bits, each exact, added in fp32: as good as fp32's own, at 2.7 times the rate of the fp32 matrix instructions.
+// What is bf16 already is one part, and its product with an fp32 value takes three; where only a bf16 result comes of it, two parts (16 bits) are kept.
+//
+// v_mfma_f32_16x16x32_bf16, lane = 16 g + c: A[row c][8 g + j], B[8 g + j][column c], j = 0..7; result[row 4 g + r][column c], r = 0..3.
+// A contraction may take its indices in any order that both operands share: with index 4 g + (j & 3) + 16 (j >> 2) in the place of
+// 8 g + j, the results of two row tiles are the B operand of the next product as they lie in their lane's registers.  So a chain of products
+// with a state, held by columns, stays inside a wavefront, without LDS or barriers.
+#pragma once
+#include "rows.hpp"
+
+namespace ard {
+
+constexpr int kChunk = ARD_GDR_CHUNK;
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// N parts of 8 values of a lane
+template <int N> struct Parts {
+  u32x4 p[N];
+};
+template <int N> __device__ __forceinline__ Parts<N> parts_of(const float (&x)[8]) {
+  Parts<N> s;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = x[2 * i], b = x[2 * i + 1];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const uint32_t hi = bf16_pair(a, b);
+      s.p[n][i] = hi;
+      a -= __uint_as_float(hi << 16), b -= __uint_as_float(hi & 0xffff0000u);
+    }
+  }
+  return s;
+}
+template <int N> __device__ __forceinline__ Parts<N> parts_of(const f32x4& lo, const f32x4& hi) {
+  const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  return parts_of<N>(x);
+}
+// the first N parts of more
+template <int N, int M> __device__ __forceinline__ Parts<N> leading(const Parts<M>& x) {
+  Parts<N> s;
+#pragma unroll
+  for (int n = 0; n < N; ++n) s.p[n] = x.p[n];
+  return s;
+}
+// acc += a b, of all products of parts those that reach the larger operand's last part; the small ones first
+template <int NA, int NB> __device__ __forceinline__ void mul_add(const Parts<NA>& a, const Parts<NB>& b, f32x4& acc) {
+  constexpr int L = NA > NB ? NA : NB;
+#pragma unroll
+  for (int s = L - 1; s >= 0; --s)
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+      if (s - i >= 0 && s - i < NB)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.p[i]), __builtin_bit_cast(bf16x8, b.p[s - i]), acc, 0, 0, 0);
+}
+// Operands in the workspace, 64 lanes x 16 bytes a part as a lane takes them.
+template <int N> __device__ __forceinline__ Parts<N> load_parts(const u32x4* base, int frag) {
+  Parts<N> s;
+#pragma unroll
+  for (int n = 0; n < N; ++n) s.p[n] = base[(frag * N + n) * 64 + (threadIdx.x & 63)];
+  return s;
+}
+template <int N> __device__ __forceinline__ void store_parts(u32x4* base, int frag, const Parts<N>& s) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) base[(frag * N + n) * 64 + (threadIdx.x & 63)] = s.p[n];
+}
+// Operands of a lower triangular 64 x 64 matrix: six tiles of 16 rows x 32 columns are not all zeros; of its transpose likewise.
+__host__ __device__ constexpr int lower_frag(int rt, int kb) { return rt < 2 ? rt : 2 * rt - 2 + kb; }
+__host__ __device__ constexpr int upper_frag(int rt, int kb) { return rt < 2 ? 2 * rt + kb : rt + 2; }
+
+// What a chunk's steps are weighed by (0 behind the sequence's end, where keys, queries and write strengths are taken for 0).
+struct Steps64 {
+  double G[kChunk];     // sums of log(a) from the chunk's first step on
+  float since[kChunk];  // exp(G_i)
+  float still[kChunk];  // exp(G_last - G_i)
+  float w[kChunk], rk[kChunk], rq[kChunk];
+  float ka[kChunk], qa[kChunk], ke[kChunk];  // rk since, scale rq since, rk still
+  float whole;          // exp(G_last)
+  float pad[7];
+};
+
+struct GdrArgs {
+  int T, B, Hk, H, Dk, Dv, group, chunks;
+  ard_steps q, k, v, f, b;
+  float scale, eps;
+  const int32_t* len;
+  // workspace: operands by (chunk, sequence, key head) and by (chunk, sequence, head)
+  u32x4 *kf, *qf, *ktf, *qtf, *mf, *pf, *mtf, *ptf;
+  Steps64* steps;
+  float *u, *dx, *ds;  // [64][dvp], [64][dvp], [dkp][dvp] of a chunk
+  int dvp;
+};
+__device__ __forceinline__ int live_steps(const GdrArgs& a, int n) { return a.len ? imin(imax(a.len[n], 0), a.T) : a.T; }
+
+template <typename T> struct GdrType;
+template <> struct GdrType<uint16_t> {
+  static constexpr int IN = 1, OUT = 2;  // parts of an input, and of a factor of a result
+};
+template <> struct GdrType<float> {
+  static constexpr int IN = 3, OUT = 3;
+};
+
+__device__ __forceinline__ float logistic(float x) {
+  const float e = expf(-fabsf(x));
+  return x >= 0.0f ? 1.0f / (1.0f + e) : e / (1.0f + e);
+}
+
+}  // namespace ard

@@ -50,7 +50,8 @@ struct PyRaised {};  // a Python exception is set
   X(ard_conv_workspace_bytes) X(ard_conv_out_size) X(ard_fmap_drop_conv) X(ard_conv_fwd_blocks) X(ard_conv_bwd_blocks) \
   X(ard_sens_regions) X(ard_sens_predict) X(ard_sens_row_pattern) X(ard_sens_block_pattern) X(ard_last_error) \
   X(ard_layer_norm_workspace_bytes) X(ard_layer_norm_fwd) X(ard_layer_norm_bwd) X(ard_glr_workspace_bytes) X(ard_glr_fwd)   \
-  X(ard_glr_bwd) X(ard_adamw_step) X(ard_adamw_values)
+  X(ard_glr_bwd) X(ard_adamw_step) X(ard_adamw_values) X(ard_embed_workspace_bytes) X(ard_embed_fwd) X(ard_embed_bwd)        \
+  X(ard_distill_fwd) X(ard_distill_bwd) X(ard_gdr_workspace_bytes) X(ard_gdr_fwd) X(ard_gdr_bwd)
 #define DECLARE(name) decltype(&::name) name = nullptr;
 struct Library {
   bool open = false;
@@ -1138,6 +1139,276 @@ PyObject* glr_bwd(const Args& a) {  // f, v, o, dh, ckpt, dcT, lengths, H, out, 
   return tensors_or_none(out, 4);
 }
 
+// The device of a call: that of its first tensor, of its stream and of all its other tensors.
+struct Here {
+  c10::Device dev;
+  Here(const at::Tensor& first, PyObject* stream, const char* what) : dev(first.device()) {
+    if (!first.is_cuda()) raise(PyExc_AssertionError, "%s: device-resident tensors only", what);
+    int at = dev.index();
+    if (stream && stream != Py_None) {  // (an object that only has an address says nothing of its device)
+      if (THPStream_Check(stream)) at = (int)reinterpret_cast<const THPStream*>(stream)->device_index;
+    } else {
+      at = c10::impl::VirtualGuardImpl(dev.type()).getDevice().index();
+    }
+    if (at != dev.index()) raise(PyExc_ValueError, "%s is on device %d, the stream on device %d", what, (int)dev.index(), at);
+  }
+  const at::Tensor& operator()(const at::Tensor& t, at::ScalarType dtype, const char* what) const {
+    on_device(t, dtype, what);
+    if (t.device() != dev) raise(PyExc_ValueError, "%s is on device %d, its companions on device %d", what, (int)t.device().index(), (int)dev.index());
+    return t;
+  }
+  const at::Tensor& contiguous(const at::Tensor& t, at::ScalarType dtype, int64_t numel, const char* what) const {
+    (*this)(t, dtype, what);
+    if (!t.is_contiguous() || t.numel() != numel) raise(PyExc_ValueError, "%s: %lld contiguous elements are wanted", what, (long long)numel);
+    return t;
+  }
+  // NULL where the argument is None
+  void* optional(const Args& a, int i, at::ScalarType dtype, int64_t numel, const char* what) const {
+    return a.given(i) ? contiguous(tensor_of(a.v[i], what), dtype, numel, what).data_ptr() : nullptr;
+  }
+  void workspace(const Args& a, int i) const {
+    if (a.given(i) && tensor_of(a.v[i], "ws").device() != dev) raise(PyExc_ValueError, "ws is on another device than its companions");
+    if (a.given(i) && !tensor_of(a.v[i], "ws").is_contiguous()) raise(PyExc_AssertionError, "ws: a contiguous tensor is wanted");
+  }
+};
+// rows that do not lie over each other, to be written
+Rows output_rows(const at::Tensor& t, int stored, const char* what) {
+  const Rows r = rows_of(t, stored, what);
+  if (r.R > 1 && r.ld < stored) raise(PyExc_ValueError, "%s: its rows overlap", what);
+  return r;
+}
+const at::Tensor* tokens(const Args& a, int i) {
+  const at::Tensor& t = tensor_of(a.v[i], "ids");
+  on_device(t, at::kInt, "ids");
+  if (!t.is_contiguous()) raise(PyExc_AssertionError, "ids: a contiguous tensor is wanted");
+  if (t.numel() > INT32_MAX) raise(PyExc_OverflowError, "ids: %lld are too many", (long long)t.numel());
+  return &t;
+}
+at::ScalarType dtype_of(PyObject* o, at::ScalarType dflt) {
+  if (!o || o == Py_None) return dflt;
+  if (!THPDtype_Check(o)) raise(PyExc_TypeError, "a torch dtype is wanted, got %s", Py_TYPE(o)->tp_name);
+  return reinterpret_cast<THPDtype*>(o)->scalar_type;
+}
+int32_t code_of(at::ScalarType t) {
+  if (t == at::kFloat) return ARD_F32;
+  if (t == at::kBFloat16) return ARD_BF16;
+  raise(PyExc_TypeError, "unsupported dtype %s", c10::toString(t));
+}
+
+PyObject* embed_fwd(const Args& a) {  // ids, E, scale, dtype, out, stream
+  const at::Tensor &ids = *tokens(a, 0), &E = ranked(tensor_of(a.v[1], "E"), 2, "E");
+  const Here here(ids, a.v[5], "ids");
+  const int32_t wt = dtype_code(here(E, E.scalar_type(), "E"));
+  const int V = dim(E, 0), D = dim(E, 1), R = (int)ids.numel();
+  const Rows table = rows_of(E, D, "E");
+  OnStream on(a.v[5]);
+  at::Tensor Y;
+  if (a.given(4)) Y = tensor_of(a.v[4], "out");
+  const at::ScalarType type = dtype_of(a.v[3], Y.defined() ? Y.scalar_type() : E.scalar_type());
+  const int32_t dt = code_of(type);
+  if (!Y.defined()) {
+    std::vector<int64_t> shape = ids.sizes().vec();
+    shape.push_back(D);
+    Y = output(shape, type, here.dev);
+  }
+  here(Y, type, "out");
+  if (R == 0) return result(a, 4, Y);
+  const Rows y = output_rows(Y, D, "out");
+  if (y.R != R) raise(PyExc_ValueError, "out: %d rows are wanted, got %d", R, y.R);
+  const float scale = (float)a.real(2, 1.0);
+  const int32_t* id = (const int32_t*)ids.data_ptr();
+  void* st = stream_of(a.v[5]);
+  enqueue(lib().ard_embed_fwd, dt, wt, R, V, D, id, (const void*)table.p, table.ld, scale, y.p, y.ld, st);
+  return result(a, 4, Y);
+}
+
+PyObject* embed_bwd(const Args& a) {  // ids, dY, V, scale, beta, dtype, out, ws, stream
+  const at::Tensor &ids = *tokens(a, 0), &dY = tensor_of(a.v[1], "dY");
+  const Here here(ids, a.v[8], "ids");
+  const int32_t dt = dtype_code(here(dY, dY.scalar_type(), "dY"));
+  if (dY.dim() < 1 || dY.size(-1) < 1) raise(PyExc_ValueError, "dY: rows of at least one element are wanted");
+  const int V = as_int(a.v[2]), D = dim(dY, (int)dY.dim() - 1), R = (int)ids.numel();
+  const Rows dy = rows_of(dY, D, "dY");
+  if (dy.R != R) raise(PyExc_ValueError, "dY: %d rows are wanted, got %d", R, dy.R);
+  if (V < 1) raise(PyExc_ValueError, "V: a table of at least one row is wanted");
+  const float scale = (float)a.real(3, 1.0), beta = (float)a.real(4, 0.0);
+  OnStream on(a.v[8]);
+  at::Tensor dE;
+  if (a.given(6)) dE = tensor_of(a.v[6], "out");
+  else if (beta != 0.0f) raise(PyExc_ValueError, "out: the gradient to add to is wanted");
+  const at::ScalarType type = dtype_of(a.v[5], dE.defined() ? dE.scalar_type() : at::kFloat);
+  const int32_t wt = code_of(type);
+  if (!dE.defined()) dE = output({V, D}, type, here.dev);
+  const Rows de = output_rows(ranked(here(dE, type, "out"), 2, "out"), D, "out");
+  if (de.R != V) raise(PyExc_ValueError, "out: %d rows are wanted, got %d", V, de.R);
+  if (R == 0) {  // no token: nothing to add
+    if (beta == 0.0f) dE.zero_();
+    return result(a, 6, dE);
+  }
+  here.workspace(a, 7);
+  SeldomWorkspace ws(a, 7, here.dev, [&] { return lib().ard_embed_workspace_bytes(R, V, D); });
+  const int32_t* id = (const int32_t*)ids.data_ptr();
+  void* st = stream_of(a.v[8]);
+  enqueue(lib().ard_embed_bwd, dt, wt, R, V, D, id, (const void*)dy.p, dy.ld, scale, beta, de.p, de.ld, ws.p, ws.bytes, st);
+  return result(a, 6, dE);
+}
+
+// the arguments that both passes of the distillation loss begin with
+struct Distill {
+  Here here;
+  Rows z;
+  int V, K = 0;
+  int32_t dt, tt;
+  const int32_t *ids = nullptr, *labels = nullptr;
+  const void* t = nullptr;
+  float temperature, alpha;
+  Distill(const Args& a, int iLabels, int iT, int iAlpha, int iStream) : here(tensor_of(a.v[0], "Z"), a.v[iStream], "Z") {
+    const at::Tensor& Z = ranked(tensor_of(a.v[0], "Z"), 2, "Z");
+    dt = tt = dtype_code(Z);
+    V = dim(Z, 1);
+    z = rows_of(Z, V, "Z");
+    if (a.given(1) != a.given(2)) raise(PyExc_ValueError, "a teacher's logits and their ids come together");
+    if (a.given(1)) {
+      const at::Tensor &i = ranked(tensor_of(a.v[1], "ids"), 2, "ids"), &l = tensor_of(a.v[2], "t");
+      K = dim(i, 1);
+      const int64_t n = (int64_t)z.R * K;
+      if (dim(i, 0) != z.R || l.sizes() != i.sizes()) raise(PyExc_ValueError, "ids and t: shape (%d, K) is wanted", z.R);
+      ids = (const int32_t*)here.contiguous(i, at::kInt, n, "ids").data_ptr();
+      tt = dtype_code(l);
+      t = here.contiguous(l, l.scalar_type(), n, "t").data_ptr();
+    }
+    labels = (const int32_t*)here.optional(a, iLabels, at::kInt, z.R, "labels");
+    temperature = (float)a.real(iT, 1.0), alpha = (float)a.real(iAlpha, 1.0);
+  }
+};
+
+PyObject* distill_fwd(const Args& a) {  // Z, ids, t, labels, temperature, alpha, dloss, grad, out, stream
+  const Distill c(a, 3, 4, 5, 9);
+  const at::Tensor& Z = tensor_of(a.v[0], "Z");
+  const float* dloss = (const float*)c.here.optional(a, 6, at::kFloat, c.z.R, "dloss");
+  at::Tensor o[3];
+  OnStream on(a.v[9]);
+  if (a.given(8)) outputs_of(a.v[8], 3, o);
+  const bool grad = a.given(7) ? a.truth(7, false) : dloss || o[2].defined();
+  if (!o[0].defined()) o[0] = output({c.z.R}, at::kFloat, c.here.dev);
+  if (!o[1].defined()) o[1] = output({c.z.R, 3}, at::kFloat, c.here.dev);
+  if (!grad) o[2] = at::Tensor();
+  else if (!o[2].defined()) o[2] = output({c.z.R, c.V}, Z.scalar_type(), c.here.dev);
+  float *loss = (float*)c.here.contiguous(o[0], at::kFloat, c.z.R, "out").data_ptr(), *stats = (float*)c.here.contiguous(o[1], at::kFloat, (int64_t)c.z.R * 3, "out").data_ptr();
+  Rows dz{nullptr, 0, 0};
+  if (grad) {
+    dz = output_rows(ranked(c.here(o[2], Z.scalar_type(), "out"), 2, "out"), c.V, "out");
+    same_rows(c.z, dz, "out");
+  }
+  if (c.z.R == 0) return tensors_or_none(o, 3);
+  void* st = stream_of(a.v[9]);
+  enqueue(lib().ard_distill_fwd, c.dt, c.tt, c.z.R, c.V, c.K, (const void*)c.z.p, c.z.ld, c.ids, c.t, c.labels, c.temperature, c.alpha, dloss, loss, stats, dz.p, dz.ld, st);
+  return tensors_or_none(o, 3);
+}
+
+PyObject* distill_bwd(const Args& a) {  // Z, ids, t, stats, dloss, labels, temperature, alpha, out, stream
+  const Distill c(a, 5, 6, 7, 9);
+  const at::Tensor& Z = tensor_of(a.v[0], "Z");
+  if (!a.given(3)) raise(PyExc_TypeError, "the statistics of the forward pass are wanted");
+  const float* stats = (const float*)c.here.optional(a, 3, at::kFloat, (int64_t)c.z.R * 3, "stats");
+  const float* dloss = (const float*)c.here.optional(a, 4, at::kFloat, c.z.R, "dloss");
+  OnStream on(a.v[9]);
+  const at::Tensor dZ = a.given(8) ? tensor_of(a.v[8], "out") : output({c.z.R, c.V}, Z.scalar_type(), c.here.dev);
+  const Rows dz = output_rows(ranked(c.here(dZ, Z.scalar_type(), "out"), 2, "out"), c.V, "out");
+  same_rows(c.z, dz, "out");
+  if (c.z.R == 0) return result(a, 8, dZ);
+  void* st = stream_of(a.v[9]);
+  enqueue(lib().ard_distill_bwd, c.dt, c.tt, c.z.R, c.V, c.K, (const void*)c.z.p, c.z.ld, c.ids, c.t, c.labels, c.temperature, c.alpha, stats, dloss, dz.p, dz.ld, st);
+  return result(a, 8, dZ);
+}
+
+// The five inputs of a gated delta rule, or tensors of their shapes.
+struct Gdr {
+  Here here;
+  int T, B, Hk, H, Dk, Dv;
+  int32_t dt;
+  at::ScalarType type;
+  ard_steps in[5];
+  Gdr(const Args& a, int iStream) : here(tensor_of(a.v[0], "q"), a.v[iStream], "q") {
+    const at::Tensor &q = ranked(tensor_of(a.v[0], "q"), 4, "q"), &v = ranked(tensor_of(a.v[2], "v"), 4, "v");
+    dt = dtype_code(q), type = q.scalar_type();
+    T = dim(q, 0), B = dim(q, 1), Hk = dim(q, 2), Dk = dim(q, 3), H = dim(v, 2), Dv = dim(v, 3);
+    if (T < 1 || B < 1 || Hk < 1 || H < 1 || Dk < 1 || Dv < 1) raise(PyExc_ValueError, "q, v: no dimension may be empty");
+    static const char* names[] = {"q", "k", "v", "f", "b"};
+    for (int i = 0; i < 5; ++i) in[i] = steps(tensor_of(a.v[i], names[i]), i, names[i]);
+  }
+  // strides of what has the shape of the i-th input
+  ard_steps steps(const at::Tensor& t, int i, const char* what) const {
+    here(t, type, what);
+    const int heads = i < 2 ? Hk : H, D = i < 2 ? Dk : i == 2 ? Dv : 1;
+    const bool shaped = i < 3 ? t.dim() == 4 && t.size(0) == T && t.size(1) == B && t.size(2) == heads && t.size(3) == D
+                              : t.dim() == 3 && t.size(0) == T && t.size(1) == B && t.size(2) == heads;
+    if (!shaped) raise(PyExc_ValueError, i < 3 ? "%s: shape (%d, %d, %d, %d) is wanted" : "%s: shape (%d, %d, %d) is wanted", what, T, B, heads, D);
+    if ((i < 3 && D > 1 && t.stride(3) != 1) || (heads > 1 && t.stride(2) != D)) raise(PyExc_AssertionError, "%s: the heads' elements of a step must be neighbours", what);
+    return {t.data_ptr(), T > 1 ? t.stride(0) : 0, B > 1 ? t.stride(1) : 0};
+  }
+  ard_steps written(const at::Tensor& t, int i, const char* what) const {
+    const ard_steps s = steps(t, i, what);
+    const int64_t wide = i < 2 ? (int64_t)Hk * Dk : i == 2 ? (int64_t)H * Dv : H;
+    const bool time_outer = s.t >= s.b;
+    const int64_t inner = time_outer ? s.b : s.t, outer = time_outer ? s.t : s.b, n = time_outer ? B : T, m = time_outer ? T : B;
+    if ((n > 1 && inner < wide) || (m > 1 && outer < (n - 1) * inner + wide)) raise(PyExc_ValueError, "%s: its elements overlap", what);
+    return s;
+  }
+  int64_t state() const { return (int64_t)B * H * Dk * Dv; }
+  int64_t chunks() const { return (T + ARD_GDR_CHUNK - 1) / ARD_GDR_CHUNK; }
+};
+
+PyObject* gdr_fwd(const Args& a) {  // q, k, v, f, b, S0, lengths, scale, eps, train, out, ws, stream
+  const Gdr c(a, 12);
+  const float* S0 = (const float*)c.here.optional(a, 5, at::kFloat, c.state(), "S0");
+  const int32_t* len = (const int32_t*)c.here.optional(a, 6, at::kInt, c.B, "lengths");
+  const float scale = a.given(7) ? (float)a.real(7, 1.0) : (float)(1.0 / std::sqrt((double)c.Dk)), eps = (float)a.real(8, 1e-6);
+  const bool train = a.truth(9, true);
+  at::Tensor out[3];
+  OnStream on(a.v[12]);
+  if (a.given(10)) outputs_of(a.v[10], 3, out);
+  if (!out[0].defined()) out[0] = output({c.T, c.B, c.H, c.Dv}, c.type, c.here.dev);
+  if (!out[1].defined()) out[1] = output({c.B, c.H, c.Dk, c.Dv}, at::kFloat, c.here.dev);
+  if (!out[2].defined() && train) out[2] = output({c.chunks(), c.B, c.H, c.Dk, c.Dv}, at::kFloat, c.here.dev);
+  const ard_steps o = c.written(out[0], 2, "out");
+  float* ST = (float*)c.here.contiguous(out[1], at::kFloat, c.state(), "out").data_ptr();
+  float* ck = out[2].defined() ? (float*)c.here.contiguous(out[2], at::kFloat, c.chunks() * c.state(), "out").data_ptr() : nullptr;
+  c.here.workspace(a, 11);
+  SeldomWorkspace ws(a, 11, c.here.dev, [&] { return lib().ard_gdr_workspace_bytes(c.dt, c.T, c.B, c.Hk, c.H, c.Dk, c.Dv, 0); });
+  const ard_steps *in = c.in, *po = &o;
+  void* st = stream_of(a.v[12]);
+  enqueue(lib().ard_gdr_fwd, c.dt, c.T, c.B, c.Hk, c.H, c.Dk, c.Dv, in, scale, eps, S0, len, po, ST, ck, ws.p, ws.bytes, st);
+  return tensors_or_none(out, 3);
+}
+
+PyObject* gdr_bwd(const Args& a) {  // q, k, v, f, b, do, ckpt, dST, lengths, scale, eps, out, ws, stream
+  const Gdr c(a, 13);
+  const ard_steps d_o = c.steps(tensor_of(a.v[5], "do"), 2, "do");
+  if (!a.given(6)) raise(PyExc_TypeError, "the states that the forward pass kept (train=True) are wanted");
+  const float* ck = (const float*)c.here.optional(a, 6, at::kFloat, c.chunks() * c.state(), "ckpt");
+  const float* dST = (const float*)c.here.optional(a, 7, at::kFloat, c.state(), "dST");
+  const int32_t* len = (const int32_t*)c.here.optional(a, 8, at::kInt, c.B, "lengths");
+  const float scale = a.given(9) ? (float)a.real(9, 1.0) : (float)(1.0 / std::sqrt((double)c.Dk)), eps = (float)a.real(10, 1e-6);
+  at::Tensor out[6];
+  OnStream on(a.v[13]);
+  if (a.given(11)) outputs_of(a.v[11], 6, out);
+  ard_steps grads[5];
+  for (int i = 0; i < 5; ++i) {
+    const int heads = i < 2 ? c.Hk : c.H;
+    if (!out[i].defined()) out[i] = i < 3 ? output({c.T, c.B, heads, i < 2 ? c.Dk : c.Dv}, c.type, c.here.dev) : output({c.T, c.B, heads}, c.type, c.here.dev);
+    grads[i] = c.written(out[i], i, "out");
+  }
+  if (!out[5].defined()) out[5] = output({c.B, c.H, c.Dk, c.Dv}, at::kFloat, c.here.dev);
+  float* dS0 = (float*)c.here.contiguous(out[5], at::kFloat, c.state(), "out").data_ptr();
+  c.here.workspace(a, 12);
+  SeldomWorkspace ws(a, 12, c.here.dev, [&] { return lib().ard_gdr_workspace_bytes(c.dt, c.T, c.B, c.Hk, c.H, c.Dk, c.Dv, 1); });
+  const ard_steps *in = c.in, *po = &d_o, *pg = grads;
+  void* st = stream_of(a.v[13]);
+  enqueue(lib().ard_gdr_bwd, c.dt, c.T, c.B, c.Hk, c.H, c.Dk, c.Dv, in, scale, eps, len, ck, po, dST, pg, dS0, ws.p, ws.bytes, st);
+  return tensors_or_none(out, 6);
+}
+
 // A list (or tuple) of tensors, one for each parameter; None: no such list.
 struct TensorList {
   PyObject* f = nullptr;
@@ -1365,6 +1636,12 @@ CALL(layer_norm_fwd, 7, 1, "X", "gamma", "beta", "eps", "D", "out", "stream")
 CALL(layer_norm_bwd, 9, 5, "dY", "X", "gamma", "mean", "rstd", "D", "out", "ws", "stream")
 CALL(glr_fwd, 10, 2, "f", "v", "o", "c0", "lengths", "train", "H", "out", "ws", "stream")
 CALL(glr_bwd, 11, 5, "f", "v", "o", "dh", "ckpt", "dcT", "lengths", "H", "out", "ws", "stream")
+CALL(gdr_fwd, 13, 5, "q", "k", "v", "f", "b", "S0", "lengths", "scale", "eps", "train", "out", "ws", "stream")
+CALL(gdr_bwd, 14, 7, "q", "k", "v", "f", "b", "do", "ckpt", "dST", "lengths", "scale", "eps", "out", "ws", "stream")
+CALL(embed_fwd, 6, 2, "ids", "E", "scale", "dtype", "out", "stream")
+CALL(embed_bwd, 9, 3, "ids", "dY", "V", "scale", "beta", "dtype", "out", "ws", "stream")
+CALL(distill_fwd, 10, 3, "Z", "ids", "t", "labels", "temperature", "alpha", "dloss", "grad", "out", "stream")
+CALL(distill_bwd, 10, 4, "Z", "ids", "t", "stats", "dloss", "labels", "temperature", "alpha", "out", "stream")
 CALL(adamw_step, 15, 4, "params", "grads", "m", "v", "m_scale", "v_scale", "copies", "lr", "beta1", "beta2", "eps", "weight_decay", "step", "grad_scale", "stream")
 CALL(adamw_values, 6, 4, "m", "v", "m_scale", "v_scale", "out", "stream")
 
@@ -1435,6 +1712,24 @@ PyMethodDef methods[] = {
                    "H: kept units of compact tensors [T, B, pad8(H)]; lengths: int32 [B], steps of each sequence."),
     ENTRY(glr_bwd, "glr_bwd($module, f, v, o, dh, ckpt, dcT=None, lengths=None, H=None, out=None, ws=None, stream=None)\n--\n\n"
                    "Gradients (df, dv, do, dc0) of glr_fwd (do: None without o); out: the first three or all four, to reuse (dc0 may be dcT)."),
+    ENTRY(gdr_fwd, "gdr_fwd($module, q, k, v, f, b, S0=None, lengths=None, scale=None, eps=1e-06, train=True, out=None, ws=None, stream=None)\n--\n\n"
+                   "Gated delta rule S = s(f) S + s(b) kh (v - s(f) S^T kh)^T, o = scale S^T qh with kh, qh the keys and queries divided by their lengths:\n"
+                   "q, k[T, B, Hk, Dk], v[T, B, H, Dv], f, b[T, B, H] (any strides of T and B) -> (o[T, B, H, Dv], ST[B, H, Dk, Dv] fp32, ckpt: the\n"
+                   "states the backward pass needs, None with train=False); out: reuse such a triple (ST may be S0).  scale: 1 / sqrt(Dk) where None.\n"
+                   "lengths: int32 [B], steps of each sequence."),
+    ENTRY(gdr_bwd, "gdr_bwd($module, q, k, v, f, b, do, ckpt, dST=None, lengths=None, scale=None, eps=1e-06, out=None, ws=None, stream=None)\n--\n\n"
+                   "Gradients (dq, dk, dv, df, db, dS0) of gdr_fwd; out: reuse such a tuple (None: a new one; dS0 may be dST)."),
+    ENTRY(embed_fwd, "embed_fwd($module, ids, E, scale=1.0, dtype=None, out=None, stream=None)\n--\n\n"
+                     "Rows scale * E[ids] of the table E[V, D], zeros where an id is outside it: ids int32 of any shape -> [*ids.shape, D] in dtype (E's\n"
+                     "where None; an fp32 table gives either)."),
+    ENTRY(embed_bwd, "embed_bwd($module, ids, dY, V, scale=1.0, beta=0.0, dtype=None, out=None, ws=None, stream=None)\n--\n\n"
+                     "Gradient beta * out + scale * (sums of dY's rows by token) of a table of V rows, in a fixed order; beta 0 or 1, dtype fp32 where None."),
+    ENTRY(distill_fwd, "distill_fwd($module, Z, ids, t, labels=None, temperature=1.0, alpha=1.0, dloss=None, grad=None, out=None, stream=None)\n--\n\n"
+                       "alpha T^2 KL(teacher's top logits t[R, K] of the elements ids | logits Z[R, V], both at temperature T) + (1 - alpha) cross entropy of\n"
+                       "the labels (int32 [R], outside Z: none): (loss[R], stats for distill_bwd, dZ).  dZ is made in the same pass where dloss[R], grad or\n"
+                       "room for it is given (else None), for dloss = 1 without one; out: reuse such a triple (dZ may be Z).  ids = t = None: labels alone."),
+    ENTRY(distill_bwd, "distill_bwd($module, Z, ids, t, stats, dloss=None, labels=None, temperature=1.0, alpha=1.0, out=None, stream=None)\n--\n\n"
+                       "Gradient dZ of distill_fwd's loss, weighted by dloss[R] (1 where None); out may be Z."),
     ENTRY(adamw_step, "adamw_step($module, params, grads, m, v, m_scale=None, v_scale=None, copies=None, lr=0.001, beta1=0.9, beta2=0.999, eps=1e-08, "
                       "weight_decay=0.01, step=1, grad_scale=None, stream=None)\n--\n\n"
                       "One AdamW step, in place, over lists of tensors: params fp32; grads fp32 or bf16; m, v fp32, or int8 and uint8 codes with\n"
