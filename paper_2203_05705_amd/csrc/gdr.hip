@@ -244,198 +244,214 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void g
 }
 
 // ---- a wavefront's columns ----------------------------------------------------------
-template <int NT> struct Columns {
-  int unit, n, h, hk, first;  // first: the lane's first column; NT = 2: the next one is its other
-  bool on;
+struct Columns {
+  int unit, n, h, hk, first;  // first: the lane's column
+  // workgroups of four wavefronts, each of one head's columns; `slices`: wavefronts' worth of columns of a head (a wavefront behind the last one
+  // has columns outside, which are 0 and stay unwritten, and helps to load)
+  __device__ __forceinline__ Columns(const GdrArgs& a, int slices) {
+    const int groups = (slices + 3) / 4;
+    unit = blockIdx.x / groups;
+    set(a, (blockIdx.x - unit * groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  }
+  // wavefronts counted through the heads
   __device__ __forceinline__ Columns(const GdrArgs& a, int index, int slices) {
-    const int g16 = threadIdx.x & 15;
-    unit = index / slices, first = (index - unit * slices) * 16 * NT + g16 * NT;
+    unit = index / slices;
+    set(a, index - unit * slices);
+  }
+  __device__ __forceinline__ void set(const GdrArgs& a, int slice) {
+    first = slice * 16 + (threadIdx.x & 15);
     n = unit / a.H, h = unit - n * a.H, hk = h / a.group;
   }
 };
-// rows 16 rt + 4 g + r of a matrix of fp32 rows `ld` apart, the lane's columns; rows and columns outside are 0
-template <int NT, int TILES> __device__ __forceinline__ void load_state(const float* p, int rows, int ld, int first, f32x4 (&S)[TILES][NT]) {
-  const int g = (threadIdx.x & 63) >> 4;
+// Rows of a matrix (steps of a chunk, or of a state) as the lanes hold them: rows 16 rt + 4 g + r at the lane's column.  Of `rows` x `wide` elements; what
+// lies outside is 0 / is not written.  NEAR: as a buffer whose end the hardware checks, so that no access needs a branch or a 64-bit address (rows that do not
+// overlap, all within 2 GB).
+template <typename T, bool NEAR> struct Window {
+  T* p;
+  int64_t step;
+  int rows;
+  bool on;
+  uint32_t at, row;  // bytes: of the lane's first element, and from row to row
+  __amdgpu_buffer_rsrc_t buffer;
+  __device__ __forceinline__ Window(const void* base, int64_t step_, int rows_, int wide, int first) : step(step_), rows(rows_) {
+    const int g = (threadIdx.x & 63) >> 4;
+    on = first < wide;
+    if constexpr (NEAR) {
+      row = (uint32_t)step * sizeof(T);
+      at = on ? 4 * g * row + first * (uint32_t)sizeof(T) : 0x80000000u;
+      buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, rows > 0 ? rows * (int)row : 0, 0x00020000);
+    } else {
+      p = (T*)const_cast<void*>(base) + 4 * g * step + first;
+      rows -= 4 * g;
+    }
+  }
+  __device__ __forceinline__ float load(int i) const {  // i = 16 rt + r
+    if constexpr (!NEAR) return on && i < rows ? ElemTraits<T>::to_f32(p[i * step]) : 0.0f;
+    else if constexpr (sizeof(T) == 2) return bf16_bits_to_f32(__builtin_amdgcn_raw_buffer_load_b16(buffer, at + i * row, 0, 0));
+    else return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer, at + i * row, 0, 0));
+  }
+  __device__ __forceinline__ void store(int i, float x) const {
+    if constexpr (!NEAR) {
+      if (on && i < rows) p[i * step] = ElemTraits<T>::from_f32(x);
+    } else if constexpr (sizeof(T) == 2) {
+      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)bf16_pair(x, 0.0f), buffer, at + i * row, 0, 0);
+    } else {
+      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), buffer, at + i * row, 0, 0);
+    }
+  }
+};
+template <int TILES, typename W> __device__ __forceinline__ void load_tiles(const W& w, f32x4 (&S)[TILES]) {
 #pragma unroll
   for (int rt = 0; rt < TILES; ++rt)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int i = rt * 16 + 4 * g + r;
-      float x[NT] = {};
-      if (i < rows) load_some<NT>(p + (int64_t)i * ld + first, ld - first, x);
-#pragma unroll
-      for (int e = 0; e < NT; ++e) S[rt][e][r] = x[e];
-    }
+    for (int r = 0; r < 4; ++r) S[rt][r] = w.load(rt * 16 + r);
 }
-template <int NT, int TILES> __device__ __forceinline__ void store_state(float* p, int rows, int ld, int first, const f32x4 (&S)[TILES][NT]) {
-  const int g = (threadIdx.x & 63) >> 4;
+template <int TILES, typename W> __device__ __forceinline__ void store_tiles(const W& w, const f32x4 (&S)[TILES]) {
 #pragma unroll
   for (int rt = 0; rt < TILES; ++rt)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int i = rt * 16 + 4 * g + r;
-      float x[NT];
-#pragma unroll
-      for (int e = 0; e < NT; ++e) x[e] = S[rt][e][r];
-      if (i < rows && first < ld) store_some<NT>(p + (int64_t)i * ld + first, ld - first, x);
-    }
+    for (int r = 0; r < 4; ++r) w.store(rt * 16 + r, S[rt][r]);
 }
-// the same of a chunk's steps in a tensor of the caller's, of which `live` count (the others are 0 / are written as 0 up to `steps`)
-template <int NT, typename T> __device__ __forceinline__ void load_chunk(const T* p, int64_t step, int live, int wide, int first, f32x4 (&S)[4][NT]) {
+// the same of steps of which only `live` count: the others are stored as 0
+template <typename W> __device__ __forceinline__ void store_live(const W& w, int live, const f32x4 (&S)[4]) {
   const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
   for (int rt = 0; rt < 4; ++rt)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int i = rt * 16 + 4 * g + r;
-      float x[NT] = {};
-      if (i < live) load_some<NT>(p + i * step + first, wide - first, x);
-#pragma unroll
-      for (int e = 0; e < NT; ++e) S[rt][e][r] = x[e];
-    }
+    for (int r = 0; r < 4; ++r) w.store(rt * 16 + r, rt * 16 + 4 * g + r < live ? S[rt][r] : 0.0f);
 }
-template <int NT, typename T> __device__ __forceinline__ void store_chunk(T* p, int64_t step, int live, int steps, int wide, int first, const f32x4 (&S)[4][NT]) {
-  const int g = (threadIdx.x & 63) >> 4;
-#pragma unroll
-  for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int i = rt * 16 + 4 * g + r;
-      float x[NT];
-#pragma unroll
-      for (int e = 0; e < NT; ++e) x[e] = i < live ? S[rt][e][r] : 0.0f;
-      if (i < steps && first < wide) store_some<NT>(p + i * step + first, wide - first, x);
-    }
-}
+typedef Window<float, true> StateWindow;
 __device__ __forceinline__ f32x4 row_weights(const float* w, int rt) { return *reinterpret_cast<const f32x4*>(w + rt * 16 + 4 * ((threadIdx.x & 63) >> 4)); }
 
-// U of a chunk: the state's columns as parts, Sp; v: the values; leaves U in x
-template <int IN, int DK, int NT>
-__device__ __forceinline__ void written_rows(const GdrArgs& a, int64_t ku, int64_t hu, const Parts<3> (&Sp)[DK / 32][NT], const f32x4 (&v)[4][NT], f32x4 (&u)[4][NT]) {
+// Weighed rows for the products with M: x = w (v - ka (K S)); k: operands of K, st: w, ka, qa, ke of the chunk
+template <int IN, int DK>
+__device__ __forceinline__ void unwritten(const u32x4* kf, const float* w, const float* ka, const Parts<3> (&Sp)[DK / 32], const f32x4 (&v)[4], f32x4 (&x)[4]) {
   constexpr int KB = DK / 32;
-  const u32x4 *kf = a.kf + ku * 4 * KB * IN * 64, *mf = a.mf + hu * 6 * 3 * 64;
-  const Steps64& st = a.steps[hu];
-  f32x4 x[4][NT];
 #pragma unroll
   for (int rt = 0; rt < 4; ++rt) {
-    f32x4 y[NT] = {};
+    f32x4 y = {};
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       const Parts<IN> k = load_parts<IN>(kf, rt * KB + kb);
-#pragma unroll
-      for (int e = 0; e < NT; ++e) mul_add(k, Sp[kb][e], y[e]);
+      mul_add(k, Sp[kb], y);
     }
-    const f32x4 ka = row_weights(st.ka, rt), wr = row_weights(st.w, rt);
-#pragma unroll
-    for (int e = 0; e < NT; ++e) x[rt][e] = wr * (v[rt][e] - ka * y[e]);
-  }
-  Parts<3> xp[2][NT];
-#pragma unroll
-  for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-    for (int e = 0; e < NT; ++e) xp[kb][e] = parts_of<3>(x[2 * kb][e], x[2 * kb + 1][e]);
-#pragma unroll
-  for (int rt = 0; rt < 4; ++rt) {
-#pragma unroll
-    for (int e = 0; e < NT; ++e) u[rt][e] = f32x4{};
-#pragma unroll
-    for (int kb = 0; kb <= rt / 2; ++kb) {
-      const Parts<3> m = load_parts<3>(mf, lower_frag(rt, kb));
-#pragma unroll
-      for (int e = 0; e < NT; ++e) mul_add(m, xp[kb][e], u[rt][e]);
-    }
+    const f32x4 kr = row_weights(ka, rt), wr = row_weights(w, rt);
+    x[rt] = wr * (v[rt] - kr * y);
   }
 }
+// y += L x of a lower triangular L (64 x 64, N parts), or of its transpose
+template <bool UPPER, int N, int M> __device__ __forceinline__ void triangle(const u32x4* f, const Parts<M> (&x)[2], f32x4 (&y)[4]) {
+#pragma unroll
+  for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+    for (int kb = UPPER ? rt / 2 : 0; kb <= (UPPER ? 1 : rt / 2); ++kb) {
+      const Parts<N> m = load_parts<N>(f, UPPER ? upper_frag(rt, kb) : lower_frag(rt, kb));
+      mul_add(m, x[kb], y[rt]);
+    }
+}
+template <int N, int TILES> __device__ __forceinline__ void column_parts(const f32x4 (&x)[TILES], Parts<N> (&p)[TILES / 2]) {
+#pragma unroll
+  for (int kb = 0; kb < TILES / 2; ++kb)
+  p[kb] = parts_of<N>(x[2 * kb], x[2 * kb + 1]);
+}
 // S += (operands of DK rows x 64 steps) x (y, weighed by rows)
-template <int IN, int DK, int NT> __device__ __forceinline__ void add_outer(const u32x4* f, const float* weights, float sign, const f32x4 (&y)[4][NT], f32x4 (&S)[DK / 16][NT]) {
-  Parts<3> p[2][NT];
+template <int IN, int DK> __device__ __forceinline__ void add_outer(const u32x4* f, const float* weights, float sign, const f32x4 (&y)[4], f32x4 (&S)[DK / 16]) {
+  Parts<3> p[2];
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) {
     const f32x4 lo = sign * row_weights(weights, 2 * kb), hi = sign * row_weights(weights, 2 * kb + 1);
-#pragma unroll
-    for (int e = 0; e < NT; ++e) p[kb][e] = parts_of<3>(lo * y[2 * kb][e], hi * y[2 * kb + 1][e]);
+    p[kb] = parts_of<3>(lo * y[2 * kb], hi * y[2 * kb + 1]);
   }
 #pragma unroll
   for (int rt = 0; rt < DK / 16; ++rt)
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       const Parts<IN> k = load_parts<IN>(f, rt * 2 + kb);
-#pragma unroll
-      for (int e = 0; e < NT; ++e) mul_add(k, p[kb][e], S[rt][e]);
+      mul_add(k, p[kb], S[rt]);
     }
 }
 
-template <typename T, int DK, int NT>
-__global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt, int slices, int waves) {
-  constexpr int IN = GdrType<T>::IN, OUT = GdrType<T>::OUT, KB = DK / 32;
-  const int index = __builtin_amdgcn_readfirstlane(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6));
-  if (index >= waves) return;
-  const Columns<NT> at(a, index, slices);
+// Four wavefronts with columns of one head walk its chunks.  They share the operands in LDS, in two groups: what the first half of a
+// chunk reads is loaded for the next chunk while the second half is worked on, and the other way about.  Operands that LDS does not hold
+// (fp32, wide heads) are read from the caches.
+template <typename T, int DK, bool NEAR>
+__global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt, int slices) {
+  constexpr int IN = GdrType<T>::IN, OUT = GdrType<T>::OUT, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3, PF = 6 * OUT;
+  constexpr bool STAGED = 2 * KF + KTF + MF + PF <= 150;
+  __shared__ u32x4 lds[STAGED ? (2 * KF + KTF + MF + PF) * 64 : 1];
+  __shared__ f32x4 weights[2][64];  // w, ka, qa, ke of a chunk
+  const Columns at(a, slices);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t matrix = (int64_t)a.Dk * a.Dv, plane = (int64_t)a.B * a.H * matrix;
-  f32x4 S[DK / 16][NT] = {};
-  if (S0) load_state<NT, DK / 16>(S0 + at.unit * matrix, a.Dk, a.Dv, at.first, S);
-  const int all = live_steps(a, at.n);
-  for (int chunk = 0; chunk < a.chunks; ++chunk) {
-    if (ckpt) store_state<NT, DK / 16>(ckpt + chunk * plane + at.unit * matrix, a.Dk, a.Dv, at.first, S);
-    const int t0 = chunk * kChunk, steps = imin(a.T - t0, kChunk), live = imin(all - t0, steps);
-    T* out = (T*)o.p + t0 * o.t + at.n * o.b + at.h * a.Dv;
-    f32x4 y[4][NT] = {}, u[4][NT];
-    if (live <= 0) {
-      store_chunk<NT>(out, o.t, 0, steps, a.Dv, at.first, y);
-      continue;
+  f32x4 S[DK / 16] = {}, v[4] = {};
+  if (S0) load_tiles(StateWindow(S0 + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
+  const int all = live_steps(a, at.n), chunks = (all + kChunk - 1) / kChunk;
+  const auto ku = [&](int chunk) { return ((int64_t)chunk * a.B + at.n) * a.Hk + at.hk; };
+  const auto hu = [&](int chunk) { return ((int64_t)chunk * a.B + at.n) * a.H + at.h; };
+  const auto first_half = [&](int chunk) {  // loads of what it reads
+    if (STAGED) stage(a.kf + ku(chunk) * KF * 64, lds, KF, wave), stage(a.qf + ku(chunk) * KF * 64, lds + KF * 64, KF, wave);
+    stage((const u32x4*)a.steps[hu(chunk)].w, (u32x4*)weights[chunk & 1], 1, wave);
+    load_tiles(Window<T, NEAR>((const T*)a.v.p + (int64_t)chunk * kChunk * a.v.t + at.n * a.v.b + at.h * a.Dv, a.v.t, imin(all - chunk * kChunk, kChunk), a.Dv, at.first), v);
+  };
+  const auto second_half = [&](int chunk) {
+    if (STAGED) {
+      stage(a.ktf + ku(chunk) * KTF * 64, lds + 2 * KF * 64, KTF, wave);
+      stage(a.mf + hu(chunk) * MF * 64, lds + (2 * KF + KTF) * 64, MF, wave), stage(a.pf + hu(chunk) * PF * 64, lds + (2 * KF + KTF + MF) * 64, PF, wave);
     }
-    const int64_t ku = ((int64_t)chunk * a.B + at.n) * a.Hk + at.hk, hu = ((int64_t)chunk * a.B + at.n) * a.H + at.h;
-    load_chunk<NT>((const T*)a.v.p + t0 * a.v.t + at.n * a.v.b + at.h * a.Dv, a.v.t, live, a.Dv, at.first, u);
-    const Steps64& st = a.steps[hu];
-    Parts<3> Sp[KB][NT];
+  };
+  if (chunks) {
+    first_half(0);
+    all_landed();
+    second_half(0);
+  }
+  for (int chunk = 0; chunk < chunks; ++chunk) {
+    const int t0 = chunk * kChunk, steps = imin(a.T - t0, kChunk), live = imin(all - t0, steps);
+    const float *w = (const float*)weights[chunk & 1], *ka = w + kChunk, *qa = w + 2 * kChunk, *ke = w + 3 * kChunk;
+    const float whole = a.steps[hu(chunk)].whole;
+    if (ckpt) store_tiles(StateWindow(ckpt + chunk * plane + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
+    f32x4 x[4], y[4] = {}, u[4] = {};
+    {
+      Parts<3> Sp[KB];
+      column_parts<3>(S, Sp);
+      const u32x4* qf = STAGED ? lds + KF * 64 : a.qf + ku(chunk) * KF * 64;
+      unwritten<IN, DK>(STAGED ? lds : a.kf + ku(chunk) * KF * 64, w, ka, Sp, v, x);
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+      for (int rt = 0; rt < 4; ++rt) {
 #pragma unroll
-      for (int e = 0; e < NT; ++e) Sp[kb][e] = parts_of<3>(S[2 * kb][e], S[2 * kb + 1][e]);
-    const u32x4* qf = a.qf + ku * 4 * KB * IN * 64;
-#pragma unroll
-    for (int rt = 0; rt < 4; ++rt) {
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const Parts<IN> q = load_parts<IN>(qf, rt * KB + kb);
-#pragma unroll
-        for (int e = 0; e < NT; ++e) mul_add(q, leading<OUT>(Sp[kb][e]), y[rt][e]);
+        for (int kb = 0; kb < KB; ++kb) {
+          const Parts<IN> q = load_parts<IN>(qf, rt * KB + kb);
+          mul_add(q, leading<OUT>(Sp[kb]), y[rt]);
+        }
+        const f32x4 qr = row_weights(qa, rt);
+        y[rt] *= qr;
       }
-      const f32x4 qa = row_weights(st.qa, rt);
-#pragma unroll
-      for (int e = 0; e < NT; ++e) y[rt][e] *= qa;
+    }
+    all_landed();
+    if (chunk + 1 < chunks) first_half(chunk + 1);
+    {
+      Parts<3> xp[2];
+      column_parts<3>(x, xp);
+      triangle<false, 3>(STAGED ? lds + (2 * KF + KTF) * 64 : a.mf + hu(chunk) * MF * 64, xp, u);
     }
     {
-      f32x4 v[4][NT];
-#pragma unroll
-      for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-        for (int e = 0; e < NT; ++e) v[rt][e] = u[rt][e];
-      written_rows<IN, DK, NT>(a, ku, hu, Sp, v, u);
+      Parts<OUT> up[2];
+      column_parts<OUT>(u, up);
+      triangle<false, OUT>(STAGED ? lds + (2 * KF + KTF + MF) * 64 : a.pf + hu(chunk) * PF * 64, up, y);
     }
-    const u32x4* pf = a.pf + hu * 6 * OUT * 64;
-    Parts<OUT> up[2][NT];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int e = 0; e < NT; ++e) up[kb][e] = parts_of<OUT>(u[2 * kb][e], u[2 * kb + 1][e]);
-#pragma unroll
-    for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-      for (int kb = 0; kb <= rt / 2; ++kb) {
-        const Parts<OUT> p = load_parts<OUT>(pf, lower_frag(rt, kb));
-#pragma unroll
-        for (int e = 0; e < NT; ++e) mul_add(p, up[kb][e], y[rt][e]);
-      }
-    store_chunk<NT>(out, o.t, live, steps, a.Dv, at.first, y);
-    const float whole = st.whole;
+    store_live(Window<T, NEAR>((T*)o.p + t0 * o.t + at.n * o.b + at.h * a.Dv, o.t, steps, a.Dv, at.first), live, y);
 #pragma unroll
     for (int rt = 0; rt < DK / 16; ++rt)
-#pragma unroll
-      for (int e = 0; e < NT; ++e) S[rt][e] *= whole;
-    add_outer<IN, DK, NT>(a.ktf + ku * (DK / 8) * IN * 64, st.ke, 1.0f, u, S);
+      S[rt] *= whole;
+    add_outer<IN, DK>(STAGED ? lds + 2 * KF * 64 : a.ktf + ku(chunk) * KTF * 64, ke, 1.0f, u, S);
+    all_landed();
+    if (chunk + 1 < chunks) second_half(chunk + 1);
   }
-  if (ST) store_state<NT, DK / 16>(ST + at.unit * matrix, a.Dk, a.Dv, at.first, S);
+  for (int chunk = chunks; chunk < a.chunks; ++chunk) {  // behind the sequence's end
+    const f32x4 none[4] = {};
+    if (ckpt) store_tiles(StateWindow(ckpt + chunk * plane + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
+    store_tiles(Window<T, NEAR>((T*)o.p + (int64_t)chunk * kChunk * o.t + at.n * o.b + at.h * a.Dv, o.t, imin(a.T - chunk * kChunk, kChunk), a.Dv, at.first), none);
+  }
+  if (ST) store_tiles(StateWindow(ST + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
 }
 
 // ---- backward -----------------------------------------------------------------------
@@ -450,119 +466,116 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
 // all other gradients, every chunk for itself.
 
 // U of every chunk
-template <typename T, int DK, int NT> __global__ __launch_bounds__(256) void gdr_rows_kernel(GdrArgs a, const float* ckpt, int slices, int waves) {
+template <typename T, int DK, bool NEAR> __global__ __launch_bounds__(256) void gdr_rows_kernel(GdrArgs a, const float* ckpt, int slices, int waves) {
   constexpr int IN = GdrType<T>::IN, KB = DK / 32;
   const int index = __builtin_amdgcn_readfirstlane(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6));
   const int chunk = index / waves;
   if (chunk >= a.chunks) return;
-  const Columns<NT> at(a, index - chunk * waves, slices);
+  const Columns at(a, index - chunk * waves, slices);
   const int t0 = chunk * kChunk, live = imin(live_steps(a, at.n) - t0, kChunk);
   if (live <= 0) return;
   const int64_t ku = ((int64_t)chunk * a.B + at.n) * a.Hk + at.hk, hu = ((int64_t)chunk * a.B + at.n) * a.H + at.h;
-  f32x4 S[DK / 16][NT], v[4][NT], u[4][NT];
-  load_state<NT, DK / 16>(ckpt + hu * a.Dk * a.Dv, a.Dk, a.Dv, at.first, S);
-  load_chunk<NT>((const T*)a.v.p + t0 * a.v.t + at.n * a.v.b + at.h * a.Dv, a.v.t, live, a.Dv, at.first, v);
-  Parts<3> Sp[KB][NT];
-#pragma unroll
-  for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-    for (int e = 0; e < NT; ++e) Sp[kb][e] = parts_of<3>(S[2 * kb][e], S[2 * kb + 1][e]);
-  written_rows<IN, DK, NT>(a, ku, hu, Sp, v, u);
-  store_chunk<NT>(a.u + hu * kChunk * a.dvp, a.dvp, kChunk, kChunk, a.dvp, at.first, u);
+  f32x4 S[DK / 16], v[4], x[4], u[4] = {};
+  load_tiles(StateWindow(ckpt + hu * a.Dk * a.Dv, a.Dv, a.Dk, a.Dv, at.first), S);
+  load_tiles(Window<T, NEAR>((const T*)a.v.p + t0 * a.v.t + at.n * a.v.b + at.h * a.Dv, a.v.t, live, a.Dv, at.first), v);
+  const Steps64& st = a.steps[hu];
+  {
+    Parts<3> Sp[KB];
+    column_parts<3>(S, Sp);
+    unwritten<IN, DK>(a.kf + ku * 4 * KB * IN * 64, st.w, st.ka, Sp, v, x);
+  }
+  Parts<3> xp[2];
+  column_parts<3>(x, xp);
+  triangle<false, 3>(a.mf + hu * 6 * 3 * 64, xp, u);
+  store_tiles(StateWindow(a.u + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp, at.first), u);
 }
 
-template <typename T, int DK, int NT>
-__global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o, const float* dST, ard_steps dv, float* dS0, int slices, int waves) {
-  constexpr int IN = GdrType<T>::IN, KB = DK / 32;
-  const int index = __builtin_amdgcn_readfirstlane(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6));
-  if (index >= waves) return;
-  const Columns<NT> at(a, index, slices);
+template <typename T, int DK, bool NEAR>
+__global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o, const float* dST, ard_steps dv, float* dS0, int slices) {
+  constexpr int IN = GdrType<T>::IN, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3;
+  constexpr bool STAGED = KF + 2 * KTF + 2 * MF <= 150;
+  __shared__ u32x4 lds[STAGED ? (KF + 2 * KTF + 2 * MF) * 64 : 1];
+  __shared__ f32x4 weights[2][64];  // w, ka, qa, ke of a chunk
+  const Columns at(a, slices);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t matrix = (int64_t)a.Dk * a.Dv;
-  f32x4 S[DK / 16][NT] = {};
-  if (dST) load_state<NT, DK / 16>(dST + at.unit * matrix, a.Dk, a.Dv, at.first, S);
-  const int all = live_steps(a, at.n);
-  for (int chunk = a.chunks - 1; chunk >= 0; --chunk) {
-    const int t0 = chunk * kChunk, steps = imin(a.T - t0, kChunk), live = imin(all - t0, steps);
-    const int64_t ku = ((int64_t)chunk * a.B + at.n) * a.Hk + at.hk, hu = ((int64_t)chunk * a.B + at.n) * a.H + at.h;
-    T* out = (T*)dv.p + t0 * dv.t + at.n * dv.b + at.h * a.Dv;
-    f32x4 y[4][NT] = {}, x[4][NT];
-    if (live <= 0) {
-      store_chunk<NT>(out, dv.t, 0, steps, a.Dv, at.first, y);
-      continue;
+  f32x4 S[DK / 16] = {}, x[4] = {};
+  if (dST) load_tiles(StateWindow(dST + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
+  const int all = live_steps(a, at.n), chunks = (all + kChunk - 1) / kChunk;
+  const auto ku = [&](int chunk) { return ((int64_t)chunk * a.B + at.n) * a.Hk + at.hk; };
+  const auto hu = [&](int chunk) { return ((int64_t)chunk * a.B + at.n) * a.H + at.h; };
+  const auto first_half = [&](int chunk) {
+    if (STAGED) stage(a.kf + ku(chunk) * KF * 64, lds, KF, wave), stage(a.ptf + hu(chunk) * MF * 64, lds + KF * 64, MF, wave);
+    stage((const u32x4*)a.steps[hu(chunk)].w, (u32x4*)weights[chunk & 1], 1, wave);
+    load_tiles(Window<T, NEAR>((const T*)d_o.p + (int64_t)chunk * kChunk * d_o.t + at.n * d_o.b + at.h * a.Dv, d_o.t, imin(all - chunk * kChunk, kChunk), a.Dv, at.first), x);
+  };
+  const auto second_half = [&](int chunk) {
+    if (STAGED) {
+      stage(a.mtf + hu(chunk) * MF * 64, lds + (KF + MF) * 64, MF, wave);
+      stage(a.qtf + ku(chunk) * KTF * 64, lds + (KF + 2 * MF) * 64, KTF, wave), stage(a.ktf + ku(chunk) * KTF * 64, lds + (KF + 2 * MF + KTF) * 64, KTF, wave);
     }
-    load_chunk<NT>((const T*)d_o.p + t0 * d_o.t + at.n * d_o.b + at.h * a.Dv, d_o.t, live, a.Dv, at.first, x);
-    store_state<NT, DK / 16>(a.ds + hu * DK * a.dvp, DK, a.dvp, at.first, S);
-    const Steps64& st = a.steps[hu];
-    const u32x4 *kf = a.kf + ku * 4 * KB * IN * 64, *ptf = a.ptf + hu * 6 * 3 * 64, *mtf = a.mtf + hu * 6 * 3 * 64;
+  };
+  for (int chunk = chunks; chunk < a.chunks; ++chunk) {  // behind the sequence's end
+    const f32x4 none[4] = {};
+    store_tiles(Window<T, NEAR>((T*)dv.p + (int64_t)chunk * kChunk * dv.t + at.n * dv.b + at.h * a.Dv, dv.t, imin(a.T - chunk * kChunk, kChunk), a.Dv, at.first), none);
+  }
+  if (chunks) {
+    first_half(chunks - 1);
+    all_landed();
+    second_half(chunks - 1);
+  }
+  for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+    const int t0 = chunk * kChunk, steps = imin(a.T - t0, kChunk), live = imin(all - t0, steps);
+    const float *w = (const float*)weights[chunk & 1], *ka = w + kChunk, *qa = w + 2 * kChunk, *ke = w + 3 * kChunk;
+    const float whole = a.steps[hu(chunk)].whole;
+    store_tiles(StateWindow(a.ds + hu(chunk) * DK * a.dvp, a.dvp, DK, a.dvp, at.first), S);
+    f32x4 y[4] = {}, dx[4] = {}, od[4];
     {
-      Parts<3> Sp[KB][NT];
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int e = 0; e < NT; ++e) Sp[kb][e] = parts_of<3>(S[2 * kb][e], S[2 * kb + 1][e]);
+      Parts<3> Sp[KB];
+      column_parts<3>(S, Sp);
+      const u32x4* kf = STAGED ? lds : a.kf + ku(chunk) * KF * 64;
 #pragma unroll
       for (int rt = 0; rt < 4; ++rt) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
           const Parts<IN> k = load_parts<IN>(kf, rt * KB + kb);
-#pragma unroll
-          for (int e = 0; e < NT; ++e) mul_add(k, Sp[kb][e], y[rt][e]);
+          mul_add(k, Sp[kb], y[rt]);
         }
-        const f32x4 ke = row_weights(st.ke, rt);
-#pragma unroll
-        for (int e = 0; e < NT; ++e) y[rt][e] *= ke;
+        const f32x4 kr = row_weights(ke, rt);
+        y[rt] *= kr;
       }
     }
     {
-      Parts<IN> p[2][NT];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int e = 0; e < NT; ++e) p[kb][e] = parts_of<IN>(x[2 * kb][e], x[2 * kb + 1][e]);
-#pragma unroll
-      for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-        for (int kb = rt / 2; kb < 2; ++kb) {
-          const Parts<3> m = load_parts<3>(ptf, upper_frag(rt, kb));
-#pragma unroll
-          for (int e = 0; e < NT; ++e) mul_add(m, p[kb][e], y[rt][e]);
-        }
+      Parts<IN> p[2];
+      column_parts<IN>(x, p);
+      triangle<true, 3>(STAGED ? lds + KF * 64 : a.ptf + hu(chunk) * MF * 64, p, y);
     }
-    const float whole = st.whole;
 #pragma unroll
-    for (int rt = 0; rt < DK / 16; ++rt)
-#pragma unroll
-      for (int e = 0; e < NT; ++e) S[rt][e] *= whole;
-    add_outer<IN, DK, NT>(a.qtf + ku * (DK / 8) * IN * 64, st.qa, 1.0f, x, S);
+    for (int rt = 0; rt < 4; ++rt)
+      od[rt] = x[rt];
+    all_landed();
+    if (chunk > 0) first_half(chunk - 1);
     {
-      Parts<3> p[2][NT];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int e = 0; e < NT; ++e) p[kb][e] = parts_of<3>(y[2 * kb][e], y[2 * kb + 1][e]);
-#pragma unroll
-      for (int rt = 0; rt < 4; ++rt) {
-#pragma unroll
-        for (int e = 0; e < NT; ++e) x[rt][e] = f32x4{};
-#pragma unroll
-        for (int kb = rt / 2; kb < 2; ++kb) {
-          const Parts<3> m = load_parts<3>(mtf, upper_frag(rt, kb));
-#pragma unroll
-          for (int e = 0; e < NT; ++e) mul_add(m, p[kb][e], x[rt][e]);
-        }
-      }
+      Parts<3> p[2];
+      column_parts<3>(y, p);
+      triangle<true, 3>(STAGED ? lds + (KF + MF) * 64 : a.mtf + hu(chunk) * MF * 64, p, dx);
     }
-    store_chunk<NT>(a.dx + hu * kChunk * a.dvp, a.dvp, kChunk, kChunk, a.dvp, at.first, x);
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt) {
-      const f32x4 wr = row_weights(st.w, rt);
-#pragma unroll
-      for (int e = 0; e < NT; ++e) x[rt][e] *= wr;
+      const f32x4 wr = row_weights(w, rt);
+      y[rt] = wr * dx[rt];
     }
-    store_chunk<NT>(out, dv.t, live, steps, a.Dv, at.first, x);
-    add_outer<IN, DK, NT>(a.ktf + ku * (DK / 8) * IN * 64, st.ka, -1.0f, x, S);
+    store_tiles(StateWindow(a.dx + hu(chunk) * kChunk * a.dvp, a.dvp, kChunk, a.dvp, at.first), dx);
+    store_live(Window<T, NEAR>((T*)dv.p + t0 * dv.t + at.n * dv.b + at.h * a.Dv, dv.t, steps, a.Dv, at.first), live, y);
+#pragma unroll
+    for (int rt = 0; rt < DK / 16; ++rt)
+      S[rt] *= whole;
+    add_outer<IN, DK>(STAGED ? lds + (KF + 2 * MF) * 64 : a.qtf + ku(chunk) * KTF * 64, qa, 1.0f, od, S);
+    add_outer<IN, DK>(STAGED ? lds + (KF + 2 * MF + KTF) * 64 : a.ktf + ku(chunk) * KTF * 64, ka, -1.0f, y, S);
+    all_landed();
+    if (chunk > 0) second_half(chunk - 1);
   }
-  if (dS0) store_state<NT, DK / 16>(dS0 + at.unit * matrix, a.Dk, a.Dv, at.first, S);
+  if (dS0) store_tiles(StateWindow(dS0 + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
 }
 
 // 8 neighbouring fp32 values of a workspace row as parts
@@ -769,7 +782,7 @@ __global__ __launch_bounds__(256) void gdr_grads_kernel(GdrArgs a, ard_steps d_o
 // ---- host ---------------------------------------------------------------------------
 struct GdrPlan {
   GdrArgs a;
-  int dk, nt, slices, waves;  // padded key size; columns of a wavefront / 16, their number in a head, and all of them
+  int dk, slices;  // padded key size; wavefronts' worth of 16 columns of a head
   size_t bytes;
 };
 // The workspace's parts, one behind the other; `base` may be NULL, when only the size is asked for.
@@ -778,9 +791,7 @@ static GdrPlan gdr_plan(int32_t dtype, int T, int B, int Hk, int H, int Dk, int 
   GdrArgs& a = p.a;
   a.T = T, a.B = B, a.Hk = Hk, a.H = H, a.Dk = Dk, a.Dv = Dv, a.group = H / Hk, a.chunks = ceil_div(T, kChunk);
   p.dk = Dk <= 64 ? 64 : 128;
-  p.nt = 1;
-  p.slices = ceil_div(Dv, 16 * p.nt);
-  p.waves = B * H * p.slices;
+  p.slices = ceil_div(Dv, 16);
   a.dvp = Dv <= 64 ? 64 : 128;
   const size_t in = dtype == ARD_F32 ? 3 : 1, out = dtype == ARD_F32 ? 3 : 2, ku = (size_t)a.chunks * B * Hk, hu = (size_t)a.chunks * B * H;
   size_t at = 0;
@@ -829,12 +840,19 @@ static int32_t gdr_numbers(float scale, float eps) {
   return ARD_OK;
 }
 
-template <class F> static int32_t gdr_instance(int32_t dtype, int dk, F&& with) {
-  using Wide = std::integral_constant<int, 128>;
-  using Narrow = std::integral_constant<int, 64>;
-  if (dtype == ARD_F32) return dk == 64 ? with(0.0f, Narrow{}) : with(0.0f, Wide{});
-  return dk == 64 ? with((uint16_t)0, Narrow{}) : with((uint16_t)0, Wide{});
+template <class F> static int32_t gdr_instance(int32_t dtype, int dk, bool near, F&& with) {
+  const auto sized = [&](auto t) {
+    using Wide = std::integral_constant<int, 128>;
+    using Narrow = std::integral_constant<int, 64>;
+    if (near) return dk == 64 ? with(t, Narrow{}, std::true_type{}) : with(t, Wide{}, std::true_type{});
+    return dk == 64 ? with(t, Narrow{}, std::false_type{}) : with(t, Wide{}, std::false_type{});
+  };
+  return dtype == ARD_F32 ? sized(0.0f) : sized((uint16_t)0);
 }
+// (a single step's stride says nothing)
+static ard_steps gdr_steps(const ard_steps& s, int T, int wide) { return T == 1 ? ard_steps{s.p, wide, s.b} : s; }
+// Window's NEAR: the steps of a chunk do not overlap and lie within 2 GB
+static bool gdr_near(const ard_steps& s, int wide) { return s.t >= wide && s.t < (int64_t)INT32_MAX / 4 / kChunk; }
 
 }  // namespace ard
 
@@ -858,19 +876,21 @@ extern "C" int32_t ard_gdr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
   GdrPlan p = gdr_plan(dtype, T, B, Hk, H, Dk, Dv, false, ws);
   if (!few && (!ws || ws_bytes < p.bytes || misaligned(ws, 16))) return fail(ARD_EWORKSPACE, "workspace too small: need %zu bytes, got %zu", p.bytes, ws ? ws_bytes : 0);
   GdrArgs& a = p.a;
-  a.q = in[0], a.k = in[1], a.v = in[2], a.f = in[3], a.b = in[4], a.scale = scale, a.eps = eps, a.len = d_lengths;
+  a.q = in[0], a.k = in[1], a.v = gdr_steps(in[2], T, H * Dv), a.f = in[3], a.b = in[4], a.scale = scale, a.eps = eps, a.len = d_lengths;
   hipStream_t st = (hipStream_t)stream;
-  return gdr_instance(dtype, p.dk, [&](auto t, auto dk) {
+  const ard_steps out = gdr_steps(*o, T, H * Dv);
+  return gdr_instance(dtype, p.dk, gdr_near(a.v, Dv) && gdr_near(out, Dv), [&](auto t, auto dk, auto near) {
     using E = decltype(t);
     constexpr int DK = decltype(dk)::value;
+    constexpr bool NEAR = decltype(near)::value;
     if (few) {
-      ARD_LAUNCH_NAMED("gdr_steps_kernel", (gdr_steps_kernel<E, DK>), dim3(B * H * ceil_div(Dv, 64)), dim3(64), 0, st, a, S0, *o, ST, ckpt);
+      ARD_LAUNCH_NAMED("gdr_steps_kernel", (gdr_steps_kernel<E, DK>), dim3(B * H * ceil_div(Dv, 64)), dim3(64), 0, st, a, S0, out, ST, ckpt);
       ARD_LAUNCH_CHECK("gdr_steps_kernel");
       return (int32_t)ARD_OK;
     }
     ARD_LAUNCH_NAMED("gdr_prep_kernel", (gdr_prep_kernel<E, DK, false>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a);
     ARD_LAUNCH_CHECK("gdr_prep_kernel");
-    ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, 1>), dim3(ceil_div(p.waves, 4)), dim3(256), 0, st, a, S0, *o, ST, ckpt, p.slices, p.waves);
+    ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR>), dim3(B * H * ceil_div(p.slices, 4)), dim3(256), 0, st, a, S0, out, ST, ckpt, p.slices);
     ARD_LAUNCH_CHECK("gdr_fwd_kernel");
     return (int32_t)ARD_OK;
   });
@@ -889,23 +909,25 @@ extern "C" int32_t ard_gdr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
   GdrPlan p = gdr_plan(dtype, T, B, Hk, H, Dk, Dv, true, ws);
   if (!ws || ws_bytes < p.bytes || misaligned(ws, 16)) return fail(ARD_EWORKSPACE, "workspace too small: need %zu bytes, got %zu", p.bytes, ws ? ws_bytes : 0);
   GdrArgs& a = p.a;
-  a.q = in[0], a.k = in[1], a.v = in[2], a.f = in[3], a.b = in[4], a.scale = scale, a.eps = eps, a.len = d_lengths;
+  a.q = in[0], a.k = in[1], a.v = gdr_steps(in[2], T, H * Dv), a.f = in[3], a.b = in[4], a.scale = scale, a.eps = eps, a.len = d_lengths;
   hipStream_t st = (hipStream_t)stream;
   // dX and U are read in whole operands of 32 columns: the wavefronts of the padded columns write them as zeros
-  const int slices = a.dvp / (16 * p.nt), waves = B * H * slices;
-  return gdr_instance(dtype, p.dk, [&](auto t, auto dk) {
+  const int slices = a.dvp / 16, waves = B * H * slices;
+  const ard_steps od = gdr_steps(*d_o, T, H * Dv), dv = gdr_steps(grads[2], T, H * Dv);
+  return gdr_instance(dtype, p.dk, gdr_near(a.v, Dv) && gdr_near(od, Dv) && gdr_near(dv, Dv), [&](auto t, auto dk, auto near) {
     using E = decltype(t);
     constexpr int DK = decltype(dk)::value;
+    constexpr bool NEAR = decltype(near)::value;
     ARD_LAUNCH_NAMED("gdr_prep_kernel", (gdr_prep_kernel<E, DK, true>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a);
     ARD_LAUNCH_CHECK("gdr_prep_kernel");
-    ARD_LAUNCH_NAMED("gdr_rows_kernel", (gdr_rows_kernel<E, DK, 1>), dim3((unsigned)(((int64_t)a.chunks * waves + 3) / 4)), dim3(256), 0, st, a, ckpt, slices, waves);
+    ARD_LAUNCH_NAMED("gdr_rows_kernel", (gdr_rows_kernel<E, DK, NEAR>), dim3((unsigned)(((int64_t)a.chunks * waves + 3) / 4)), dim3(256), 0, st, a, ckpt, slices, waves);
     ARD_LAUNCH_CHECK("gdr_rows_kernel");
-    ARD_LAUNCH_NAMED("gdr_back_kernel", (gdr_back_kernel<E, DK, 1>), dim3(ceil_div(waves, 4)), dim3(256), 0, st, a, *d_o, dST, grads[2], dS0, slices, waves);
+    ARD_LAUNCH_NAMED("gdr_back_kernel", (gdr_back_kernel<E, DK, NEAR>), dim3(B * H * ceil_div(slices, 4)), dim3(256), 0, st, a, od, dST, dv, dS0, slices);
     ARD_LAUNCH_CHECK("gdr_back_kernel");
     if (a.dvp == 64)
-      ARD_LAUNCH_NAMED("gdr_grads_kernel", (gdr_grads_kernel<E, DK, 64>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a, *d_o, ckpt, grads[0], grads[1], grads[3], grads[4]);
+      ARD_LAUNCH_NAMED("gdr_grads_kernel", (gdr_grads_kernel<E, DK, 64>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a, od, ckpt, grads[0], grads[1], grads[3], grads[4]);
     else
-      ARD_LAUNCH_NAMED("gdr_grads_kernel", (gdr_grads_kernel<E, DK, 128>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a, *d_o, ckpt, grads[0], grads[1], grads[3], grads[4]);
+      ARD_LAUNCH_NAMED("gdr_grads_kernel", (gdr_grads_kernel<E, DK, 128>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a, od, ckpt, grads[0], grads[1], grads[3], grads[4]);
     ARD_LAUNCH_CHECK("gdr_grads_kernel");
     return (int32_t)ARD_OK;
   });

@@ -69,6 +69,21 @@ template <int N> __device__ __forceinline__ void store_parts(u32x4* base, int fr
 #pragma unroll
   for (int n = 0; n < N; ++n) base[(frag * N + n) * 64 + (threadIdx.x & 63)] = s.p[n];
 }
+// `frags` x 1 KB from global memory to the same order in LDS, dealt to a workgroup's four wavefronts, without a register in between.
+__device__ __forceinline__ void stage(const u32x4* from, u32x4* lds, int frags, int wave) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < (frags + 3) / 4; ++i) {
+    const int j = i * 4 + wave;
+    if (j < frags)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(from + j * 64 + lane), (__attribute__((address_space(3))) uint32_t*)(lds + j * 64), 16, 0, 0);
+  }
+}
+// all of this wavefront's loads and stores have ended, and every wavefront's
+__device__ __forceinline__ void all_landed() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
 // Operands of a lower triangular 64 x 64 matrix: six tiles of 16 rows x 32 columns are not all zeros; of its transpose likewise.
 __host__ __device__ constexpr int lower_frag(int rt, int kb) { return rt < 2 ? rt : 2 * rt - 2 + kb; }
 __host__ __device__ constexpr int upper_frag(int rt, int kb) { return rt < 2 ? 2 * rt + kb : rt + 2; }
@@ -78,8 +93,8 @@ struct Steps64 {
   double G[kChunk];     // sums of log(a) from the chunk's first step on
   float since[kChunk];  // exp(G_i)
   float still[kChunk];  // exp(G_last - G_i)
-  float w[kChunk], rk[kChunk], rq[kChunk];
-  float ka[kChunk], qa[kChunk], ke[kChunk];  // rk since, scale rq since, rk still
+  float rk[kChunk], rq[kChunk];
+  float w[kChunk], ka[kChunk], qa[kChunk], ke[kChunk];  // w, rk since, scale rq since, rk still: what the passes over the states read, 1 KB
   float whole;          // exp(G_last)
   float pad[7];
 };
