@@ -11,8 +11,6 @@
 // A first launch, over all chunks at once, makes what does not depend on the states: A, P, M (blocks of 16 by substitution, the rest by
 // fp32 matrix instructions), written as operands of the second.  The second walks the chunks; a wavefront holds 16 or 32 columns of S in registers and
 // needs no other's: everything a chunk does to a column is a chain of products in its own registers (gdr.hpp).
-#include <type_traits>
-
 #include "gdr.hpp"
 
 namespace ard {
@@ -130,7 +128,8 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void g
   __syncthreads();
   f32x4 kk[4] = {}, qk[4] = {};
   {
-    u32x4 *kf = a.kf + (int64_t)unit * 4 * KB * IN * 64, *qf = a.qf + (int64_t)unit * 4 * KB * IN * 64;
+    constexpr int KF = 4 * KB * IN, KTF = DK / 8 * IN;
+    u32x4 *kf = a.rows + (int64_t)unit * 2 * KF * 64, *qf = kf + KF * 64;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       const Parts<IN> ka = row_parts<IN>(sh.k, w * 16 + c, kb, g), qa = row_parts<IN>(sh.q, w * 16 + c, kb, g);
@@ -144,7 +143,7 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void g
           mul_add(qa, b, qk[ct]);
         }
     }
-    u32x4 *ktf = a.ktf + (int64_t)unit * (DK / 16) * 2 * IN * 64, *qtf = a.qtf + (int64_t)unit * (DK / 16) * 2 * IN * 64;
+    u32x4 *ktf = a.cols + (int64_t)unit * (BWD ? 2 : 1) * KTF * 64, *qtf = ktf + KTF * 64;
     for (int i = w; i < DK / 8; i += 4) {
       store_parts(ktf, i, col_parts<IN>(sh.k, (i >> 1) * 16 + c, i & 1, g));
       if (BWD) store_parts(qtf, i, col_parts<IN>(sh.q, (i >> 1) * 16 + c, i & 1, g));
@@ -229,7 +228,7 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void g
     }
     __syncthreads();
     constexpr int PP = BWD ? 3 : OUT;
-    u32x4 *mf = a.mf + out * 6 * 3 * 64, *pf = a.pf + out * 6 * OUT * 64, *mtf = a.mtf + out * 6 * 3 * 64, *ptf = a.ptf + out * 6 * PP * 64;
+    u32x4 *mf = a.tri + out * (BWD ? 54 : 18 + 6 * OUT) * 64, *pf = mf + 18 * 64, *mtf = mf + 18 * 64, *ptf = mf + 36 * 64;
     for (int i = w; i < 6; i += 4) {
       const int rt = i < 2 ? i : 1 + i / 2, kb = i < 2 ? 0 : i & 1;  // (lower_frag's)
       store_parts(mf, i, row_parts<3>(sh.M, rt * 16 + c, kb, g));
@@ -271,32 +270,36 @@ template <typename T, bool NEAR> struct Window {
   int64_t step;
   int rows;
   bool on;
-  uint32_t at, row;  // bytes: of the lane's first element, and from row to row
+  uint32_t at[4], tile;  // bytes: of the lane's element in the first four rows, and from a tile of rows to the next
   __amdgpu_buffer_rsrc_t buffer;
   __device__ __forceinline__ Window(const void* base, int64_t step_, int rows_, int wide, int first) : step(step_), rows(rows_) {
     const int g = (threadIdx.x & 63) >> 4;
     on = first < wide;
     if constexpr (NEAR) {
-      row = (uint32_t)step * sizeof(T);
-      at = on ? 4 * g * row + first * (uint32_t)sizeof(T) : 0x80000000u;
+      const uint32_t row = (uint32_t)step * sizeof(T);
+      tile = 16 * row;
+      at[0] = on ? 4 * g * row + first * (uint32_t)sizeof(T) : 0x80000000u;
+      at[1] = at[0] + row, at[2] = at[1] + row, at[3] = at[2] + row;
       buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, rows > 0 ? rows * (int)row : 0, 0x00020000);
     } else {
       p = (T*)const_cast<void*>(base) + 4 * g * step + first;
       rows -= 4 * g;
     }
   }
-  __device__ __forceinline__ float load(int i) const {  // i = 16 rt + r
+  __device__ __forceinline__ float load(int rt, int r) const {
+    const int i = rt * 16 + r;
     if constexpr (!NEAR) return on && i < rows ? ElemTraits<T>::to_f32(p[i * step]) : 0.0f;
-    else if constexpr (sizeof(T) == 2) return bf16_bits_to_f32(__builtin_amdgcn_raw_buffer_load_b16(buffer, at + i * row, 0, 0));
-    else return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer, at + i * row, 0, 0));
+    else if constexpr (sizeof(T) == 2) return bf16_bits_to_f32(__builtin_amdgcn_raw_buffer_load_b16(buffer, at[r] + rt * tile, 0, 0));
+    else return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer, at[r] + rt * tile, 0, 0));
   }
-  __device__ __forceinline__ void store(int i, float x) const {
+  __device__ __forceinline__ void store(int rt, int r, float x) const {
+    const int i = rt * 16 + r;
     if constexpr (!NEAR) {
       if (on && i < rows) p[i * step] = ElemTraits<T>::from_f32(x);
     } else if constexpr (sizeof(T) == 2) {
-      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)bf16_pair(x, 0.0f), buffer, at + i * row, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)bf16_pair(x, 0.0f), buffer, at[r] + rt * tile, 0, 0);
     } else {
-      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), buffer, at + i * row, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), buffer, at[r] + rt * tile, 0, 0);
     }
   }
 };
@@ -304,13 +307,13 @@ template <int TILES, typename W> __device__ __forceinline__ void load_tiles(cons
 #pragma unroll
   for (int rt = 0; rt < TILES; ++rt)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) S[rt][r] = w.load(rt * 16 + r);
+    for (int r = 0; r < 4; ++r) S[rt][r] = w.load(rt, r);
 }
 template <int TILES, typename W> __device__ __forceinline__ void store_tiles(const W& w, const f32x4 (&S)[TILES]) {
 #pragma unroll
   for (int rt = 0; rt < TILES; ++rt)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) w.store(rt * 16 + r, S[rt][r]);
+    for (int r = 0; r < 4; ++r) w.store(rt, r, S[rt][r]);
 }
 // the same of steps of which only `live` count: the others are stored as 0
 template <typename W> __device__ __forceinline__ void store_live(const W& w, int live, const f32x4 (&S)[4]) {
@@ -318,7 +321,7 @@ template <typename W> __device__ __forceinline__ void store_live(const W& w, int
 #pragma unroll
   for (int rt = 0; rt < 4; ++rt)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) w.store(rt * 16 + r, rt * 16 + 4 * g + r < live ? S[rt][r] : 0.0f);
+    for (int r = 0; r < 4; ++r) w.store(rt, r, rt * 16 + 4 * g + r < live ? S[rt][r] : 0.0f);
 }
 typedef Window<float, true> StateWindow;
 __device__ __forceinline__ f32x4 row_weights(const float* w, int rt) { return *reinterpret_cast<const f32x4*>(w + rt * 16 + 4 * ((threadIdx.x & 63) >> 4)); }
@@ -327,27 +330,32 @@ __device__ __forceinline__ f32x4 row_weights(const float* w, int rt) { return *r
 template <int IN, int DK>
 __device__ __forceinline__ void unwritten(const u32x4* kf, const float* w, const float* ka, const Parts<3> (&Sp)[DK / 32], const f32x4 (&v)[4], f32x4 (&x)[4]) {
   constexpr int KB = DK / 32;
+  f32x4 y[4] = {};
 #pragma unroll
-  for (int rt = 0; rt < 4; ++rt) {
-    f32x4 y = {};
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const Parts<IN> k = load_parts<IN>(kf, rt * KB + kb);
-      mul_add(k, Sp[kb], y);
-    }
-    const f32x4 kr = row_weights(ka, rt), wr = row_weights(w, rt);
-    x[rt] = wr * (v[rt] - kr * y);
+  for (int kb = 0; kb < KB; ++kb) {
+    Parts<IN> k[4];
+    load_parts(kf, kb, KB, k);
+    mul_add(k, Sp[kb], y);
   }
+#pragma unroll
+  for (int rt = 0; rt < 4; ++rt) x[rt] = row_weights(w, rt) * (v[rt] - row_weights(ka, rt) * y[rt]);
 }
 // y += L x of a lower triangular L (64 x 64, N parts), or of its transpose
 template <bool UPPER, int N, int M> __device__ __forceinline__ void triangle(const u32x4* f, const Parts<M> (&x)[2], f32x4 (&y)[4]) {
+  Parts<N> two[2], four[4];
+  if (UPPER) {  // of all rows the last 32 columns, of the first two tiles of rows the first 32 as well
+    load_parts(f, 0, 2, two);
+    mul_add(two, x[0], reinterpret_cast<f32x4(&)[2]>(y[0]));
 #pragma unroll
-  for (int rt = 0; rt < 4; ++rt)
+    for (int rt = 0; rt < 4; ++rt) four[rt] = load_parts<N>(f, upper_frag(rt, 1));
+    mul_add(four, x[1], y);
+  } else {
 #pragma unroll
-    for (int kb = UPPER ? rt / 2 : 0; kb <= (UPPER ? 1 : rt / 2); ++kb) {
-      const Parts<N> m = load_parts<N>(f, UPPER ? upper_frag(rt, kb) : lower_frag(rt, kb));
-      mul_add(m, x[kb], y[rt]);
-    }
+    for (int rt = 0; rt < 4; ++rt) four[rt] = load_parts<N>(f, lower_frag(rt, 0));
+    mul_add(four, x[0], y);
+    load_parts(f, 3, 2, two);
+    mul_add(two, x[1], reinterpret_cast<f32x4(&)[2]>(y[2]));
+  }
 }
 template <int N, int TILES> __device__ __forceinline__ void column_parts(const f32x4 (&x)[TILES], Parts<N> (&p)[TILES / 2]) {
 #pragma unroll
@@ -363,11 +371,12 @@ template <int IN, int DK> __device__ __forceinline__ void add_outer(const u32x4*
     p[kb] = parts_of<3>(lo * y[2 * kb], hi * y[2 * kb + 1]);
   }
 #pragma unroll
-  for (int rt = 0; rt < DK / 16; ++rt)
+  for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      const Parts<IN> k = load_parts<IN>(f, rt * 2 + kb);
-      mul_add(k, p[kb], S[rt]);
+    for (int rt = 0; rt < DK / 16; rt += 4) {
+      Parts<IN> k[4];
+      load_parts(f, rt * 2 + kb, 2, k);
+      mul_add(k, p[kb], reinterpret_cast<f32x4(&)[4]>(S[rt]));
     }
 }
 
@@ -377,7 +386,7 @@ template <int IN, int DK> __device__ __forceinline__ void add_outer(const u32x4*
 template <typename T, int DK, bool NEAR>
 __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt, int slices) {
   constexpr int IN = GdrType<T>::IN, OUT = GdrType<T>::OUT, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3, PF = 6 * OUT;
-  constexpr bool STAGED = 2 * KF + KTF + MF + PF <= 150;
+  constexpr bool STAGED = 2 * KF + KTF + MF + PF <= 150;  // KB of LDS
   __shared__ u32x4 lds[STAGED ? (2 * KF + KTF + MF + PF) * 64 : 1];
   __shared__ f32x4 weights[2][64];  // w, ka, qa, ke of a chunk
   const Columns at(a, slices);
@@ -386,70 +395,80 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
   f32x4 S[DK / 16] = {}, v[4] = {};
   if (S0) load_tiles(StateWindow(S0 + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
   const int all = live_steps(a, at.n), chunks = (all + kChunk - 1) / kChunk;
-  const auto ku = [&](int chunk) { return ((int64_t)chunk * a.B + at.n) * a.Hk + at.hk; };
-  const auto hu = [&](int chunk) { return ((int64_t)chunk * a.B + at.n) * a.H + at.h; };
+  const auto ku = [&](int chunk) { return (int64_t)((chunk * a.B + at.n) * a.Hk + at.hk); };
+  const auto hu = [&](int chunk) { return (int64_t)((chunk * a.B + at.n) * a.H + at.h); };
+  const T* vp = (const T*)a.v.p + at.n * a.v.b + at.h * a.Dv;
+  T* op = (T*)o.p + at.n * o.b + at.h * a.Dv;
+  float* kept = ckpt + at.unit * matrix;
   const auto first_half = [&](int chunk) {  // loads of what it reads
-    if (STAGED) stage(a.kf + ku(chunk) * KF * 64, lds, KF, wave), stage(a.qf + ku(chunk) * KF * 64, lds + KF * 64, KF, wave);
-    stage((const u32x4*)a.steps[hu(chunk)].w, (u32x4*)weights[chunk & 1], 1, wave);
-    load_tiles(Window<T, NEAR>((const T*)a.v.p + (int64_t)chunk * kChunk * a.v.t + at.n * a.v.b + at.h * a.Dv, a.v.t, imin(all - chunk * kChunk, kChunk), a.Dv, at.first), v);
+    if (STAGED) stage<2 * KF>(a.rows + ku(chunk) * (2 * KF * 64), lds, wave);
+    if (wave == 0) stage<4>((const u32x4*)a.steps[hu(chunk)].w, (u32x4*)weights[chunk & 1], 0);
+    load_tiles(Window<T, NEAR>(vp, a.v.t, imin(all - chunk * kChunk, kChunk), a.Dv, at.first), v);
+    vp += kChunk * a.v.t;
   };
   const auto second_half = [&](int chunk) {
-    if (STAGED) {
-      stage(a.ktf + ku(chunk) * KTF * 64, lds + 2 * KF * 64, KTF, wave);
-      stage(a.mf + hu(chunk) * MF * 64, lds + (2 * KF + KTF) * 64, MF, wave), stage(a.pf + hu(chunk) * PF * 64, lds + (2 * KF + KTF + MF) * 64, PF, wave);
-    }
+    if (STAGED) stage<KTF>(a.cols + ku(chunk) * (KTF * 64), lds + 2 * KF * 64, wave), stage<MF + PF>(a.tri + hu(chunk) * ((MF + PF) * 64), lds + (2 * KF + KTF) * 64, wave);
   };
+  constexpr int COUNT = STAGED && NEAR;  // (elsewhere accesses are not counted: all are waited for)
   if (chunks) {
     first_half(0);
-    all_landed();
+    staged();
+    all_landed<0>();
     second_half(0);
+    staged();
   }
   for (int chunk = 0; chunk < chunks; ++chunk) {
-    const int t0 = chunk * kChunk, steps = imin(a.T - t0, kChunk), live = imin(all - t0, steps);
+    const int steps = imin(a.T - chunk * kChunk, kChunk), live = imin(all - chunk * kChunk, steps);
     const float *w = (const float*)weights[chunk & 1], *ka = w + kChunk, *qa = w + 2 * kChunk, *ke = w + 3 * kChunk;
+    const u32x4 *rows = STAGED ? lds : a.rows + ku(chunk) * (2 * KF * 64), *cols = STAGED ? lds + 2 * KF * 64 : a.cols + ku(chunk) * (KTF * 64),
+                *tri = STAGED ? lds + (2 * KF + KTF) * 64 : a.tri + hu(chunk) * ((MF + PF) * 64);
     const float whole = a.steps[hu(chunk)].whole;
-    if (ckpt) store_tiles(StateWindow(ckpt + chunk * plane + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
+    if (ckpt) {
+      store_tiles(StateWindow(kept, a.Dv, a.Dk, a.Dv, at.first), S);
+      kept += plane;
+    }
     f32x4 x[4], y[4] = {}, u[4] = {};
     {
       Parts<3> Sp[KB];
       column_parts<3>(S, Sp);
-      const u32x4* qf = STAGED ? lds + KF * 64 : a.qf + ku(chunk) * KF * 64;
-      unwritten<IN, DK>(STAGED ? lds : a.kf + ku(chunk) * KF * 64, w, ka, Sp, v, x);
+      unwritten<IN, DK>(rows, w, ka, Sp, v, x);
 #pragma unroll
-      for (int rt = 0; rt < 4; ++rt) {
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-          const Parts<IN> q = load_parts<IN>(qf, rt * KB + kb);
-          mul_add(q, leading<OUT>(Sp[kb]), y[rt]);
-        }
-        const f32x4 qr = row_weights(qa, rt);
-        y[rt] *= qr;
+      for (int kb = 0; kb < KB; ++kb) {
+        Parts<IN> q[4];
+        load_parts(rows + KF * 64, kb, KB, q);
+        mul_add(q, leading<OUT>(Sp[kb]), y);
       }
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) y[rt] *= row_weights(qa, rt);
     }
-    all_landed();
+    if (ckpt) all_landed<COUNT * (DK / 4)>();
+    else all_landed<0>();
     if (chunk + 1 < chunks) first_half(chunk + 1);
+    staged();
     {
       Parts<3> xp[2];
       column_parts<3>(x, xp);
-      triangle<false, 3>(STAGED ? lds + (2 * KF + KTF) * 64 : a.mf + hu(chunk) * MF * 64, xp, u);
+      triangle<false, 3>(tri, xp, u);
     }
     {
       Parts<OUT> up[2];
       column_parts<OUT>(u, up);
-      triangle<false, OUT>(STAGED ? lds + (2 * KF + KTF + MF) * 64 : a.pf + hu(chunk) * PF * 64, up, y);
+      triangle<false, OUT>(tri + MF * 64, up, y);
     }
-    store_live(Window<T, NEAR>((T*)o.p + t0 * o.t + at.n * o.b + at.h * a.Dv, o.t, steps, a.Dv, at.first), live, y);
+    store_live(Window<T, NEAR>(op, o.t, steps, a.Dv, at.first), live, y);
+    op += kChunk * o.t;
 #pragma unroll
-    for (int rt = 0; rt < DK / 16; ++rt)
-      S[rt] *= whole;
-    add_outer<IN, DK>(STAGED ? lds + 2 * KF * 64 : a.ktf + ku(chunk) * KTF * 64, ke, 1.0f, u, S);
-    all_landed();
+    for (int rt = 0; rt < DK / 16; ++rt) S[rt] *= whole;
+    add_outer<IN, DK>(cols, ke, 1.0f, u, S);
+    all_landed<COUNT * 16>();
     if (chunk + 1 < chunks) second_half(chunk + 1);
+    staged();
   }
   for (int chunk = chunks; chunk < a.chunks; ++chunk) {  // behind the sequence's end
     const f32x4 none[4] = {};
-    if (ckpt) store_tiles(StateWindow(ckpt + chunk * plane + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
-    store_tiles(Window<T, NEAR>((T*)o.p + (int64_t)chunk * kChunk * o.t + at.n * o.b + at.h * a.Dv, o.t, imin(a.T - chunk * kChunk, kChunk), a.Dv, at.first), none);
+    if (ckpt) store_tiles(StateWindow(kept, a.Dv, a.Dk, a.Dv, at.first), S);
+    store_tiles(Window<T, NEAR>(op, o.t, imin(a.T - chunk * kChunk, kChunk), a.Dv, at.first), none);
+    kept += plane, op += kChunk * o.t;
   }
   if (ST) store_tiles(StateWindow(ST + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
 }
@@ -482,11 +501,11 @@ template <typename T, int DK, bool NEAR> __global__ __launch_bounds__(256) void 
   {
     Parts<3> Sp[KB];
     column_parts<3>(S, Sp);
-    unwritten<IN, DK>(a.kf + ku * 4 * KB * IN * 64, st.w, st.ka, Sp, v, x);
+    unwritten<IN, DK>(a.rows + ku * 2 * 4 * KB * IN * 64, st.w, st.ka, Sp, v, x);
   }
   Parts<3> xp[2];
   column_parts<3>(x, xp);
-  triangle<false, 3>(a.mf + hu * 6 * 3 * 64, xp, u);
+  triangle<false, 3>(a.tri + hu * 54 * 64, xp, u);
   store_tiles(StateWindow(a.u + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp, at.first), u);
 }
 
@@ -502,226 +521,347 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
   f32x4 S[DK / 16] = {}, x[4] = {};
   if (dST) load_tiles(StateWindow(dST + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
   const int all = live_steps(a, at.n), chunks = (all + kChunk - 1) / kChunk;
-  const auto ku = [&](int chunk) { return ((int64_t)chunk * a.B + at.n) * a.Hk + at.hk; };
-  const auto hu = [&](int chunk) { return ((int64_t)chunk * a.B + at.n) * a.H + at.h; };
+  const auto ku = [&](int chunk) { return (int64_t)((chunk * a.B + at.n) * a.Hk + at.hk); };
+  const auto hu = [&](int chunk) { return (int64_t)((chunk * a.B + at.n) * a.H + at.h); };
+  const T* gp = (const T*)d_o.p + at.n * d_o.b + at.h * a.Dv;
+  T* vp = (T*)dv.p + at.n * dv.b + at.h * a.Dv;
   const auto first_half = [&](int chunk) {
-    if (STAGED) stage(a.kf + ku(chunk) * KF * 64, lds, KF, wave), stage(a.ptf + hu(chunk) * MF * 64, lds + KF * 64, MF, wave);
-    stage((const u32x4*)a.steps[hu(chunk)].w, (u32x4*)weights[chunk & 1], 1, wave);
-    load_tiles(Window<T, NEAR>((const T*)d_o.p + (int64_t)chunk * kChunk * d_o.t + at.n * d_o.b + at.h * a.Dv, d_o.t, imin(all - chunk * kChunk, kChunk), a.Dv, at.first), x);
+    if (STAGED) stage<KF>(a.rows + ku(chunk) * (2 * KF * 64), lds, wave), stage<MF>(a.tri + hu(chunk) * (3 * MF * 64) + 2 * MF * 64, lds + KF * 64, wave);
+    if (wave == 0) stage<4>((const u32x4*)a.steps[hu(chunk)].w, (u32x4*)weights[chunk & 1], 0);
+    load_tiles(Window<T, NEAR>(gp + (int64_t)chunk * kChunk * d_o.t, d_o.t, imin(all - chunk * kChunk, kChunk), a.Dv, at.first), x);
   };
   const auto second_half = [&](int chunk) {
-    if (STAGED) {
-      stage(a.mtf + hu(chunk) * MF * 64, lds + (KF + MF) * 64, MF, wave);
-      stage(a.qtf + ku(chunk) * KTF * 64, lds + (KF + 2 * MF) * 64, KTF, wave), stage(a.ktf + ku(chunk) * KTF * 64, lds + (KF + 2 * MF + KTF) * 64, KTF, wave);
-    }
+    if (STAGED) stage<MF>(a.tri + hu(chunk) * (3 * MF * 64) + MF * 64, lds + (KF + MF) * 64, wave), stage<2 * KTF>(a.cols + ku(chunk) * (2 * KTF * 64), lds + (KF + 2 * MF) * 64, wave);
   };
   for (int chunk = chunks; chunk < a.chunks; ++chunk) {  // behind the sequence's end
     const f32x4 none[4] = {};
-    store_tiles(Window<T, NEAR>((T*)dv.p + (int64_t)chunk * kChunk * dv.t + at.n * dv.b + at.h * a.Dv, dv.t, imin(a.T - chunk * kChunk, kChunk), a.Dv, at.first), none);
+    store_tiles(Window<T, NEAR>(vp + (int64_t)chunk * kChunk * dv.t, dv.t, imin(a.T - chunk * kChunk, kChunk), a.Dv, at.first), none);
   }
+  constexpr int COUNT = STAGED && NEAR;
   if (chunks) {
     first_half(chunks - 1);
-    all_landed();
+    staged();
+    all_landed<0>();
     second_half(chunks - 1);
+    staged();
   }
   for (int chunk = chunks - 1; chunk >= 0; --chunk) {
-    const int t0 = chunk * kChunk, steps = imin(a.T - t0, kChunk), live = imin(all - t0, steps);
+    const int steps = imin(a.T - chunk * kChunk, kChunk), live = imin(all - chunk * kChunk, steps);
     const float *w = (const float*)weights[chunk & 1], *ka = w + kChunk, *qa = w + 2 * kChunk, *ke = w + 3 * kChunk;
+    const u32x4 *kf = STAGED ? lds : a.rows + ku(chunk) * (2 * KF * 64), *cols = STAGED ? lds + (KF + 2 * MF) * 64 : a.cols + ku(chunk) * (2 * KTF * 64),
+                *ptf = STAGED ? lds + KF * 64 : a.tri + hu(chunk) * (3 * MF * 64) + 2 * MF * 64, *mtf = STAGED ? lds + (KF + MF) * 64 : a.tri + hu(chunk) * (3 * MF * 64) + MF * 64;
     const float whole = a.steps[hu(chunk)].whole;
     store_tiles(StateWindow(a.ds + hu(chunk) * DK * a.dvp, a.dvp, DK, a.dvp, at.first), S);
     f32x4 y[4] = {}, dx[4] = {}, od[4];
     {
       Parts<3> Sp[KB];
       column_parts<3>(S, Sp);
-      const u32x4* kf = STAGED ? lds : a.kf + ku(chunk) * KF * 64;
 #pragma unroll
-      for (int rt = 0; rt < 4; ++rt) {
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-          const Parts<IN> k = load_parts<IN>(kf, rt * KB + kb);
-          mul_add(k, Sp[kb], y[rt]);
-        }
-        const f32x4 kr = row_weights(ke, rt);
-        y[rt] *= kr;
+      for (int kb = 0; kb < KB; ++kb) {
+        Parts<IN> k[4];
+        load_parts(kf, kb, KB, k);
+        mul_add(k, Sp[kb], y);
       }
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) y[rt] *= row_weights(ke, rt);
     }
     {
       Parts<IN> p[2];
       column_parts<IN>(x, p);
-      triangle<true, 3>(STAGED ? lds + KF * 64 : a.ptf + hu(chunk) * MF * 64, p, y);
+      triangle<true, 3>(ptf, p, y);
     }
 #pragma unroll
-    for (int rt = 0; rt < 4; ++rt)
-      od[rt] = x[rt];
-    all_landed();
+    for (int rt = 0; rt < 4; ++rt) od[rt] = x[rt];
+    all_landed<COUNT * (DK / 4)>();
     if (chunk > 0) first_half(chunk - 1);
+    staged();
     {
       Parts<3> p[2];
       column_parts<3>(y, p);
-      triangle<true, 3>(STAGED ? lds + (KF + MF) * 64 : a.mtf + hu(chunk) * MF * 64, p, dx);
+      triangle<true, 3>(mtf, p, dx);
     }
 #pragma unroll
-    for (int rt = 0; rt < 4; ++rt) {
-      const f32x4 wr = row_weights(w, rt);
-      y[rt] = wr * dx[rt];
-    }
+    for (int rt = 0; rt < 4; ++rt) y[rt] = row_weights(w, rt) * dx[rt];
     store_tiles(StateWindow(a.dx + hu(chunk) * kChunk * a.dvp, a.dvp, kChunk, a.dvp, at.first), dx);
-    store_live(Window<T, NEAR>((T*)dv.p + t0 * dv.t + at.n * dv.b + at.h * a.Dv, dv.t, steps, a.Dv, at.first), live, y);
+    store_live(Window<T, NEAR>(vp + (int64_t)chunk * kChunk * dv.t, dv.t, steps, a.Dv, at.first), live, y);
 #pragma unroll
-    for (int rt = 0; rt < DK / 16; ++rt)
-      S[rt] *= whole;
-    add_outer<IN, DK>(STAGED ? lds + (KF + 2 * MF) * 64 : a.qtf + ku(chunk) * KTF * 64, qa, 1.0f, od, S);
-    add_outer<IN, DK>(STAGED ? lds + (KF + 2 * MF + KTF) * 64 : a.ktf + ku(chunk) * KTF * 64, ka, -1.0f, y, S);
-    all_landed();
+    for (int rt = 0; rt < DK / 16; ++rt) S[rt] *= whole;
+    add_outer<IN, DK>(cols + KTF * 64, qa, 1.0f, od, S);
+    add_outer<IN, DK>(cols, ka, -1.0f, y, S);
+    all_landed<COUNT * 32>();
     if (chunk > 0) second_half(chunk - 1);
+    staged();
   }
   if (dS0) store_tiles(StateWindow(dS0 + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
 }
 
-// 8 neighbouring fp32 values of a workspace row as parts
-template <int N> __device__ __forceinline__ Parts<N> run_parts(const float* p) {
-  float x[8];
-  load_run<8>(p, x);
-  return parts_of<N>(x);
-}
 __device__ __forceinline__ float over_rows(float x) {  // the sum over the lanes that share a column
   x += __shfl_xor(x, 16);
   return x + __shfl_xor(x, 32);
 }
 
-// The gradients of queries, keys and gates of a chunk and a key head: wavefront w has the 16 steps from 16 w on, as columns.
-template <typename T, int DK, int DV>
-__global__ __launch_bounds__(256) void gdr_grads_kernel(GdrArgs a, ard_steps d_o, const float* ckpt, ard_steps dq, ard_steps dk, ard_steps df, ard_steps db) {
-  constexpr int IN = GdrType<T>::IN, N = GdrType<T>::OUT, VB = DV / 32, RT = DK / 16;
-  __shared__ double dG[kChunk];
-  __shared__ float ends[4];
+// Neighbouring elements of a lane's rows, 0 where they are outside.  QUICK: by one access whose end the hardware checks, without a branch: for rows whose runs of
+// N are inside or outside as a whole, and within 2 GB.
+template <typename T, int N, bool QUICK> struct Runs {
+  const T* p;
+  int64_t step;
+  int rows, wide;
+  __amdgpu_buffer_rsrc_t buffer;
+  __device__ __forceinline__ Runs(const void* base, int64_t step_, int rows_, int wide_) : p((const T*)base), step(step_), rows(rows_), wide(wide_) {
+    if constexpr (QUICK) buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, rows > 0 ? rows * (int)step * (int)sizeof(T) : 0, 0x00020000);
+  }
+  __device__ __forceinline__ void load(int row, int at, float (&x)[N]) const {
+    if constexpr (QUICK) {
+      const uint32_t from = at < wide ? ((uint32_t)row * (uint32_t)step + (uint32_t)at) * (uint32_t)sizeof(T) : 0x80000000u;
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < N; j += 4) {
+          const auto v = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer, from + j * 4, 0, 0));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[j + e] = v[e];
+        }
+      } else if constexpr (N == 8) {
+        const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer, from, 0, 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[2 * e] = __uint_as_float(v[e] << 16), x[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+      } else {
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(buffer, from, 0, 0));
+#pragma unroll
+        for (int e = 0; e < 2; ++e) x[2 * e] = __uint_as_float(v[e] << 16), x[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+      }
+    } else {
+      load_some<N>(p + row * step + at, row < rows ? wide - at : 0, x);
+    }
+  }
+};
+
+// Four values as they were stored.
+template <typename T> struct Four;
+template <> struct Four<float> {
+  float v[4];
+  __device__ __forceinline__ void set(const float (&x)[4]) { v[0] = x[0], v[1] = x[1], v[2] = x[2], v[3] = x[3]; }
+  __device__ __forceinline__ float at(int r) const { return v[r]; }
+};
+template <> struct Four<uint16_t> {
+  uint32_t v[2];
+  __device__ __forceinline__ void set(const float (&x)[4]) { v[0] = bf16_pair(x[0], x[1]), v[1] = bf16_pair(x[2], x[3]); }
+  __device__ __forceinline__ float at(int r) const { return __uint_as_float(r & 1 ? v[r / 2] & 0xffff0000u : v[r / 2] << 16); }
+};
+
+// The gradients of queries, keys and gates of a chunk and a key head, by four wavefronts, or eight for wide keys.  Wavefront w has the steps of tile w % 4 as columns, and all
+// rows of Dk or half of them.  U, dX and dO become parts once and go around through LDS, each tile the right hand operand of its own wavefronts and the left hand one of the others; S and
+// dS' follow there.  Operands are read from LDS where they are used, for all of a wavefront's rows at once: its registers hold sums, not operands (with those of its own
+// steps in registers too, 256 were not enough, and what was spilled took most of the time).  Where LDS does not hold rows and states together (fp32, wide heads) they are.
+template <typename T, int DK, int DV, bool QUICK>
+__global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps d_o, const float* ckpt, ard_steps dq, ard_steps dk, ard_steps df, ard_steps db) {
+  constexpr int IN = GdrType<T>::IN, N = GdrType<T>::OUT, VB = DV / 32, RT = DK / 16, HALVES = DK / 64, WAVES = 4 * HALVES, OWN = RT / HALVES, MINE = RT * VB / WAVES;
+  constexpr int ROWS = 4 * VB * (2 * N + IN), STATE = RT * VB * N;
+  constexpr bool KEEP = ROWS + STATE <= 152;
+  __shared__ u32x4 lds[(KEEP ? ROWS + STATE : ROWS > STATE ? ROWS : STATE) * 64];
+  __shared__ double dG[HALVES][kChunk];
+  __shared__ float ends[WAVES], dots[2][HALVES][kChunk];
+  __shared__ Steps64 st;
+  u32x4 *lu = lds, *lx = lds + 4 * VB * N * 64, *lo = lds + 8 * VB * N * 64, *ls = KEEP ? lds + ROWS * 64 : lds;
   const int unit = blockIdx.x, chunk = unit / (a.B * a.Hk), n = (unit - chunk * a.B * a.Hk) / a.Hk, hk = unit % a.Hk;
   const int t0 = chunk * kChunk, steps = imin(a.T - t0, kChunk), live = imin(live_steps(a, n) - t0, steps);
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, mine = w * 16 + c;
-  T *dqp = (T*)dq.p + (int64_t)(t0 + mine) * dq.t + n * dq.b + hk * a.Dk, *dkp = (T*)dk.p + (int64_t)(t0 + mine) * dk.t + n * dk.b + hk * a.Dk;
-  f32x4 sumq[RT] = {}, sumk[RT] = {};
+  const int w8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = w8 & 3, half = HALVES > 1 ? w8 >> 2 : 0, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, mine = w * 16 + c;
+  f32x4 sumq[OWN] = {}, sumk[OWN] = {};
   if (live > 0) {
-    const T *kp = (const T*)a.k.p + (int64_t)(t0 + mine) * a.k.t + n * a.k.b + hk * a.Dk, *qp = (const T*)a.q.p + (int64_t)(t0 + mine) * a.q.t + n * a.q.b + hk * a.Dk;
-    const u32x4 *ktf = a.ktf + (int64_t)unit * (DK / 8) * IN * 64, *qtf = a.qtf + (int64_t)unit * (DK / 8) * IN * 64;
+    const Runs<T, 4, QUICK> keys((const T*)a.k.p + t0 * a.k.t + n * a.k.b + hk * a.Dk, a.k.t, live, a.Dk), queries((const T*)a.q.p + t0 * a.q.t + n * a.q.b + hk * a.Dk, a.q.t, live, a.Dk);
+    Four<T> kx[OWN], qx[OWN];  // of the wavefront's own steps, where its sums lie
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+      const int at = (half * OWN + i) * 16 + 4 * g;
+      float x[4], y[4];
+      keys.load(mine, at, x), queries.load(mine, at, y);
+      kx[i].set(x), qx[i].set(y);
+    }
+    const u32x4 *ktf = a.cols + (int64_t)unit * (DK / 4) * IN * 64, *qtf = ktf + DK / 8 * IN * 64;
+    const Steps64& any = a.steps[((int64_t)chunk * a.B + n) * a.H + hk * a.group];
+    const float rkm = any.rk[mine], rqm = any.rq[mine];
     for (int s = 0; s < a.group; ++s) {
       const int h = hk * a.group + s;
       const int64_t hu = ((int64_t)chunk * a.B + n) * a.H + h;
-      const Steps64& st = a.steps[hu];
-      const float *u = a.u + hu * kChunk * a.dvp, *dx = a.dx + hu * kChunk * a.dvp, *ds = a.ds + hu * DK * a.dvp, *S = ckpt + hu * a.Dk * a.Dv;
-      const T* dop = (const T*)d_o.p + t0 * d_o.t + n * d_o.b + h * a.Dv;
-      const auto of_do = [&](int row, int kb) {
-        float x[8] = {};
-        const int at = kb * 32 + 8 * g;
-        if (row < live) load_some<8>(dop + row * d_o.t + at, a.Dv - at, x);
-        return parts_of<IN>(x);
-      };
-      Parts<N> ub[VB], xb[VB];
-      Parts<IN> ob[VB];
-#pragma unroll
-      for (int kb = 0; kb < VB; ++kb) {
-        ub[kb] = run_parts<N>(u + mine * a.dvp + kb * 32 + 8 * g);
-        xb[kb] = run_parts<N>(dx + mine * a.dvp + kb * 32 + 8 * g);
-        ob[kb] = of_do(mine, kb);
-      }
-      const double Gm = st.G[mine];
-      const float wm = st.w[mine];
-      float dw = 0.0f;
-      // by pairs of row tiles: what the wavefront's steps take from the keys and queries of others, ready as operands
-      Parts<N> below[2], belowq[2], above[2], aboveq[2];  // N_ij K_i and R_ij Q_i of later rows i; N_ij K_j and R_ij K_j of earlier rows j
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        f32x4 lo[2] = {}, loq[2] = {}, up[2] = {}, upq[2] = {};
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int rt = 2 * kb + half;
-          const f32x4 rk = row_weights(st.rk, rt);
-          float fade[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) fade[r] = expf(-(float)fabs(st.G[rt * 16 + 4 * g + r] - Gm));
-          if (rt >= w) {
-            f32x4 E = {}, F = {};
-#pragma unroll
-            for (int vb = 0; vb < VB; ++vb) {
-              mul_add(run_parts<N>(dx + (rt * 16 + c) * a.dvp + vb * 32 + 8 * g), ub[vb], E);
-              mul_add(of_do(rt * 16 + c, vb), ub[vb], F);
-            }
-            const f32x4 wr = row_weights(st.w, rt), rq = row_weights(st.rq, rt);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int i = rt * 16 + 4 * g + r;
-              if (i == mine) dw = E[r];
-              lo[half][r] = i > mine ? -E[r] * wr[r] * fade[r] * rk[r] : 0.0f;
-              loq[half][r] = i >= mine ? F[r] * a.scale * fade[r] * rq[r] : 0.0f;
-            }
-          }
-          if (rt <= w) {
-            f32x4 E = {}, F = {};
-#pragma unroll
-            for (int vb = 0; vb < VB; ++vb) {
-              const Parts<N> x = run_parts<N>(u + (rt * 16 + c) * a.dvp + vb * 32 + 8 * g);
-              mul_add(x, xb[vb], E);
-              mul_add(x, ob[vb], F);
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int j = rt * 16 + 4 * g + r;
-              up[half][r] = j < mine ? -E[r] * wm * fade[r] * rk[r] : 0.0f;
-              upq[half][r] = j <= mine ? F[r] * a.scale * fade[r] * rk[r] : 0.0f;
-            }
-          }
-        }
-        below[kb] = parts_of<N>(lo[0], lo[1]), belowq[kb] = parts_of<N>(loq[0], loq[1]);
-        above[kb] = parts_of<N>(up[0], up[1]), aboveq[kb] = parts_of<N>(upq[0], upq[1]);
-      }
-      const float since = st.since[mine], still = st.still[mine], rkm = st.rk[mine], rqm = st.rq[mine];
-      float moved = 0.0f, into = 0.0f, both = 0.0f;
-#pragma unroll 1
-      for (int rt = 0; rt < RT; ++rt) {
-        f32x4 sq = {}, sx = {}, su = {};
-        const int row = rt * 16 + c;
+      // (addresses made from these are made in the loop: taken out of it, they alone would not fit the registers)
+      int g = lane >> 4, c = lane & 15;
+      asm volatile("" : "+v"(g), "+v"(c));
+      const int mine = w * 16 + c;
+      const Runs<float, 8, QUICK> S(ckpt + hu * a.Dk * a.Dv, a.Dv, a.Dk, a.Dv);
+      const Runs<float, 8, true> ds(a.ds + hu * DK * a.dvp, a.dvp, DK, a.dvp);
+      {
+        // (of two halves the second takes dX)
+        const Runs<float, 8, true> rows((half ? a.dx : a.u) + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp), dx(a.dx + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp);
+        const Runs<T, 8, QUICK> go((const T*)d_o.p + t0 * d_o.t + n * d_o.b + h * a.Dv, d_o.t, live, a.Dv);
+        float x[VB][8], y[VB][8], z[HALVES > 1 ? 1 : VB][8];
 #pragma unroll
         for (int vb = 0; vb < VB; ++vb) {
           const int at = vb * 32 + 8 * g;
-          float x[8] = {}, y[8];
-          if (row < a.Dk) load_some<8>(S + (int64_t)row * a.Dv + at, a.Dv - at, x);
-          load_run<8>(ds + (int64_t)row * a.dvp + at, y);
-          const Parts<N> xs = parts_of<N>(x), ys = parts_of<N>(y);
-          mul_add(xs, ob[vb], sq);
-          mul_add(xs, xb[vb], sx);
-          mul_add(ys, ub[vb], su);
-          if (rt % 4 == w)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) both = fmaf(x[j], y[j], both);
+          rows.load(mine, at, x[vb]);
+          if (HALVES == 1) dx.load(mine, at, z[HALVES > 1 ? 0 : vb]);
+          if (half == 0) go.load(mine, at, y[vb]);
         }
-        f32x4 tq = sq * (a.scale * since), tp = sx * (-wm * since), te = su * still, tm = {};
+        __syncthreads();  // (the head before has been read)
+        if (w8 < 3) {
+          u32x4* to = (u32x4*)&st + w8 * 64 + lane;
+          *to = ((const u32x4*)&a.steps[hu])[w8 * 64 + lane];
+        }
+#pragma unroll
+        for (int vb = 0; vb < VB; ++vb) {
+          store_parts<N>(half ? lx : lu, w * VB + vb, parts_of<N>(x[vb]));
+          if (HALVES == 1) store_parts<N>(lx, w * VB + vb, parts_of<N>(z[HALVES > 1 ? 0 : vb]));
+          if (half == 0) store_parts<IN>(lo, w * VB + vb, parts_of<IN>(y[vb]));
+        }
+      }
+      float Sx[MINE][8], Dx[MINE][8];
+#pragma unroll
+      for (int i = 0; i < MINE; ++i) {
+        const int rt = (i * WAVES + w8) / VB, vb = (i * WAVES + w8) % VB;
+        S.load(rt * 16 + c, vb * 32 + 8 * g, Sx[i]);
+      }
+      // the gates whose slopes the end needs: f by the first wavefront, b by those of the first half
+      float fg = 0.0f, bg = 0.0f;
+      if (w8 == 0 && 63 - lane < live) fg = ElemTraits<T>::to_f32(((const T*)a.f.p)[(int64_t)(t0 + 63 - lane) * a.f.t + n * a.f.b + h]);
+      if (half == 0 && mine < live) bg = ElemTraits<T>::to_f32(((const T*)a.b.p)[(int64_t)(t0 + mine) * a.b.t + n * a.b.b + h]);
+      __syncthreads();
+      Parts<N> ub[KEEP ? 1 : VB], xb[KEEP ? 1 : VB];
+      Parts<IN> ob[KEEP ? 1 : VB];
+      if constexpr (!KEEP) {
+#pragma unroll
+        for (int vb = 0; vb < VB; ++vb) ub[vb] = load_parts<N>(lu, w * VB + vb), xb[vb] = load_parts<N>(lx, w * VB + vb), ob[vb] = load_parts<IN>(lo, w * VB + vb);
+      }
+      const auto of_u = [&](int vb) { return KEEP ? load_parts<N>(lu, w * VB + vb) : ub[KEEP ? 0 : vb]; };
+      const auto of_x = [&](int vb) { return KEEP ? load_parts<N>(lx, w * VB + vb) : xb[KEEP ? 0 : vb]; };
+      const auto of_o = [&](int vb) { return KEEP ? load_parts<IN>(lo, w * VB + vb) : ob[KEEP ? 0 : vb]; };
+      const double Gm = st.G[mine];
+      const float wm = st.w[mine];
+      float dw = 0.0f;
+      // by pairs of row tiles, ready as operands: N_ij and R_ij of later rows i, of earlier rows j.  (All tiles are multiplied, though some are not needed:
+      // a branch around each would make the next one's operands wait for it.)
+      Parts<N> below[2], belowq[2], above[2], aboveq[2];
+      {
+        f32x4 dn[4] = {}, dnq[4] = {}, up[4] = {}, upq[4] = {};
+#pragma unroll
+        for (int vb = 0; vb < VB; ++vb) {
+          const Parts<N> u = of_u(vb), x = of_x(vb);
+          const Parts<IN> o = of_o(vb);
+          Parts<N> y[4];
+          Parts<IN> z[4];
+          load_parts(lx, vb, VB, y);
+          mul_add(y, u, dn);
+          load_parts(lo, vb, VB, z);
+          mul_add(z, u, dnq);
+          load_parts(lu, vb, VB, y);
+          mul_add(y, x, up);
+          mul_add(y, o, upq);
+        }
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) {
+          const f32x4 rk = row_weights(st.rk, rt), rq = row_weights(st.rq, rt), wr = row_weights(st.w, rt);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int i = rt * 16 + 4 * g + r;
+            const float fade = exp_of(-(float)fabs(st.G[i] - Gm));
+            if (i == mine) dw = dn[rt][r];
+            dn[rt][r] = i > mine ? -dn[rt][r] * (wr[r] * rk[r] * fade) : 0.0f;
+            dnq[rt][r] = i >= mine ? dnq[rt][r] * (a.scale * rq[r] * fade) : 0.0f;
+            up[rt][r] = i < mine ? -up[rt][r] * (wm * rk[r] * fade) : 0.0f;
+            upq[rt][r] = i <= mine ? upq[rt][r] * (a.scale * rk[r] * fade) : 0.0f;
+          }
+        }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-          const Parts<IN> k = load_parts<IN>(ktf, rt * 2 + kb), q = load_parts<IN>(qtf, rt * 2 + kb);
-          if (2 * kb + 1 >= w) mul_add(k, below[kb], tm), mul_add(q, belowq[kb], tm);
-          if (2 * kb <= w) mul_add(k, above[kb], tp), mul_add(k, aboveq[kb], tq);
+          below[kb] = parts_of<N>(dn[2 * kb], dn[2 * kb + 1]), belowq[kb] = parts_of<N>(dnq[2 * kb], dnq[2 * kb + 1]);
+          above[kb] = parts_of<N>(up[2 * kb], up[2 * kb + 1]), aboveq[kb] = parts_of<N>(upq[2 * kb], upq[2 * kb + 1]);
         }
-        float kx[4] = {}, qx[4] = {};
-        const int at = rt * 16 + 4 * g;
-        if (mine < live) load_some<4>(kp + at, a.Dk - at, kx), load_some<4>(qp + at, a.Dk - at, qx);
+      }
+      const float since = st.since[mine], still = st.still[mine];
+      float moved = 0.0f, into = 0.0f, both = 0.0f;
+      if (!KEEP) __syncthreads();
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          into = fmaf(kx[r] * rkm, te[r], into);
-          moved = fmaf(qx[r] * rqm, tq[r], fmaf(kx[r] * rkm, tp[r] - tm[r], moved));
+      for (int i = 0; i < MINE; ++i) {
+        const int rt = (i * WAVES + w8) / VB, vb = (i * WAVES + w8) % VB;
+        store_parts<N>(ls, i * WAVES + w8, parts_of<N>(Sx[i]));
+        ds.load(rt * 16 + c, vb * 32 + 8 * g, Dx[i]);
+      }
+      __syncthreads();
+      {
+        f32x4 tq[OWN] = {}, tp[OWN] = {};
+#pragma unroll
+        for (int vb = 0; vb < VB; ++vb) {
+          const Parts<N> x = of_x(vb);
+          const Parts<IN> o = of_o(vb);
+          Parts<N> y[OWN];
+          load_parts(ls, half * OWN * VB + vb, VB, y);
+          mul_add(y, o, tq);
+          mul_add(y, x, tp);
         }
-        tm += te;
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
-          if (i == rt) sumq[i] += tq, sumk[i] += tp + tm;
+        for (int i = 0; i < OWN; ++i) tq[i] *= a.scale * since, tp[i] *= -wm * since;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          Parts<IN> k[OWN];
+          load_parts(ktf, half * OWN * 2 + kb, 2, k);
+          mul_add(k, above[kb], tp);
+          mul_add(k, aboveq[kb], tq);
+        }
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) {
+          float mk = 0.0f, mq = 0.0f;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) mk = fmaf(kx[i].at(r), tp[i][r], mk), mq = fmaf(qx[i].at(r), tq[i][r], mq);
+          moved += rkm * mk + rqm * mq;
+          sumq[i] += tq[i], sumk[i] += tp[i];
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < MINE; ++i) {
+        store_parts<N>(ls, i * WAVES + w8, parts_of<N>(Dx[i]));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) both = fmaf(Sx[i][e], Dx[i][e], both);
+      }
+      __syncthreads();
+      {
+        f32x4 te[OWN] = {};
+#pragma unroll
+        for (int vb = 0; vb < VB; ++vb) {
+          const Parts<N> u = of_u(vb);
+          Parts<N> y[OWN];
+          load_parts(ls, half * OWN * VB + vb, VB, y);
+          mul_add(y, u, te);
+        }
+        f32x4 tm[OWN] = {};
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          Parts<IN> k[OWN];
+          load_parts(ktf, half * OWN * 2 + kb, 2, k);
+          mul_add(k, below[kb], tm);
+          load_parts(qtf, half * OWN * 2 + kb, 2, k);
+          mul_add(k, belowq[kb], tm);
+        }
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) {
+          float me = 0.0f, mm = 0.0f;
+          te[i] *= still;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) me = fmaf(kx[i].at(r), te[i][r], me), mm = fmaf(kx[i].at(r), tm[i][r], mm);
+          into += rkm * me, moved -= rkm * mm;
+          sumk[i] += te[i] + tm[i];
+        }
       }
       dw = over_rows(dw), moved = over_rows(moved), into = over_rows(into);
       both = wave_sum(both);
-      if (g == 0) dG[mine] = (double)moved - (double)into;
+      if (g == 0) dG[half][mine] = (double)moved - (double)into;
       into = row_sum(into);
-      if (lane == 0) ends[w] = into + both * st.whole;
+      if (lane == 0) ends[w8] = into + both * st.whole;
       __syncthreads();
-      if (w == 0) {
-        double x = dG[63 - lane];
-        if (lane == 0) x += ((double)ends[0] + ends[1]) + ((double)ends[2] + ends[3]);
+      if (w8 == 0) {
+        double x = dG[0][63 - lane] + (HALVES > 1 ? dG[HALVES - 1][63 - lane] : 0.0);
+        if (lane == 0) {
+#pragma unroll
+          for (int i = 0; i < WAVES; ++i) x += ends[i];
+        }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
           const double before = __shfl_up(x, d);
@@ -730,35 +870,32 @@ __global__ __launch_bounds__(256) void gdr_grads_kernel(GdrArgs a, ard_steps d_o
         const int i = 63 - lane;
         const int64_t t = t0 + i;
         float grad = 0.0f;
-        if (i < live) grad = (float)x * logistic(-ElemTraits<T>::to_f32(((const T*)a.f.p)[t * a.f.t + n * a.f.b + h]));
+        if (i < live) grad = (float)x * logistic(-fg);
         if (i < steps) ((T*)df.p)[t * df.t + n * df.b + h] = ElemTraits<T>::from_f32(grad);
       }
-      if (g == 0 && mine < steps) {
+      if (half == 0 && g == 0 && mine < steps) {
         const int64_t t = t0 + mine;
         float grad = 0.0f;
-        if (mine < live) grad = dw * logistic(-ElemTraits<T>::to_f32(((const T*)a.b.p)[t * a.b.t + n * a.b.b + h]));
+        if (mine < live) grad = dw * logistic(-bg);
         ((T*)db.p)[t * db.t + n * db.b + h] = ElemTraits<T>::from_f32(grad);
       }
-      __syncthreads();
     }
     // through the division by the length
     float kd = 0.0f, qd = 0.0f;
-    const float rkm = a.steps[((int64_t)chunk * a.B + n) * a.H + hk * a.group].rk[mine], rqm = a.steps[((int64_t)chunk * a.B + n) * a.H + hk * a.group].rq[mine];
-    f32x4 kh[RT], qh[RT];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      float kx[4] = {}, qx[4] = {};
-      const int at = rt * 16 + 4 * g;
-      if (mine < live) load_some<4>(kp + at, a.Dk - at, kx), load_some<4>(qp + at, a.Dk - at, qx);
+    for (int i = 0; i < OWN; ++i) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        kh[rt][r] = kx[r] * rkm, qh[rt][r] = qx[r] * rqm;
-        kd = fmaf(kh[rt][r], sumk[rt][r], kd), qd = fmaf(qh[rt][r], sumq[rt][r], qd);
-      }
+      for (int r = 0; r < 4; ++r) kd = fmaf(kx[i].at(r), sumk[i][r], kd), qd = fmaf(qx[i].at(r), sumq[i][r], qd);
     }
     kd = over_rows(kd), qd = over_rows(qd);
+    if (g == 0) dots[0][half][mine] = kd, dots[1][half][mine] = qd;
+    __syncthreads();
+    kd = rkm * rkm * (dots[0][0][mine] + (HALVES > 1 ? dots[0][HALVES - 1][mine] : 0.0f)), qd = rqm * rqm * (dots[1][0][mine] + (HALVES > 1 ? dots[1][HALVES - 1][mine] : 0.0f));
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) sumk[rt] = rkm * (sumk[rt] - kh[rt] * kd), sumq[rt] = rqm * (sumq[rt] - qh[rt] * qd);
+    for (int i = 0; i < OWN; ++i) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sumk[i][r] = rkm * fmaf(-kx[i].at(r), kd, sumk[i][r]), sumq[i][r] = rqm * fmaf(-qx[i].at(r), qd, sumq[i][r]);
+    }
   } else if ((int)threadIdx.x < steps) {
     const int64_t t = t0 + threadIdx.x;
     for (int s = 0; s < a.group; ++s) {
@@ -768,14 +905,19 @@ __global__ __launch_bounds__(256) void gdr_grads_kernel(GdrArgs a, ard_steps d_o
     }
   }
   if (mine >= steps) return;
+  T *dqp = (T*)dq.p + (int64_t)(t0 + mine) * dq.t + n * dq.b + hk * a.Dk, *dkp = (T*)dk.p + (int64_t)(t0 + mine) * dk.t + n * dk.b + hk * a.Dk;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int at = rt * 16 + 4 * g;
+  for (int i = 0; i < OWN; ++i) {
+    const int at = (half * OWN + i) * 16 + 4 * g;
     float x[4], y[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) x[r] = mine < live ? sumq[rt][r] : 0.0f, y[r] = mine < live ? sumk[rt][r] : 0.0f;
-    store_some<4>(dqp + at, a.Dk - at, x);
-    store_some<4>(dkp + at, a.Dk - at, y);
+    for (int r = 0; r < 4; ++r) x[r] = mine < live ? sumq[i][r] : 0.0f, y[r] = mine < live ? sumk[i][r] : 0.0f;
+    if (QUICK) {
+      if (at < a.Dk) store_run<4>(dqp + at, x), store_run<4>(dkp + at, y);
+    } else {
+      store_some<4>(dqp + at, a.Dk - at, x);
+      store_some<4>(dkp + at, a.Dk - at, y);
+    }
   }
 }
 
@@ -801,13 +943,9 @@ static GdrPlan gdr_plan(int32_t dtype, int T, int B, int Hk, int H, int Dk, int 
   };
   const size_t rows = (size_t)4 * (p.dk / 32) * in * 1024, cols = (size_t)(p.dk / 8) * in * 1024;
   take(a.steps, hu * sizeof(Steps64));
-  take(a.kf, ku * rows), take(a.qf, ku * rows), take(a.ktf, ku * cols);
-  take(a.mf, hu * 6 * 3 * 1024);
+  take(a.rows, ku * rows * 2), take(a.cols, ku * cols * (backward ? 2 : 1)), take(a.tri, hu * 6 * (backward ? 9 : 3 + out) * 1024);
   if (backward) {
-    take(a.qtf, ku * cols), take(a.mtf, hu * 6 * 3 * 1024), take(a.ptf, hu * 6 * 3 * 1024);
     take(a.u, hu * kChunk * a.dvp * 4), take(a.dx, hu * kChunk * a.dvp * 4), take(a.ds, hu * p.dk * a.dvp * 4);
-  } else {
-    take(a.pf, hu * 6 * out * 1024);
   }
   p.bytes = at;
   return p;
@@ -876,7 +1014,7 @@ extern "C" int32_t ard_gdr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
   GdrPlan p = gdr_plan(dtype, T, B, Hk, H, Dk, Dv, false, ws);
   if (!few && (!ws || ws_bytes < p.bytes || misaligned(ws, 16))) return fail(ARD_EWORKSPACE, "workspace too small: need %zu bytes, got %zu", p.bytes, ws ? ws_bytes : 0);
   GdrArgs& a = p.a;
-  a.q = in[0], a.k = in[1], a.v = gdr_steps(in[2], T, H * Dv), a.f = in[3], a.b = in[4], a.scale = scale, a.eps = eps, a.len = d_lengths;
+  a.q = gdr_steps(in[0], T, Hk * Dk), a.k = gdr_steps(in[1], T, Hk * Dk), a.v = gdr_steps(in[2], T, H * Dv), a.f = in[3], a.b = in[4], a.scale = scale, a.eps = eps, a.len = d_lengths;
   hipStream_t st = (hipStream_t)stream;
   const ard_steps out = gdr_steps(*o, T, H * Dv);
   return gdr_instance(dtype, p.dk, gdr_near(a.v, Dv) && gdr_near(out, Dv), [&](auto t, auto dk, auto near) {
@@ -909,7 +1047,7 @@ extern "C" int32_t ard_gdr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
   GdrPlan p = gdr_plan(dtype, T, B, Hk, H, Dk, Dv, true, ws);
   if (!ws || ws_bytes < p.bytes || misaligned(ws, 16)) return fail(ARD_EWORKSPACE, "workspace too small: need %zu bytes, got %zu", p.bytes, ws ? ws_bytes : 0);
   GdrArgs& a = p.a;
-  a.q = in[0], a.k = in[1], a.v = gdr_steps(in[2], T, H * Dv), a.f = in[3], a.b = in[4], a.scale = scale, a.eps = eps, a.len = d_lengths;
+  a.q = gdr_steps(in[0], T, Hk * Dk), a.k = gdr_steps(in[1], T, Hk * Dk), a.v = gdr_steps(in[2], T, H * Dv), a.f = in[3], a.b = in[4], a.scale = scale, a.eps = eps, a.len = d_lengths;
   hipStream_t st = (hipStream_t)stream;
   // dX and U are read in whole operands of 32 columns: the wavefronts of the padded columns write them as zeros
   const int slices = a.dvp / 16, waves = B * H * slices;
@@ -924,10 +1062,14 @@ extern "C" int32_t ard_gdr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
     ARD_LAUNCH_CHECK("gdr_rows_kernel");
     ARD_LAUNCH_NAMED("gdr_back_kernel", (gdr_back_kernel<E, DK, NEAR>), dim3(B * H * ceil_div(slices, 4)), dim3(256), 0, st, a, od, dST, dv, dS0, slices);
     ARD_LAUNCH_CHECK("gdr_back_kernel");
-    if (a.dvp == 64)
-      ARD_LAUNCH_NAMED("gdr_grads_kernel", (gdr_grads_kernel<E, DK, 64>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a, od, ckpt, grads[0], grads[1], grads[3], grads[4]);
-    else
-      ARD_LAUNCH_NAMED("gdr_grads_kernel", (gdr_grads_kernel<E, DK, 128>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a, od, ckpt, grads[0], grads[1], grads[3], grads[4]);
+    const auto grads_of = [&](auto dv_, auto quick) {
+      constexpr int DV = decltype(dv_)::value;
+      constexpr bool QUICK = decltype(quick)::value;
+      ARD_LAUNCH_NAMED("gdr_grads_kernel", (gdr_grads_kernel<E, DK, DV, QUICK>), dim3(a.chunks * B * Hk), dim3(DK * 4), 0, st, a, od, ckpt, grads[0], grads[1], grads[3], grads[4]);
+    };
+    const bool quick = Dk % 4 == 0 && Dv % 8 == 0 && gdr_near(a.q, Dk) && gdr_near(a.k, Dk) && gdr_near(od, Dv);
+    if (a.dvp == 64) quick ? grads_of(std::integral_constant<int, 64>{}, std::true_type{}) : grads_of(std::integral_constant<int, 64>{}, std::false_type{});
+    else quick ? grads_of(std::integral_constant<int, 128>{}, std::true_type{}) : grads_of(std::integral_constant<int, 128>{}, std::false_type{});
     ARD_LAUNCH_CHECK("gdr_grads_kernel");
     return (int32_t)ARD_OK;
   });

@@ -9,6 +9,8 @@
 // 8 g + j, the results of two row tiles are the B operand of the next product as they lie in their lane's registers.  So a chain of products
 // with a state, held by columns, stays inside a wavefront, without LDS or barriers.
 #pragma once
+#include <type_traits>
+
 #include "rows.hpp"
 
 namespace ard {
@@ -58,6 +60,19 @@ template <int NA, int NB> __device__ __forceinline__ void mul_add(const Parts<NA
       if (s - i >= 0 && s - i < NB)
         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.p[i]), __builtin_bit_cast(bf16x8, b.p[s - i]), acc, 0, 0, 0);
 }
+// The same of several tiles of rows, in turn: a product waits for the one before it in its own sum, not for the others.
+template <int TILES, int NA, int NB> __device__ __forceinline__ void mul_add(const Parts<NA> (&a)[TILES], const Parts<NB>& b, f32x4 (&acc)[TILES]) {
+  constexpr int L = NA > NB ? NA : NB;
+#pragma unroll
+  for (int s = L - 1; s >= 0; --s)
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+      if (s - i >= 0 && s - i < NB) {
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+          acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[t].p[i]), __builtin_bit_cast(bf16x8, b.p[s - i]), acc[t], 0, 0, 0);
+      }
+}
 // Operands in the workspace, 64 lanes x 16 bytes a part as a lane takes them.
 template <int N> __device__ __forceinline__ Parts<N> load_parts(const u32x4* base, int frag) {
   Parts<N> s;
@@ -65,24 +80,46 @@ template <int N> __device__ __forceinline__ Parts<N> load_parts(const u32x4* bas
   for (int n = 0; n < N; ++n) s.p[n] = base[(frag * N + n) * 64 + (threadIdx.x & 63)];
   return s;
 }
+// of TILES tiles of rows, `step` operands from one to the next
+template <int TILES, int N> __device__ __forceinline__ void load_parts(const u32x4* base, int first, int step, Parts<N> (&s)[TILES]) {
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) s[t] = load_parts<N>(base, first + t * step);
+}
 template <int N> __device__ __forceinline__ void store_parts(u32x4* base, int frag, const Parts<N>& s) {
 #pragma unroll
   for (int n = 0; n < N; ++n) base[(frag * N + n) * 64 + (threadIdx.x & 63)] = s.p[n];
 }
-// `frags` x 1 KB from global memory to the same order in LDS, dealt to a workgroup's four wavefronts, without a register in between.
-__device__ __forceinline__ void stage(const u32x4* from, u32x4* lds, int frags, int wave) {
-  const int lane = threadIdx.x & 63;
+// FRAGS x 1 KB from global memory to the same order in LDS, without a register in between: each of a workgroup's four wavefronts its share of
+// neighbours, four to an address.
+template <int FRAGS> __device__ __forceinline__ void stage(const u32x4* from, u32x4* lds, int wave) {
+  constexpr int PER = (FRAGS + 3) / 4;
+  const u32x4* src = from + wave * PER * 64 + (threadIdx.x & 63);
+  u32x4* dst = lds + wave * PER * 64;
+#define ARD_GDR_STAGE(i, offset)                                                                                                   \
+  if ((i) < PER && (FRAGS % 4 == 0 || wave * PER + (i) < FRAGS))                                                                     \
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(src + ((i) - offset) * 64),                   \
+                                   (__attribute__((address_space(3))) uint32_t*)(dst + ((i) - offset) * 64), 16, offset * 1024, 0)
 #pragma unroll
-  for (int i = 0; i < (frags + 3) / 4; ++i) {
-    const int j = i * 4 + wave;
-    if (j < frags)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(from + j * 64 + lane), (__attribute__((address_space(3))) uint32_t*)(lds + j * 64), 16, 0, 0);
+  for (int i = 0; i < PER; i += 4) {
+    ARD_GDR_STAGE(i, 0);
+    ARD_GDR_STAGE(i + 1, 1);
+    ARD_GDR_STAGE(i + 2, 2);
+    ARD_GDR_STAGE(i + 3, 3);
   }
+#undef ARD_GDR_STAGE
 }
-// all of this wavefront's loads and stores have ended, and every wavefront's
-__device__ __forceinline__ void all_landed() {
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
+// All of this wavefront's loads have ended but what came behind its last `later` accesses (a wavefront's accesses end in their order; the stores of a
+// half chunk take longer than what was staged before them), and every wavefront's.
+template <int LATER> __device__ __forceinline__ void all_landed() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LATER) : "memory");
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+}
+// nothing moves past this: accesses are counted from here on
+__device__ __forceinline__ void staged() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
 }
 // Operands of a lower triangular 64 x 64 matrix: six tiles of 16 rows x 32 columns are not all zeros; of its transpose likewise.
 __host__ __device__ constexpr int lower_frag(int rt, int kb) { return rt < 2 ? rt : 2 * rt - 2 + kb; }
@@ -96,8 +133,9 @@ struct Steps64 {
   float rk[kChunk], rq[kChunk];
   float w[kChunk], ka[kChunk], qa[kChunk], ke[kChunk];  // w, rk since, scale rq since, rk still: what the passes over the states read, 1 KB
   float whole;          // exp(G_last)
-  float pad[7];
+  float pad[127];
 };
+static_assert(sizeof(Steps64) == 3 * 1024, "it goes to LDS in whole KB");
 
 struct GdrArgs {
   int T, B, Hk, H, Dk, Dv, group, chunks;
@@ -105,7 +143,7 @@ struct GdrArgs {
   float scale, eps;
   const int32_t* len;
   // workspace: operands by (chunk, sequence, key head) and by (chunk, sequence, head)
-  u32x4 *kf, *qf, *ktf, *qtf, *mf, *pf, *mtf, *ptf;
+  u32x4 *rows, *cols, *tri;  // K and Q; their transposes (Q's for the backward pass); M and P, or M and the transposes of M and P
   Steps64* steps;
   float *u, *dx, *ds;  // [64][dvp], [64][dvp], [dkp][dvp] of a chunk
   int dvp;
@@ -120,6 +158,8 @@ template <> struct GdrType<float> {
   static constexpr int IN = 3, OUT = 3;
 };
 
+// exp(x), x <= 0: the argument's rounding costs |x| 2^-24 of it, and |x| < 104 where it is not 0
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 __device__ __forceinline__ float logistic(float x) {
   const float e = expf(-fabsf(x));
   return x >= 0.0f ? 1.0f / (1.0f + e) : e / (1.0f + e);
