@@ -11,6 +11,8 @@
 // A first launch, over all chunks at once, makes what does not depend on the states: A, P, M (blocks of 16 by substitution, the rest by
 // fp32 matrix instructions), written as operands of the second.  The second walks the chunks; a wavefront holds 16 or 32 columns of S in registers and
 // needs no other's: everything a chunk does to a column is a chain of products in its own registers (gdr.hpp).
+#include <type_traits>
+
 #include "gdr.hpp"
 
 namespace ard {
@@ -286,12 +288,14 @@ template <typename T, bool NEAR> struct Window {
       rows -= 4 * g;
     }
   }
-  __device__ __forceinline__ float load(int rt, int r) const {
+  // as it is stored (T's bits): what is made of it has to wait for it
+  __device__ __forceinline__ uint32_t load(int rt, int r) const {
     const int i = rt * 16 + r;
-    if constexpr (!NEAR) return on && i < rows ? ElemTraits<T>::to_f32(p[i * step]) : 0.0f;
-    else if constexpr (sizeof(T) == 2) return bf16_bits_to_f32(__builtin_amdgcn_raw_buffer_load_b16(buffer, at[r] + rt * tile, 0, 0));
-    else return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer, at[r] + rt * tile, 0, 0));
+    if constexpr (!NEAR) return on && i < rows ? __builtin_bit_cast(std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t>, p[i * step]) : 0u;
+    else if constexpr (sizeof(T) == 2) return __builtin_amdgcn_raw_buffer_load_b16(buffer, at[r] + rt * tile, 0, 0);
+    else return __builtin_amdgcn_raw_buffer_load_b32(buffer, at[r] + rt * tile, 0, 0);
   }
+  __device__ __forceinline__ static float value(uint32_t bits) { return __uint_as_float(sizeof(T) == 2 ? bits << 16 : bits); }
   __device__ __forceinline__ void store(int rt, int r, float x) const {
     const int i = rt * 16 + r;
     if constexpr (!NEAR) {
@@ -307,7 +311,23 @@ template <int TILES, typename W> __device__ __forceinline__ void load_tiles(cons
 #pragma unroll
   for (int rt = 0; rt < TILES; ++rt)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) S[rt][r] = w.load(rt, r);
+    for (int r = 0; r < 4; ++r) S[rt][r] = W::value(w.load(rt, r));
+}
+// a chunk's rows as they are stored, and their values
+struct RawRows {
+  uint32_t v[4][4];
+};
+template <typename W> __device__ __forceinline__ void load_raw(const W& w, RawRows& x) {
+#pragma unroll
+  for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x.v[rt][r] = w.load(rt, r);
+}
+template <typename W> __device__ __forceinline__ void values_of_rows(const RawRows& x, f32x4 (&S)[4]) {
+#pragma unroll
+  for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) S[rt][r] = W::value(x.v[rt][r]);
 }
 template <int TILES, typename W> __device__ __forceinline__ void store_tiles(const W& w, const f32x4 (&S)[TILES]) {
 #pragma unroll
@@ -383,11 +403,12 @@ template <int IN, int DK> __device__ __forceinline__ void add_outer(const u32x4*
 // Four wavefronts with columns of one head walk its chunks.  They share the operands in LDS, in two groups: what the first half of a
 // chunk reads is loaded for the next chunk while the second half is worked on, and the other way about.  Operands that LDS does not hold
 // (fp32, wide heads) are read from the caches.
-template <typename T, int DK, bool NEAR>
+// KEPT: the states before the chunks are stored, in ckpt.
+template <typename T, int DK, bool NEAR, bool KEPT>
 __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt, int slices) {
   constexpr int IN = GdrType<T>::IN, OUT = GdrType<T>::OUT, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3, PF = 6 * OUT;
   constexpr bool STAGED = 2 * KF + KTF + MF + PF <= 150;  // KB of LDS
-  __shared__ u32x4 lds[STAGED ? (2 * KF + KTF + MF + PF) * 64 : 1];
+  __shared__ u32x4 one[STAGED ? 2 * KF * 64 : 1], two[STAGED ? (KTF + MF + PF) * 64 : 1];  // what the halves read
   __shared__ f32x4 weights[2][64];  // w, ka, qa, ke of a chunk
   const Columns at(a, slices);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -400,19 +421,25 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
   const T* vp = (const T*)a.v.p + at.n * a.v.b + at.h * a.Dv;
   T* op = (T*)o.p + at.n * o.b + at.h * a.Dv;
   float* kept = ckpt + at.unit * matrix;
+  RawRows next;
+  f32x4 sw;  // the chunk's weights, which go to LDS by way of a register: loads straight into an array let every later read of it wait for them
+  float next_whole = 0.0f;
+  int zero = 0;
+  asm volatile("" : "+v"(zero));  // (a vector load: one by the scalar unit would let every read of LDS wait for it)
   const auto first_half = [&](int chunk) {  // loads of what it reads
-    if (STAGED) stage<2 * KF>(a.rows + ku(chunk) * (2 * KF * 64), lds, wave);
-    if (wave == 0) stage<4>((const u32x4*)a.steps[hu(chunk)].w, (u32x4*)weights[chunk & 1], 0);
-    load_tiles(Window<T, NEAR>(vp, a.v.t, imin(all - chunk * kChunk, kChunk), a.Dv, at.first), v);
-    vp += kChunk * a.v.t;
+    if (STAGED) stage<2 * KF>(a.rows + ku(chunk) * (2 * KF * 64), one, wave);
+    sw = *reinterpret_cast<const f32x4*>(a.steps[hu(chunk)].w + (threadIdx.x & 63) * 4);
+    load_raw(Window<T, NEAR>(vp + (int64_t)chunk * kChunk * a.v.t, a.v.t, imin(all - chunk * kChunk, kChunk), a.Dv, at.first), next);
+    next_whole = (&a.steps[hu(chunk)].whole)[zero];
   };
   const auto second_half = [&](int chunk) {
-    if (STAGED) stage<KTF>(a.cols + ku(chunk) * (KTF * 64), lds + 2 * KF * 64, wave), stage<MF + PF>(a.tri + hu(chunk) * ((MF + PF) * 64), lds + (2 * KF + KTF) * 64, wave);
+    if (STAGED) stage<KTF>(a.cols + ku(chunk) * (KTF * 64), two, wave), stage<MF + PF>(a.tri + hu(chunk) * ((MF + PF) * 64), two + KTF * 64, wave);
   };
   constexpr int COUNT = STAGED && NEAR;  // (elsewhere accesses are not counted: all are waited for)
   if (chunks) {
     first_half(0);
     staged();
+    weights[0][threadIdx.x & 63] = sw;
     all_landed<0>();
     second_half(0);
     staged();
@@ -420,10 +447,11 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
   for (int chunk = 0; chunk < chunks; ++chunk) {
     const int steps = imin(a.T - chunk * kChunk, kChunk), live = imin(all - chunk * kChunk, steps);
     const float *w = (const float*)weights[chunk & 1], *ka = w + kChunk, *qa = w + 2 * kChunk, *ke = w + 3 * kChunk;
-    const u32x4 *rows = STAGED ? lds : a.rows + ku(chunk) * (2 * KF * 64), *cols = STAGED ? lds + 2 * KF * 64 : a.cols + ku(chunk) * (KTF * 64),
-                *tri = STAGED ? lds + (2 * KF + KTF) * 64 : a.tri + hu(chunk) * ((MF + PF) * 64);
-    const float whole = a.steps[hu(chunk)].whole;
-    if (ckpt) {
+    const u32x4 *rows = STAGED ? one : a.rows + ku(chunk) * (2 * KF * 64), *cols = STAGED ? two : a.cols + ku(chunk) * (KTF * 64),
+                *tri = STAGED ? two + KTF * 64 : a.tri + hu(chunk) * ((MF + PF) * 64);
+    const float whole = next_whole;
+    values_of_rows<Window<T, NEAR>>(next, v);
+    if (KEPT) {
       store_tiles(StateWindow(kept, a.Dv, a.Dk, a.Dv, at.first), S);
       kept += plane;
     }
@@ -441,9 +469,8 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
 #pragma unroll
       for (int rt = 0; rt < 4; ++rt) y[rt] *= row_weights(qa, rt);
     }
-    if (ckpt) all_landed<COUNT * (DK / 4)>();
-    else all_landed<0>();
-    if (chunk + 1 < chunks) first_half(chunk + 1);
+    all_landed<KEPT * COUNT * (DK / 4)>();
+    first_half(imin(chunk + 1, chunks - 1));  // (behind the last chunk its own once more: accesses that are counted are made on every way)
     staged();
     {
       Parts<3> xp[2];
@@ -455,18 +482,20 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
       column_parts<OUT>(u, up);
       triangle<false, OUT>(tri + MF * 64, up, y);
     }
+    weights[(chunk + 1) & 1][threadIdx.x & 63] = sw;  // (waits for all accesses: in front of the stores)
     store_live(Window<T, NEAR>(op, o.t, steps, a.Dv, at.first), live, y);
     op += kChunk * o.t;
 #pragma unroll
     for (int rt = 0; rt < DK / 16; ++rt) S[rt] *= whole;
     add_outer<IN, DK>(cols, ke, 1.0f, u, S);
     all_landed<COUNT * 16>();
-    if (chunk + 1 < chunks) second_half(chunk + 1);
+    second_half(imin(chunk + 1, chunks - 1));
     staged();
   }
+  all_landed<0>();  // (nothing may arrive in LDS once the wavefront has ended)
   for (int chunk = chunks; chunk < a.chunks; ++chunk) {  // behind the sequence's end
     const f32x4 none[4] = {};
-    if (ckpt) store_tiles(StateWindow(kept, a.Dv, a.Dk, a.Dv, at.first), S);
+    if (KEPT) store_tiles(StateWindow(kept, a.Dv, a.Dk, a.Dv, at.first), S);
     store_tiles(Window<T, NEAR>(op, o.t, imin(a.T - chunk * kChunk, kChunk), a.Dv, at.first), none);
     kept += plane, op += kChunk * o.t;
   }
@@ -513,7 +542,7 @@ template <typename T, int DK, bool NEAR>
 __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o, const float* dST, ard_steps dv, float* dS0, int slices) {
   constexpr int IN = GdrType<T>::IN, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3;
   constexpr bool STAGED = KF + 2 * KTF + 2 * MF <= 150;
-  __shared__ u32x4 lds[STAGED ? (KF + 2 * KTF + 2 * MF) * 64 : 1];
+  __shared__ u32x4 one[STAGED ? (KF + MF) * 64 : 1], two[STAGED ? (2 * KTF + MF) * 64 : 1];
   __shared__ f32x4 weights[2][64];  // w, ka, qa, ke of a chunk
   const Columns at(a, slices);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -525,13 +554,19 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
   const auto hu = [&](int chunk) { return (int64_t)((chunk * a.B + at.n) * a.H + at.h); };
   const T* gp = (const T*)d_o.p + at.n * d_o.b + at.h * a.Dv;
   T* vp = (T*)dv.p + at.n * dv.b + at.h * a.Dv;
+  RawRows next;
+  f32x4 sw;
+  float next_whole = 0.0f;
+  int zero = 0;
+  asm volatile("" : "+v"(zero));
   const auto first_half = [&](int chunk) {
-    if (STAGED) stage<KF>(a.rows + ku(chunk) * (2 * KF * 64), lds, wave), stage<MF>(a.tri + hu(chunk) * (3 * MF * 64) + 2 * MF * 64, lds + KF * 64, wave);
-    if (wave == 0) stage<4>((const u32x4*)a.steps[hu(chunk)].w, (u32x4*)weights[chunk & 1], 0);
-    load_tiles(Window<T, NEAR>(gp + (int64_t)chunk * kChunk * d_o.t, d_o.t, imin(all - chunk * kChunk, kChunk), a.Dv, at.first), x);
+    if (STAGED) stage<KF>(a.rows + ku(chunk) * (2 * KF * 64), one, wave), stage<MF>(a.tri + hu(chunk) * (3 * MF * 64) + 2 * MF * 64, one + KF * 64, wave);
+    sw = *reinterpret_cast<const f32x4*>(a.steps[hu(chunk)].w + (threadIdx.x & 63) * 4);
+    load_raw(Window<T, NEAR>(gp + (int64_t)chunk * kChunk * d_o.t, d_o.t, imin(all - chunk * kChunk, kChunk), a.Dv, at.first), next);
+    next_whole = (&a.steps[hu(chunk)].whole)[zero];
   };
   const auto second_half = [&](int chunk) {
-    if (STAGED) stage<MF>(a.tri + hu(chunk) * (3 * MF * 64) + MF * 64, lds + (KF + MF) * 64, wave), stage<2 * KTF>(a.cols + ku(chunk) * (2 * KTF * 64), lds + (KF + 2 * MF) * 64, wave);
+    if (STAGED) stage<MF>(a.tri + hu(chunk) * (3 * MF * 64) + MF * 64, two, wave), stage<2 * KTF>(a.cols + ku(chunk) * (2 * KTF * 64), two + MF * 64, wave);
   };
   for (int chunk = chunks; chunk < a.chunks; ++chunk) {  // behind the sequence's end
     const f32x4 none[4] = {};
@@ -541,6 +576,7 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
   if (chunks) {
     first_half(chunks - 1);
     staged();
+    weights[(chunks - 1) & 1][threadIdx.x & 63] = sw;
     all_landed<0>();
     second_half(chunks - 1);
     staged();
@@ -548,9 +584,10 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
   for (int chunk = chunks - 1; chunk >= 0; --chunk) {
     const int steps = imin(a.T - chunk * kChunk, kChunk), live = imin(all - chunk * kChunk, steps);
     const float *w = (const float*)weights[chunk & 1], *ka = w + kChunk, *qa = w + 2 * kChunk, *ke = w + 3 * kChunk;
-    const u32x4 *kf = STAGED ? lds : a.rows + ku(chunk) * (2 * KF * 64), *cols = STAGED ? lds + (KF + 2 * MF) * 64 : a.cols + ku(chunk) * (2 * KTF * 64),
-                *ptf = STAGED ? lds + KF * 64 : a.tri + hu(chunk) * (3 * MF * 64) + 2 * MF * 64, *mtf = STAGED ? lds + (KF + MF) * 64 : a.tri + hu(chunk) * (3 * MF * 64) + MF * 64;
-    const float whole = a.steps[hu(chunk)].whole;
+    const u32x4 *kf = STAGED ? one : a.rows + ku(chunk) * (2 * KF * 64), *cols = STAGED ? two + MF * 64 : a.cols + ku(chunk) * (2 * KTF * 64),
+                *ptf = STAGED ? one + KF * 64 : a.tri + hu(chunk) * (3 * MF * 64) + 2 * MF * 64, *mtf = STAGED ? two : a.tri + hu(chunk) * (3 * MF * 64) + MF * 64;
+    const float whole = next_whole;
+    values_of_rows<Window<T, NEAR>>(next, x);
     store_tiles(StateWindow(a.ds + hu(chunk) * DK * a.dvp, a.dvp, DK, a.dvp, at.first), S);
     f32x4 y[4] = {}, dx[4] = {}, od[4];
     {
@@ -573,7 +610,7 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt) od[rt] = x[rt];
     all_landed<COUNT * (DK / 4)>();
-    if (chunk > 0) first_half(chunk - 1);
+    first_half(imax(chunk - 1, 0));
     staged();
     {
       Parts<3> p[2];
@@ -582,6 +619,7 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
     }
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt) y[rt] = row_weights(w, rt) * dx[rt];
+    weights[(chunk + 1) & 1][threadIdx.x & 63] = sw;
     store_tiles(StateWindow(a.dx + hu(chunk) * kChunk * a.dvp, a.dvp, kChunk, a.dvp, at.first), dx);
     store_live(Window<T, NEAR>(vp + (int64_t)chunk * kChunk * dv.t, dv.t, steps, a.Dv, at.first), live, y);
 #pragma unroll
@@ -589,9 +627,10 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
     add_outer<IN, DK>(cols + KTF * 64, qa, 1.0f, od, S);
     add_outer<IN, DK>(cols, ka, -1.0f, y, S);
     all_landed<COUNT * 32>();
-    if (chunk > 0) second_half(chunk - 1);
+    second_half(imax(chunk - 1, 0));
     staged();
   }
+  all_landed<0>();
   if (dS0) store_tiles(StateWindow(dS0 + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
 }
 
@@ -1028,7 +1067,9 @@ extern "C" int32_t ard_gdr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
     }
     ARD_LAUNCH_NAMED("gdr_prep_kernel", (gdr_prep_kernel<E, DK, false>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a);
     ARD_LAUNCH_CHECK("gdr_prep_kernel");
-    ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR>), dim3(B * H * ceil_div(p.slices, 4)), dim3(256), 0, st, a, S0, out, ST, ckpt, p.slices);
+    const dim3 grid(B * H * ceil_div(p.slices, 4));
+    if (ckpt) ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, true>), grid, dim3(256), 0, st, a, S0, out, ST, ckpt, p.slices);
+    else ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, false>), grid, dim3(256), 0, st, a, S0, out, ST, ckpt, p.slices);
     ARD_LAUNCH_CHECK("gdr_fwd_kernel");
     return (int32_t)ARD_OK;
   });

@@ -91,12 +91,22 @@ template <int N> __device__ __forceinline__ void store_parts(u32x4* base, int fr
 }
 // FRAGS x 1 KB from global memory to the same order in LDS, without a register in between: each of a workgroup's four wavefronts its share of
 // neighbours, four to an address.
+// (The last wavefront's share may reach behind the end: it takes the last operand again, so that every wavefront makes as many accesses.)
 template <int FRAGS> __device__ __forceinline__ void stage(const u32x4* from, u32x4* lds, int wave) {
   constexpr int PER = (FRAGS + 3) / 4;
+  if constexpr (FRAGS % 4 != 0) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int j = imin(wave * PER + i, FRAGS - 1);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(from + j * 64 + (threadIdx.x & 63)), (__attribute__((address_space(3))) uint32_t*)(lds + j * 64),
+                                       16, 0, 0);
+    }
+    return;
+  }
   const u32x4* src = from + wave * PER * 64 + (threadIdx.x & 63);
   u32x4* dst = lds + wave * PER * 64;
 #define ARD_GDR_STAGE(i, offset)                                                                                                   \
-  if ((i) < PER && (FRAGS % 4 == 0 || wave * PER + (i) < FRAGS))                                                                     \
+  if ((i) < PER)                                                                                                                     \
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(src + ((i) - offset) * 64),                   \
                                    (__attribute__((address_space(3))) uint32_t*)(dst + ((i) - offset) * 64), 16, offset * 1024, 0)
 #pragma unroll
@@ -111,9 +121,10 @@ template <int FRAGS> __device__ __forceinline__ void stage(const u32x4* from, u3
 // All of this wavefront's loads have ended but what came behind its last `later` accesses (a wavefront's accesses end in their order; the stores of a
 // half chunk take longer than what was staged before them), and every wavefront's.
 template <int LATER> __device__ __forceinline__ void all_landed() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LATER) : "memory");
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((LATER & 15) | (LATER >> 4) << 14 | 0x70);  // vmcnt(LATER) lgkmcnt(0)
   __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
 // nothing moves past this: accesses are counted from here on
