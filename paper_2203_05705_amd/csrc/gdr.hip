@@ -507,9 +507,11 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
 //   dX = M^T (P^T dO + still K dS'),  dV = w dX,  dS = exp(G_last) dS' + scale Q^T (since dO) - K^T (since w dX)
 //   dA = -E (j < i),  dP = F (j <= i), and with N_ij = -E_ij w_i Gamma_ij, R_ij = F_ij scale Gamma_ij:
 //   dQ_i = scale since_i S dO_i + sum_j R_ij K_j
-//   dK_i = [sum_j N_ij K_j - w_i since_i S dX_i] + [sum_j N_ji K_j + sum_j R_ji Q_j + still_i dS' U_i]      = dK+ + dK-
+//   dK_i = sum_j N_ij K_j - w_i since_i S dX_i + sum_j N_ji K_j + sum_j R_ji Q_j + still_i dS' U_i
 //   dw_i / w_i = E_ii  (dX_i . X_i less what A's own w_i takes back; no division by a small w)
-//   d log(a_t) = the sum over i >= t of Q_i.dQ_i + K_i.dK+_i - K_i.dK-_i, and of what G_last moves: sum_i still_i K_i.dS' U_i + exp(G_last) <S, dS'>
+//   d log(a_t) = sum_{i >= t > j} (N_ij K_i.K_j + R_ij Q_i.K_j) + sum_{i >= t} (scale since_i Q_i.S dO_i - w_i since_i K_i.S dX_i)
+//                + sum_{j < t} still_j K_j.dS' U_j + exp(G_last) <S, dS'>,
+// terms that all have a_t as a factor (as differences of sums over i and over j, K.dK and Q.dQ, a step that forgets all would be left with their rounding).
 // Three launches after the first: U of every chunk from the states kept; the chunks from the last to the first, which leaves dX and dS' of each; and
 // all other gradients, every chunk for itself.
 
@@ -698,8 +700,9 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
   constexpr int ROWS = 4 * VB * (2 * N + IN), STATE = RT * VB * N;
   constexpr bool KEEP = ROWS + STATE <= 152;
   __shared__ u32x4 lds[(KEEP ? ROWS + STATE : ROWS > STATE ? ROWS : STATE) * 64];
-  __shared__ double dG[HALVES][kChunk];
+  __shared__ double dG[HALVES][2][kChunk];
   __shared__ float ends[WAVES], dots[2][HALVES][kChunk];
+  __shared__ float crossing[WAVES][kChunk];
   __shared__ Steps64 st;
   u32x4 *lu = lds, *lx = lds + 4 * VB * N * 64, *lo = lds + 8 * VB * N * 64, *ls = KEEP ? lds + ROWS * 64 : lds;
   const int unit = blockIdx.x, chunk = unit / (a.B * a.Hk), n = (unit - chunk * a.B * a.Hk) / a.Hk, hk = unit % a.Hk;
@@ -716,7 +719,7 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
       keys.load(mine, at, x), queries.load(mine, at, y);
       kx[i].set(x), qx[i].set(y);
     }
-    const u32x4 *ktf = a.cols + (int64_t)unit * (DK / 4) * IN * 64, *qtf = ktf + DK / 8 * IN * 64;
+    const u32x4 *ktf = a.cols + (int64_t)unit * (DK / 4) * IN * 64, *qtf = ktf + DK / 8 * IN * 64, *rows = a.rows + (int64_t)unit * (DK / 4) * IN * 64;
     const Steps64& any = a.steps[((int64_t)chunk * a.B + n) * a.H + hk * a.group];
     const float rkm = any.rk[mine], rqm = any.rq[mine];
     for (int s = 0; s < a.group; ++s) {
@@ -782,17 +785,20 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
         f32x4 dn[4] = {}, dnq[4] = {}, up[4] = {}, upq[4] = {};
 #pragma unroll
         for (int vb = 0; vb < VB; ++vb) {
-          const Parts<N> u = of_u(vb), x = of_x(vb);
-          const Parts<IN> o = of_o(vb);
           Parts<N> y[4];
-          Parts<IN> z[4];
-          load_parts(lx, vb, VB, y);
-          mul_add(y, u, dn);
-          load_parts(lo, vb, VB, z);
-          mul_add(z, u, dnq);
+          {
+            Parts<IN> z[4];
+            const Parts<N> u = of_u(vb);
+            load_parts(lx, vb, VB, y);
+            mul_add(y, u, dn);
+            load_parts(lo, vb, VB, z);
+            mul_add(z, u, dnq);
+          }
+          __builtin_amdgcn_sched_barrier(0);  // (operands read further ahead would not fit the registers)
           load_parts(lu, vb, VB, y);
-          mul_add(y, x, up);
-          mul_add(y, o, upq);
+          mul_add(y, of_x(vb), up);
+          mul_add(y, of_o(vb), upq);
+          __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt) {
@@ -806,6 +812,36 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
             dnq[rt][r] = i >= mine ? dnq[rt][r] * (a.scale * rq[r] * fade) : 0.0f;
             up[rt][r] = i < mine ? -up[rt][r] * (wm * rk[r] * fade) : 0.0f;
             upq[rt][r] = i <= mine ? upq[rt][r] * (a.scale * rk[r] * fade) : 0.0f;
+          }
+        }
+        // what the pairs (i, the lane's step j) give to every step from behind j up to i: of two halves the first takes N, the second R
+        f32x4 cross[4] = {};
+#pragma unroll
+        for (int which = 0; which < 2; ++which)
+          if (HALVES == 1 || half == which) {
+            f32x4 dots[4] = {};
+#pragma unroll
+            for (int kb = 0; kb < DK / 32; ++kb) {
+              Parts<IN> m[4];
+              load_parts(rows + which * (DK / 8) * IN * 64, kb, DK / 32, m);
+              mul_add(m, load_parts<IN>(rows, w * (DK / 32) + kb), dots);
+            }
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) cross[rt] += (which ? dnq[rt] : dn[rt]) * dots[rt];
+          }
+        float behind = 0.0f;  // of later tiles of rows
+#pragma unroll
+        for (int rt = 3; rt >= 0; --rt) {
+          f32x4 x = cross[rt] * rkm;
+          x[2] += x[3], x[1] += x[2], x[0] += x[1];
+          const float whole = x[0], n1 = __shfl_down(whole, 16), n2 = __shfl_down(whole, 32), n3 = __shfl_down(whole, 48);
+          const float later = behind + ((g < 3 ? n1 : 0.0f) + (g < 2 ? n2 : 0.0f) + (g < 1 ? n3 : 0.0f));
+          behind += over_rows(whole);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int t = rt * 16 + 4 * g + r;
+            const float sum = row_sum(t > mine ? x[r] + later : 0.0f);
+            if (c == 0) crossing[w8][t] = sum;
           }
         }
 #pragma unroll
@@ -836,7 +872,13 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
           mul_add(y, x, tp);
         }
 #pragma unroll
-        for (int i = 0; i < OWN; ++i) tq[i] *= a.scale * since, tp[i] *= -wm * since;
+        for (int i = 0; i < OWN; ++i) {
+          tq[i] *= a.scale * since, tp[i] *= -wm * since;
+          float mk = 0.0f, mq = 0.0f;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) mk = fmaf(kx[i].at(r), tp[i][r], mk), mq = fmaf(qx[i].at(r), tq[i][r], mq);
+          moved += rkm * mk + rqm * mq;
+        }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
           Parts<IN> k[OWN];
@@ -845,13 +887,7 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
           mul_add(k, aboveq[kb], tq);
         }
 #pragma unroll
-        for (int i = 0; i < OWN; ++i) {
-          float mk = 0.0f, mq = 0.0f;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) mk = fmaf(kx[i].at(r), tp[i][r], mk), mq = fmaf(qx[i].at(r), tq[i][r], mq);
-          moved += rkm * mk + rqm * mq;
-          sumq[i] += tq[i], sumk[i] += tp[i];
-        }
+        for (int i = 0; i < OWN; ++i) sumq[i] += tq[i], sumk[i] += tp[i];
       }
       __syncthreads();
 #pragma unroll
@@ -881,31 +917,32 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
         }
 #pragma unroll
         for (int i = 0; i < OWN; ++i) {
-          float me = 0.0f, mm = 0.0f;
+          float me = 0.0f;
           te[i] *= still;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) me = fmaf(kx[i].at(r), te[i][r], me), mm = fmaf(kx[i].at(r), tm[i][r], mm);
-          into += rkm * me, moved -= rkm * mm;
+          for (int r = 0; r < 4; ++r) me = fmaf(kx[i].at(r), te[i][r], me);
+          into += rkm * me;
           sumk[i] += te[i] + tm[i];
         }
       }
       dw = over_rows(dw), moved = over_rows(moved), into = over_rows(into);
       both = wave_sum(both);
-      if (g == 0) dG[half][mine] = (double)moved - (double)into;
-      into = row_sum(into);
-      if (lane == 0) ends[w8] = into + both * st.whole;
+      if (g == 0) dG[half][0][mine] = moved, dG[half][1][mine] = into;
+      if (lane == 0) ends[w8] = both * st.whole;
       __syncthreads();
       if (w8 == 0) {
-        double x = dG[0][63 - lane] + (HALVES > 1 ? dG[HALVES - 1][63 - lane] : 0.0);
-        if (lane == 0) {
-#pragma unroll
-          for (int i = 0; i < WAVES; ++i) x += ends[i];
-        }
+        // lane t' = 63 - t: what later steps read, and what earlier ones wrote
+        double x = dG[0][0][63 - lane], y = lane < 63 ? dG[0][1][62 - lane] : 0.0;
+        if (HALVES > 1) x += dG[HALVES - 1][0][63 - lane], y += lane < 63 ? dG[HALVES - 1][1][62 - lane] : 0.0;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
-          const double before = __shfl_up(x, d);
+          const double before = __shfl_up(x, d), after = __shfl_down(y, d);
           if (lane >= d) x += before;
+          if (lane + d < 64) y += after;
         }
+        x += y;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) x += (double)ends[i] + (double)crossing[i][63 - lane];
         const int i = 63 - lane;
         const int64_t t = t0 + i;
         float grad = 0.0f;
@@ -933,7 +970,11 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sumk[i][r] = rkm * fmaf(-kx[i].at(r), kd, sumk[i][r]), sumq[i][r] = rqm * fmaf(-qx[i].at(r), qd, sumq[i][r]);
+      for (int r = 0; r < 4; ++r) {
+        // (of a single element only eps is left of 1 - kh^2, which a difference would lose)
+        sumk[i][r] = rkm * (a.Dk == 1 ? a.eps * rkm * rkm * sumk[i][r] : fmaf(-kx[i].at(r), kd, sumk[i][r]));
+        sumq[i][r] = rqm * (a.Dk == 1 ? a.eps * rqm * rqm * sumq[i][r] : fmaf(-qx[i].at(r), qd, sumq[i][r]));
+      }
     }
   } else if ((int)threadIdx.x < steps) {
     const int64_t t = t0 + threadIdx.x;
