@@ -131,7 +131,7 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void g
   f32x4 kk[4] = {}, qk[4] = {};
   {
     constexpr int KF = 4 * KB * IN, KTF = DK / 8 * IN;
-    u32x4 *kf = a.rows + (int64_t)unit * 2 * KF * 64, *qf = kf + KF * 64;
+    u32x4 *kf = a.rows + (int64_t)unit * 2 * KF * 64 + lane, *qf = kf + KF * 64;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       const Parts<IN> ka = row_parts<IN>(sh.k, w * 16 + c, kb, g), qa = row_parts<IN>(sh.q, w * 16 + c, kb, g);
@@ -145,7 +145,7 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void g
           mul_add(qa, b, qk[ct]);
         }
     }
-    u32x4 *ktf = a.cols + (int64_t)unit * (BWD ? 2 : 1) * KTF * 64, *qtf = ktf + KTF * 64;
+    u32x4 *ktf = a.cols + (int64_t)unit * (BWD ? 2 : 1) * KTF * 64 + lane, *qtf = ktf + KTF * 64;
     for (int i = w; i < DK / 8; i += 4) {
       store_parts(ktf, i, col_parts<IN>(sh.k, (i >> 1) * 16 + c, i & 1, g));
       if (BWD) store_parts(qtf, i, col_parts<IN>(sh.q, (i >> 1) * 16 + c, i & 1, g));
@@ -230,7 +230,7 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void g
     }
     __syncthreads();
     constexpr int PP = BWD ? 3 : OUT;
-    u32x4 *mf = a.tri + out * (BWD ? 54 : 18 + 6 * OUT) * 64, *pf = mf + 18 * 64, *mtf = mf + 18 * 64, *ptf = mf + 36 * 64;
+    u32x4 *mf = a.tri + out * (BWD ? 54 : 18 + 6 * OUT) * 64 + lane, *pf = mf + 18 * 64, *mtf = mf + 18 * 64, *ptf = mf + 36 * 64;
     for (int i = w; i < 6; i += 4) {
       const int rt = i < 2 ? i : 1 + i / 2, kb = i < 2 ? 0 : i & 1;  // (lower_frag's)
       store_parts(mf, i, row_parts<3>(sh.M, rt * 16 + c, kb, g));
@@ -447,8 +447,9 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
   for (int chunk = 0; chunk < chunks; ++chunk) {
     const int steps = imin(a.T - chunk * kChunk, kChunk), live = imin(all - chunk * kChunk, steps);
     const float *w = (const float*)weights[chunk & 1], *ka = w + kChunk, *qa = w + 2 * kChunk, *ke = w + 3 * kChunk;
-    const u32x4 *rows = STAGED ? one : a.rows + ku(chunk) * (2 * KF * 64), *cols = STAGED ? two : a.cols + ku(chunk) * (KTF * 64),
-                *tri = STAGED ? two + KTF * 64 : a.tri + hu(chunk) * ((MF + PF) * 64);
+    const int lane = threadIdx.x & 63;
+    const u32x4 *rows = (STAGED ? one : a.rows + ku(chunk) * (2 * KF * 64)) + lane, *cols = (STAGED ? two : a.cols + ku(chunk) * (KTF * 64)) + lane,
+                *tri = (STAGED ? two + KTF * 64 : a.tri + hu(chunk) * ((MF + PF) * 64)) + lane;
     const float whole = next_whole;
     values_of_rows<Window<T, NEAR>>(next, v);
     if (KEPT) {
@@ -532,11 +533,11 @@ template <typename T, int DK, bool NEAR> __global__ __launch_bounds__(256) void 
   {
     Parts<3> Sp[KB];
     column_parts<3>(S, Sp);
-    unwritten<IN, DK>(a.rows + ku * 2 * 4 * KB * IN * 64, st.w, st.ka, Sp, v, x);
+    unwritten<IN, DK>(a.rows + ku * 2 * 4 * KB * IN * 64 + (threadIdx.x & 63), st.w, st.ka, Sp, v, x);
   }
   Parts<3> xp[2];
   column_parts<3>(x, xp);
-  triangle<false, 3>(a.tri + hu * 54 * 64, xp, u);
+  triangle<false, 3>(a.tri + hu * 54 * 64 + (threadIdx.x & 63), xp, u);
   store_tiles(StateWindow(a.u + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp, at.first), u);
 }
 
@@ -586,8 +587,10 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
   for (int chunk = chunks - 1; chunk >= 0; --chunk) {
     const int steps = imin(a.T - chunk * kChunk, kChunk), live = imin(all - chunk * kChunk, steps);
     const float *w = (const float*)weights[chunk & 1], *ka = w + kChunk, *qa = w + 2 * kChunk, *ke = w + 3 * kChunk;
-    const u32x4 *kf = STAGED ? one : a.rows + ku(chunk) * (2 * KF * 64), *cols = STAGED ? two + MF * 64 : a.cols + ku(chunk) * (2 * KTF * 64),
-                *ptf = STAGED ? one + KF * 64 : a.tri + hu(chunk) * (3 * MF * 64) + 2 * MF * 64, *mtf = STAGED ? two : a.tri + hu(chunk) * (3 * MF * 64) + MF * 64;
+    const int lane = threadIdx.x & 63;
+    const u32x4 *kf = (STAGED ? one : a.rows + ku(chunk) * (2 * KF * 64)) + lane, *cols = (STAGED ? two + MF * 64 : a.cols + ku(chunk) * (2 * KTF * 64)) + lane,
+                *ptf = (STAGED ? one + KF * 64 : a.tri + hu(chunk) * (3 * MF * 64) + 2 * MF * 64) + lane,
+                *mtf = (STAGED ? two : a.tri + hu(chunk) * (3 * MF * 64) + MF * 64) + lane;
     const float whole = next_whole;
     values_of_rows<Window<T, NEAR>>(next, x);
     store_tiles(StateWindow(a.ds + hu(chunk) * DK * a.dvp, a.dvp, DK, a.dvp, at.first), S);
@@ -704,7 +707,6 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
   __shared__ float ends[WAVES], dots[2][HALVES][kChunk];
   __shared__ float crossing[WAVES][kChunk];
   __shared__ Steps64 st;
-  u32x4 *lu = lds, *lx = lds + 4 * VB * N * 64, *lo = lds + 8 * VB * N * 64, *ls = KEEP ? lds + ROWS * 64 : lds;
   const int unit = blockIdx.x, chunk = unit / (a.B * a.Hk), n = (unit - chunk * a.B * a.Hk) / a.Hk, hk = unit % a.Hk;
   const int t0 = chunk * kChunk, steps = imin(a.T - t0, kChunk), live = imin(live_steps(a, n) - t0, steps);
   const int w8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = w8 & 3, half = HALVES > 1 ? w8 >> 2 : 0, lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, mine = w * 16 + c;
@@ -719,40 +721,64 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
       keys.load(mine, at, x), queries.load(mine, at, y);
       kx[i].set(x), qx[i].set(y);
     }
-    const u32x4 *ktf = a.cols + (int64_t)unit * (DK / 4) * IN * 64, *qtf = ktf + DK / 8 * IN * 64, *rows = a.rows + (int64_t)unit * (DK / 4) * IN * 64;
     const Steps64& any = a.steps[((int64_t)chunk * a.B + n) * a.H + hk * a.group];
     const float rkm = any.rk[mine], rqm = any.rq[mine];
+    // products of keys and of queries (rows) with the lane's step's key; of two halves the first has the keys', the second the queries'
+    f32x4 pairs[HALVES == 1 ? 2 : 1][4] = {};
+    {
+      const u32x4* rows = a.rows + (int64_t)unit * (DK / 4) * IN * 64 + lane;
+#pragma unroll
+      for (int kb = 0; kb < DK / 32; ++kb) {
+        const Parts<IN> own = load_parts<IN>(rows, w * (DK / 32) + kb);
+        Parts<IN> m[4];
+        load_parts(rows + half * (DK / 8) * IN * 64, kb, DK / 32, m);
+        mul_add(m, own, pairs[0]);
+        if (HALVES == 1) {
+          load_parts(rows + (DK / 8) * IN * 64, kb, DK / 32, m);
+          mul_add(m, own, pairs[HALVES == 1]);
+        }
+      }
+    }
     for (int s = 0; s < a.group; ++s) {
       const int h = hk * a.group + s;
       const int64_t hu = ((int64_t)chunk * a.B + n) * a.H + h;
       // (addresses made from these are made in the loop: taken out of it, they alone would not fit the registers)
       int g = lane >> 4, c = lane & 15;
-      asm volatile("" : "+v"(g), "+v"(c));
+      int at_lane = lane;
+      asm volatile("" : "+v"(g), "+v"(c), "+v"(at_lane));
+      const u32x4 *ktf = a.cols + (int64_t)unit * (DK / 4) * IN * 64 + at_lane, *qtf = ktf + DK / 8 * IN * 64;
+      u32x4 *lu = lds + at_lane, *lx = lu + 4 * VB * N * 64, *lo = lu + 8 * VB * N * 64, *ls = KEEP ? lu + ROWS * 64 : lu;
       const int mine = w * 16 + c;
       const Runs<float, 8, QUICK> S(ckpt + hu * a.Dk * a.Dv, a.Dv, a.Dk, a.Dv);
       const Runs<float, 8, true> ds(a.ds + hu * DK * a.dvp, a.dvp, DK, a.dvp);
       {
         // (of two halves the second takes dX)
-        const Runs<float, 8, true> rows((half ? a.dx : a.u) + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp), dx(a.dx + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp);
+        const Runs<float, 8, true> rows_of_mine((half ? a.dx : a.u) + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp), dx(a.dx + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp);
         const Runs<T, 8, QUICK> go((const T*)d_o.p + t0 * d_o.t + n * d_o.b + h * a.Dv, d_o.t, live, a.Dv);
         float x[VB][8], y[VB][8], z[HALVES > 1 ? 1 : VB][8];
 #pragma unroll
-        for (int vb = 0; vb < VB; ++vb) {
-          const int at = vb * 32 + 8 * g;
-          rows.load(mine, at, x[vb]);
-          if (HALVES == 1) dx.load(mine, at, z[HALVES > 1 ? 0 : vb]);
-          if (half == 0) go.load(mine, at, y[vb]);
-        }
-        __syncthreads();  // (the head before has been read)
-        if (w8 < 3) {
-          u32x4* to = (u32x4*)&st + w8 * 64 + lane;
-          *to = ((const u32x4*)&a.steps[hu])[w8 * 64 + lane];
-        }
+        for (int vb = 0; vb < VB; ++vb) rows_of_mine.load(mine, vb * 32 + 8 * g, x[vb]);
+        if (HALVES == 1) {
 #pragma unroll
-        for (int vb = 0; vb < VB; ++vb) {
-          store_parts<N>(half ? lx : lu, w * VB + vb, parts_of<N>(x[vb]));
-          if (HALVES == 1) store_parts<N>(lx, w * VB + vb, parts_of<N>(z[HALVES > 1 ? 0 : vb]));
-          if (half == 0) store_parts<IN>(lo, w * VB + vb, parts_of<IN>(y[vb]));
+          for (int vb = 0; vb < VB; ++vb) dx.load(mine, vb * 32 + 8 * g, z[HALVES > 1 ? 0 : vb]);
+        }
+        if (half == 0) {
+#pragma unroll
+          for (int vb = 0; vb < VB; ++vb) go.load(mine, vb * 32 + 8 * g, y[vb]);
+        }
+        const u32x4 weights = w8 < 3 ? ((const u32x4*)&a.steps[hu])[w8 * 64 + lane] : u32x4{};
+        __syncthreads();  // (the head before has been read)
+        if (w8 < 3) ((u32x4*)&st)[w8 * 64 + lane] = weights;
+        u32x4* to = half ? lx : lu;
+#pragma unroll
+        for (int vb = 0; vb < VB; ++vb) store_parts<N>(to, w * VB + vb, parts_of<N>(x[vb]));
+        if (HALVES == 1) {
+#pragma unroll
+          for (int vb = 0; vb < VB; ++vb) store_parts<N>(lx, w * VB + vb, parts_of<N>(z[HALVES > 1 ? 0 : vb]));
+        }
+        if (half == 0) {
+#pragma unroll
+          for (int vb = 0; vb < VB; ++vb) store_parts<IN>(lo, w * VB + vb, parts_of<IN>(y[vb]));
         }
       }
       float Sx[MINE][8], Dx[MINE][8];
@@ -814,22 +840,11 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
             upq[rt][r] = i <= mine ? upq[rt][r] * (a.scale * rk[r] * fade) : 0.0f;
           }
         }
-        // what the pairs (i, the lane's step j) give to every step from behind j up to i: of two halves the first takes N, the second R
-        f32x4 cross[4] = {};
+        // what the pairs (i, the lane's step j) give to every step from behind j up to i
+        f32x4 cross[4];
 #pragma unroll
-        for (int which = 0; which < 2; ++which)
-          if (HALVES == 1 || half == which) {
-            f32x4 dots[4] = {};
-#pragma unroll
-            for (int kb = 0; kb < DK / 32; ++kb) {
-              Parts<IN> m[4];
-              load_parts(rows + which * (DK / 8) * IN * 64, kb, DK / 32, m);
-              mul_add(m, load_parts<IN>(rows, w * (DK / 32) + kb), dots);
-            }
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) cross[rt] += (which ? dnq[rt] : dn[rt]) * dots[rt];
-          }
-        float behind = 0.0f;  // of later tiles of rows
+        for (int rt = 0; rt < 4; ++rt) cross[rt] = HALVES == 1 ? dn[rt] * pairs[0][rt] + dnq[rt] * pairs[HALVES == 1][rt] : (half ? dnq[rt] : dn[rt]) * pairs[0][rt];
+        float behind = 0.0f, crossed = 0.0f;  // of later tiles of rows; of the step whose sum the lane keeps
 #pragma unroll
         for (int rt = 3; rt >= 0; --rt) {
           f32x4 x = cross[rt] * rkm;
@@ -839,11 +854,11 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
           behind += over_rows(whole);
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int t = rt * 16 + 4 * g + r;
-            const float sum = row_sum(t > mine ? x[r] + later : 0.0f);
-            if (c == 0) crossing[w8][t] = sum;
+            const float sum = row_sum(rt * 16 + 4 * g + r > mine ? x[r] + later : 0.0f);
+            crossed = c == rt * 4 + r ? sum : crossed;
           }
         }
+        crossing[w8][(c >> 2) * 16 + 4 * g + (c & 3)] = crossed;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
           below[kb] = parts_of<N>(dn[2 * kb], dn[2 * kb + 1]), belowq[kb] = parts_of<N>(dnq[2 * kb], dnq[2 * kb + 1]);

@@ -73,11 +73,11 @@ template <int TILES, int NA, int NB> __device__ __forceinline__ void mul_add(con
           acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[t].p[i]), __builtin_bit_cast(bf16x8, b.p[s - i]), acc[t], 0, 0, 0);
       }
 }
-// Operands in the workspace, 64 lanes x 16 bytes a part as a lane takes them.
+// Operands in the workspace or in LDS, 64 lanes x 16 bytes a part as a lane takes them; base: the lane's place in the first.
 template <int N> __device__ __forceinline__ Parts<N> load_parts(const u32x4* base, int frag) {
   Parts<N> s;
 #pragma unroll
-  for (int n = 0; n < N; ++n) s.p[n] = base[(frag * N + n) * 64 + (threadIdx.x & 63)];
+  for (int n = 0; n < N; ++n) s.p[n] = base[(frag * N + n) * 64];
   return s;
 }
 // of TILES tiles of rows, `step` operands from one to the next
@@ -87,7 +87,7 @@ template <int TILES, int N> __device__ __forceinline__ void load_parts(const u32
 }
 template <int N> __device__ __forceinline__ void store_parts(u32x4* base, int frag, const Parts<N>& s) {
 #pragma unroll
-  for (int n = 0; n < N; ++n) base[(frag * N + n) * 64 + (threadIdx.x & 63)] = s.p[n];
+  for (int n = 0; n < N; ++n) base[(frag * N + n) * 64] = s.p[n];
 }
 // FRAGS x 1 KB from global memory to the same order in LDS, without a register in between: each of a workgroup's four wavefronts its share of
 // neighbours, four to an address.
