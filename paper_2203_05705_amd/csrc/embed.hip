@@ -16,8 +16,9 @@ namespace ard {
 
 constexpr int kSortWaves = 16;     // wavefronts of a sorting workgroup
 constexpr int kMaxSpan = 1024;     // ids that one may own: counts of span x wavefronts in LDS
-constexpr int kPiece = 64;         // sorted positions whose sum is a piece of a long row
-constexpr int kLong = 128;         // tokens from which on a row is summed in pieces (at least kPiece + 1: a piece meets two long rows at most)
+constexpr int kPiece = 32;         // sorted positions whose sum is a piece of a long row
+constexpr int kLong = 32;          // tokens beyond which a row is summed in pieces (no fewer than kPiece: a piece meets two long rows at most)
+constexpr int kAhead = 8;          // loads of ids asked for together
 constexpr int kInFlight = 8;       // rows of dY asked for together
 constexpr int kMaxGrid = 1 << 20;
 
@@ -58,10 +59,15 @@ __global__ __launch_bounds__(64 * kSortWaves) void embed_sort_kernel(int R, int 
   __syncthreads();
   const int per = ((R + kSortWaves - 1) / kSortWaves + 63) & ~63, r0 = (int)((int64_t)w * per < R ? w * per : R), r1 = R - r0 < per ? R : r0 + per;
   int before = 0;  // tokens of smaller ids
-  for (int r = r0 + lane; r < r1; r += 64) {
-    const int id = ids[r];
-    if (id >= lo && id < lo + n) atomicAdd(&at[(id - lo) * kSortWaves + w], 1);
-    before += id >= 0 && id < lo;
+  for (int r = r0; r < r1; r += 64 * kAhead) {
+    int id[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) id[k] = r + k * 64 + lane < r1 ? ids[r + k * 64 + lane] : -1;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (id[k] >= lo && id[k] < lo + n) atomicAdd(&at[(id[k] - lo) * kSortWaves + w], 1);
+      before += id[k] >= 0 && id[k] < lo;
+    }
   }
   __syncthreads();
   // exclusive prefix sums over [id][wavefront], a run of counts a thread
@@ -88,21 +94,27 @@ __global__ __launch_bounds__(64 * kSortWaves) void embed_sort_kernel(int R, int 
   }
   if (lo + n == V && i0 < i1 && i1 == n * kSortWaves) start[V] = base;
   __syncthreads();
-  for (int r = r0; r < r1; r += 64) {
-    const int id = r + lane < r1 ? ids[r + lane] : -1;
-    unsigned long long left = __ballot(id >= lo && id < lo + n);
-    while (left) {  // one id at a time: its lanes take places in their order
-      const int key = __builtin_amdgcn_readlane(id, __ffsll(left) - 1);
-      const unsigned long long same = __ballot(id == key) & left;
-      const int cell = (key - lo) * kSortWaves + w, place = at[cell];
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // every lane has read the place before one moves it, and before the next id's is read
-      if (id == key) {
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        sorted[place + rank] = r + lane;
-        if (rank == 0) at[cell] = place + __popcll(same);
+  for (int r = r0; r < r1; r += 64 * kAhead) {
+    int ahead[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) ahead[k] = r + k * 64 + lane < r1 ? ids[r + k * 64 + lane] : -1;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int id = ahead[k];
+      unsigned long long left = __ballot(id >= lo && id < lo + n);
+      while (left) {  // one id at a time: its lanes take places in their order
+        const int key = __builtin_amdgcn_readlane(id, __ffsll(left) - 1);
+        const unsigned long long same = __ballot(id == key) & left;
+        const int cell = (key - lo) * kSortWaves + w, place = at[cell];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // every lane has read the place before one moves it, and before the next id's is read
+        if (id == key) {
+          const int rank = __popcll(same & ((1ull << lane) - 1));
+          sorted[place + rank] = r + k * 64 + lane;
+          if (rank == 0) at[cell] = place + __popcll(same);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        left &= ~same;
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      left &= ~same;
     }
   }
 }
