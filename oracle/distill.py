@@ -5,9 +5,11 @@ import numpy as np
 
 
 def _softmax(x):
-    m = x.max()
-    e = np.exp(x - m)
-    return e / e.sum(), m + np.log(e.sum())
+    """Shares and their logarithms, from differences to the largest (whose place alone would take all digits of a far row)."""
+    with np.errstate(invalid="ignore"):
+        x = x - x.max()
+    e = np.exp(x)
+    return e / e.sum(), x - np.log(e.sum())
 
 
 def distill(Z, ids, t, labels=None, temperature=1.0, alpha=1.0, dloss=None):
@@ -21,17 +23,17 @@ def distill(Z, ids, t, labels=None, temperature=1.0, alpha=1.0, dloss=None):
         if alpha > 0 and ids is not None:
             there = [(i, x) for i, x in zip(ids[r], t[r]) if 0 <= i < V and x != -np.inf]
             if there:
-                p, lse = _softmax(np.array([x for _, x in there]) / temperature)
-                qT, zlse = _softmax(z / temperature)
+                p, logp = _softmax(np.array([x for _, x in there]) / temperature)
+                qT, logq = _softmax(z / temperature)
                 target = np.zeros(V)
-                for (i, x), pk in zip(there, p):
+                for (i, _), pk, lp in zip(there, p, logp):
                     target[i] += pk
                     if pk > 0:
-                        loss[r] += alpha * temperature ** 2 * pk * ((x / temperature - lse) - (z[i] / temperature - zlse))
+                        loss[r] += alpha * temperature ** 2 * pk * (lp - logq[i])
                 dZ[r] += alpha * temperature * (qT - target)
         if alpha < 1 and labels is not None and 0 <= labels[r] < V:
-            q, lse = _softmax(z)
-            loss[r] += (1 - alpha) * (lse - z[labels[r]])
+            q, logq = _softmax(z)
+            loss[r] -= (1 - alpha) * logq[labels[r]]
             q[labels[r]] -= 1
             dZ[r] += (1 - alpha) * q
         if dloss is not None:

@@ -106,6 +106,23 @@ def test_masks_and_rows_that_they_leave_empty(dtype):
     assert not raw_bits(loss)[[0, 4]].any() and bool((dZ[0] == 0).all()) and bool((dZ[4] == 0).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1.0, 2.0, 4.0, 0.75])
+def test_rows_of_a_masks_lowest_value(dtype, T):
+    """All logits at the type's lowest value are as good as equal ones; one that is not takes the row."""
+    R, V, K = 4, 300, 6
+    Z, ids, t, y, dloss = _case(R, V, K, dtype, "f32", 9)
+    lowest = float(torch.finfo(torch.bfloat16 if dtype == "bf16" else torch.float32).min)
+    Z[0] = lowest
+    Z[1] = lowest
+    Z[1, 7], ids[1], y[1] = 3.0, 7, 7
+    Z[2] = 2.0 ** 40
+    Z[3, ::2] = lowest
+    ids[3], y[3] = 2 * np.arange(K) + 1, 11
+    y[0], t[0] = 5, lowest
+    _check(R, V, K, dtype, "f32", T, 0.6, case=(Z, ids, t, y, dloss))
+
+
 def test_a_nan_stays_in_its_row():
     R, V, K = 4, 3000, 5
     Z, ids, t, y, dloss = _case(R, V, K, "f32", "f32", 5)

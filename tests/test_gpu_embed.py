@@ -60,9 +60,9 @@ def test_sizes(R, V, D, dtype, wdtype):
 
 @pytest.mark.parametrize("dtype,wdtype", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
 @pytest.mark.parametrize("kind", ["one", "frequent", "padded"])
-@pytest.mark.parametrize("R,V", [(128, 9), (129, 9), (130, 300), (1000, 40), (3000, 500)])
+@pytest.mark.parametrize("R,V", [(32, 9), (33, 9), (64, 9), (65, 9), (128, 9), (129, 9), (130, 300), (1000, 40), (3000, 500)])
 def test_frequent_tokens_and_padding(R, V, kind, dtype, wdtype):
-    """Rows of 128 tokens are summed at once, of 129 in pieces."""
+    """Rows of 32 tokens are summed at once, of 33 in pieces of 32."""
     _check(R, V, 24, dtype, wdtype, kind, scale=0.5, seed=R)
     _check(R, V, 24, dtype, wdtype, kind, scale=-3.0, add=True, seed=R + 1)
 
