@@ -254,6 +254,14 @@ struct Columns {
     unit = blockIdx.x / groups;
     set(a, (blockIdx.x - unit * groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
   }
+  // the same with the DK columns of a transition behind those of the state; true: they are a transition's
+  __device__ __forceinline__ Columns(const GdrArgs& a, int slices, int dk, bool& transition) {
+    const int states = (slices + 3) / 4, groups = states + dk / 64;
+    unit = blockIdx.x / groups;
+    const int group = blockIdx.x - unit * groups;
+    transition = group >= states;
+    set(a, (transition ? group - states : group) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  }
   // wavefronts counted through the heads
   __device__ __forceinline__ Columns(const GdrArgs& a, int index, int slices) {
     unit = index / slices;
@@ -403,48 +411,119 @@ template <int IN, int DK> __device__ __forceinline__ void add_outer(const u32x4*
 // Four wavefronts with columns of one head walk its chunks.  They share the operands in LDS, in two groups: what the first half of a
 // chunk reads is loaded for the next chunk while the second half is worked on, and the other way about.  Operands that LDS does not hold
 // (fp32, wide heads) are read from the caches.
-// KEPT: the states before the chunks are stored, in ckpt.
-template <typename T, int DK, bool NEAR, bool KEPT>
+// KEEP: the states before the chunks are stored, in ckpt.
+//
+// Few heads leave most of the chip idle, and their chunks follow one another.  So a long sequence is cut into segments.  A segment is linear in the
+// state before it: S' = F S + Z.  SUM walks all but the last segment at once, for Z (from a state of zeros) and F (DK more columns, from the
+// unit matrix, without values); gdr_join_kernel makes the states between the segments of them, and then all segments are walked at once.
+enum { DROP, KEEP, SUM };
+template <int DK> __device__ __forceinline__ void unit_columns(int first, f32x4 (&S)[DK / 16]) {
+  const int row = 4 * ((threadIdx.x & 63) >> 4);
+#pragma unroll
+  for (int rt = 0; rt < DK / 16; ++rt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) S[rt][r] = rt * 16 + row + r == first ? 1.0f : 0.0f;
+}
+template <int DK> __device__ __forceinline__ StateWindow sum_window(const GdrArgs& a, int index, const Columns& at, bool transition) {
+  const int wide = a.dvp + DK;
+  return StateWindow(a.sums + ((int64_t)index * a.B * a.H + at.unit) * DK * wide, wide, DK, wide, transition ? a.dvp + at.first : at.first);
+}
+template <int DK> __device__ __forceinline__ StateWindow start_window(const GdrArgs& a, int index, const Columns& at) {
+  return StateWindow(a.starts + ((int64_t)index * a.B * a.H + at.unit) * DK * a.dvp, a.dvp, DK, a.dvp, at.first);
+}
+// The states before all segments but the first, one behind the other: S_{i + 1} = F_i S_i + Z_i, where Z_0 holds what S_0 gave; S_0 is copied (the last
+// segment may write where it lies).  F goes to LDS in parts, each of four wavefronts a quarter.  Segments count in the order of the walk.
+template <int DK> __global__ __launch_bounds__(256) void gdr_join_kernel(GdrArgs a, const float* S0, int slices) {
+  constexpr int KB = DK / 32, FRAGS = DK / 16 * KB, PER = FRAGS / 4;
+  __shared__ u32x4 parts[FRAGS * 3 * 64];
+  const Columns at(a, slices);
+  const int lane = threadIdx.x & 63, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wide = a.dvp + DK;
+  f32x4 S[DK / 16] = {}, Z[DK / 16], F[PER][2];
+  if (S0) load_tiles(StateWindow(S0 + (int64_t)at.unit * a.Dk * a.Dv, a.Dv, a.Dk, a.Dv, at.first), S);
+  store_tiles(start_window<DK>(a, 0, at), S);
+  load_tiles(sum_window<DK>(a, 0, at, false), S);
+  store_tiles(start_window<DK>(a, 1, at), S);
+  const auto load = [&](int index) {
+    load_tiles(sum_window<DK>(a, index, at, false), Z);
+    const float* f = a.sums + ((int64_t)index * a.B * a.H + at.unit) * DK * wide + a.dvp + (lane & 15) * wide + 4 * g;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int frag = wave * PER + i, rt = frag / KB, kb = frag - rt * KB;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) F[i][half] = *reinterpret_cast<const f32x4*>(f + (int64_t)rt * 16 * wide + kb * 32 + half * 16);
+    }
+  };
+  if (a.segments > 2) load(1);
+  for (int index = 1; index < a.segments - 1; ++index) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) store_parts(parts + lane, wave * PER + i, parts_of<3>(F[i][0], F[i][1]));
+    __syncthreads();
+    Parts<3> Sp[KB];
+    column_parts<3>(S, Sp);
+#pragma unroll
+    for (int rt = 0; rt < DK / 16; ++rt) S[rt] = Z[rt];
+    if (index + 1 < a.segments - 1) load(index + 1);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int rt = 0; rt < DK / 16; rt += 4) {
+        Parts<3> f[4];
+        load_parts(parts + lane, rt * KB + kb, KB, f);
+        mul_add(f, Sp[kb], reinterpret_cast<f32x4(&)[4]>(S[rt]));
+      }
+    store_tiles(start_window<DK>(a, index + 1, at), S);
+    __syncthreads();
+  }
+}
+
+template <typename T, int DK, bool NEAR, int MODE>
 __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt, int slices) {
   constexpr int IN = GdrType<T>::IN, OUT = GdrType<T>::OUT, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3, PF = 6 * OUT;
+  constexpr bool KEPT = MODE == KEEP, OUTPUT = MODE != SUM;
+  constexpr int RF = OUTPUT ? 2 * KF : KF, TF = OUTPUT ? MF + PF : MF;  // (the operands of Q and P are read for o alone)
   constexpr bool STAGED = 2 * KF + KTF + MF + PF <= 150;  // KB of LDS
-  __shared__ u32x4 one[STAGED ? 2 * KF * 64 : 1], two[STAGED ? (KTF + MF + PF) * 64 : 1];  // what the halves read
+  __shared__ u32x4 one[STAGED ? RF * 64 : 1], two[STAGED ? (KTF + TF) * 64 : 1];  // what the halves read
   __shared__ f32x4 weights[2][64];  // w, ka, qa, ke of a chunk
-  const Columns at(a, slices);
+  bool transition = false;
+  const Columns at = OUTPUT ? Columns(a, slices) : Columns(a, slices, DK, transition);
+  const int segment = blockIdx.y, begin = segment * a.span, end = imin(begin + a.span, a.chunks);
+  if (transition && segment == 0) return;  // (all wavefronts: the first segment's state is S0's)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t matrix = (int64_t)a.Dk * a.Dv, plane = (int64_t)a.B * a.H * matrix;
   f32x4 S[DK / 16] = {}, v[4] = {};
-  if (S0) load_tiles(StateWindow(S0 + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
-  const int all = live_steps(a, at.n), chunks = (all + kChunk - 1) / kChunk;
+  if (OUTPUT && a.segments > 1) load_tiles(start_window<DK>(a, segment, at), S);
+  else if (transition) unit_columns<DK>(at.first, S);
+  else if (S0 && segment == 0) load_tiles(StateWindow(S0 + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
+  const int all = live_steps(a, at.n), chunks = imin((all + kChunk - 1) / kChunk, end), given = transition ? 0 : all;
   const auto ku = [&](int chunk) { return (int64_t)((chunk * a.B + at.n) * a.Hk + at.hk); };
   const auto hu = [&](int chunk) { return (int64_t)((chunk * a.B + at.n) * a.H + at.h); };
   const T* vp = (const T*)a.v.p + at.n * a.v.b + at.h * a.Dv;
-  T* op = (T*)o.p + at.n * o.b + at.h * a.Dv;
-  float* kept = ckpt + at.unit * matrix;
+  T* op = (T*)o.p + at.n * o.b + at.h * a.Dv + (int64_t)begin * kChunk * o.t;
+  float* kept = ckpt + at.unit * matrix + begin * plane;
   RawRows next;
   f32x4 sw;  // the chunk's weights, which go to LDS by way of a register: loads straight into an array let every later read of it wait for them
   float next_whole = 0.0f;
   int zero = 0;
   asm volatile("" : "+v"(zero));  // (a vector load: one by the scalar unit would let every read of LDS wait for it)
   const auto first_half = [&](int chunk) {  // loads of what it reads
-    if (STAGED) stage<2 * KF>(a.rows + ku(chunk) * (2 * KF * 64), one, wave);
+    if (STAGED) stage<RF>(a.rows + ku(chunk) * (2 * KF * 64), one, wave);
     sw = *reinterpret_cast<const f32x4*>(a.steps[hu(chunk)].w + (threadIdx.x & 63) * 4);
-    load_raw(Window<T, NEAR>(vp + (int64_t)chunk * kChunk * a.v.t, a.v.t, imin(all - chunk * kChunk, kChunk), a.Dv, at.first), next);
+    load_raw(Window<T, NEAR>(vp + (int64_t)chunk * kChunk * a.v.t, a.v.t, imin(given - chunk * kChunk, kChunk), a.Dv, at.first), next);
     next_whole = (&a.steps[hu(chunk)].whole)[zero];
   };
   const auto second_half = [&](int chunk) {
-    if (STAGED) stage<KTF>(a.cols + ku(chunk) * (KTF * 64), two, wave), stage<MF + PF>(a.tri + hu(chunk) * ((MF + PF) * 64), two + KTF * 64, wave);
+    if (STAGED) stage<KTF>(a.cols + ku(chunk) * (KTF * 64), two, wave), stage<TF>(a.tri + hu(chunk) * ((MF + PF) * 64), two + KTF * 64, wave);
   };
   constexpr int COUNT = STAGED && NEAR;  // (elsewhere accesses are not counted: all are waited for)
-  if (chunks) {
-    first_half(0);
+  if (begin < chunks) {
+    first_half(begin);
     staged();
-    weights[0][threadIdx.x & 63] = sw;
+    weights[begin & 1][threadIdx.x & 63] = sw;
     all_landed<0>();
-    second_half(0);
+    second_half(begin);
     staged();
   }
-  for (int chunk = 0; chunk < chunks; ++chunk) {
+  for (int chunk = begin; chunk < chunks; ++chunk) {
     const int steps = imin(a.T - chunk * kChunk, kChunk), live = imin(all - chunk * kChunk, steps);
     const float *w = (const float*)weights[chunk & 1], *ka = w + kChunk, *qa = w + 2 * kChunk, *ke = w + 3 * kChunk;
     const int lane = threadIdx.x & 63;
@@ -461,14 +540,16 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
       Parts<3> Sp[KB];
       column_parts<3>(S, Sp);
       unwritten<IN, DK>(rows, w, ka, Sp, v, x);
+      if constexpr (OUTPUT) {
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        Parts<IN> q[4];
-        load_parts(rows + KF * 64, kb, KB, q);
-        mul_add(q, leading<OUT>(Sp[kb]), y);
+        for (int kb = 0; kb < KB; ++kb) {
+          Parts<IN> q[4];
+          load_parts(rows + KF * 64, kb, KB, q);
+          mul_add(q, leading<OUT>(Sp[kb]), y);
+        }
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) y[rt] *= row_weights(qa, rt);
       }
-#pragma unroll
-      for (int rt = 0; rt < 4; ++rt) y[rt] *= row_weights(qa, rt);
     }
     all_landed<KEPT * COUNT * (DK / 4)>();
     first_half(imin(chunk + 1, chunks - 1));  // (behind the last chunk its own once more: accesses that are counted are made on every way)
@@ -478,29 +559,33 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
       column_parts<3>(x, xp);
       triangle<false, 3>(tri, xp, u);
     }
-    {
+    if constexpr (OUTPUT) {
       Parts<OUT> up[2];
       column_parts<OUT>(u, up);
       triangle<false, OUT>(tri + MF * 64, up, y);
     }
     weights[(chunk + 1) & 1][threadIdx.x & 63] = sw;  // (waits for all accesses: in front of the stores)
-    store_live(Window<T, NEAR>(op, o.t, steps, a.Dv, at.first), live, y);
+    if constexpr (OUTPUT) store_live(Window<T, NEAR>(op, o.t, steps, a.Dv, at.first), live, y);
     op += kChunk * o.t;
 #pragma unroll
     for (int rt = 0; rt < DK / 16; ++rt) S[rt] *= whole;
     add_outer<IN, DK>(cols, ke, 1.0f, u, S);
-    all_landed<COUNT * 16>();
+    all_landed<OUTPUT * COUNT * 16>();
     second_half(imin(chunk + 1, chunks - 1));
     staged();
   }
   all_landed<0>();  // (nothing may arrive in LDS once the wavefront has ended)
-  for (int chunk = chunks; chunk < a.chunks; ++chunk) {  // behind the sequence's end
+  if constexpr (!OUTPUT) {
+    store_tiles(sum_window<DK>(a, segment, at, transition), S);
+    return;
+  }
+  for (int chunk = imax(chunks, begin); chunk < end; ++chunk) {  // behind the sequence's end
     const f32x4 none[4] = {};
     if (KEPT) store_tiles(StateWindow(kept, a.Dv, a.Dk, a.Dv, at.first), S);
     store_tiles(Window<T, NEAR>(op, o.t, imin(a.T - chunk * kChunk, kChunk), a.Dv, at.first), none);
     kept += plane, op += kChunk * o.t;
   }
-  if (ST) store_tiles(StateWindow(ST + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
+  if (ST && end == a.chunks) store_tiles(StateWindow(ST + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
 }
 
 // ---- backward -----------------------------------------------------------------------
@@ -541,18 +626,25 @@ template <typename T, int DK, bool NEAR> __global__ __launch_bounds__(256) void 
   store_tiles(StateWindow(a.u + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp, at.first), u);
 }
 
-template <typename T, int DK, bool NEAR>
+// SUM: as forward, of segments from the last on.
+template <typename T, int DK, bool NEAR, int MODE>
 __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o, const float* dST, ard_steps dv, float* dS0, int slices) {
   constexpr int IN = GdrType<T>::IN, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3;
   constexpr bool STAGED = KF + 2 * KTF + 2 * MF <= 150;
+  constexpr bool OUTPUT = MODE != SUM;
   __shared__ u32x4 one[STAGED ? (KF + MF) * 64 : 1], two[STAGED ? (2 * KTF + MF) * 64 : 1];
   __shared__ f32x4 weights[2][64];  // w, ka, qa, ke of a chunk
-  const Columns at(a, slices);
+  bool transition = false;
+  const Columns at = OUTPUT ? Columns(a, slices) : Columns(a, slices, DK, transition);
+  const int segment = blockIdx.y, begin = (a.segments - 1 - segment) * a.span, end = imin(begin + a.span, a.chunks);
+  if (transition && segment == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t matrix = (int64_t)a.Dk * a.Dv;
   f32x4 S[DK / 16] = {}, x[4] = {};
-  if (dST) load_tiles(StateWindow(dST + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
-  const int all = live_steps(a, at.n), chunks = (all + kChunk - 1) / kChunk;
+  if (OUTPUT && a.segments > 1) load_tiles(start_window<DK>(a, segment, at), S);
+  else if (transition) unit_columns<DK>(at.first, S);
+  else if (dST && segment == 0) load_tiles(StateWindow(dST + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
+  const int all = live_steps(a, at.n), chunks = imin((all + kChunk - 1) / kChunk, end), given = transition ? 0 : all;
   const auto ku = [&](int chunk) { return (int64_t)((chunk * a.B + at.n) * a.Hk + at.hk); };
   const auto hu = [&](int chunk) { return (int64_t)((chunk * a.B + at.n) * a.H + at.h); };
   const T* gp = (const T*)d_o.p + at.n * d_o.b + at.h * a.Dv;
@@ -565,18 +657,18 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
   const auto first_half = [&](int chunk) {
     if (STAGED) stage<KF>(a.rows + ku(chunk) * (2 * KF * 64), one, wave), stage<MF>(a.tri + hu(chunk) * (3 * MF * 64) + 2 * MF * 64, one + KF * 64, wave);
     sw = *reinterpret_cast<const f32x4*>(a.steps[hu(chunk)].w + (threadIdx.x & 63) * 4);
-    load_raw(Window<T, NEAR>(gp + (int64_t)chunk * kChunk * d_o.t, d_o.t, imin(all - chunk * kChunk, kChunk), a.Dv, at.first), next);
+    load_raw(Window<T, NEAR>(gp + (int64_t)chunk * kChunk * d_o.t, d_o.t, imin(given - chunk * kChunk, kChunk), a.Dv, at.first), next);
     next_whole = (&a.steps[hu(chunk)].whole)[zero];
   };
   const auto second_half = [&](int chunk) {
     if (STAGED) stage<MF>(a.tri + hu(chunk) * (3 * MF * 64) + MF * 64, two, wave), stage<2 * KTF>(a.cols + ku(chunk) * (2 * KTF * 64), two + MF * 64, wave);
   };
-  for (int chunk = chunks; chunk < a.chunks; ++chunk) {  // behind the sequence's end
+  for (int chunk = OUTPUT ? imax(chunks, begin) : end; chunk < end; ++chunk) {  // behind the sequence's end
     const f32x4 none[4] = {};
     store_tiles(Window<T, NEAR>(vp + (int64_t)chunk * kChunk * dv.t, dv.t, imin(a.T - chunk * kChunk, kChunk), a.Dv, at.first), none);
   }
   constexpr int COUNT = STAGED && NEAR;
-  if (chunks) {
+  if (begin < chunks) {
     first_half(chunks - 1);
     staged();
     weights[(chunks - 1) & 1][threadIdx.x & 63] = sw;
@@ -584,7 +676,7 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
     second_half(chunks - 1);
     staged();
   }
-  for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+  for (int chunk = chunks - 1; chunk >= begin; --chunk) {
     const int steps = imin(a.T - chunk * kChunk, kChunk), live = imin(all - chunk * kChunk, steps);
     const float *w = (const float*)weights[chunk & 1], *ka = w + kChunk, *qa = w + 2 * kChunk, *ke = w + 3 * kChunk;
     const int lane = threadIdx.x & 63;
@@ -593,7 +685,7 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
                 *mtf = (STAGED ? two : a.tri + hu(chunk) * (3 * MF * 64) + MF * 64) + lane;
     const float whole = next_whole;
     values_of_rows<Window<T, NEAR>>(next, x);
-    store_tiles(StateWindow(a.ds + hu(chunk) * DK * a.dvp, a.dvp, DK, a.dvp, at.first), S);
+    if constexpr (OUTPUT) store_tiles(StateWindow(a.ds + hu(chunk) * DK * a.dvp, a.dvp, DK, a.dvp, at.first), S);
     f32x4 y[4] = {}, dx[4] = {}, od[4];
     {
       Parts<3> Sp[KB];
@@ -614,8 +706,8 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
     }
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt) od[rt] = x[rt];
-    all_landed<COUNT * (DK / 4)>();
-    first_half(imax(chunk - 1, 0));
+    all_landed<OUTPUT * COUNT * (DK / 4)>();
+    first_half(imax(chunk - 1, begin));
     staged();
     {
       Parts<3> p[2];
@@ -625,18 +717,24 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt) y[rt] = row_weights(w, rt) * dx[rt];
     weights[(chunk + 1) & 1][threadIdx.x & 63] = sw;
-    store_tiles(StateWindow(a.dx + hu(chunk) * kChunk * a.dvp, a.dvp, kChunk, a.dvp, at.first), dx);
-    store_live(Window<T, NEAR>(vp + (int64_t)chunk * kChunk * dv.t, dv.t, steps, a.Dv, at.first), live, y);
+    if constexpr (OUTPUT) {
+      store_tiles(StateWindow(a.dx + hu(chunk) * kChunk * a.dvp, a.dvp, kChunk, a.dvp, at.first), dx);
+      store_live(Window<T, NEAR>(vp + (int64_t)chunk * kChunk * dv.t, dv.t, steps, a.Dv, at.first), live, y);
+    }
 #pragma unroll
     for (int rt = 0; rt < DK / 16; ++rt) S[rt] *= whole;
     add_outer<IN, DK>(cols + KTF * 64, qa, 1.0f, od, S);
     add_outer<IN, DK>(cols, ka, -1.0f, y, S);
-    all_landed<COUNT * 32>();
-    second_half(imax(chunk - 1, 0));
+    all_landed<OUTPUT * COUNT * 32>();
+    second_half(imax(chunk - 1, begin));
     staged();
   }
   all_landed<0>();
-  if (dS0) store_tiles(StateWindow(dS0 + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
+  if constexpr (!OUTPUT) {
+    store_tiles(sum_window<DK>(a, segment, at, transition), S);
+    return;
+  }
+  if (dS0 && begin == 0) store_tiles(StateWindow(dS0 + at.unit * matrix, a.Dv, a.Dk, a.Dv, at.first), S);
 }
 
 __device__ __forceinline__ float over_rows(float x) {  // the sum over the lanes that share a column
@@ -1022,6 +1120,19 @@ struct GdrPlan {
   int dk, slices;  // padded key size; wavefronts' worth of 16 columns of a head
   size_t bytes;
 };
+// Chunks of a segment: all, or where workgroups of all heads' columns leave compute units idle, what brings the steps that follow one another down most:
+// twice a segment's chunks (the sums' cost 0.7 of the others') and a product of a state for every segment.
+static int segment_span(int chunks, int workgroups) {
+  constexpr int kUnits = 256;
+  int best = chunks;
+  float least = 0.85f * chunks;
+  for (int n = 2; n * workgroups <= kUnits && n <= chunks; ++n) {
+    const int span = ceil_div(chunks, n);
+    const float cost = 1.7f * span + 0.7f * ceil_div(chunks, span) + 2.0f;
+    if (cost < least) least = cost, best = span;
+  }
+  return best;
+}
 // The workspace's parts, one behind the other; `base` may be NULL, when only the size is asked for.
 static GdrPlan gdr_plan(int32_t dtype, int T, int B, int Hk, int H, int Dk, int Dv, bool backward, void* base) {
   GdrPlan p{};
@@ -1039,6 +1150,13 @@ static GdrPlan gdr_plan(int32_t dtype, int T, int B, int Hk, int H, int Dk, int 
   const size_t rows = (size_t)4 * (p.dk / 32) * in * 1024, cols = (size_t)(p.dk / 8) * in * 1024;
   take(a.steps, hu * sizeof(Steps64));
   take(a.rows, ku * rows * 2), take(a.cols, ku * cols * (backward ? 2 : 1)), take(a.tri, hu * 6 * (backward ? 9 : 3 + out) * 1024);
+  // (the backward pass's wavefronts cover the padded columns)
+  a.span = segment_span(a.chunks, B * H * ceil_div(backward ? a.dvp / 16 : p.slices, 4));
+  a.segments = ceil_div(a.chunks, a.span);
+  if (a.segments > 1) {
+    const size_t n = (size_t)a.segments * B * H * p.dk * 4;
+    take(a.sums, n * (a.dvp + p.dk)), take(a.starts, n * a.dvp);
+  }
   if (backward) {
     take(a.u, hu * kChunk * a.dvp * 4), take(a.dx, hu * kChunk * a.dvp * 4), take(a.ds, hu * p.dk * a.dvp * 4);
   }
@@ -1123,9 +1241,16 @@ extern "C" int32_t ard_gdr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
     }
     ARD_LAUNCH_NAMED("gdr_prep_kernel", (gdr_prep_kernel<E, DK, false>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a);
     ARD_LAUNCH_CHECK("gdr_prep_kernel");
-    const dim3 grid(B * H * ceil_div(p.slices, 4));
-    if (ckpt) ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, true>), grid, dim3(256), 0, st, a, S0, out, ST, ckpt, p.slices);
-    else ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, false>), grid, dim3(256), 0, st, a, S0, out, ST, ckpt, p.slices);
+    const int groups = ceil_div(p.slices, 4);
+    if (a.segments > 1) {
+      ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, SUM>), dim3(B * H * (groups + DK / 64), a.segments - 1), dim3(256), 0, st, a, S0, out, ST, ckpt, p.slices);
+      ARD_LAUNCH_CHECK("gdr_fwd_kernel");
+      ARD_LAUNCH_NAMED("gdr_join_kernel", (gdr_join_kernel<DK>), dim3(B * H * groups), dim3(256), 0, st, a, S0, p.slices);
+      ARD_LAUNCH_CHECK("gdr_join_kernel");
+    }
+    const dim3 grid(B * H * groups, a.segments);
+    if (ckpt) ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, KEEP>), grid, dim3(256), 0, st, a, S0, out, ST, ckpt, p.slices);
+    else ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, DROP>), grid, dim3(256), 0, st, a, S0, out, ST, ckpt, p.slices);
     ARD_LAUNCH_CHECK("gdr_fwd_kernel");
     return (int32_t)ARD_OK;
   });
@@ -1157,7 +1282,14 @@ extern "C" int32_t ard_gdr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
     ARD_LAUNCH_CHECK("gdr_prep_kernel");
     ARD_LAUNCH_NAMED("gdr_rows_kernel", (gdr_rows_kernel<E, DK, NEAR>), dim3((unsigned)(((int64_t)a.chunks * waves + 3) / 4)), dim3(256), 0, st, a, ckpt, slices, waves);
     ARD_LAUNCH_CHECK("gdr_rows_kernel");
-    ARD_LAUNCH_NAMED("gdr_back_kernel", (gdr_back_kernel<E, DK, NEAR>), dim3(B * H * ceil_div(slices, 4)), dim3(256), 0, st, a, od, dST, dv, dS0, slices);
+    const int groups = ceil_div(slices, 4);
+    if (a.segments > 1) {
+      ARD_LAUNCH_NAMED("gdr_back_kernel", (gdr_back_kernel<E, DK, NEAR, SUM>), dim3(B * H * (groups + DK / 64), a.segments - 1), dim3(256), 0, st, a, od, dST, dv, dS0, slices);
+      ARD_LAUNCH_CHECK("gdr_back_kernel");
+      ARD_LAUNCH_NAMED("gdr_join_kernel", (gdr_join_kernel<DK>), dim3(B * H * groups), dim3(256), 0, st, a, dST, slices);
+      ARD_LAUNCH_CHECK("gdr_join_kernel");
+    }
+    ARD_LAUNCH_NAMED("gdr_back_kernel", (gdr_back_kernel<E, DK, NEAR, KEEP>), dim3(B * H * groups, a.segments), dim3(256), 0, st, a, od, dST, dv, dS0, slices);
     ARD_LAUNCH_CHECK("gdr_back_kernel");
     const auto grads_of = [&](auto dv_, auto quick) {
       constexpr int DV = decltype(dv_)::value;

@@ -158,6 +158,8 @@ struct GdrArgs {
   Steps64* steps;
   float *u, *dx, *ds;  // [64][dvp], [64][dvp], [dkp][dvp] of a chunk
   int dvp;
+  int span, segments;   // chunks of a segment, and their number
+  float *sums, *starts; // of a segment [DK][dvp + DK]: what it leaves of a state of zeros, and its transition; [DK][dvp]: the state before it
 };
 __device__ __forceinline__ int live_steps(const GdrArgs& a, int n) { return a.len ? imin(imax(a.len[n], 0), a.T) : a.T; }
 

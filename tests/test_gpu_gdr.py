@@ -114,6 +114,46 @@ def test_many_chunks(Dk, Dv, dtype):
     _check(700, 3, 2, 2, Dk, Dv, dtype, ragged=True, seed=2)
 
 
+# Few heads of a long sequence are walked in segments: a state passes their transitions as products, which have the chunks' own digits.
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,B,H,Dk,Dv", [(1024, 1, 1, 64, 64), (1100, 2, 1, 128, 128), (1473, 1, 2, 30, 72), (2049, 1, 1, 96, 10), (1601, 3, 2, 64, 33)])
+def test_segments_of_long_sequences(T, B, H, Dk, Dv, dtype):
+    _check(T, B, 1, H, Dk, Dv, dtype, seed=T)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("start", [True, False])
+def test_segments_behind_a_sequences_end(start, dtype):
+    _check(1700, 7, 1, 1, 40, 70, dtype, ragged=True, start=start, seed=17)
+    _check(2500, 6, 1, 1, 66, 24, dtype, ragged=True, start=start, seed=18, spread=9.0)   # (states that last through segments)
+
+
+def test_segments_of_states_in_the_place_of_what_they_are_made_from():
+    T = 1300
+    x, do, S0, dST = _inputs(T, 2, 1, 1, 64, 100, "bf16", 3, 9.0)
+    xd, dod, s, d = [from_vals(t, "bf16") for t in x], from_vals(do, "bf16"), from_vals(S0, "f32"), from_vals(dST, "f32")
+    o, ST, ck = ard.gdr_fwd(*xd, S0=s)
+    *g, dS0 = ard.gdr_bwd(*xd, dod, ck, dST=d)
+    o2, same, _ = ard.gdr_fwd(*xd, S0=s, out=(None, s, None))
+    assert same is s and torch.equal(s, ST) and np.array_equal(raw_bits(o2), raw_bits(o))
+    *g2, same = ard.gdr_bwd(*xd, dod, ck, dST=d, out=(None,) * 5 + (d,))
+    assert same is d and torch.equal(d, dS0)
+    for a, b in zip(g, g2):
+        assert np.array_equal(raw_bits(a), raw_bits(b))
+
+
+def test_a_nan_passes_segments_in_its_column_alone():
+    T = 1500
+    x, do, S0, _ = _inputs(T, 1, 1, 1, 32, 40, "f32", 5)
+    xd = [from_vals(t, "f32") for t in x]
+    clean = ard.gdr_fwd(*xd)
+    xd[2][10, 0, 0, 7] = float("nan")
+    o, ST, ck = ard.gdr_fwd(*xd)
+    others = [c for c in range(40) if c != 7]
+    assert bool(torch.isnan(ST[..., 7]).all()) and torch.equal(ST[..., others], clean[1][..., others])
+    assert bool(torch.isnan(o[64:, ..., 7]).all()) and torch.equal(o[..., others], clean[0][..., others])
+
+
 @pytest.mark.parametrize("T", [3, 40, 140])
 def test_gates_that_let_nothing_or_all_through(T):
     x, *_ = _inputs(T, 2, 1, 3, 16, 16, "f32", 5)
