@@ -247,28 +247,24 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void g
 // ---- a wavefront's columns ----------------------------------------------------------
 struct Columns {
   int unit, n, h, hk, first;  // first: the lane's column
-  // workgroups of four wavefronts, each of one head's columns; `slices`: wavefronts' worth of columns of a head (a wavefront behind the last one
-  // has columns outside, which are 0 and stay unwritten, and helps to load)
-  __device__ __forceinline__ Columns(const GdrArgs& a, int slices) {
-    const int groups = (slices + 3) / 4;
-    unit = blockIdx.x / groups;
-    set(a, (blockIdx.x - unit * groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  int segment;
+  // Workgroups of four wavefronts, each of 64 of one head's columns, in one segment: `groups` of them a head (a wavefront behind the last column has columns outside,
+  // which are 0 and stay unwritten, and helps to load).  Those of one segment that read the same keys take turns of 8 in the grid, which goes round
+  // the 8 dies: what one has loaded, the others find in their die's cache.
+  __device__ __forceinline__ Columns(const GdrArgs& a, int groups, int* taken) {
+    const int team = groups * a.group, heads = a.B * a.Hk, teams = gridDim.x / team, turned = teams & ~7, id = blockIdx.x;
+    const int beyond = id - turned * team, turn = id >> 3;
+    const int which = beyond < 0 ? turn / team * 8 + (id & 7) : turned + beyond / team, member = beyond < 0 ? turn % team : beyond % team;
+    segment = which / heads;
+    const int head = which - segment * heads, part = member / groups;
+    *taken = member - part * groups;
+    n = head / a.Hk, hk = head - n * a.Hk, h = hk * a.group + part, unit = n * a.H + h;
   }
-  // the same with the DK columns of a transition behind those of the state; true: they are a transition's
-  __device__ __forceinline__ Columns(const GdrArgs& a, int slices, int dk, bool& transition) {
-    const int states = (slices + 3) / 4, groups = states + dk / 64;
-    unit = blockIdx.x / groups;
-    const int group = blockIdx.x - unit * groups;
-    transition = group >= states;
-    set(a, (transition ? group - states : group) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
-  }
+  __device__ __forceinline__ void take(int group) { first = group * 64 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 16 + (threadIdx.x & 15); }
   // wavefronts counted through the heads
   __device__ __forceinline__ Columns(const GdrArgs& a, int index, int slices) {
-    unit = index / slices;
-    set(a, index - unit * slices);
-  }
-  __device__ __forceinline__ void set(const GdrArgs& a, int slice) {
-    first = slice * 16 + (threadIdx.x & 15);
+    unit = index / slices, segment = 0;
+    first = (index - unit * slices) * 16 + (threadIdx.x & 15);
     n = unit / a.H, h = unit - n * a.H, hk = h / a.group;
   }
 };
@@ -432,61 +428,70 @@ template <int DK> __device__ __forceinline__ StateWindow start_window(const GdrA
   return StateWindow(a.starts + ((int64_t)index * a.B * a.H + at.unit) * DK * a.dvp, a.dvp, DK, a.dvp, at.first);
 }
 // The states before all segments but the first, one behind the other: S_{i + 1} = F_i S_i + Z_i, where Z_0 holds what S_0 gave; S_0 is copied (the last
-// segment may write where it lies).  F goes to LDS in parts, each of four wavefronts a quarter.  Segments count in the order of the walk.
+// segment may write where it lies).  A workgroup takes 16 columns, each of its four wavefronts a quarter of the rows, for which it has the next F and Z
+// on the way; the state goes round through LDS, in parts.  Segments count in the order of the walk.
 template <int DK> __global__ __launch_bounds__(256) void gdr_join_kernel(GdrArgs a, const float* S0, int slices) {
-  constexpr int KB = DK / 32, FRAGS = DK / 16 * KB, PER = FRAGS / 4;
-  __shared__ u32x4 parts[FRAGS * 3 * 64];
-  const Columns at(a, slices);
-  const int lane = threadIdx.x & 63, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wide = a.dvp + DK;
-  f32x4 S[DK / 16] = {}, Z[DK / 16], F[PER][2];
-  if (S0) load_tiles(StateWindow(S0 + (int64_t)at.unit * a.Dk * a.Dv, a.Dv, a.Dk, a.Dv, at.first), S);
-  store_tiles(start_window<DK>(a, 0, at), S);
-  load_tiles(sum_window<DK>(a, 0, at, false), S);
-  store_tiles(start_window<DK>(a, 1, at), S);
+  constexpr int KB = DK / 32, TILES = DK / 64;
+  __shared__ u32x4 parts[2][KB * 3 * 64];
+  const int lane = threadIdx.x & 63, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wide = a.dvp + DK, row = wave * (DK / 4);
+  const int unit = blockIdx.x / slices, column = (blockIdx.x - unit * slices) * 16 + (lane & 15), units = a.B * a.H;
+  f32x4 S[TILES] = {}, Z[TILES], F[TILES][KB][2];
+  const auto starts = [&](int index) { return StateWindow(a.starts + (((int64_t)index * units + unit) * DK + row) * a.dvp, a.dvp, DK / 4, a.dvp, column); };
+  const float* sums = a.sums + ((int64_t)unit * DK + row) * wide;
+  const int64_t step = (int64_t)units * DK * wide;
+  if (S0 && row < a.Dk) load_tiles(StateWindow(S0 + ((int64_t)unit * a.Dk + row) * a.Dv, a.Dv, a.Dk - row, a.Dv, column), S);
+  store_tiles(starts(0), S);
+  load_tiles(StateWindow(sums, wide, DK / 4, wide, column), S);
+  store_tiles(starts(1), S);
   const auto load = [&](int index) {
-    load_tiles(sum_window<DK>(a, index, at, false), Z);
-    const float* f = a.sums + ((int64_t)index * a.B * a.H + at.unit) * DK * wide + a.dvp + (lane & 15) * wide + 4 * g;
+    const float *z = sums + index * step, *f = z + a.dvp + (lane & 15) * wide + 4 * g;
+    load_tiles(StateWindow(z, wide, DK / 4, wide, column), Z);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int frag = wave * PER + i, rt = frag / KB, kb = frag - rt * KB;
+    for (int t = 0; t < TILES; ++t)
 #pragma unroll
-      for (int half = 0; half < 2; ++half) F[i][half] = *reinterpret_cast<const f32x4*>(f + (int64_t)rt * 16 * wide + kb * 32 + half * 16);
-    }
+      for (int i = 0; i < KB * 2; ++i) F[t][i >> 1][i & 1] = *reinterpret_cast<const f32x4*>(f + t * 16 * wide + i * 16);
   };
-  if (a.segments > 2) load(1);
-  for (int index = 1; index < a.segments - 1; ++index) {
+  const int last = a.segments - 1;
+  if (last > 1) load(1);
+  for (int index = 1; index < last; ++index) {
+    // rows 16 or 32 of the state are half or all of an operand of 32
+    if constexpr (TILES == 2) {
+      store_parts(parts[index & 1] + lane, wave, parts_of<3>(S[0], S[1]));
+    } else {
+      const float x[8] = {S[0][0], S[0][1], S[0][2], S[0][3]};
+      const Parts<3> p = parts_of<3>(x);
+      typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int i = 0; i < PER; ++i) store_parts(parts + lane, wave * PER + i, parts_of<3>(F[i][0], F[i][1]));
-    __syncthreads();
-    Parts<3> Sp[KB];
-    column_parts<3>(S, Sp);
-#pragma unroll
-    for (int rt = 0; rt < DK / 16; ++rt) S[rt] = Z[rt];
-    if (index + 1 < a.segments - 1) load(index + 1);
+      for (int i = 0; i < 3; ++i) reinterpret_cast<u32x2*>(&parts[index & 1][((wave >> 1) * 3 + i) * 64 + lane])[wave & 1] = u32x2{p.p[i][0], p.p[i][1]};
+    }
+    Parts<3> f[KB][TILES];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int rt = 0; rt < DK / 16; rt += 4) {
-        Parts<3> f[4];
-        load_parts(parts + lane, rt * KB + kb, KB, f);
-        mul_add(f, Sp[kb], reinterpret_cast<f32x4(&)[4]>(S[rt]));
-      }
-    store_tiles(start_window<DK>(a, index + 1, at), S);
-    __syncthreads();
+      for (int t = 0; t < TILES; ++t) f[kb][t] = parts_of<3>(F[t][kb][0], F[t][kb][1]);
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) S[t] = Z[t];
+    load(imin(index + 1, last - 1));
+    __syncthreads();  // (one a segment: the other half of `parts` was last read before the one before)
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) mul_add(f[kb], load_parts<3>(parts[index & 1] + lane, kb), S);
+    store_tiles(starts(index + 1), S);
   }
 }
 
 template <typename T, int DK, bool NEAR, int MODE>
-__global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt, int slices) {
+__global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt, int groups) {
   constexpr int IN = GdrType<T>::IN, OUT = GdrType<T>::OUT, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3, PF = 6 * OUT;
   constexpr bool KEPT = MODE == KEEP, OUTPUT = MODE != SUM;
   constexpr int RF = OUTPUT ? 2 * KF : KF, TF = OUTPUT ? MF + PF : MF;  // (the operands of Q and P are read for o alone)
   constexpr bool STAGED = 2 * KF + KTF + MF + PF <= 150;  // KB of LDS
   __shared__ u32x4 one[STAGED ? RF * 64 : 1], two[STAGED ? (KTF + TF) * 64 : 1];  // what the halves read
   __shared__ f32x4 weights[2][64];  // w, ka, qa, ke of a chunk
-  bool transition = false;
-  const Columns at = OUTPUT ? Columns(a, slices) : Columns(a, slices, DK, transition);
-  const int segment = blockIdx.y, begin = segment * a.span, end = imin(begin + a.span, a.chunks);
+  int group;
+  Columns at(a, OUTPUT ? groups : groups + DK / 64, &group);  // (a sum's transition is the last columns)
+  const bool transition = !OUTPUT && group >= groups;
+  at.take(transition ? group - groups : group);
+  const int segment = at.segment, begin = segment * a.span, end = imin(begin + a.span, a.chunks);
   if (transition && segment == 0) return;  // (all wavefronts: the first segment's state is S0's)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t matrix = (int64_t)a.Dk * a.Dv, plane = (int64_t)a.B * a.H * matrix;
@@ -628,15 +633,17 @@ template <typename T, int DK, bool NEAR> __global__ __launch_bounds__(256) void 
 
 // SUM: as forward, of segments from the last on.
 template <typename T, int DK, bool NEAR, int MODE>
-__global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o, const float* dST, ard_steps dv, float* dS0, int slices) {
+__global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o, const float* dST, ard_steps dv, float* dS0, int groups) {
   constexpr int IN = GdrType<T>::IN, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3;
   constexpr bool STAGED = KF + 2 * KTF + 2 * MF <= 150;
   constexpr bool OUTPUT = MODE != SUM;
   __shared__ u32x4 one[STAGED ? (KF + MF) * 64 : 1], two[STAGED ? (2 * KTF + MF) * 64 : 1];
   __shared__ f32x4 weights[2][64];  // w, ka, qa, ke of a chunk
-  bool transition = false;
-  const Columns at = OUTPUT ? Columns(a, slices) : Columns(a, slices, DK, transition);
-  const int segment = blockIdx.y, begin = (a.segments - 1 - segment) * a.span, end = imin(begin + a.span, a.chunks);
+  int group;
+  Columns at(a, OUTPUT ? groups : groups + DK / 64, &group);  // (a sum's transition is the last columns)
+  const bool transition = !OUTPUT && group >= groups;
+  at.take(transition ? group - groups : group);
+  const int segment = at.segment, begin = (a.segments - 1 - segment) * a.span, end = imin(begin + a.span, a.chunks);
   if (transition && segment == 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t matrix = (int64_t)a.Dk * a.Dv;
@@ -1243,14 +1250,14 @@ extern "C" int32_t ard_gdr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
     ARD_LAUNCH_CHECK("gdr_prep_kernel");
     const int groups = ceil_div(p.slices, 4);
     if (a.segments > 1) {
-      ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, SUM>), dim3(B * H * (groups + DK / 64), a.segments - 1), dim3(256), 0, st, a, S0, out, ST, ckpt, p.slices);
+      ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, SUM>), dim3(B * H * (groups + DK / 64) * (a.segments - 1)), dim3(256), 0, st, a, S0, out, ST, ckpt, groups);
       ARD_LAUNCH_CHECK("gdr_fwd_kernel");
-      ARD_LAUNCH_NAMED("gdr_join_kernel", (gdr_join_kernel<DK>), dim3(B * H * groups), dim3(256), 0, st, a, S0, p.slices);
+      ARD_LAUNCH_NAMED("gdr_join_kernel", (gdr_join_kernel<DK>), dim3(B * H * p.slices), dim3(256), 0, st, a, S0, p.slices);
       ARD_LAUNCH_CHECK("gdr_join_kernel");
     }
-    const dim3 grid(B * H * groups, a.segments);
-    if (ckpt) ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, KEEP>), grid, dim3(256), 0, st, a, S0, out, ST, ckpt, p.slices);
-    else ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, DROP>), grid, dim3(256), 0, st, a, S0, out, ST, ckpt, p.slices);
+    const dim3 grid(B * H * groups * a.segments);
+    if (ckpt) ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, KEEP>), grid, dim3(256), 0, st, a, S0, out, ST, ckpt, groups);
+    else ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, DROP>), grid, dim3(256), 0, st, a, S0, out, ST, ckpt, groups);
     ARD_LAUNCH_CHECK("gdr_fwd_kernel");
     return (int32_t)ARD_OK;
   });
@@ -1284,12 +1291,12 @@ extern "C" int32_t ard_gdr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
     ARD_LAUNCH_CHECK("gdr_rows_kernel");
     const int groups = ceil_div(slices, 4);
     if (a.segments > 1) {
-      ARD_LAUNCH_NAMED("gdr_back_kernel", (gdr_back_kernel<E, DK, NEAR, SUM>), dim3(B * H * (groups + DK / 64), a.segments - 1), dim3(256), 0, st, a, od, dST, dv, dS0, slices);
+      ARD_LAUNCH_NAMED("gdr_back_kernel", (gdr_back_kernel<E, DK, NEAR, SUM>), dim3(B * H * (groups + DK / 64) * (a.segments - 1)), dim3(256), 0, st, a, od, dST, dv, dS0, groups);
       ARD_LAUNCH_CHECK("gdr_back_kernel");
-      ARD_LAUNCH_NAMED("gdr_join_kernel", (gdr_join_kernel<DK>), dim3(B * H * groups), dim3(256), 0, st, a, dST, slices);
+      ARD_LAUNCH_NAMED("gdr_join_kernel", (gdr_join_kernel<DK>), dim3(B * H * slices), dim3(256), 0, st, a, dST, slices);
       ARD_LAUNCH_CHECK("gdr_join_kernel");
     }
-    ARD_LAUNCH_NAMED("gdr_back_kernel", (gdr_back_kernel<E, DK, NEAR, KEEP>), dim3(B * H * groups, a.segments), dim3(256), 0, st, a, od, dST, dv, dS0, slices);
+    ARD_LAUNCH_NAMED("gdr_back_kernel", (gdr_back_kernel<E, DK, NEAR, KEEP>), dim3(B * H * groups * a.segments), dim3(256), 0, st, a, od, dST, dv, dS0, groups);
     ARD_LAUNCH_CHECK("gdr_back_kernel");
     const auto grads_of = [&](auto dv_, auto quick) {
       constexpr int DV = decltype(dv_)::value;
