@@ -783,18 +783,39 @@ template <typename T, int N, bool QUICK> struct Runs {
       load_some<N>(p + row * step + at, row < rows ? wide - at : 0, x);
     }
   }
+  // eight as an operand's parts will be made of: bf16 is one already, and taken apart on the way its loads would be waited for
+  struct Eight {
+    std::conditional_t<sizeof(T) == 2, u32x4, float[8]> v;
+    __device__ __forceinline__ Parts<GdrType<T>::IN> parts() const {
+      if constexpr (sizeof(T) == 2) return Parts<1>{{v}};
+      else return parts_of<3>(v);
+    }
+  };
+  __device__ __forceinline__ void load(int row, int at, Eight& x) const {
+    if constexpr (sizeof(T) == 4) {
+      load(row, at, x.v);
+    } else if constexpr (QUICK) {
+      x.v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer, at < wide ? ((uint32_t)row * (uint32_t)step + (uint32_t)at) * 2u : 0x80000000u, 0, 0));
+    } else {
+      float y[8];
+      load(row, at, y);
+      x.v = parts_of<1>(y).p[0];
+    }
+  }
 };
 
-// Four values as they were stored.
+// Four values as they were stored.  again(): they are taken apart anew from here on, not kept so.
 template <typename T> struct Four;
 template <> struct Four<float> {
   float v[4];
   __device__ __forceinline__ void set(const float (&x)[4]) { v[0] = x[0], v[1] = x[1], v[2] = x[2], v[3] = x[3]; }
   __device__ __forceinline__ float at(int r) const { return v[r]; }
+  __device__ __forceinline__ void again() {}
 };
 template <> struct Four<uint16_t> {
   uint32_t v[2];
   __device__ __forceinline__ void set(const float (&x)[4]) { v[0] = bf16_pair(x[0], x[1]), v[1] = bf16_pair(x[2], x[3]); }
+  __device__ __forceinline__ void again() { asm volatile("" : "+v"(v[0]), "+v"(v[1])); }
   __device__ __forceinline__ float at(int r) const { return __uint_as_float(r & 1 ? v[r / 2] & 0xffff0000u : v[r / 2] << 16); }
 };
 
@@ -847,20 +868,26 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
     for (int s = 0; s < a.group; ++s) {
       const int h = hk * a.group + s;
       const int64_t hu = ((int64_t)chunk * a.B + n) * a.H + h;
-      // (addresses made from these are made in the loop: taken out of it, they alone would not fit the registers)
-      int g = lane >> 4, c = lane & 15;
-      int at_lane = lane;
-      asm volatile("" : "+v"(g), "+v"(c), "+v"(at_lane));
+      // (what is made from these is made in the loop: taken out of it, it alone would not fit the registers)
+      int at_lane = threadIdx.x & 63;
+      asm volatile("" : "+v"(at_lane));
+      const int lane = at_lane, g = lane >> 4, c = lane & 15;
+#pragma unroll
+      for (int i = 0; i < OWN; ++i) kx[i].again(), qx[i].again();
       const u32x4 *ktf = a.cols + (int64_t)unit * (DK / 4) * IN * 64 + at_lane, *qtf = ktf + DK / 8 * IN * 64;
       u32x4 *lu = lds + at_lane, *lx = lu + 4 * VB * N * 64, *lo = lu + 8 * VB * N * 64, *ls = KEEP ? lu + ROWS * 64 : lu;
       const int mine = w * 16 + c;
       const Runs<float, 8, QUICK> S(ckpt + hu * a.Dk * a.Dv, a.Dv, a.Dk, a.Dv);
       const Runs<float, 8, true> ds(a.ds + hu * DK * a.dvp, a.dvp, DK, a.dvp);
+      // the gates whose slopes the end needs, as they are stored: f for the first wavefront, b for those of the first half (by all lanes and without a
+      // branch, of the last step for lanes behind it: registers that are moved aside where lanes come together again have lost those lanes' values)
+      T fg, bg;
       {
         // (of two halves the second takes dX)
         const Runs<float, 8, true> rows_of_mine((half ? a.dx : a.u) + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp), dx(a.dx + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp);
         const Runs<T, 8, QUICK> go((const T*)d_o.p + t0 * d_o.t + n * d_o.b + h * a.Dv, d_o.t, live, a.Dv);
-        float x[VB][8], y[VB][8], z[HALVES > 1 ? 1 : VB][8];
+        float x[VB][8], z[HALVES > 1 ? 1 : VB][8];
+        typename Runs<T, 8, QUICK>::Eight y[VB];
 #pragma unroll
         for (int vb = 0; vb < VB; ++vb) rows_of_mine.load(mine, vb * 32 + 8 * g, x[vb]);
         if (HALVES == 1) {
@@ -872,6 +899,8 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
           for (int vb = 0; vb < VB; ++vb) go.load(mine, vb * 32 + 8 * g, y[vb]);
         }
         const u32x4 weights = w8 < 3 ? ((const u32x4*)&a.steps[hu])[w8 * 64 + lane] : u32x4{};
+        fg = ((const T*)a.f.p)[(int64_t)(t0 + imin(63 - lane, live - 1)) * a.f.t + n * a.f.b + h];
+        bg = ((const T*)a.b.p)[(int64_t)(t0 + imin(mine, live - 1)) * a.b.t + n * a.b.b + h];
         __syncthreads();  // (the head before has been read)
         if (w8 < 3) ((u32x4*)&st)[w8 * 64 + lane] = weights;
         u32x4* to = half ? lx : lu;
@@ -883,7 +912,7 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
         }
         if (half == 0) {
 #pragma unroll
-          for (int vb = 0; vb < VB; ++vb) store_parts<IN>(lo, w * VB + vb, parts_of<IN>(y[vb]));
+          for (int vb = 0; vb < VB; ++vb) store_parts<IN>(lo, w * VB + vb, y[vb].parts());
         }
       }
       float Sx[MINE][8], Dx[MINE][8];
@@ -892,10 +921,6 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
         const int rt = (i * WAVES + w8) / VB, vb = (i * WAVES + w8) % VB;
         S.load(rt * 16 + c, vb * 32 + 8 * g, Sx[i]);
       }
-      // the gates whose slopes the end needs: f by the first wavefront, b by those of the first half
-      float fg = 0.0f, bg = 0.0f;
-      if (w8 == 0 && 63 - lane < live) fg = ElemTraits<T>::to_f32(((const T*)a.f.p)[(int64_t)(t0 + 63 - lane) * a.f.t + n * a.f.b + h]);
-      if (half == 0 && mine < live) bg = ElemTraits<T>::to_f32(((const T*)a.b.p)[(int64_t)(t0 + mine) * a.b.t + n * a.b.b + h]);
       __syncthreads();
       Parts<N> ub[KEEP ? 1 : VB], xb[KEEP ? 1 : VB];
       Parts<IN> ob[KEEP ? 1 : VB];
@@ -909,26 +934,44 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
       const double Gm = st.G[mine];
       const float wm = st.w[mine];
       float dw = 0.0f;
-      // by pairs of row tiles, ready as operands: N_ij and R_ij of later rows i, of earlier rows j.  (All tiles are multiplied, though some are not needed:
-      // a branch around each would make the next one's operands wait for it.)
+      // By pairs of row tiles, ready as operands: N_ij and R_ij of earlier rows j, and of later rows i; each shortly before its products where LDS still has the rows
+      // then.  (All tiles are multiplied, though some are not needed: a branch around each would make the next one's operands wait for it.)
       Parts<N> below[2], belowq[2], above[2], aboveq[2];
-      {
-        f32x4 dn[4] = {}, dnq[4] = {}, up[4] = {}, upq[4] = {};
+      const auto earlier = [&] {
+        f32x4 up[4] = {}, upq[4] = {};
 #pragma unroll
         for (int vb = 0; vb < VB; ++vb) {
           Parts<N> y[4];
-          {
-            Parts<IN> z[4];
-            const Parts<N> u = of_u(vb);
-            load_parts(lx, vb, VB, y);
-            mul_add(y, u, dn);
-            load_parts(lo, vb, VB, z);
-            mul_add(z, u, dnq);
-          }
-          __builtin_amdgcn_sched_barrier(0);  // (operands read further ahead would not fit the registers)
           load_parts(lu, vb, VB, y);
           mul_add(y, of_x(vb), up);
           mul_add(y, of_o(vb), upq);
+          __builtin_amdgcn_sched_barrier(0);  // (operands read further ahead would not fit the registers)
+        }
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) {
+          const f32x4 rk = row_weights(st.rk, rt);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int i = rt * 16 + 4 * g + r;
+            const float fade = rk[r] * exp_of(-(float)fabs(st.G[i] - Gm));
+            up[rt][r] = i < mine ? -up[rt][r] * (wm * fade) : 0.0f;
+            upq[rt][r] = i <= mine ? upq[rt][r] * (a.scale * fade) : 0.0f;
+          }
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) above[kb] = parts_of<N>(up[2 * kb], up[2 * kb + 1]), aboveq[kb] = parts_of<N>(upq[2 * kb], upq[2 * kb + 1]);
+      };
+      const auto later = [&] {
+        f32x4 dn[4] = {}, dnq[4] = {};
+#pragma unroll
+        for (int vb = 0; vb < VB; ++vb) {
+          Parts<N> y[4];
+          Parts<IN> z[4];
+          const Parts<N> u = of_u(vb);
+          load_parts(lx, vb, VB, y);
+          mul_add(y, u, dn);
+          load_parts(lo, vb, VB, z);
+          mul_add(z, u, dnq);
           __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
@@ -941,8 +984,6 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
             if (i == mine) dw = dn[rt][r];
             dn[rt][r] = i > mine ? -dn[rt][r] * (wr[r] * rk[r] * fade) : 0.0f;
             dnq[rt][r] = i >= mine ? dnq[rt][r] * (a.scale * rq[r] * fade) : 0.0f;
-            up[rt][r] = i < mine ? -up[rt][r] * (wm * rk[r] * fade) : 0.0f;
-            upq[rt][r] = i <= mine ? upq[rt][r] * (a.scale * rk[r] * fade) : 0.0f;
           }
         }
         // what the pairs (i, the lane's step j) give to every step from behind j up to i
@@ -955,21 +996,20 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
           f32x4 x = cross[rt] * rkm;
           x[2] += x[3], x[1] += x[2], x[0] += x[1];
           const float whole = x[0], n1 = __shfl_down(whole, 16), n2 = __shfl_down(whole, 32), n3 = __shfl_down(whole, 48);
-          const float later = behind + ((g < 3 ? n1 : 0.0f) + (g < 2 ? n2 : 0.0f) + (g < 1 ? n3 : 0.0f));
+          const float more = behind + ((g < 3 ? n1 : 0.0f) + (g < 2 ? n2 : 0.0f) + (g < 1 ? n3 : 0.0f));
           behind += over_rows(whole);
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float sum = row_sum(rt * 16 + 4 * g + r > mine ? x[r] + later : 0.0f);
+            const float sum = row_sum(rt * 16 + 4 * g + r > mine ? x[r] + more : 0.0f);
             crossed = c == rt * 4 + r ? sum : crossed;
           }
         }
         crossing[w8][(c >> 2) * 16 + 4 * g + (c & 3)] = crossed;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          below[kb] = parts_of<N>(dn[2 * kb], dn[2 * kb + 1]), belowq[kb] = parts_of<N>(dnq[2 * kb], dnq[2 * kb + 1]);
-          above[kb] = parts_of<N>(up[2 * kb], up[2 * kb + 1]), aboveq[kb] = parts_of<N>(upq[2 * kb], upq[2 * kb + 1]);
-        }
-      }
+        for (int kb = 0; kb < 2; ++kb) below[kb] = parts_of<N>(dn[2 * kb], dn[2 * kb + 1]), belowq[kb] = parts_of<N>(dnq[2 * kb], dnq[2 * kb + 1]);
+      };
+      earlier();
+      if (!KEEP) later();
       const float since = st.since[mine], still = st.still[mine];
       float moved = 0.0f, into = 0.0f, both = 0.0f;
       if (!KEEP) __syncthreads();
@@ -1016,6 +1056,7 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
 #pragma unroll
         for (int e = 0; e < 8; ++e) both = fmaf(Sx[i][e], Dx[i][e], both);
       }
+      if (KEEP) later();
       __syncthreads();
       {
         f32x4 te[OWN] = {};
@@ -1066,13 +1107,13 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
         const int i = 63 - lane;
         const int64_t t = t0 + i;
         float grad = 0.0f;
-        if (i < live) grad = (float)x * logistic(-fg);
+        if (i < live) grad = (float)x * logistic(-ElemTraits<T>::to_f32(fg));
         if (i < steps) ((T*)df.p)[t * df.t + n * df.b + h] = ElemTraits<T>::from_f32(grad);
       }
       if (half == 0 && g == 0 && mine < steps) {
         const int64_t t = t0 + mine;
         float grad = 0.0f;
-        if (mine < live) grad = dw * logistic(-bg);
+        if (mine < live) grad = dw * logistic(-ElemTraits<T>::to_f32(bg));
         ((T*)db.p)[t * db.t + n * db.b + h] = ElemTraits<T>::from_f32(grad);
       }
     }
