@@ -77,10 +77,10 @@ __global__ __launch_bounds__(64) void gdr_steps_kernel(GdrArgs a, const float* S
 }
 
 // ---- what does not depend on the states -------------------------------------------
-template <int DK> struct PrepShared {
+template <typename T, int DK> struct PrepShared {
   union {
     struct {
-      float k[kChunk][DK + 4], q[kChunk][DK + 4];
+      T k[kChunk][DK + 16 / sizeof(T)], q[kChunk][DK + 16 / sizeof(T)];  // as they are stored
     };
     struct {
       float A[kChunk][kChunk + 4], M[kChunk][kChunk + 4], P[kChunk][kChunk + 4];
@@ -95,6 +95,12 @@ template <int N, int LD> __device__ __forceinline__ Parts<N> row_parts(const flo
   const f32x4 lo = *reinterpret_cast<const f32x4*>(&m[row][kb * 32 + 4 * g]), hi = *reinterpret_cast<const f32x4*>(&m[row][kb * 32 + 16 + 4 * g]);
   return parts_of<N>(lo, hi);
 }
+template <int N, int LD> __device__ __forceinline__ Parts<N> row_parts(const uint16_t (*m)[LD], int row, int kb, int g) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  static_assert(N == 1, "");
+  const u32x2 lo = *reinterpret_cast<const u32x2*>(&m[row][kb * 32 + 4 * g]), hi = *reinterpret_cast<const u32x2*>(&m[row][kb * 32 + 16 + 4 * g]);
+  return Parts<1>{{u32x4{lo[0], lo[1], hi[0], hi[1]}}};
+}
 // the same of the transpose: of column `col`, rows in that order
 template <int N, int LD> __device__ __forceinline__ Parts<N> col_parts(const float (*m)[LD], int col, int kb, int g) {
   float x[8];
@@ -102,14 +108,44 @@ template <int N, int LD> __device__ __forceinline__ Parts<N> col_parts(const flo
   for (int j = 0; j < 8; ++j) x[j] = m[kb * 32 + 4 * g + (j & 3) + 16 * (j >> 2)][col];
   return parts_of<N>(x);
 }
+template <int N, int LD> __device__ __forceinline__ Parts<N> col_parts(const uint16_t (*m)[LD], int col, int kb, int g) {
+  static_assert(N == 1, "");
+  Parts<1> s;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int row = kb * 32 + 4 * g + (2 * j & 3) + 16 * (j >> 1);
+    s.p[0][j] = m[row][col] | (uint32_t)m[row + 1][col] << 16;
+  }
+  return s;
+}
 
-template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void gdr_prep_kernel(GdrArgs a) {
+template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 3 : 2) void gdr_prep_kernel(GdrArgs a) {
   constexpr int IN = GdrType<T>::IN, OUT = GdrType<T>::OUT, KB = DK / 32;
-  __shared__ PrepShared<DK> sh;
+  __shared__ PrepShared<T, DK> sh;
   const int unit = blockIdx.x, chunk = unit / (a.B * a.Hk), n = (unit - chunk * a.B * a.Hk) / a.Hk, hk = unit % a.Hk;
   const int t0 = chunk * kChunk, live = imin(live_steps(a, n) - t0, kChunk);
   if (live <= 0) return;  // (nobody reads this chunk's operands)
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  // sums of log(a) and write strengths of a head, by one wavefront
+  const auto gates = [&](int h) {
+    const int64_t t = t0 + lane;
+    double G = 0.0;
+    float wr = 0.0f;
+    if (lane < live) {
+      const float f = ElemTraits<T>::to_f32(((const T*)a.f.p)[t * a.f.t + n * a.f.b + h]);
+      wr = logistic(ElemTraits<T>::to_f32(((const T*)a.b.p)[t * a.b.t + n * a.b.b + h]));
+      // log(sg(f)); below -1e4 its exponential is 0 as well, and sums stay finite
+      const float l = fminf(f, 0.0f) - log1pf(expf(-fabsf(f)));
+      G = (double)(l < -1e4f ? -1e4f : l);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const double before = __shfl_up(G, d);
+      if (lane >= d) G += before;
+    }
+    sh.G[lane] = G, sh.w[lane] = wr;
+  };
+  if (w == 3) gates(hk * a.group);
   {
     const int row = threadIdx.x >> 2, part = threadIdx.x & 3;
     const int64_t t = t0 + row;
@@ -120,8 +156,9 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void g
       const int at = (part + 4 * i) * 8;
       float x[8] = {}, y[8] = {};
       if (row < live) load_some<8>(kp + at, a.Dk - at, x), load_some<8>(qp + at, a.Dk - at, y);
+      store_run<8>(&sh.k[row][at], x), store_run<8>(&sh.q[row][at], y);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) ks = fmaf(x[j], x[j], ks), qs = fmaf(y[j], y[j], qs), sh.k[row][at + j] = x[j], sh.q[row][at + j] = y[j];
+      for (int j = 0; j < 8; ++j) ks = fmaf(x[j], x[j], ks), qs = fmaf(y[j], y[j], qs);
     }
     ks += __shfl_xor(ks, 1), qs += __shfl_xor(qs, 1);
     ks += __shfl_xor(ks, 2), qs += __shfl_xor(qs, 2);
@@ -155,31 +192,15 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void g
     const int h = hk * a.group + s;
     const int64_t out = ((int64_t)chunk * a.B + n) * a.H + h;
     __syncthreads();  // keys and queries, or the head before, have been read
-    if (w == 0) {
-      const int64_t t = t0 + lane;
-      double G = 0.0;
-      float wr = 0.0f;
-      if (lane < live) {
-        const float f = ElemTraits<T>::to_f32(((const T*)a.f.p)[t * a.f.t + n * a.f.b + h]);
-        wr = logistic(ElemTraits<T>::to_f32(((const T*)a.b.p)[t * a.b.t + n * a.b.b + h]));
-        // log(sg(f)); below -1e4 its exponential is 0 as well, and sums stay finite
-        const float l = fminf(f, 0.0f) - log1pf(expf(-fabsf(f)));
-        G = (double)(l < -1e4f ? -1e4f : l);
-      }
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const double before = __shfl_up(G, d);
-        if (lane >= d) G += before;
-      }
-      sh.G[lane] = G, sh.w[lane] = wr;
-      const double last = __shfl(G, 63);
+    if (w == 3) {  // (it has the fewest blocks to multiply)
       Steps64& st = a.steps[out];
-      const float rk = sh.rk[lane], rq = sh.rq[lane], since = expf((float)G), still = expf((float)(last - G));
+      const double G = sh.G[lane], last = sh.G[63];
+      const float wr = sh.w[lane], rk = sh.rk[lane], rq = sh.rq[lane], since = expf((float)G), still = expf((float)(last - G));
       st.G[lane] = G, st.since[lane] = since, st.still[lane] = still, st.w[lane] = wr, st.rk[lane] = rk, st.rq[lane] = rq;
       st.ka[lane] = rk * since, st.qa[lane] = a.scale * rq * since, st.ke[lane] = rk * still;
       if (lane == 63) st.whole = since;
     }
-    __syncthreads();
+    f32x4 own = {};  // of A's diagonal block
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) {
       const int j = ct * 16 + c;
@@ -188,28 +209,31 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void g
         const int i = w * 16 + 4 * g + r;
         float A = 0.0f, P = 0.0f;
         if (j <= i) {
-          const float fade = expf((float)(sh.G[i] - sh.G[j])) * sh.rk[j];
+          const float fade = exp_of((float)(sh.G[i] - sh.G[j])) * sh.rk[j];
           A = j < i ? sh.w[i] * sh.rk[i] * fade * kk[ct][r] : 0.0f;
           P = a.scale * sh.rq[i] * fade * qk[ct][r];
         }
-        sh.A[i][j] = A, sh.P[i][j] = P, sh.M[i][j] = 0.0f;
+        sh.A[i][j] = A, sh.P[i][j] = P;
+        if (ct == w) own[r] = A;
+        else sh.M[i][j] = 0.0f;
       }
     }
-    __syncthreads();
-    {  // the diagonal blocks' inverses, a column a lane
+    {  // the diagonal blocks' inverses, a column a lane; A's elements go from the lanes that made them to the scalar registers, without LDS
       float x[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         float s0 = i == c ? 1.0f : 0.0f, s1 = 0.0f;
 #pragma unroll
         for (int j = 0; j < i; ++j) {
-          const float m = sh.A[w * 16 + i][w * 16 + j];
+          const float m = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(own[i & 3]), 16 * (i >> 2) + j));
           if (j & 1) s1 = fmaf(-m, x[j], s1);
           else s0 = fmaf(-m, x[j], s0);
         }
         x[i] = s0 + s1;
-        if (g == 0) sh.M[w * 16 + i][w * 16 + c] = x[i];
       }
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (g == 0) sh.M[w * 16 + i][w * 16 + c] = x[i];
     }
 #pragma unroll
     for (int d = 1; d < 4; ++d) {  // the blocks d below: M_rc = -M_rr sum_m A_rm M_mc
@@ -229,6 +253,7 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256) void g
       }
     }
     __syncthreads();
+    if (w == 3 && s + 1 < a.group) gates(h + 1);  // (it has one operand less to store)
     constexpr int PP = BWD ? 3 : OUT;
     u32x4 *mf = a.tri + out * (BWD ? 54 : 18 + 6 * OUT) * 64 + lane, *pf = mf + 18 * 64, *mtf = mf + 18 * 64, *ptf = mf + 36 * 64;
     for (int i = w; i < 6; i += 4) {
