@@ -18,62 +18,90 @@
 namespace ard {
 
 // ---- step by step ---------------------------------------------------------------
-// A lane holds a column of S, a wavefront 64 of a head's; keys and queries reach the lanes through LDS.
-template <typename T, int DK>
-__global__ __launch_bounds__(64) void gdr_steps_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt) {
-  __shared__ float kq[2][DK];
-  const int slices = (a.Dv + 63) / 64, lane = threadIdx.x;
-  const int unit = blockIdx.x / slices, col = (blockIdx.x - unit * slices) * 64 + lane, n = unit / a.H, h = unit - n * a.H, hk = h / a.group;
-  const bool on = col < a.Dv;
-  const int64_t state = (int64_t)unit * a.Dk * a.Dv + col, plane = (int64_t)a.B * a.H * a.Dk * a.Dv;
-  float S[DK];
+// A wavefront holds 32 columns of a head's S: V of them (4, if rows are whole runs of 4) and a share of the rows a lane, which has these rows' keys and queries too; sums
+// over rows go round the lanes.  Reading and writing the states bounds a generation step: 128-byte pieces of rows, 64 registers a lane for them, so that
+// four wavefronts a SIMD have theirs on the way.
+template <typename T, int DK, int V>
+__global__ __launch_bounds__(256) void gdr_steps_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt, int slices) {
+  constexpr int ACROSS = 32 / V, R = DK * ACROSS / 64;  // lanes of a row; rows of a lane
+  const int index = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), unit = index / slices;
+  if (unit >= a.B * a.H) return;
+  const int lane = threadIdx.x & 63, col = (index - unit * slices) * 32 + lane % ACROSS * V, row = lane / ACROSS * R;
+  const int n = unit / a.H, h = unit - n * a.H, hk = h / a.group;
+  const int64_t matrix = (int64_t)a.Dk * a.Dv, plane = (int64_t)a.B * a.H * matrix;
+  const uint32_t at = col < a.Dv ? (uint32_t)(row * a.Dv + col) * 4u : 0x80000000u, step = a.Dv * 4u;
+  const auto states = [&](const float* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p + unit * matrix), 0, (int)matrix * 4, 0x00020000); };
+  float S[R][V];
+  const auto store = [&](float* p) {
+    const auto buffer = states(p);
 #pragma unroll
-  for (int i = 0; i < DK; ++i) S[i] = S0 && on && i < a.Dk ? S0[state + (int64_t)i * a.Dv] : 0.0f;
+    for (int i = 0; i < R; ++i) {
+      if constexpr (V == 4) __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(S[i][0]), __float_as_uint(S[i][1]), __float_as_uint(S[i][2]), __float_as_uint(S[i][3])}, buffer, at + i * step, 0, 0);
+      else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[i][0]), buffer, at + i * step, 0, 0);
+    }
+  };
+  const auto over_rows = [&](float x) {
+#pragma unroll
+    for (int d = ACROSS; d < 64; d *= 2) x += __shfl_xor(x, d);
+    return x;
+  };
+  float k[R], q[R], v[V], f, b;
+  const auto inputs = [&](int t) {
+    const T *kp = (const T*)a.k.p + t * a.k.t + n * a.k.b + hk * a.Dk + row, *qp = (const T*)a.q.p + t * a.q.t + n * a.q.b + hk * a.Dk + row;
+#pragma unroll
+    for (int i = 0; i < R; i += 8) load_some<8>(kp + i, a.Dk - row - i, reinterpret_cast<float(&)[8]>(k[i])), load_some<8>(qp + i, a.Dk - row - i, reinterpret_cast<float(&)[8]>(q[i]));
+    load_some<V>((const T*)a.v.p + t * a.v.t + n * a.v.b + h * a.Dv + col, a.Dv - col, v);
+    f = ElemTraits<T>::to_f32(((const T*)a.f.p)[t * a.f.t + n * a.f.b + h]), b = ElemTraits<T>::to_f32(((const T*)a.b.p)[t * a.b.t + n * a.b.b + h]);
+  };
   const int live = live_steps(a, n);
+  if (S0) {
+    const auto buffer = states(S0);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if constexpr (V == 4) {
+        const f32x4 x = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer, at + i * step, 0, 0));
+        S[i][0] = x[0], S[i][1] = x[1], S[i][2] = x[2], S[i][3] = x[3];
+      } else {
+        S[i][0] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer, at + i * step, 0, 0));
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) S[i][e] = 0.0f;
+  }
   for (int t = 0; t < a.T; ++t) {
-    if (ckpt && t % kChunk == 0 && on) {
-#pragma unroll
-      for (int i = 0; i < DK; ++i)
-        if (i < a.Dk) ckpt[(t / kChunk) * plane + state + (int64_t)i * a.Dv] = S[i];
-    }
+    if (ckpt && t % kChunk == 0) store(ckpt + (t / kChunk) * plane);
     T* out = (T*)o.p + t * o.t + n * o.b + h * a.Dv + col;
-    if (t >= live) {
-      if (on) *out = ElemTraits<T>::from_f32(0.0f);
-      continue;
+    float y[V] = {};
+    if (t < live) {
+      inputs(t);
+      float ks = 0.0f, qs = 0.0f, e[V] = {};
+#pragma unroll
+      for (int i = 0; i < R; ++i) ks = fmaf(k[i], k[i], ks), qs = fmaf(q[i], q[i], qs);
+      const float al = logistic(f), w = logistic(b), rk = 1.0f / sqrtf(over_rows(ks) + a.eps), rq = a.scale / sqrtf(over_rows(qs) + a.eps);
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        k[i] *= rk, q[i] *= rq;
+#pragma unroll
+        for (int j = 0; j < V; ++j) e[j] = fmaf(k[i], S[i][j], e[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) e[j] = w * (v[j] - al * over_rows(e[j]));
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          S[i][j] = fmaf(k[i], e[j], al * S[i][j]);
+          y[j] = fmaf(q[i], S[i][j], y[j]);
+        }
+#pragma unroll
+      for (int j = 0; j < V; ++j) y[j] = over_rows(y[j]);
     }
-    const T* kp = (const T*)a.k.p + t * a.k.t + n * a.k.b + hk * a.Dk;
-    const T* qp = (const T*)a.q.p + t * a.q.t + n * a.q.b + hk * a.Dk;
-    float kx[DK / 64], qx[DK / 64], ks = 0.0f, qs = 0.0f;
-#pragma unroll
-    for (int i = 0; i < DK / 64; ++i) {
-      const int c = lane + 64 * i;
-      kx[i] = c < a.Dk ? ElemTraits<T>::to_f32(kp[c]) : 0.0f, qx[i] = c < a.Dk ? ElemTraits<T>::to_f32(qp[c]) : 0.0f;
-      ks = fmaf(kx[i], kx[i], ks), qs = fmaf(qx[i], qx[i], qs);
-    }
-    const float al = logistic(ElemTraits<T>::to_f32(((const T*)a.f.p)[t * a.f.t + n * a.f.b + h]));
-    const float w = logistic(ElemTraits<T>::to_f32(((const T*)a.b.p)[t * a.b.t + n * a.b.b + h]));
-    const float v = on ? ElemTraits<T>::to_f32(((const T*)a.v.p)[t * a.v.t + n * a.v.b + h * a.Dv + col]) : 0.0f;
-    const float rk = 1.0f / sqrtf(wave_sum(ks) + a.eps), rq = a.scale / sqrtf(wave_sum(qs) + a.eps);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < DK / 64; ++i) kq[0][lane + 64 * i] = kx[i] * rk, kq[1][lane + 64 * i] = qx[i] * rq;
-    __syncthreads();
-    float p[4] = {}, y[4] = {};
-#pragma unroll
-    for (int i = 0; i < DK; ++i) p[i & 3] = fmaf(kq[0][i], S[i], p[i & 3]);
-    const float e = w * (v - al * ((p[0] + p[1]) + (p[2] + p[3])));
-#pragma unroll
-    for (int i = 0; i < DK; ++i) {
-      S[i] = fmaf(kq[0][i], e, al * S[i]);
-      y[i & 3] = fmaf(kq[1][i], S[i], y[i & 3]);
-    }
-    if (on) *out = ElemTraits<T>::from_f32((y[0] + y[1]) + (y[2] + y[3]));
+    if (row == 0 && col < a.Dv) store_some<V>(out, a.Dv - col, y);
   }
-  if (ST && on) {
-#pragma unroll
-    for (int i = 0; i < DK; ++i)
-      if (i < a.Dk) ST[state + (int64_t)i * a.Dv] = S[i];
-  }
+  if (ST) store(ST);
 }
 
 // ---- what does not depend on the states -------------------------------------------
@@ -1308,7 +1336,10 @@ extern "C" int32_t ard_gdr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
     constexpr int DK = decltype(dk)::value;
     constexpr bool NEAR = decltype(near)::value;
     if (few) {
-      ARD_LAUNCH_NAMED("gdr_steps_kernel", (gdr_steps_kernel<E, DK>), dim3(B * H * ceil_div(Dv, 64)), dim3(64), 0, st, a, S0, out, ST, ckpt);
+      const int slices = ceil_div(Dv, 32);
+      const dim3 grid(ceil_div(B * H * slices, 4));
+      if (Dv % 4 == 0) ARD_LAUNCH_NAMED("gdr_steps_kernel", (gdr_steps_kernel<E, DK, 4>), grid, dim3(256), 0, st, a, S0, out, ST, ckpt, slices);
+      else ARD_LAUNCH_NAMED("gdr_steps_kernel", (gdr_steps_kernel<E, DK, 1>), grid, dim3(256), 0, st, a, S0, out, ST, ckpt, slices);
       ARD_LAUNCH_CHECK("gdr_steps_kernel");
       return (int32_t)ARD_OK;
     }
