@@ -1221,15 +1221,18 @@ struct GdrPlan {
   int dk, slices;  // padded key size; wavefronts' worth of 16 columns of a head
   size_t bytes;
 };
-// Chunks of a segment: all, or where workgroups of all heads' columns leave compute units idle, what brings the steps that follow one another down most:
-// twice a segment's chunks (the sums' cost 0.7 of the others') and a product of a state for every segment.
-static int segment_span(int chunks, int workgroups) {
+// Chunks of a segment: all, or, where the workgroups of all heads' columns leave compute units idle, what is estimated (in chunks' times) to end first: a segment's chunks,
+// before them 0.7 of their time for the sums, as often as their workgroups (`sums` of a segment) fill the chip, and a product of a state for every segment.
+// Measured, in segments against at once, forward / backward, us: bf16 1 x 8 heads of 64 x 64, 512 steps (not cut) 38 / 58, 1024 steps 38 / 62 and 61 / 83, 4096 61 / 106 and
+// 200 / 248; 4 x 16 of 64 x 64, 1024 65 / 151 and 76 / 151, 4096 210 / 598 and 306 / 669; 2 x 8 of 128 x 128, 768 57 / 103 and 63 / 110, 4096 128 / 388 and 269 / 501; fp32 1 x 8 of
+// 128 x 128, 1024 83 / 190 and 175 / 317.
+static int segment_span(int chunks, int workgroups, int sums, int resident) {
   constexpr int kUnits = 256;
   int best = chunks;
   float least = 0.85f * chunks;
   for (int n = 2; n * workgroups <= kUnits && n <= chunks; ++n) {
     const int span = ceil_div(chunks, n);
-    const float cost = 1.7f * span + 0.7f * ceil_div(chunks, span) + 2.0f;
+    const float cost = span * (1.0f + 0.7f * ceil_div((n - 1) * sums, kUnits * resident)) + 0.7f * ceil_div(chunks, span) + 2.0f;
     if (cost < least) least = cost, best = span;
   }
   return best;
@@ -1252,7 +1255,8 @@ static GdrPlan gdr_plan(int32_t dtype, int T, int B, int Hk, int H, int Dk, int 
   take(a.steps, hu * sizeof(Steps64));
   take(a.rows, ku * rows * 2), take(a.cols, ku * cols * (backward ? 2 : 1)), take(a.tri, hu * 6 * (backward ? 9 : 3 + out) * 1024);
   // (the backward pass's wavefronts cover the padded columns)
-  a.span = segment_span(a.chunks, B * H * ceil_div(backward ? a.dvp / 16 : p.slices, 4));
+  const int groups = ceil_div(backward ? a.dvp / 16 : p.slices, 4);
+  a.span = segment_span(a.chunks, B * H * groups, B * H * (groups + p.dk / 64), backward && p.dk == 128 && dtype == ARD_BF16 ? 1 : 2);  // (LDS holds the operands of one of these)
   a.segments = ceil_div(a.chunks, a.span);
   if (a.segments > 1) {
     const size_t n = (size_t)a.segments * B * H * p.dk * 4;
@@ -1265,8 +1269,10 @@ static GdrPlan gdr_plan(int32_t dtype, int T, int B, int Hk, int H, int Dk, int 
   return p;
 }
 
-// Up to this many steps go one by one.
-constexpr int kFewSteps = 4;
+// Up to this many steps go one by one, as a chunk costs as much with few steps as with 64.  Measured, one by one against a chunk, 8 steps, us: bf16 16.1 and 17.6
+// (8 sequences x 8 heads of 64 x 64), 16.9 and 25.7 (32 x 16 of 64 x 64), 19.4 and 19.6 (1 x 8 of 128 x 128), 57 and 73 (128 x 8 of 128 x 128); 12 steps 22.4 and 17.6,
+// 22.9 and 25.7, 27.4 and 19.6, 76 and 74.  fp32 gains until 12 to 32.
+constexpr int kFewSteps = 8;
 
 static int32_t gdr_check(int32_t dtype, int32_t T, int32_t B, int32_t Hk, int32_t H, int32_t Dk, int32_t Dv) {
   if (dtype != ARD_F32 && dtype != ARD_BF16) return fail(ARD_EDTYPE, "unknown dtype %d", dtype);

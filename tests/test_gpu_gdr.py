@@ -81,7 +81,7 @@ def _check(T, B, Hk, H, Dk, Dv, dtype="f32", ragged=False, start=True, seed=0, s
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("T", [1, 2, 4, 5, 15, 16, 17, 31, 33, 48, 63, 64, 65, 127, 128, 129, 200, 321])
+@pytest.mark.parametrize("T", [1, 2, 4, 5, 8, 9, 15, 16, 17, 31, 33, 48, 63, 64, 65, 127, 128, 129, 200, 321])
 def test_steps_around_the_chunks(T, dtype):
     _check(T, 2, 1, 2, 24, 40, dtype, seed=T)
 
@@ -91,6 +91,7 @@ def test_steps_around_the_chunks(T, dtype):
                                    (128, 64), (128, 128)])
 def test_sizes_of_heads(Dk, Dv, dtype):
     _check(70, 2, 1, 1, Dk, Dv, dtype, seed=Dk + Dv)
+    _check(7, 2, 1, 2, Dk, Dv, dtype, ragged=True, seed=Dk * Dv)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -113,11 +113,11 @@ def test_delta_rule_accepts_and_refuses():
     with D.dry_run() as lib:
         heap = D.FakeHeap()
         assert lib.ard_gdr_chunk() == ard.GDR_CHUNK == 64
-        for T in (1, 2, 4, 5, 63, 64, 65, 1000):
+        for T in (1, 2, 8, 9, 63, 64, 65, 1000):
             for change in ({}, dict(dtype=ard.F32), dict(S0=None), dict(ST=None), dict(ckpt=None), dict(lengths=None), dict(Dk=128, Dv=128), dict(Dk=1, Dv=1, Hk=4)):
                 assert lib.ard_gdr_fwd(*_gdr_args(heap, T=T, **change).values()) == 0, change
                 n, names = D.launches(lib)
-                assert names == (["gdr_steps_kernel"] if T <= 4 else names) and n == (1 if T <= 4 else len(names)) and names[-1] in ("gdr_steps_kernel", "gdr_fwd_kernel")
+                assert names == (["gdr_steps_kernel"] if T <= 8 else names) and n == (1 if T <= 8 else len(names)) and names[-1] in ("gdr_steps_kernel", "gdr_fwd_kernel")
                 assert lib.ard_gdr_bwd(*_gdr_bwd_args(heap, T=T, **{k: v for k, v in change.items() if k in ("dtype", "lengths", "Dk", "Dv", "Hk")}).values()) == 0
                 assert D.launches(lib)[1][-1] == "gdr_grads_kernel"
         assert lib.ard_gdr_bwd(*_gdr_bwd_args(heap, dST=None, dS0=None).values()) == 0
@@ -146,11 +146,11 @@ def test_delta_rule_accepts_and_refuses():
 def test_delta_rule_workspaces(dtype):
     with D.dry_run() as lib:
         heap = D.FakeHeap()
-        for T, B, Hk, H, Dk, Dv in ((1, 1, 1, 1, 1, 1), (5, 2, 1, 3, 64, 64), (64, 2, 2, 2, 65, 16), (65, 1, 1, 8, 128, 128), (16384, 1, 8, 8, 128, 128)):
+        for T, B, Hk, H, Dk, Dv in ((1, 1, 1, 1, 1, 1), (8, 2, 1, 3, 64, 64), (9, 2, 1, 3, 64, 64), (64, 2, 2, 2, 65, 16), (65, 1, 1, 8, 128, 128), (16384, 1, 8, 8, 128, 128)):
             sizes = dict(dtype=dtype, T=T, B=B, Hk=Hk, H=H, Dk=Dk, Dv=Dv)
             for back, call, args in ((0, lib.ard_gdr_fwd, _gdr_args), (1, lib.ard_gdr_bwd, _gdr_bwd_args)):
                 need = lib.ard_gdr_workspace_bytes(*sizes.values(), back)
-                assert (need > 0) == bool(back or T > 4)
+                assert (need > 0) == bool(back or T > 8)
                 assert call(*args(heap, **sizes, ws_bytes=need).values()) == 0
                 if need:
                     assert call(*args(heap, **sizes, ws_bytes=need - 1).values()) == -4
