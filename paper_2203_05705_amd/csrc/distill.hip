@@ -209,7 +209,8 @@ __global__ __launch_bounds__(1024, C <= 4 ? 8 : 4) void distill_kernel(DistillAr
       values(c, x);
 #pragma unroll
       for (int e = 0; e < N; ++e) x[e] = dense(x[e]);
-      store_some<N>(dz + j, V - j, x);
+      if (V - j >= N) store_run_past(dz + j, x);  // (270 us of passes in a row, with stores that stay in the caches 278)
+      else store_some<N>(dz + j, V - j, x);
     });
   } else {
     const float none[N] = {};

@@ -68,12 +68,27 @@ template <int N> __device__ __forceinline__ void store_run(uint16_t* p, const fl
 }
 // the same past the caches' order of use, for what nothing reads again soon
 template <int N> __device__ __forceinline__ void store_run_past(float* p, const float (&x)[N]) {
-  static_assert(N == 1, "");
-  __builtin_nontemporal_store(x[0], p);
+  if constexpr (N == 1) {
+    __builtin_nontemporal_store(x[0], p);
+  } else {
+    using V = typename Run<float, 4>::V;
+#pragma unroll
+    for (int j = 0; j < N; j += 4) __builtin_nontemporal_store(V{x[j], x[j + 1], x[j + 2], x[j + 3]}, reinterpret_cast<V*>(p + j));
+  }
 }
 template <int N> __device__ __forceinline__ void store_run_past(uint16_t* p, const float (&x)[N]) {
-  if constexpr (N == 1) __builtin_nontemporal_store((uint16_t)bf16_pair(x[0], 0.0f), p);
-  else __builtin_nontemporal_store(bf16_pair(x[0], x[1]), reinterpret_cast<typename Run<uint16_t, N>::V*>(p));
+  if constexpr (N == 1) {
+    __builtin_nontemporal_store((uint16_t)bf16_pair(x[0], 0.0f), p);
+  } else {
+    typename Run<uint16_t, N>::V v;
+    if constexpr (N == 2) {
+      v = bf16_pair(x[0], x[1]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) v[j] = bf16_pair(x[2 * j], x[2 * j + 1]);
+    }
+    __builtin_nontemporal_store(v, reinterpret_cast<typename Run<uint16_t, N>::V*>(p));
+  }
 }
 
 // A run of a lane as it lies in memory, to be taken apart where it is used (two bf16 stay one register until then).
