@@ -1,7 +1,7 @@
 // Gated delta rule: a recurrence whose state of a head is a matrix.
 //   S_t = a_t S_{t-1} + w_t kh_t (v_t - a_t S_{t-1}^T kh_t)^T,  o_t = scale S_t^T qh_t
 //
-// Few steps (a generation step above all) go one by one: a lane holds a column of S.  More steps are taken in chunks of 64.  With
+// Few steps (a generation step above all) go one by one.  More steps are taken in chunks of 64.  With
 // G_i the sum of log(a) inside the chunk up to step i, Gamma_ij = exp(G_i - G_j), K and Q the unit keys and queries by rows, S the state before the chunk:
 //   A_ij = w_i Gamma_ij K_i.K_j (j < i),  P_ij = scale Gamma_ij Q_i.K_j (j <= i),  M = (I + A)^-1
 //   X_i = w_i (v_i - exp(G_i) S^T K_i),  U = M X                  (the rows that the steps write beside their keys)
@@ -9,7 +9,7 @@
 // All factors are at most 1 and every G_i - G_j comes from fp64 sums, so no decay loses digits, however fast.
 //
 // A first launch, over all chunks at once, makes what does not depend on the states: A, P, M (blocks of 16 by substitution, the rest by
-// fp32 matrix instructions), written as operands of the second.  The second walks the chunks; a wavefront holds 16 or 32 columns of S in registers and
+// fp32 matrix instructions), written as operands of the second.  The second walks the chunks; a wavefront holds 16 columns of S in registers and
 // needs no other's: everything a chunk does to a column is a chain of products in its own registers (gdr.hpp).
 #include <type_traits>
 
@@ -20,7 +20,8 @@ namespace ard {
 // ---- step by step ---------------------------------------------------------------
 // A wavefront holds 32 columns of a head's S: V of them (4, if rows are whole runs of 4) and a share of the rows a lane, which has these rows' keys and queries too; sums
 // over rows go round the lanes.  Reading and writing the states bounds a generation step: 128-byte pieces of rows, 64 registers a lane for them, so that
-// four wavefronts a SIMD have theirs on the way.
+// four wavefronts a SIMD have theirs on the way.  Measured, bf16, 128 sequences x 8 heads of 128 x 128: 26.1 us, 5.1 TB/s, what a copy reaches (a column a lane, 4-byte
+// accesses: 53.7).
 template <typename T, int DK, int V>
 __global__ __launch_bounds__(256) void gdr_steps_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt, int slices) {
   constexpr int ACROSS = 32 / V, R = DK * ACROSS / 64;  // lanes of a row; rows of a lane
@@ -147,6 +148,11 @@ template <int N, int LD> __device__ __forceinline__ Parts<N> col_parts(const uin
   return s;
 }
 
+// A workgroup of four wavefronts makes the operands of a chunk and a key head, then of its heads in turn; wavefront w has rows 16 w .. 16 w + 15.  Phases of few
+// instructions with barriers between them bound it, more than its stores do (2.5 TB/s), so three workgroups share a compute unit, which takes keys and
+// queries as stored (not as fp32) in LDS; the gates' sums are made where their wavefront has least else to do.  Measured, bf16, forward / backward: 4096 x 4 x 16 heads of
+// 64 x 64 77 / 88 us, 16384 x 1 x 8 of 128 x 128 66; two workgroups, diagonal blocks inverted by way of LDS: 91 / 102, 77.  Without its loads, its stores, the inverses or
+// the products each it would take 0.75 to 0.95 of its time: no one of them.
 template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 3 : 2) void gdr_prep_kernel(GdrArgs a) {
   constexpr int IN = GdrType<T>::IN, OUT = GdrType<T>::OUT, KB = DK / 32;
   __shared__ PrepShared<T, DK> sh;
@@ -461,6 +467,8 @@ template <int IN, int DK> __device__ __forceinline__ void add_outer(const u32x4*
 // chunk reads is loaded for the next chunk while the second half is worked on, and the other way about.  Operands that LDS does not hold
 // (fp32, wide heads) are read from the caches.
 // KEEP: the states before the chunks are stored, in ckpt.
+// A chunk is a chain of products that wait for each other: 3.8 us with one workgroup of a head on the chip, 5 with 256.  Measured, bf16: 8 x 1024 x 8 heads of 128 x 128 78 us;
+// 16384 x 1 x 8 of 128 x 128 in 16 segments 89 + 44 + 83, at once 965; 4096 x 4 x 16 of 64 x 64 in 4 segments 58 + 6 + 74, at once 216.
 //
 // Few heads leave most of the chip idle, and their chunks follow one another.  So a long sequence is cut into segments.  A segment is linear in the
 // state before it: S' = F S + Z.  SUM walks all but the last segment at once, for Z (from a state of zeros) and F (DK more columns, from the
@@ -659,7 +667,7 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
 // Three launches after the first: U of every chunk from the states kept; the chunks from the last to the first, which leaves dX and dS' of each; and
 // all other gradients, every chunk for itself.
 
-// U of every chunk
+// U of every chunk.  Reading the states bounds it: bf16 8 x 1024 x 8 heads of 128 x 128 43 us, 2.8 TB/s.
 template <typename T, int DK, bool NEAR> __global__ __launch_bounds__(256) void gdr_rows_kernel(GdrArgs a, const float* ckpt, int slices, int waves) {
   constexpr int IN = GdrType<T>::IN, KB = DK / 32;
   const int index = __builtin_amdgcn_readfirstlane(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6));
@@ -684,7 +692,7 @@ template <typename T, int DK, bool NEAR> __global__ __launch_bounds__(256) void 
   store_tiles(StateWindow(a.u + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp, at.first), u);
 }
 
-// SUM: as forward, of segments from the last on.
+// SUM: as forward, of segments from the last on.  Measured, bf16: 8 x 1024 x 8 heads of 128 x 128 91 us; 4096 x 4 x 16 of 64 x 64 in 4 segments 88 + 6 + 82, at once 239.
 template <typename T, int DK, bool NEAR, int MODE>
 __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o, const float* dST, ard_steps dv, float* dS0, int groups) {
   constexpr int IN = GdrType<T>::IN, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3;
@@ -876,6 +884,9 @@ template <> struct Four<uint16_t> {
 // rows of Dk or half of them.  U, dX and dO become parts once and go around through LDS, each tile the right hand operand of its own wavefronts and the left hand one of the others; S and
 // dS' follow there.  Operands are read from LDS where they are used, for all of a wavefront's rows at once: its registers hold sums, not operands (with those of its own
 // steps in registers too, 256 were not enough, and what was spilled took most of the time).  Where LDS does not hold rows and states together (fp32, wide heads) they are.
+// What later and earlier steps give is made apart, each before its own products, so that the operands of one are gone when the other's come (163 us for both at once 191).
+// Measured, bf16: 8 x 1024 x 8 heads of 128 x 128 163 us, 4096 x 4 x 16 of 64 x 64 with 8 key heads 214, a twelfth of it matrix instructions, a third vector ones; the rest
+// are waits between the phases, which one workgroup a compute unit (LDS, registers) cannot fill; two, at 256 registers of which some are spilled, took as long.
 template <typename T, int DK, int DV, bool QUICK>
 __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps d_o, const float* ckpt, ard_steps dq, ard_steps dk, ard_steps df, ard_steps db) {
   constexpr int IN = GdrType<T>::IN, N = GdrType<T>::OUT, VB = DV / 32, RT = DK / 16, HALVES = DK / 64, WAVES = 4 * HALVES, OWN = RT / HALVES, MINE = RT * VB / WAVES;
