@@ -11,9 +11,9 @@
 // Summing: a row's team of lanes walks its tokens, kInFlight at a time.  Frequent tokens would leave one team behind: a row of more than
 // kLong tokens is summed in pieces of kPiece sorted positions each by a launch before, and its team adds the pieces up.
 //
-// Measured, passes in a row: 8192 tokens, bf16 rows of 1024 into an fp32 table of 32768 66 us with the forward pass (7 + 7 + 15 + 40 us of launches, 2.8 TB/s; pieces of 128 and
-// rows of up to 128 at once, two loads of ids ahead: 179 with stores through the caches, now 107 with them); 131072 tokens and a table of 50000 added to
-// 371 us (96 + 51 + 74 + 152).  One generation step, 64 tokens: 2.6 us.
+// Measured, passes in a row with the forward pass: 8192 tokens, bf16 rows of 1024, an fp32 table of 32768 66 us (launches of 7 + 7 + 15 + 40 us, 2.8 TB/s); 131072 tokens, a table of
+// 50000 added to 371 us (96 + 51 + 74 + 152).  Pieces of 128 and two loads of ids ahead took 179 and 489 us in the gradient's launches, these 62 and 277.
+// One generation step, 64 tokens: 2.6 us.
 #include "rows.hpp"
 
 namespace ard {
