@@ -12,7 +12,7 @@
 // while the other waits for memory.  That takes 64 registers a lane (one workgroup with 83: 333 us).
 
 // The K entries change few elements: the gradient is stored first as if there were none, then again at the entries, computed anew
-// rather than corrected, so that it is rounded once.  Entries that name one element twice each store the sum of all its p; the label is one more entry.
+// rather than corrected, so that it is rounded once.  Entries that name one element twice each store the sum of all its p; the label, if no entry names it, is one more.
 #include "rows.hpp"
 
 namespace ard {
@@ -230,9 +230,9 @@ __global__ __launch_bounds__(1024, C <= 4 ? 8 : 4) void distill_kernel(DistillAr
     dz[id] = ElemTraits<T>::from_f32(x);
   }
   if (labelled && threadIdx.x == threads - 1) {
-    float p = 0.0f;
-    for (int i = 0; i < (taught ? K : 0); ++i) p += sh.id[i] == y ? sh.p[i] : 0.0f;
-    dz[y] = ElemTraits<T>::from_f32((dense(zy) - soft * p) - hard);
+    bool named = false;  // an entry names it: that one's lane has stored it
+    for (int i = 0; i < (taught ? K : 0); ++i) named |= sh.id[i] == y;
+    if (!named) dz[y] = ElemTraits<T>::from_f32(dense(zy) - hard);
   }
 }
 

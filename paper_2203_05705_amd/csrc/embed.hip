@@ -144,19 +144,20 @@ template <typename T> __device__ __forceinline__ void add_rows(const int32_t* so
 template <typename T>
 __global__ __launch_bounds__(256) void embed_pieces_kernel(int V, int D, const int32_t* ids, const int32_t* start, const int32_t* sorted, const T* dY, int64_t lddy,
                                                            float* pieces) {
-  const int all = start[V], a = blockIdx.x * kPiece;
-  if (a >= all) return;
-  const int b = imin(a + kPiece, all), first = ids[sorted[a]], last = ids[sorted[b - 1]];
+  const int all = start[V], count = (all + kPiece - 1) / kPiece;
+  for (int p = blockIdx.x; p < count; p += gridDim.x) {
+    const int a = p * kPiece, b = imin(a + kPiece, all), first = ids[sorted[a]], last = ids[sorted[b - 1]];
 #pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    const int id = side ? last : first;
-    if (side && last == first) break;
-    const int s = start[id], e = start[id + 1];
-    if (e - s <= kLong) continue;
-    for (int c = threadIdx.x * 8; c < D; c += 256 * 8) {
-      float sum[8] = {};
-      add_rows(sorted, imax(a, s), imin(b, e), dY, lddy, c, D - c, sum);
-      store_some<8>(pieces + ((int64_t)blockIdx.x * 2 + side) * D + c, D - c, sum);
+    for (int side = 0; side < 2; ++side) {
+      const int id = side ? last : first;
+      if (side && last == first) break;
+      const int s = start[id], e = start[id + 1];
+      if (e - s <= kLong) continue;
+      for (int c = threadIdx.x * 8; c < D; c += 256 * 8) {
+        float sum[8] = {};
+        add_rows(sorted, imax(a, s), imin(b, e), dY, lddy, c, D - c, sum);
+        store_some<8>(pieces + ((int64_t)p * 2 + side) * D + c, D - c, sum);
+      }
     }
   }
 }
@@ -272,7 +273,8 @@ extern "C" int32_t ard_embed_bwd(int32_t dtype, int32_t wdtype, int32_t R, int32
     using T = decltype(a);
     using W = decltype(b);
     if (R > kLong) {
-      ARD_LAUNCH_NAMED("embed_pieces_kernel", (embed_pieces_kernel<T>), dim3(ceil_div(R, kPiece)), dim3(256), 0, st, V, D, d_ids, start, sorted, (const T*)dY, lddy, pieces);
+      const int blocks = imin(ceil_div(R, kPiece), kMaxGrid);
+      ARD_LAUNCH_NAMED(launch_instance("embed_pieces_kernel", blocks, kPiece, 256), (embed_pieces_kernel<T>), dim3(blocks), dim3(256), 0, st, V, D, d_ids, start, sorted, (const T*)dY, lddy, pieces);
       ARD_LAUNCH_CHECK("embed_pieces_kernel");
     }
     if (beta == 0.0f)

@@ -72,6 +72,14 @@ def test_tables_around_the_shares_of_sorting_workgroups(V):
     _check(2000, V, 8, "f32", "f32", "padded", seed=V)
 
 
+def test_more_pieces_than_workgroups():
+    """2^25 tokens and some: a workgroup takes more than one piece.  Sums of ones below 2^24 are exact."""
+    R = (1 << 25) + 32 * 1000 + 5
+    ids = (torch.arange(R, device="cuda", dtype=torch.int32) % 5) - 1
+    got = ard.embed_bwd(ids, torch.ones((R, 1), dtype=torch.bfloat16, device="cuda"), 4)
+    assert got[:, 0].tolist() == [float((R - v + 3) // 5) for v in range(4)]
+
+
 def test_nothing_but_padding():
     ids = torch.full((5, 3), -1, dtype=torch.int32, device="cuda")
     E = torch.full((4, 6), float("nan"), device="cuda")

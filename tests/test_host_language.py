@@ -68,6 +68,17 @@ def test_embedding_gradient_accepts_and_refuses():
             assert lib.ard_embed_workspace_bytes(*sizes) == 0
 
 
+def test_pieces_of_the_most_tokens_have_a_grid():
+    """HIP counts the threads along an axis of a grid in 32 bits."""
+    with D.dry_run() as lib:
+        heap = D.FakeHeap()
+        for R in (33, 1 << 25, (1 << 25) + 1, 1 << 29, 1 << 30):
+            need = lib.ard_embed_workspace_bytes(R, 9, 24)
+            assert lib.ard_embed_bwd(*_embed_bwd_args(heap, R=R, ws_bytes=need).values()) == 0
+            blocks, piece, threads = (int(v) for v in next(i for i in D.instances(lib) if i.startswith("embed_pieces_kernel")).split("<")[1][:-1].split(","))
+            assert blocks * threads < 1 << 32 and piece * blocks >= min(R, 1 << 25)
+
+
 # ---- gated delta rule ------------------------------------------------------------------------
 
 def _steps(*all_):
