@@ -11,6 +11,7 @@
 // A first launch, over all chunks at once, makes what does not depend on the states: A, P, M (blocks of 16 by substitution, the rest by
 // fp32 matrix instructions), written as operands of the second.  The second walks the chunks; a wavefront holds 16 columns of S in registers and
 // needs no other's: everything a chunk does to a column is a chain of products in its own registers (gdr.hpp).
+#include <algorithm>
 #include <type_traits>
 
 #include "gdr.hpp"
@@ -148,15 +149,15 @@ template <int N, int LD> __device__ __forceinline__ Parts<N> col_parts(const uin
   return s;
 }
 
-// A workgroup of four wavefronts makes the operands of a chunk and a key head, then of its heads in turn; wavefront w has rows 16 w .. 16 w + 15.  Phases of few
+// A workgroup of four wavefronts makes the operands of a chunk and a key head, then of its heads, or a share of them, in turn; wavefront w has rows 16 w .. 16 w + 15.  Phases of few
 // instructions with barriers between them bound it, more than its stores do (2.5 TB/s), so three workgroups share a compute unit, which takes keys and
 // queries as stored (not as fp32) in LDS; the gates' sums are made where their wavefront has least else to do.  Measured, bf16, forward / backward: 4096 x 4 x 16 heads of
 // 64 x 64 77 / 88 us, 16384 x 1 x 8 of 128 x 128 66; two workgroups, diagonal blocks inverted by way of LDS: 91 / 102, 77.  Without its loads, its stores, the inverses or
 // the products each it would take 0.75 to 0.95 of its time: no one of them.
-template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 3 : 2) void gdr_prep_kernel(GdrArgs a) {
+template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 3 : 2) void gdr_prep_kernel(GdrArgs a, int splits) {
   constexpr int IN = GdrType<T>::IN, OUT = GdrType<T>::OUT, KB = DK / 32;
   __shared__ PrepShared<T, DK> sh;
-  const int unit = blockIdx.x, chunk = unit / (a.B * a.Hk), n = (unit - chunk * a.B * a.Hk) / a.Hk, hk = unit % a.Hk;
+  const int unit = blockIdx.x / splits, part = blockIdx.x - unit * splits, chunk = unit / (a.B * a.Hk), n = (unit - chunk * a.B * a.Hk) / a.Hk, hk = unit % a.Hk;
   const int t0 = chunk * kChunk, live = imin(live_steps(a, n) - t0, kChunk);
   if (live <= 0) return;  // (nobody reads this chunk's operands)
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
@@ -179,7 +180,8 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256, sizeof
     }
     sh.G[lane] = G, sh.w[lane] = wr;
   };
-  if (w == 3) gates(hk * a.group);
+  const int first = part * a.group / splits, end = (part + 1) * a.group / splits;  // of the key head's heads
+  if (w == 3) gates(hk * a.group + first);
   {
     const int row = threadIdx.x >> 2, part = threadIdx.x & 3;
     const int64_t t = t0 + row;
@@ -206,8 +208,7 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256, sizeof
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       const Parts<IN> ka = row_parts<IN>(sh.k, w * 16 + c, kb, g), qa = row_parts<IN>(sh.q, w * 16 + c, kb, g);
-      store_parts(kf, w * KB + kb, ka);
-      store_parts(qf, w * KB + kb, qa);
+      if (part == 0) store_parts(kf, w * KB + kb, ka), store_parts(qf, w * KB + kb, qa);
 #pragma unroll
       for (int ct = 0; ct < 4; ++ct)
         if (ct <= w) {
@@ -217,12 +218,12 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256, sizeof
         }
     }
     u32x4 *ktf = a.cols + (int64_t)unit * (BWD ? 2 : 1) * KTF * 64 + lane, *qtf = ktf + KTF * 64;
-    for (int i = w; i < DK / 8; i += 4) {
+    for (int i = w; part == 0 && i < DK / 8; i += 4) {
       store_parts(ktf, i, col_parts<IN>(sh.k, (i >> 1) * 16 + c, i & 1, g));
       if (BWD) store_parts(qtf, i, col_parts<IN>(sh.q, (i >> 1) * 16 + c, i & 1, g));
     }
   }
-  for (int s = 0; s < a.group; ++s) {
+  for (int s = first; s < end; ++s) {
     const int h = hk * a.group + s;
     const int64_t out = ((int64_t)chunk * a.B + n) * a.H + h;
     __syncthreads();  // keys and queries, or the head before, have been read
@@ -287,7 +288,7 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256, sizeof
       }
     }
     __syncthreads();
-    if (w == 3 && s + 1 < a.group) gates(h + 1);  // (it has one operand less to store)
+    if (w == 3 && s + 1 < end) gates(h + 1);  // (it has one operand less to store)
     constexpr int PP = BWD ? 3 : OUT;
     u32x4 *mf = a.tri + out * (BWD ? 54 : 18 + 6 * OUT) * 64 + lane, *pf = mf + 18 * 64, *mtf = mf + 18 * 64, *ptf = mf + 36 * 64;
     for (int i = w; i < 6; i += 4) {
@@ -1309,6 +1310,14 @@ static int32_t gdr_numbers(float scale, float eps) {
   return ARD_OK;
 }
 
+// Workgroups of the operands of a chunk and a key head: more than one, each with a share of its heads, where one each would not fill the chip (keys' and
+// queries' products are made by each of them).  Measured, shared out against one each, forward / backward of 64 steps x 16 x 8 heads of 128 x 128, 2 key heads, bf16: 24 / 120 and
+// 42 / 139 us; 2048 x 1 x 32 of 64 x 64, 4 key heads: 68 / 159 and 101 / 195; 256 x 8 x 24 of 64 x 64, 12 key heads (384 workgroups): 37 / 93 and 40 / 99.
+static int prep_splits(const GdrArgs& a) {
+  const int64_t units = (int64_t)a.chunks * a.B * a.Hk;
+  return units * 2 <= 768 ? (int)std::min<int64_t>(a.group, 768 / units) : 1;
+}
+
 template <class F> static int32_t gdr_instance(int32_t dtype, int dk, bool near, F&& with) {
   const auto sized = [&](auto t) {
     using Wide = std::integral_constant<int, 128>;
@@ -1348,6 +1357,7 @@ extern "C" int32_t ard_gdr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
   a.q = gdr_steps(in[0], T, Hk * Dk), a.k = gdr_steps(in[1], T, Hk * Dk), a.v = gdr_steps(in[2], T, H * Dv), a.f = in[3], a.b = in[4], a.scale = scale, a.eps = eps, a.len = d_lengths;
   hipStream_t st = (hipStream_t)stream;
   const ard_steps out = gdr_steps(*o, T, H * Dv);
+  const int splits = prep_splits(a);
   return gdr_instance(dtype, p.dk, gdr_near(a.v, Dv) && gdr_near(out, Dv), [&](auto t, auto dk, auto near) {
     using E = decltype(t);
     constexpr int DK = decltype(dk)::value;
@@ -1360,7 +1370,7 @@ extern "C" int32_t ard_gdr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
       ARD_LAUNCH_CHECK("gdr_steps_kernel");
       return (int32_t)ARD_OK;
     }
-    ARD_LAUNCH_NAMED("gdr_prep_kernel", (gdr_prep_kernel<E, DK, false>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a);
+    ARD_LAUNCH_NAMED("gdr_prep_kernel", (gdr_prep_kernel<E, DK, false>), dim3(a.chunks * B * Hk * splits), dim3(256), 0, st, a, splits);
     ARD_LAUNCH_CHECK("gdr_prep_kernel");
     const int groups = ceil_div(p.slices, 4);
     if (a.segments > 1) {
@@ -1395,11 +1405,12 @@ extern "C" int32_t ard_gdr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
   // dX and U are read in whole operands of 32 columns: the wavefronts of the padded columns write them as zeros
   const int slices = a.dvp / 16, waves = B * H * slices;
   const ard_steps od = gdr_steps(*d_o, T, H * Dv), dv = gdr_steps(grads[2], T, H * Dv);
+  const int splits = prep_splits(a);
   return gdr_instance(dtype, p.dk, gdr_near(a.v, Dv) && gdr_near(od, Dv) && gdr_near(dv, Dv), [&](auto t, auto dk, auto near) {
     using E = decltype(t);
     constexpr int DK = decltype(dk)::value;
     constexpr bool NEAR = decltype(near)::value;
-    ARD_LAUNCH_NAMED("gdr_prep_kernel", (gdr_prep_kernel<E, DK, true>), dim3(a.chunks * B * Hk), dim3(256), 0, st, a);
+    ARD_LAUNCH_NAMED("gdr_prep_kernel", (gdr_prep_kernel<E, DK, true>), dim3(a.chunks * B * Hk * splits), dim3(256), 0, st, a, splits);
     ARD_LAUNCH_CHECK("gdr_prep_kernel");
     ARD_LAUNCH_NAMED("gdr_rows_kernel", (gdr_rows_kernel<E, DK, NEAR>), dim3((unsigned)(((int64_t)a.chunks * waves + 3) / 4)), dim3(256), 0, st, a, ckpt, slices, waves);
     ARD_LAUNCH_CHECK("gdr_rows_kernel");
