@@ -155,7 +155,7 @@ template <int N, int LD> __device__ __forceinline__ Parts<N> col_parts(const uin
 // 64 x 64 77 / 88 us, 16384 x 1 x 8 of 128 x 128 66; two workgroups, diagonal blocks inverted by way of LDS: 91 / 102, 77.  Without its loads, its stores, the inverses or
 // the products each it would take 0.75 to 0.95 of its time: no one of them.
 template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 3 : 2) void gdr_prep_kernel(GdrArgs a, int splits) {
-  constexpr int IN = GdrType<T>::IN, OUT = GdrType<T>::OUT, KB = DK / 32;
+  constexpr int IN = kInput<T>, KB = DK / 32;
   __shared__ PrepShared<T, DK> sh;
   const int unit = blockIdx.x / splits, part = blockIdx.x - unit * splits, chunk = unit / (a.B * a.Hk), n = (unit - chunk * a.B * a.Hk) / a.Hk, hk = unit % a.Hk;
   const int t0 = chunk * kChunk, live = imin(live_steps(a, n) - t0, kChunk);
@@ -289,16 +289,15 @@ template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256, sizeof
     }
     __syncthreads();
     if (w == 3 && s + 1 < end) gates(h + 1);  // (it has one operand less to store)
-    constexpr int PP = BWD ? 3 : OUT;
-    u32x4 *mf = a.tri + out * (BWD ? 54 : 18 + 6 * OUT) * 64 + lane, *pf = mf + 18 * 64, *mtf = mf + 18 * 64, *ptf = mf + 36 * 64;
+    u32x4 *mf = a.tri + out * (BWD ? 54 : 18 + 6 * Operands<true>::PER) * 64 + lane, *pf = mf + 18 * 64, *mtf = mf + 18 * 64, *ptf = mf + 36 * 64;
     for (int i = w; i < 6; i += 4) {
       const int rt = i < 2 ? i : 1 + i / 2, kb = i < 2 ? 0 : i & 1;  // (lower_frag's)
       store_parts(mf, i, row_parts<3>(sh.M, rt * 16 + c, kb, g));
-      if (!BWD) store_parts(pf, i, row_parts<OUT>(sh.P, rt * 16 + c, kb, g));
+      if (!BWD) Operands<true>::store(pf, i, *reinterpret_cast<const f32x4*>(&sh.P[rt * 16 + c][kb * 32 + 4 * g]), *reinterpret_cast<const f32x4*>(&sh.P[rt * 16 + c][kb * 32 + 16 + 4 * g]));
       if (BWD) {
         const int ut = i < 4 ? i / 2 : i - 2, ub = i < 4 ? i & 1 : 1;  // (upper_frag's)
         store_parts(mtf, i, col_parts<3>(sh.M, ut * 16 + c, ub, g));
-        store_parts(ptf, i, col_parts<PP>(sh.P, ut * 16 + c, ub, g));
+        store_parts(ptf, i, col_parts<3>(sh.P, ut * 16 + c, ub, g));
       }
     }
   }
@@ -424,20 +423,21 @@ __device__ __forceinline__ void unwritten(const u32x4* kf, const float* w, const
 #pragma unroll
   for (int rt = 0; rt < 4; ++rt) x[rt] = row_weights(w, rt) * (v[rt] - row_weights(ka, rt) * y[rt]);
 }
-// y += L x of a lower triangular L (64 x 64, N parts), or of its transpose
-template <bool UPPER, int N, int M> __device__ __forceinline__ void triangle(const u32x4* f, const Parts<M> (&x)[2], f32x4 (&y)[4]) {
-  Parts<N> two[2], four[4];
+// y += L x of a lower triangular L (64 x 64), or of its transpose
+template <bool UPPER, bool FLOATS, int M> __device__ __forceinline__ void triangle(const u32x4* f, const Parts<M> (&x)[2], f32x4 (&y)[4]) {
+  using L = Operands<FLOATS>;
+  Parts<3> two[2], four[4];
   if (UPPER) {  // of all rows the last 32 columns, of the first two tiles of rows the first 32 as well
-    load_parts(f, 0, 2, two);
+    L::load(f, 0, 2, two);
     mul_add(two, x[0], reinterpret_cast<f32x4(&)[2]>(y[0]));
 #pragma unroll
-    for (int rt = 0; rt < 4; ++rt) four[rt] = load_parts<N>(f, upper_frag(rt, 1));
+    for (int rt = 0; rt < 4; ++rt) four[rt] = L::load(f, upper_frag(rt, 1));
     mul_add(four, x[1], y);
   } else {
 #pragma unroll
-    for (int rt = 0; rt < 4; ++rt) four[rt] = load_parts<N>(f, lower_frag(rt, 0));
+    for (int rt = 0; rt < 4; ++rt) four[rt] = L::load(f, lower_frag(rt, 0));
     mul_add(four, x[0], y);
-    load_parts(f, 3, 2, two);
+    L::load(f, 3, 2, two);
     mul_add(two, x[1], reinterpret_cast<f32x4(&)[2]>(y[2]));
   }
 }
@@ -467,6 +467,8 @@ template <int IN, int DK> __device__ __forceinline__ void add_outer(const u32x4*
 // Four wavefronts with columns of one head walk its chunks.  They share the operands in LDS, in two groups: what the first half of a
 // chunk reads is loaded for the next chunk while the second half is worked on, and the other way about.  Operands that LDS does not hold
 // (fp32, wide heads) are read from the caches.
+// P lies there as values, which become parts where they are used: so the operands of heads of 128 take 80 KB, and two workgroups share a compute unit where nothing is kept
+// (bf16, 512 x 32 x 16 heads of 128 x 128: 262 us with the operands' launch, one workgroup, or P in parts, 300).
 // KEEP: the states before the chunks are stored, in ckpt.
 // A chunk is a chain of products that wait for each other: 3.8 us with one workgroup of a head on the chip, 5 with 256.  Measured, bf16: 8 x 1024 x 8 heads of 128 x 128 78 us;
 // 16384 x 1 x 8 of 128 x 128 in 16 segments 89 + 44 + 83, at once 965; 4096 x 4 x 16 of 64 x 64 in 4 segments 58 + 6 + 74, at once 216.
@@ -542,8 +544,8 @@ template <int DK> __global__ __launch_bounds__(256) void gdr_join_kernel(GdrArgs
 }
 
 template <typename T, int DK, bool NEAR, int MODE>
-__global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt, int groups) {
-  constexpr int IN = GdrType<T>::IN, OUT = GdrType<T>::OUT, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3, PF = 6 * OUT;
+__global__ __launch_bounds__(256, MODE == DROP && sizeof(T) == 2 ? 2 : 1) void gdr_fwd_kernel(GdrArgs a, const float* S0, ard_steps o, float* ST, float* ckpt, int groups) {
+  constexpr int IN = kInput<T>, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3, PF = 6 * Operands<true>::PER;
   constexpr bool KEPT = MODE == KEEP, OUTPUT = MODE != SUM;
   constexpr int RF = OUTPUT ? 2 * KF : KF, TF = OUTPUT ? MF + PF : MF;  // (the operands of Q and P are read for o alone)
   constexpr bool STAGED = 2 * KF + KTF + MF + PF <= 150;  // KB of LDS
@@ -612,7 +614,7 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
         for (int kb = 0; kb < KB; ++kb) {
           Parts<IN> q[4];
           load_parts(rows + KF * 64, kb, KB, q);
-          mul_add(q, leading<OUT>(Sp[kb]), y);
+          mul_add(q, Sp[kb], y);
         }
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt) y[rt] *= row_weights(qa, rt);
@@ -624,12 +626,12 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
     {
       Parts<3> xp[2];
       column_parts<3>(x, xp);
-      triangle<false, 3>(tri, xp, u);
+      triangle<false, false>(tri, xp, u);
     }
     if constexpr (OUTPUT) {
-      Parts<OUT> up[2];
-      column_parts<OUT>(u, up);
-      triangle<false, OUT>(tri + MF * 64, up, y);
+      Parts<3> up[2];
+      column_parts<3>(u, up);
+      triangle<false, true>(tri + MF * 64, up, y);
     }
     weights[(chunk + 1) & 1][threadIdx.x & 63] = sw;  // (waits for all accesses: in front of the stores)
     if constexpr (OUTPUT) store_live(Window<T, NEAR>(op, o.t, steps, a.Dv, at.first), live, y);
@@ -670,7 +672,7 @@ __global__ __launch_bounds__(256) void gdr_fwd_kernel(GdrArgs a, const float* S0
 
 // U of every chunk.  Reading the states bounds it: bf16 8 x 1024 x 8 heads of 128 x 128 43 us, 2.8 TB/s.
 template <typename T, int DK, bool NEAR> __global__ __launch_bounds__(256) void gdr_rows_kernel(GdrArgs a, const float* ckpt, int slices, int waves) {
-  constexpr int IN = GdrType<T>::IN, KB = DK / 32;
+  constexpr int IN = kInput<T>, KB = DK / 32;
   const int index = __builtin_amdgcn_readfirstlane(blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6));
   const int chunk = index / waves;
   if (chunk >= a.chunks) return;
@@ -689,14 +691,14 @@ template <typename T, int DK, bool NEAR> __global__ __launch_bounds__(256) void 
   }
   Parts<3> xp[2];
   column_parts<3>(x, xp);
-  triangle<false, 3>(a.tri + hu * 54 * 64 + (threadIdx.x & 63), xp, u);
+  triangle<false, false>(a.tri + hu * 54 * 64 + (threadIdx.x & 63), xp, u);
   store_tiles(StateWindow(a.u + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp, at.first), u);
 }
 
 // SUM: as forward, of segments from the last on.  Measured, bf16: 8 x 1024 x 8 heads of 128 x 128 91 us; 4096 x 4 x 16 of 64 x 64 in 4 segments 88 + 6 + 82, at once 239.
 template <typename T, int DK, bool NEAR, int MODE>
 __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o, const float* dST, ard_steps dv, float* dS0, int groups) {
-  constexpr int IN = GdrType<T>::IN, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3;
+  constexpr int IN = kInput<T>, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3;
   constexpr bool STAGED = KF + 2 * KTF + 2 * MF <= 150;
   constexpr bool OUTPUT = MODE != SUM;
   __shared__ u32x4 one[STAGED ? (KF + MF) * 64 : 1], two[STAGED ? (2 * KTF + MF) * 64 : 1];
@@ -771,7 +773,7 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
     {
       Parts<IN> p[2];
       column_parts<IN>(x, p);
-      triangle<true, 3>(ptf, p, y);
+      triangle<true, false>(ptf, p, y);
     }
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt) od[rt] = x[rt];
@@ -781,7 +783,7 @@ __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o,
     {
       Parts<3> p[2];
       column_parts<3>(y, p);
-      triangle<true, 3>(mtf, p, dx);
+      triangle<true, false>(mtf, p, dx);
     }
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt) y[rt] = row_weights(w, rt) * dx[rt];
@@ -848,7 +850,7 @@ template <typename T, int N, bool QUICK> struct Runs {
   // eight as an operand's parts will be made of: bf16 is one already, and taken apart on the way its loads would be waited for
   struct Eight {
     std::conditional_t<sizeof(T) == 2, u32x4, float[8]> v;
-    __device__ __forceinline__ Parts<GdrType<T>::IN> parts() const {
+    __device__ __forceinline__ Parts<kInput<T>> parts() const {
       if constexpr (sizeof(T) == 2) return Parts<1>{{v}};
       else return parts_of<3>(v);
     }
@@ -882,18 +884,26 @@ template <> struct Four<uint16_t> {
 };
 
 // The gradients of queries, keys and gates of a chunk and a key head, by four wavefronts, or eight for wide keys.  Wavefront w has the steps of tile w % 4 as columns, and all
-// rows of Dk or half of them.  U, dX and dO become parts once and go around through LDS, each tile the right hand operand of its own wavefronts and the left hand one of the others; S and
-// dS' follow there.  Operands are read from LDS where they are used, for all of a wavefront's rows at once: its registers hold sums, not operands (with those of its own
-// steps in registers too, 256 were not enough, and what was spilled took most of the time).  Where LDS does not hold rows and states together (fp32, wide heads) they are.
-// What later and earlier steps give is made apart, each before its own products, so that the operands of one are gone when the other's come (163 us for both at once 191).
-// Measured, bf16: 8 x 1024 x 8 heads of 128 x 128 163 us, 4096 x 4 x 16 of 64 x 64 with 8 key heads 214, a twelfth of it matrix instructions, a third vector ones; the rest
-// are waits between the phases, which one workgroup a compute unit (LDS, registers) cannot fill; two, at 256 registers of which some are spilled, took as long.
+// rows of Dk or half of them.  U, dX and dO go around through LDS, each tile the right hand operand of its own wavefronts and the left hand one of the others; S and dS' follow there in
+// pieces of 32 columns, a tile of rows from each wavefront, one stored while the one before it is multiplied.  Operands are read from LDS where they are used, for all of a wavefront's
+// rows at once: its registers hold sums, not operands (with those of its own steps in registers too, 256 were not enough, and what was spilled took most of the time).  They are parts, made
+// once; where LDS does not hold all of them so, dX, then U, then dO are values there (bf16, heads of 128 x 128: whole states and all three as values 246 us, so 190).
+// What later and earlier steps give is made apart, each before its own products, so that the operands of one are gone when the other's come.
+// Measured, bf16: 8 x 1024 x 8 heads of 128 x 128 190 us, 4096 x 4 x 16 of 64 x 64 with 8 key heads 234; matrix and vector instructions follow one another in
+// the same phases, and one workgroup a compute unit (LDS, registers) cannot fill the waits between them.
 template <typename T, int DK, int DV, bool QUICK>
 __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps d_o, const float* ckpt, ard_steps dq, ard_steps dk, ard_steps df, ard_steps db) {
-  constexpr int IN = GdrType<T>::IN, N = GdrType<T>::OUT, VB = DV / 32, RT = DK / 16, HALVES = DK / 64, WAVES = 4 * HALVES, OWN = RT / HALVES, MINE = RT * VB / WAVES;
-  constexpr int ROWS = 4 * VB * (2 * N + IN), STATE = RT * VB * N;
-  constexpr bool KEEP = ROWS + STATE <= 152;
-  __shared__ u32x4 lds[(KEEP ? ROWS + STATE : ROWS > STATE ? ROWS : STATE) * 64];
+  constexpr int IN = kInput<T>, VB = DV / 32, RT = DK / 16, HALVES = DK / 64, WAVES = 4 * HALVES, OWN = RT / HALVES;
+  static_assert(RT == WAVES && VB % 2 == 0, "a tile of a state's rows each, and two slots in turn");
+  // KB of LDS: two slots of a state's pieces; dX, U and dO as parts, or, one after the other as far as need be, as values
+  constexpr int SLOT = RT * 3, TILES = 4 * VB, ROOM = 152 - 2 * SLOT;
+  constexpr bool VALUES_X = TILES * (6 + IN) > ROOM, VALUES_U = TILES * (5 + IN) > ROOM, VALUES_O = IN == 3 && TILES * (4 + IN) > ROOM;
+  using HeldX = Operands<VALUES_X>;
+  using HeldU = Operands<VALUES_U>;
+  using HeldO = Operands<VALUES_O>;
+  constexpr int ROWS = TILES * (HeldU::PER + HeldX::PER + (IN == 3 ? HeldO::PER : IN));
+  static_assert(ROWS <= ROOM, "");
+  __shared__ u32x4 lds[(ROWS + 2 * SLOT) * 64];
   __shared__ double dG[HALVES][2][kChunk];
   __shared__ float ends[WAVES], dots[2][HALVES][kChunk];
   __shared__ float crossing[WAVES][kChunk];
@@ -940,7 +950,7 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
 #pragma unroll
       for (int i = 0; i < OWN; ++i) kx[i].again(), qx[i].again();
       const u32x4 *ktf = a.cols + (int64_t)unit * (DK / 4) * IN * 64 + at_lane, *qtf = ktf + DK / 8 * IN * 64;
-      u32x4 *lu = lds + at_lane, *lx = lu + 4 * VB * N * 64, *lo = lu + 8 * VB * N * 64, *ls = KEEP ? lu + ROWS * 64 : lu;
+      u32x4 *lu = lds + at_lane, *lx = lu + TILES * HeldU::PER * 64, *lo = lx + TILES * HeldX::PER * 64, *ls = lu + ROWS * 64;
       const int mine = w * 16 + c;
       const Runs<float, 8, QUICK> S(ckpt + hu * a.Dk * a.Dv, a.Dv, a.Dk, a.Dv);
       const Runs<float, 8, true> ds(a.ds + hu * DK * a.dvp, a.dvp, DK, a.dvp);
@@ -968,46 +978,53 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
         bg = ((const T*)a.b.p)[(int64_t)(t0 + imin(mine, live - 1)) * a.b.t + n * a.b.b + h];
         __syncthreads();  // (the head before has been read)
         if (w8 < 3) ((u32x4*)&st)[w8 * 64 + lane] = weights;
-        u32x4* to = half ? lx : lu;
 #pragma unroll
-        for (int vb = 0; vb < VB; ++vb) store_parts<N>(to, w * VB + vb, parts_of<N>(x[vb]));
-        if (HALVES == 1) {
-#pragma unroll
-          for (int vb = 0; vb < VB; ++vb) store_parts<N>(lx, w * VB + vb, parts_of<N>(z[HALVES > 1 ? 0 : vb]));
+        for (int vb = 0; vb < VB; ++vb) {
+          if (half) HeldX::store(lx, w * VB + vb, x[vb]);
+          else HeldU::store(lu, w * VB + vb, x[vb]);
+          if (HALVES == 1) HeldX::store(lx, w * VB + vb, z[HALVES > 1 ? 0 : vb]);
         }
         if (half == 0) {
 #pragma unroll
-          for (int vb = 0; vb < VB; ++vb) store_parts<IN>(lo, w * VB + vb, y[vb].parts());
+          for (int vb = 0; vb < VB; ++vb) {
+            if constexpr (IN == 3) HeldO::store(lo, w * VB + vb, y[vb].v);
+            else store_parts<IN>(lo, w * VB + vb, y[vb].parts());
+          }
         }
       }
-      float Sx[MINE][8], Dx[MINE][8];
+      float Sx[VB][8], Dx[VB][8];  // S and dS' by pieces of 32 columns, a tile of rows a wavefront
 #pragma unroll
-      for (int i = 0; i < MINE; ++i) {
-        const int rt = (i * WAVES + w8) / VB, vb = (i * WAVES + w8) % VB;
-        S.load(rt * 16 + c, vb * 32 + 8 * g, Sx[i]);
-      }
+      for (int vb = 0; vb < VB; ++vb) S.load(w8 * 16 + c, vb * 32 + 8 * g, Sx[vb]);
+      const auto piece = [&](int vb) { return ls + (vb & 1) * SLOT * 64; };
       __syncthreads();
-      Parts<N> ub[KEEP ? 1 : VB], xb[KEEP ? 1 : VB];
-      Parts<IN> ob[KEEP ? 1 : VB];
-      if constexpr (!KEEP) {
-#pragma unroll
-        for (int vb = 0; vb < VB; ++vb) ub[vb] = load_parts<N>(lu, w * VB + vb), xb[vb] = load_parts<N>(lx, w * VB + vb), ob[vb] = load_parts<IN>(lo, w * VB + vb);
-      }
-      const auto of_u = [&](int vb) { return KEEP ? load_parts<N>(lu, w * VB + vb) : ub[KEEP ? 0 : vb]; };
-      const auto of_x = [&](int vb) { return KEEP ? load_parts<N>(lx, w * VB + vb) : xb[KEEP ? 0 : vb]; };
-      const auto of_o = [&](int vb) { return KEEP ? load_parts<IN>(lo, w * VB + vb) : ob[KEEP ? 0 : vb]; };
+      const auto given = [&](int frag) {
+        if constexpr (IN == 3) return HeldO::load(lo, frag);
+        else return load_parts<IN>(lo, frag);
+      };
+      const auto of_u = [&](int vb) { return HeldU::load(lu, w * VB + vb); };
+      const auto of_x = [&](int vb) { return HeldX::load(lx, w * VB + vb); };
+      const auto of_o = [&](int vb) { return given(w * VB + vb); };
       const double Gm = st.G[mine];
       const float wm = st.w[mine];
       float dw = 0.0f;
-      // By pairs of row tiles, ready as operands: N_ij and R_ij of earlier rows j, and of later rows i; each shortly before its products where LDS still has the rows
-      // then.  (All tiles are multiplied, though some are not needed: a branch around each would make the next one's operands wait for it.)
-      Parts<N> below[2], belowq[2], above[2], aboveq[2];
+      // By pairs of row tiles, ready as operands: N_ij and R_ij of earlier rows j, and of later rows i; each shortly before its products.  (All tiles
+      // are multiplied, though some are not needed: a branch around each would make the next one's operands wait for it.)
+      Parts<3> below[2], belowq[2], above[2], aboveq[2];
+      // sums of keys or queries with these weights
+      const auto weighed = [&](const u32x4* columns, const Parts<3> (&weights)[2], f32x4 (&sum)[OWN]) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          Parts<IN> k[OWN];
+          load_parts(columns, half * OWN * 2 + kb, 2, k);
+          mul_add(k, weights[kb], sum);
+        }
+      };
       const auto earlier = [&] {
         f32x4 up[4] = {}, upq[4] = {};
 #pragma unroll
         for (int vb = 0; vb < VB; ++vb) {
-          Parts<N> y[4];
-          load_parts(lu, vb, VB, y);
+          Parts<3> y[4];
+          HeldU::load(lu, vb, VB, y);
           mul_add(y, of_x(vb), up);
           mul_add(y, of_o(vb), upq);
           __builtin_amdgcn_sched_barrier(0);  // (operands read further ahead would not fit the registers)
@@ -1024,18 +1041,19 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
           }
         }
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) above[kb] = parts_of<N>(up[2 * kb], up[2 * kb + 1]), aboveq[kb] = parts_of<N>(upq[2 * kb], upq[2 * kb + 1]);
+        for (int kb = 0; kb < 2; ++kb) above[kb] = parts_of<3>(up[2 * kb], up[2 * kb + 1]), aboveq[kb] = parts_of<3>(upq[2 * kb], upq[2 * kb + 1]);
       };
       const auto later = [&] {
         f32x4 dn[4] = {}, dnq[4] = {};
 #pragma unroll
         for (int vb = 0; vb < VB; ++vb) {
-          Parts<N> y[4];
+          Parts<3> y[4];
           Parts<IN> z[4];
-          const Parts<N> u = of_u(vb);
-          load_parts(lx, vb, VB, y);
+          const Parts<3> u = of_u(vb);
+          HeldX::load(lx, vb, VB, y);
           mul_add(y, u, dn);
-          load_parts(lo, vb, VB, z);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) z[t] = given(t * VB + vb);
           mul_add(z, u, dnq);
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -1071,28 +1089,38 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
         }
         crossing[w8][(c >> 2) * 16 + 4 * g + (c & 3)] = crossed;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) below[kb] = parts_of<N>(dn[2 * kb], dn[2 * kb + 1]), belowq[kb] = parts_of<N>(dnq[2 * kb], dnq[2 * kb + 1]);
+        for (int kb = 0; kb < 2; ++kb) below[kb] = parts_of<3>(dn[2 * kb], dn[2 * kb + 1]), belowq[kb] = parts_of<3>(dnq[2 * kb], dnq[2 * kb + 1]);
       };
       earlier();
-      if (!KEEP) later();
       const float since = st.since[mine], still = st.still[mine];
       float moved = 0.0f, into = 0.0f, both = 0.0f;
-      if (!KEEP) __syncthreads();
+      // A piece is stored while the one before it, in the other slot, is multiplied.
+      const auto next_of_S = [&](int vb) {
+        store_parts<3>(piece(vb), w8, parts_of<3>(Sx[vb]));
+        ds.load(w8 * 16 + c, vb * 32 + 8 * g, Dx[vb]);
+      };
+      const auto product = [&](int vb) {
 #pragma unroll
-      for (int i = 0; i < MINE; ++i) {
-        const int rt = (i * WAVES + w8) / VB, vb = (i * WAVES + w8) % VB;
-        store_parts<N>(ls, i * WAVES + w8, parts_of<N>(Sx[i]));
-        ds.load(rt * 16 + c, vb * 32 + 8 * g, Dx[i]);
-      }
-      __syncthreads();
+        for (int e = 0; e < 8; ++e) both = fmaf(Sx[vb][e], Dx[vb][e], both);
+      };
+      const auto next_of_dS = [&](int vb) { store_parts<3>(piece(vb), w8, parts_of<3>(Dx[vb])); };
+      next_of_S(0);
+      // (at once where registers are short, so that the weights are gone when the states' pieces come: 8 x 1024 x 8 heads of 128 x 128 353 us of backward pass, behind the pieces 394; else
+      // behind them, whose products the keys' loads are waited for beside: 4096 x 4 x 16 of 64 x 64 531, at once 552)
+      constexpr bool AT_ONCE = HALVES > 1;
+      if (AT_ONCE) weighed(ktf, above, sumk), weighed(ktf, aboveq, sumq);
       {
         f32x4 tq[OWN] = {}, tp[OWN] = {};
 #pragma unroll
         for (int vb = 0; vb < VB; ++vb) {
-          const Parts<N> x = of_x(vb);
+          __syncthreads();
+          if (vb + 1 < VB) next_of_S(vb + 1);
+          else next_of_dS(0);
+          if (vb > 0) product(vb - 1);
+          const Parts<3> x = of_x(vb);
           const Parts<IN> o = of_o(vb);
-          Parts<N> y[OWN];
-          load_parts(ls, half * OWN * VB + vb, VB, y);
+          Parts<3> y[OWN];
+          load_parts(piece(vb), half * OWN, 1, y);
           mul_add(y, o, tq);
           mul_add(y, x, tp);
         }
@@ -1103,43 +1131,23 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
 #pragma unroll
           for (int r = 0; r < 4; ++r) mk = fmaf(kx[i].at(r), tp[i][r], mk), mq = fmaf(qx[i].at(r), tq[i][r], mq);
           moved += rkm * mk + rqm * mq;
+          sumq[i] += tq[i], sumk[i] += tp[i];
         }
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          Parts<IN> k[OWN];
-          load_parts(ktf, half * OWN * 2 + kb, 2, k);
-          mul_add(k, above[kb], tp);
-          mul_add(k, aboveq[kb], tq);
-        }
-#pragma unroll
-        for (int i = 0; i < OWN; ++i) sumq[i] += tq[i], sumk[i] += tp[i];
+        product(VB - 1);
       }
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < MINE; ++i) {
-        store_parts<N>(ls, i * WAVES + w8, parts_of<N>(Dx[i]));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) both = fmaf(Sx[i][e], Dx[i][e], both);
-      }
-      if (KEEP) later();
-      __syncthreads();
+      if (!AT_ONCE) weighed(ktf, above, sumk), weighed(ktf, aboveq, sumq);
+      later();
+      if (AT_ONCE) weighed(ktf, below, sumk), weighed(qtf, belowq, sumk);
       {
         f32x4 te[OWN] = {};
 #pragma unroll
         for (int vb = 0; vb < VB; ++vb) {
-          const Parts<N> u = of_u(vb);
-          Parts<N> y[OWN];
-          load_parts(ls, half * OWN * VB + vb, VB, y);
+          __syncthreads();
+          if (vb + 1 < VB) next_of_dS(vb + 1);
+          const Parts<3> u = of_u(vb);
+          Parts<3> y[OWN];
+          load_parts(piece(vb), half * OWN, 1, y);
           mul_add(y, u, te);
-        }
-        f32x4 tm[OWN] = {};
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          Parts<IN> k[OWN];
-          load_parts(ktf, half * OWN * 2 + kb, 2, k);
-          mul_add(k, below[kb], tm);
-          load_parts(qtf, half * OWN * 2 + kb, 2, k);
-          mul_add(k, belowq[kb], tm);
         }
 #pragma unroll
         for (int i = 0; i < OWN; ++i) {
@@ -1148,9 +1156,10 @@ __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps 
 #pragma unroll
           for (int r = 0; r < 4; ++r) me = fmaf(kx[i].at(r), te[i][r], me);
           into += rkm * me;
-          sumk[i] += te[i] + tm[i];
+          sumk[i] += te[i];
         }
       }
+      if (!AT_ONCE) weighed(ktf, below, sumk), weighed(qtf, belowq, sumk);
       dw = over_rows(dw), moved = over_rows(moved), into = over_rows(into);
       both = wave_sum(both);
       if (g == 0) dG[half][0][mine] = moved, dG[half][1][mine] = into;
@@ -1257,7 +1266,7 @@ static GdrPlan gdr_plan(int32_t dtype, int T, int B, int Hk, int H, int Dk, int 
   p.dk = Dk <= 64 ? 64 : 128;
   p.slices = ceil_div(Dv, 16);
   a.dvp = Dv <= 64 ? 64 : 128;
-  const size_t in = dtype == ARD_F32 ? 3 : 1, out = dtype == ARD_F32 ? 3 : 2, ku = (size_t)a.chunks * B * Hk, hu = (size_t)a.chunks * B * H;
+  const size_t in = dtype == ARD_F32 ? 3 : 1, ku = (size_t)a.chunks * B * Hk, hu = (size_t)a.chunks * B * H;
   size_t at = 0;
   const auto take = [&](auto*& ptr, size_t n) {
     ptr = (std::decay_t<decltype(ptr)>)((char*)base + at);
@@ -1265,7 +1274,7 @@ static GdrPlan gdr_plan(int32_t dtype, int T, int B, int Hk, int H, int Dk, int 
   };
   const size_t rows = (size_t)4 * (p.dk / 32) * in * 1024, cols = (size_t)(p.dk / 8) * in * 1024;
   take(a.steps, hu * sizeof(Steps64));
-  take(a.rows, ku * rows * 2), take(a.cols, ku * cols * (backward ? 2 : 1)), take(a.tri, hu * 6 * (backward ? 9 : 3 + out) * 1024);
+  take(a.rows, ku * rows * 2), take(a.cols, ku * cols * (backward ? 2 : 1)), take(a.tri, hu * 6 * (backward ? 9 : 3 + Operands<true>::PER) * 1024);
   // (the backward pass's wavefronts cover the padded columns)
   const int groups = ceil_div(backward ? a.dvp / 16 : p.slices, 4);
   a.span = segment_span(a.chunks, B * H * groups, B * H * (groups + p.dk / 64), backward && p.dk == 128 && dtype == ARD_BF16 ? 1 : 2);  // (LDS holds the operands of one of these)

@@ -2,7 +2,8 @@
 //
 // An fp32 value is the sum of three bf16 values (8 bits of its 24 each), so a product of two is the sum of the six products of parts that
 // reach its 24 bits, each exact, added in fp32: as good as fp32's own, at 2.7 times the rate of the fp32 matrix instructions.
-// What is bf16 already is one part, and its product with an fp32 value takes three; where only a bf16 result comes of it, two parts (16 bits) are kept.
+// What is bf16 already is one part, and its product with an fp32 value takes three.  A result that is rounded to bf16 needs its factors' 24 bits too: with two parts
+// (16 bits) of them 3e-4 to 1e-3 of all results are rounded to bf16's other neighbour, with three under 7e-5.
 //
 // v_mfma_f32_16x16x32_bf16, lane = 16 g + c: A[row c][8 g + j], B[8 g + j][column c], j = 0..7; result[row 4 g + r][column c], r = 0..3.
 // A contraction may take its indices in any order that both operands share: with index 4 g + (j & 3) + 16 (j >> 2) in the place of
@@ -43,13 +44,6 @@ template <int N> __device__ __forceinline__ Parts<N> parts_of(const f32x4& lo, c
   const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
   return parts_of<N>(x);
 }
-// the first N parts of more
-template <int N, int M> __device__ __forceinline__ Parts<N> leading(const Parts<M>& x) {
-  Parts<N> s;
-#pragma unroll
-  for (int n = 0; n < N; ++n) s.p[n] = x.p[n];
-  return s;
-}
 // acc += a b, of all products of parts those that reach the larger operand's last part; the small ones first
 template <int NA, int NB> __device__ __forceinline__ void mul_add(const Parts<NA>& a, const Parts<NB>& b, f32x4& acc) {
   constexpr int L = NA > NB ? NA : NB;
@@ -89,6 +83,23 @@ template <int N> __device__ __forceinline__ void store_parts(u32x4* base, int fr
 #pragma unroll
   for (int n = 0; n < N; ++n) base[(frag * N + n) * 64] = s.p[n];
 }
+// Operands of fp32 values: their three parts, or, in two thirds of the room, the values (FLOATS), which become parts where they are used.
+template <bool FLOATS> struct Operands {
+  static constexpr int PER = FLOATS ? 2 : 3;  // KB of an operand
+  static __device__ __forceinline__ void store(u32x4* base, int frag, const f32x4& lo, const f32x4& hi) {
+    if constexpr (FLOATS) base[frag * 2 * 64] = __builtin_bit_cast(u32x4, lo), base[(frag * 2 + 1) * 64] = __builtin_bit_cast(u32x4, hi);
+    else store_parts<3>(base, frag, parts_of<3>(lo, hi));
+  }
+  static __device__ __forceinline__ void store(u32x4* base, int frag, const float (&x)[8]) { store(base, frag, f32x4{x[0], x[1], x[2], x[3]}, f32x4{x[4], x[5], x[6], x[7]}); }
+  static __device__ __forceinline__ Parts<3> load(const u32x4* base, int frag) {
+    if constexpr (FLOATS) return parts_of<3>(__builtin_bit_cast(f32x4, base[frag * 2 * 64]), __builtin_bit_cast(f32x4, base[(frag * 2 + 1) * 64]));
+    else return load_parts<3>(base, frag);
+  }
+  template <int TILES> static __device__ __forceinline__ void load(const u32x4* base, int first, int step, Parts<3> (&s)[TILES]) {
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) s[t] = load(base, first + t * step);
+  }
+};
 // FRAGS x 1 KB from global memory to the same order in LDS, without a register in between: each of a workgroup's four wavefronts its share of
 // neighbours, four to an address.
 // (The last wavefront's share may reach behind the end: it takes the last operand again, so that every wavefront makes as many accesses.)
@@ -163,13 +174,7 @@ struct GdrArgs {
 };
 __device__ __forceinline__ int live_steps(const GdrArgs& a, int n) { return a.len ? imin(imax(a.len[n], 0), a.T) : a.T; }
 
-template <typename T> struct GdrType;
-template <> struct GdrType<uint16_t> {
-  static constexpr int IN = 1, OUT = 2;  // parts of an input, and of a factor of a result
-};
-template <> struct GdrType<float> {
-  static constexpr int IN = 3, OUT = 3;
-};
+template <typename T> constexpr int kInput = sizeof(T) == 2 ? 1 : 3;  // parts of an input
 
 // exp(x), x <= 0: the argument's rounding costs |x| 2^-24 of it, and |x| < 104 where it is not 0
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
