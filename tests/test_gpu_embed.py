@@ -172,3 +172,20 @@ def test_a_stream_of_its_own():
     side.synchronize()
     size = L.embed_bwd(ids, np.abs(dY), 60)
     assert np.all(np.abs(to_host(dE) - L.embed_bwd(ids, dY, 60)) <= 402 * 2.0 ** -24 * size)
+
+
+@pytest.mark.parametrize("dtype,wdtype", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("scale", [-3.0, -1.0, 0.0, float("inf"), float("-inf"), float("nan")])
+def test_rows_that_no_token_meets_are_zero_whatever_the_scale(scale, dtype, wdtype):
+    R, V, D = 130, 300, 21
+    ids, t = _ids(R, V, 8, "padded"), torch.float32 if wdtype == "f32" else torch.bfloat16
+    dY = stored(np.random.default_rng(9).uniform(1, 2, (R, D)), dtype)
+    dE = ard.embed_bwd(torch.from_numpy(ids).cuda(), from_vals(dY, dtype), V, scale=scale, dtype=t)
+    met = np.zeros(V, bool)
+    met[ids[(ids >= 0) & (ids < V)]] = True
+    assert 0 < met.sum() < V and not raw_bits(dE)[~met].any()
+    if np.isfinite(scale):
+        assert_parity(dE, L.embed_bwd(ids, dY, V, scale), wdtype, None, "dE")
+    else:
+        want = np.full((int(met.sum()), D), scale)      # sums are positive
+        assert np.array_equal(to_host(dE)[met], want, equal_nan=True)
