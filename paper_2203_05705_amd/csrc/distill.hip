@@ -256,9 +256,8 @@ static int32_t distill_check(int32_t dtype, int32_t tdtype, int32_t R, int32_t V
 }
 
 template <typename T, typename S, int MODE, int TWO, int C> static int32_t distill_launch(const DistillArgs& a, int threads, hipStream_t st) {
-  const int x = imin(a.R, 1 << 20);
-  const char* name = launch_instance("distill_kernel", MODE, TWO, C);
-  ARD_LAUNCH_NAMED(name, (distill_kernel<T, S, MODE, TWO, C>), dim3(x, ceil_div(a.R, x)), dim3(threads), 0, st, a);
+  const int x = imin(a.R, 1 << 20), y = (int)(((int64_t)a.R + x - 1) / x);  // (a sum of R and x may pass 32 bits)
+  ARD_LAUNCH_NAMED(launch_instance("distill_kernel", x, y, threads), (distill_kernel<T, S, MODE, TWO, C>), dim3(x, y), dim3(threads), 0, st, a);
   ARD_LAUNCH_CHECK("distill_kernel");
   return ARD_OK;
 }

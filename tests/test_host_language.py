@@ -224,6 +224,18 @@ def test_distillation_accepts_and_refuses():
             assert call(*a.values()) == 0
 
 
+@pytest.mark.parametrize("R", [1, 700, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, 1 << 30, (1 << 31) - (1 << 20), (1 << 31) - (1 << 20) + 1, (1 << 31) - 1])
+def test_the_most_rows_of_logits_have_a_grid(R):
+    """A workgroup for every row; HIP counts the threads along an axis of a grid in 32 bits and takes 65535 workgroups along its second."""
+    with D.dry_run() as lib:
+        heap = D.FakeHeap()
+        for V in (100, 200000):
+            for call, args in ((lib.ard_distill_fwd, _distill_args), (lib.ard_distill_bwd, _distill_bwd_args)):
+                assert call(*args(heap, R=R, V=V, ldz=V, lddz=V).values()) == 0
+                x, y, threads = (int(v) for v in D.instances(lib)[0].split("<")[1][:-1].split(","))
+                assert 0 < x and x * threads < 1 << 32 and 0 < y <= 65535 and R <= x * y < R + x
+
+
 # ---- through the binding ---------------------------------------------------------------------
 
 def test_calls_of_the_binding():
