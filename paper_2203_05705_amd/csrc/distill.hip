@@ -201,7 +201,8 @@ __global__ __launch_bounds__(1024, C <= 4 ? 8 : 4) void distill_kernel(DistillAr
     const float p = exp2_of(above(x, top, a.tau));
     return TWO ? fmaf(fT, p, f1 * at_one(p, x, top)) : (fT + f1) * p;
   };
-  if (any) {
+  const bool shared = any && (taught || labelled);  // (nothing of a row that neither teaches: NaN and infinities of padding have no part either)
+  if (shared) {
     each([&](int c) {
       const int j = at(c);
       if (j >= V) return;
@@ -218,7 +219,7 @@ __global__ __launch_bounds__(1024, C <= 4 ? 8 : 4) void distill_kernel(DistillAr
       if (at(c) < V) store_some<N>(dz + at(c), V - at(c), none);
     });
   }
-  if (!any || (!taught && !labelled)) return;
+  if (!shared) return;
   __syncthreads();
   for (int k = threadIdx.x; k < (taught ? K : 0); k += threads) {
     const int id = sh.id[k];

@@ -196,3 +196,24 @@ def test_gradient_against_differences_of_the_loss():
     way, e = np.random.default_rng(11).standard_normal(Z.shape), 1e-5
     diff = ((L.distill(Z + e * way, ids, t, y, 2.0, 0.5)[0] - L.distill(Z - e * way, ids, t, y, 2.0, 0.5)[0]) * dloss).sum() / (2 * e)
     assert abs(diff - (to_host(dZ) * way).sum()) <= 1e-5 * np.abs(to_host(dZ) * way).sum() + 1e-8
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,alpha", [(1.0, 0.5), (2.0, 0.5), (1.5, 0.5), (2.0, 1.0), (1.0, 0.0)])
+@pytest.mark.parametrize("V", [70, 9000, 140000])
+def test_a_row_without_entries_and_label_is_left_out_whatever_it_holds(V, T, alpha, dtype):
+    R, K = 6, 5
+    Z, ids, t, y, dloss = _case(R, V, K, dtype, "f32", 11)
+    y[:] = 4
+    y[1:5], ids[1:5] = -1, -1
+    ids[4], t[4] = 3, -np.inf       # entries without a share
+    clean = Z.copy()
+    Z[1, ::3], Z[2, 7], Z[3, :], Z[4, 5] = np.nan, np.inf, np.nan, -np.inf
+    args, kw = (torch.from_numpy(ids).cuda(), from_vals(t, "f32")), dict(labels=torch.from_numpy(y).cuda(), temperature=T, alpha=alpha)
+    dl, place, Zd = from_vals(np.where(np.arange(R) == 4, np.nan, dloss), "f32"), from_vals(Z, dtype), from_vals(Z, dtype)
+    rloss, rdZ = L.distill(clean, ids, t, y, T, alpha, dloss)
+    loss, stats, dZ = ard.distill_fwd(Zd, *args, dloss=dl, **kw)
+    for l, d in ((loss, dZ), (loss, ard.distill_bwd(Zd, *args, stats, dl, **kw)), ard.distill_fwd(place, *args, dloss=dl, out=(None, None, place), **kw)[::2]):
+        assert not raw_bits(l)[1:5].any() and not raw_bits(d)[1:5].any()
+        assert_parity(l, rloss, "f32", None, "loss")
+        assert_parity(d, rdZ, dtype, None, "dZ")
