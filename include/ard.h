@@ -577,7 +577,7 @@ int32_t ard_embed_bwd(int32_t dtype, int32_t wdtype, int32_t R, int32_t V, int32
 /*
  * Loss of R rows of V logits Z against a teacher's K largest logits t[R x K] of the elements d_ids[R x K], and labels d_labels[R] (or NULL):
  *   p = softmax(t / T) over the row's entries, qT = softmax(z / T), q = softmax(z) over all V,
- *   loss[r] = alpha T^2 sum_k p_k (log p_k - log qT[id_k]) + (1 - alpha) (-log q[label]),       T = temperature > 0, alpha from 0 to 1
+ *   loss[r] = alpha T^2 sum_k p_k (log p_k - log qT[id_k]) + (1 - alpha) (-log q[label]),       T = temperature, from 2^-60 to 2^60, alpha from 0 to 1
  *   dZ = dloss[r] (alpha T (qT - the p at their elements) + (1 - alpha) (q - 1 at the label)).
  * An id outside 0 .. V-1 or a teacher's logit of -infinity is an entry that has no part; a label outside 0 .. V-1 is a row without one; what a row has
  * no entries or label for is left out of its sums, as is all of a row whose logits are all -infinity.  A logit of -infinity (masked) has no share.

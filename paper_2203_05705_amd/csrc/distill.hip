@@ -246,7 +246,7 @@ static int32_t distill_check(int32_t dtype, int32_t tdtype, int32_t R, int32_t V
   if (V > 1 << 30) return fail(ARD_ESHAPE, "V = %d is too large", V);
   if (K > kMaxTop) return fail(ARD_EUNSUPPORTED, "a row has at most %d teacher's logits (got %d)", kMaxTop, K);
   if (ldz < V) return fail(ARD_ESHAPE, "the logits' leading dimension must be at least V");
-  if (!(temperature > 0.0f) || !(temperature < INFINITY)) return fail(ARD_EINVAL, "the temperature must be positive and finite (got %g)", temperature);
+  if (!(temperature >= 0x1p-60f && temperature <= 0x1p60f)) return fail(ARD_EINVAL, "the temperature must be from 2^-60 to 2^60 (got %g)", temperature);
   if (!(alpha >= 0.0f && alpha <= 1.0f)) return fail(ARD_EINVAL, "alpha must be from 0 to 1 (got %g)", alpha);
   if (!Z) return fail(ARD_EINVAL, "null tensor pointer");
   if (alpha > 0.0f && K > 0 && (!d_ids || !t)) return fail(ARD_EINVAL, "a teacher's share needs its logits and their ids");

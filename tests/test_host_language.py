@@ -224,6 +224,18 @@ def test_distillation_accepts_and_refuses():
             assert call(*a.values()) == 0
 
 
+def test_temperatures_whose_square_or_reciprocal_is_no_number_are_refused():
+    """T^2 weighs the loss and log2(e) / T the logits: both are normal fp32 numbers from 2^-60 to 2^60."""
+    with D.dry_run() as lib:
+        heap = D.FakeHeap()
+        for call, args in ((lib.ard_distill_fwd, _distill_args), (lib.ard_distill_bwd, _distill_bwd_args)):
+            for T in (1e-45, 1e-39, 1e-30, 2.0 ** -60 * 0.999, 2.0 ** 60 * 1.001, 1e20, 3e38):
+                for alpha in (0.0, 0.5, 1.0):
+                    assert call(*args(heap, temperature=T, alpha=alpha).values()) == -1 and lib.ard_last_error(), T
+            for T in (2.0 ** -60, 1e-3, 100.0, 2.0 ** 60):
+                assert call(*args(heap, temperature=T).values()) == 0, T
+
+
 @pytest.mark.parametrize("R", [1, 700, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, 1 << 30, (1 << 31) - (1 << 20), (1 << 31) - (1 << 20) + 1, (1 << 31) - 1])
 def test_the_most_rows_of_logits_have_a_grid(R):
     """A workgroup for every row; HIP counts the threads along an axis of a grid in 32 bits and takes 65535 workgroups along its second."""
