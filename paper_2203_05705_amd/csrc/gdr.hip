@@ -548,7 +548,8 @@ __global__ __launch_bounds__(256, MODE == DROP && sizeof(T) == 2 ? 2 : 1) void g
   constexpr int IN = kInput<T>, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3, PF = 6 * Operands<true>::PER;
   constexpr bool KEPT = MODE == KEEP, OUTPUT = MODE != SUM;
   constexpr int RF = OUTPUT ? 2 * KF : KF, TF = OUTPUT ? MF + PF : MF;  // (the operands of Q and P are read for o alone)
-  constexpr bool STAGED = 2 * KF + KTF + MF + PF <= 150;  // KB of LDS
+  constexpr bool STAGED = walk_operands(false, MODE == SUM, DK, IN) > 0;
+  static_assert(!STAGED || walk_operands(false, MODE == SUM, DK, IN) == RF + KTF + TF, "");
   __shared__ u32x4 one[STAGED ? RF * 64 : 1], two[STAGED ? (KTF + TF) * 64 : 1];  // what the halves read
   __shared__ f32x4 weights[2][64];  // w, ka, qa, ke of a chunk
   int group;
@@ -699,7 +700,8 @@ template <typename T, int DK, bool NEAR> __global__ __launch_bounds__(256) void 
 template <typename T, int DK, bool NEAR, int MODE>
 __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o, const float* dST, ard_steps dv, float* dS0, int groups) {
   constexpr int IN = kInput<T>, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3;
-  constexpr bool STAGED = KF + 2 * KTF + 2 * MF <= 150;
+  constexpr bool STAGED = walk_operands(true, MODE == SUM, DK, IN) > 0;
+  static_assert(!STAGED || walk_operands(true, MODE == SUM, DK, IN) == KF + 2 * KTF + 2 * MF, "");
   constexpr bool OUTPUT = MODE != SUM;
   __shared__ u32x4 one[STAGED ? (KF + MF) * 64 : 1], two[STAGED ? (2 * KTF + MF) * 64 : 1];
   __shared__ f32x4 weights[2][64];  // w, ka, qa, ke of a chunk
@@ -1244,9 +1246,10 @@ struct GdrPlan {
 };
 // Chunks of a segment: all, or, where the workgroups of all heads' columns leave compute units idle, what is estimated (in chunks' times) to end first: a segment's chunks,
 // before them 0.7 of their time for the sums, as often as their workgroups (`sums` of a segment) fill the chip, and a product of a state for every segment.
-// Measured, in segments against at once, forward / backward, us: bf16 1 x 8 heads of 64 x 64, 512 steps (not cut) 38 / 58, 1024 steps 38 / 62 and 61 / 83, 4096 61 / 106 and
-// 200 / 248; 4 x 16 of 64 x 64, 1024 65 / 151 and 76 / 151, 4096 210 / 598 and 306 / 669; 2 x 8 of 128 x 128, 768 57 / 103 and 63 / 110, 4096 128 / 388 and 269 / 501; fp32 1 x 8 of
-// 128 x 128, 1024 83 / 190 and 175 / 317.
+// Measured, in segments against at once, forward / backward, us: bf16 1 x 8 heads of 64 x 64, 512 steps (not cut) 43 / 58, 1024 steps 40 / 64 and 71 / 82, 4096 66 / 110 and
+// 241 / 252; 4 x 16 of 64 x 64, 1024 70 / 158 and 87 / 158, 4096 221 / 618 and 348 / 690; 2 x 8 of 128 x 128, 768 59 / 111 and 71 / 120, 4096 134 / 418 and 312 / 535; fp32 1 x 8 of
+// 128 x 128, 1024 84 / 180 and 180 / 307; backward fp32, of whose sums LDS holds one workgroup: 4096 steps, 2 x 4 of 64 x 128 172 (11 segments; 13, as if it held two, 188) and 361,
+// 4 x 4 of 64 x 64 264 (8; 13: 269) and 448.
 static int segment_span(int chunks, int workgroups, int sums, int resident) {
   constexpr int kUnits = 256;
   int best = chunks;
@@ -1277,7 +1280,9 @@ static GdrPlan gdr_plan(int32_t dtype, int T, int B, int Hk, int H, int Dk, int 
   take(a.rows, ku * rows * 2), take(a.cols, ku * cols * (backward ? 2 : 1)), take(a.tri, hu * 6 * (backward ? 9 : 3 + Operands<true>::PER) * 1024);
   // (the backward pass's wavefronts cover the padded columns)
   const int groups = ceil_div(backward ? a.dvp / 16 : p.slices, 4);
-  a.span = segment_span(a.chunks, B * H * groups, B * H * (groups + p.dk / 64), backward && p.dk == 128 && dtype == ARD_BF16 ? 1 : 2);  // (LDS holds the operands of one of these)
+  // workgroups of sums that a compute unit holds: their registers allow two, LDS (with 2 KB of weights each) one or two
+  const int resident = imin(2, 160 / (walk_operands(backward, true, p.dk, (int)in) + 2));
+  a.span = segment_span(a.chunks, B * H * groups, B * H * (groups + p.dk / 64), resident);
   a.segments = ceil_div(a.chunks, a.span);
   if (a.segments > 1) {
     const size_t n = (size_t)a.segments * B * H * p.dk * 4;
@@ -1383,7 +1388,8 @@ extern "C" int32_t ard_gdr_fwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
     ARD_LAUNCH_CHECK("gdr_prep_kernel");
     const int groups = ceil_div(p.slices, 4);
     if (a.segments > 1) {
-      ARD_LAUNCH_NAMED("gdr_fwd_kernel", (gdr_fwd_kernel<E, DK, NEAR, SUM>), dim3(B * H * (groups + DK / 64) * (a.segments - 1)), dim3(256), 0, st, a, S0, out, ST, ckpt, groups);
+      const int sums = B * H * (groups + DK / 64) * (a.segments - 1);
+      ARD_LAUNCH_NAMED(launch_instance("gdr_fwd_kernel", sums, a.segments, a.span), (gdr_fwd_kernel<E, DK, NEAR, SUM>), dim3(sums), dim3(256), 0, st, a, S0, out, ST, ckpt, groups);
       ARD_LAUNCH_CHECK("gdr_fwd_kernel");
       ARD_LAUNCH_NAMED("gdr_join_kernel", (gdr_join_kernel<DK>), dim3(B * H * p.slices), dim3(256), 0, st, a, S0, p.slices);
       ARD_LAUNCH_CHECK("gdr_join_kernel");
@@ -1425,7 +1431,8 @@ extern "C" int32_t ard_gdr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t Hk, 
     ARD_LAUNCH_CHECK("gdr_rows_kernel");
     const int groups = ceil_div(slices, 4);
     if (a.segments > 1) {
-      ARD_LAUNCH_NAMED("gdr_back_kernel", (gdr_back_kernel<E, DK, NEAR, SUM>), dim3(B * H * (groups + DK / 64) * (a.segments - 1)), dim3(256), 0, st, a, od, dST, dv, dS0, groups);
+      const int sums = B * H * (groups + DK / 64) * (a.segments - 1);
+      ARD_LAUNCH_NAMED(launch_instance("gdr_back_kernel", sums, a.segments, a.span), (gdr_back_kernel<E, DK, NEAR, SUM>), dim3(sums), dim3(256), 0, st, a, od, dST, dv, dS0, groups);
       ARD_LAUNCH_CHECK("gdr_back_kernel");
       ARD_LAUNCH_NAMED("gdr_join_kernel", (gdr_join_kernel<DK>), dim3(B * H * slices), dim3(256), 0, st, a, dST, slices);
       ARD_LAUNCH_CHECK("gdr_join_kernel");

@@ -176,6 +176,13 @@ __device__ __forceinline__ int live_steps(const GdrArgs& a, int n) { return a.le
 
 template <typename T> constexpr int kInput = sizeof(T) == 2 ? 1 : 3;  // parts of an input
 
+// KB of LDS that the operands of a walk over the chunks take, of keys of DK with IN parts: of both halves of a chunk, in which forward has K, Q, the columns of K, M and P (for
+// sums no Q and no P), backward K, the columns of K and Q, and the transposes of M and P.  0: LDS does not hold them, they are read from the caches.
+constexpr int walk_operands(bool backward, bool sum, int DK, int IN) {
+  const int keys = DK / 8 * IN, m = 6 * 3, p = 6 * Operands<true>::PER, all = backward ? 3 * keys + 2 * m : 3 * keys + m + p;
+  return all > 150 ? 0 : sum && !backward ? 2 * keys + m : all;
+}
+
 // exp(x), x <= 0: the argument's rounding costs |x| 2^-24 of it, and |x| < 104 where it is not 0
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 __device__ __forceinline__ float logistic(float x) {

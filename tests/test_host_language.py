@@ -177,6 +177,22 @@ def test_delta_rule_workspaces(dtype):
         assert s["T"] == 100
 
 
+@pytest.mark.parametrize("dtype,T,B,Hk,H,Dk,Dv,back,segments", [
+    (ard.F32, 4096, 2, 4, 4, 64, 128, 1, 11), (ard.F32, 4096, 4, 4, 4, 60, 64, 1, 8), (ard.F32, 2048, 4, 8, 8, 64, 64, 1, 8),   # LDS holds the operands of one workgroup
+    (ard.BF16, 4096, 2, 8, 8, 128, 128, 1, 8), (ard.BF16, 16384, 1, 8, 8, 128, 128, 1, 16),
+    (ard.BF16, 4096, 4, 8, 16, 64, 64, 1, 4), (ard.BF16, 16384, 1, 8, 8, 128, 128, 0, 16), (ard.F32, 4096, 4, 4, 4, 64, 64, 0, 13)])      # two, and their registers allow no more
+def test_segments_go_by_what_a_compute_unit_holds_of_their_sums(dtype, T, B, Hk, H, Dk, Dv, back, segments):
+    with D.dry_run() as lib:
+        heap = D.FakeHeap()
+        sizes = dict(dtype=dtype, T=T, B=B, Hk=Hk, H=H, Dk=Dk, Dv=Dv)
+        call, args = (lib.ard_gdr_bwd, _gdr_bwd_args) if back else (lib.ard_gdr_fwd, _gdr_args)
+        assert call(*args(heap, **sizes, ws_bytes=lib.ard_gdr_workspace_bytes(*sizes.values(), back)).values()) == 0
+        sums = next(i for i in D.instances(lib) if i.startswith("gdr_back_kernel<" if back else "gdr_fwd_kernel<"))
+        workgroups, n, span = (int(v) for v in sums.split("<")[1][:-1].split(","))
+        groups = -(-(128 if Dv > 64 else 64) // 64) if back else -(-Dv // 64)
+        assert n == segments == -(-(-(-T // 64)) // span) and workgroups == B * H * (groups + (2 if Dk > 64 else 1)) * (n - 1)
+
+
 # ---- distillation ----------------------------------------------------------------------------
 
 def _distill_args(heap, **change):
