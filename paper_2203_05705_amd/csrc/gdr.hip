@@ -1319,7 +1319,7 @@ static int32_t gdr_tensors(int32_t dtype, const ard_steps* s, int n, const char*
   return ARD_OK;
 }
 static int32_t gdr_numbers(float scale, float eps) {
-  if (!(eps > 0.0f && eps < INFINITY)) return fail(ARD_EINVAL, "eps must be positive and finite (got %g)", eps);
+  if (!(eps >= 0x1p-100f && eps < INFINITY)) return fail(ARD_EINVAL, "eps must be finite and at least 2^-100 (got %g)", eps);  // (1 / eps, times the scale, meets a product of zeros)
   if (!(scale > -INFINITY && scale < INFINITY)) return fail(ARD_EINVAL, "scale must be finite (got %g)", scale);
   return ARD_OK;
 }

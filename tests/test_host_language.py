@@ -153,6 +153,17 @@ def test_delta_rule_accepts_and_refuses():
         assert D.launches(lib)[0] == 0
 
 
+def test_an_eps_whose_reciprocal_is_no_number_is_refused():
+    """A key of zeros has the reciprocal length 1 / sqrt(eps); the product of two of them and a scale has to stay a number, as it meets a product of zeros."""
+    with D.dry_run() as lib:
+        heap = D.FakeHeap()
+        for call, args in ((lib.ard_gdr_fwd, _gdr_args), (lib.ard_gdr_bwd, _gdr_bwd_args)):
+            for eps in (1e-45, 1e-39, 1e-35, 2.0 ** -100 * 0.999):
+                assert call(*args(heap, eps=eps).values()) == -1 and lib.ard_last_error(), eps
+            for eps in (2.0 ** -100, 1e-30, 1e-12, 1.0):
+                assert call(*args(heap, eps=eps).values()) == 0, eps
+
+
 @pytest.mark.parametrize("dtype", [ard.F32, ard.BF16])
 def test_delta_rule_workspaces(dtype):
     with D.dry_run() as lib:
