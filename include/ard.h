@@ -584,7 +584,8 @@ int32_t ard_embed_bwd(int32_t dtype, int32_t wdtype, int32_t R, int32_t V, int32
  * no entries or label for is left out of its sums, as is all of a row whose logits are all -infinity.  A logit of -infinity (masked) has no share.
  * An element may be named more than once: its entries' shares are added.  K = 0 or alpha = 0 is the labels' cross entropy (times 1 - alpha), t and d_ids may then
  * be NULL.  dtype: of Z and dZ, rows ldz and lddz elements apart (at least V), which start at any element; tdtype: of t, ARD_F32 or dtype.
- * stats[R x 3] (fp32): the largest logit and the sums of the exponentials at T and at 1, what ard_distill_bwd reads.  Statistics and sums are fp32.
+ * stats[R x 3] (fp32): the largest logit and the sums of the exponentials at T and at 1, what ard_distill_bwd reads.  Statistics and sums are fp32
+ * (the loss's logarithms are off by up to some 2^-20, the loss by alpha T^2 times that).
  * ard_distill_fwd with dZ (may be NULL) makes the gradient of dloss[R] (d_dloss, fp32; NULL: 1) in the same reading of Z.  dZ may lie where Z does (the same address
  * and leading dimension); otherwise no output may overlap an input.  K is at most 1024 (else ARD_EUNSUPPORTED).
  */

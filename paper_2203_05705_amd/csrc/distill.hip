@@ -5,11 +5,12 @@
 //
 // A workgroup takes a row.  It holds the row in registers as it was read, so that the largest logit, both sums of exponentials and the
 // gradient come from one reading: the bytes of z and dz are what bounds it.  Rows longer than its registers hold are read again for each of
-// the three (out of the caches, mostly).  Sums and statistics are fp32.
+// the three (out of the caches, mostly).  Sums and statistics are fp32, a lane's of up to 128 values one after the other (more of rows that are read again), the lanes' in trees.
 //
-// Measured, bf16, 8192 x 32768, K = 64, T = 2 with labels, loss and gradient: 296 us, 3.6 TB/s of the 1.07 GB (a large copy: 5.2 TB/s).  Beside the
-// bytes it has about 22 vector instructions an element, 2 of them exponentials; so two workgroups share a compute unit, one in its arithmetic
-// while the other waits for memory.  That takes 64 registers a lane (one workgroup with 83: 333 us).
+// Measured, bf16, 8192 x 32768, K = 64, T = 2 with labels, loss and gradient: 270 us, 4.0 TB/s of the 1.07 GB (a large copy: 5.1 TB/s); the loss alone 133, the gradient from its
+// statistics 224; labels alone 87, 211 with the gradient, 207 from statistics.  Beside the bytes it has about 22 vector instructions an element, 2 of them exponentials; so two workgroups
+// share a compute unit, one in its arithmetic while the other waits for memory.  That takes 64 registers a lane (one workgroup with 83: an eighth more).
+// Rows that are read again, loss / with the gradient: fp32 1024 x 131072 159 / 332 us, bf16 2048 x 151936 186 / 363, 3.2 to 3.4 TB/s of z and dz once.
 
 // The K entries change few elements: the gradient is stored first as if there were none, then again at the entries, computed anew
 // rather than corrected, so that it is rounded once.  Entries that name one element twice each store the sum of all its p; the label, if no entry names it, is one more.
@@ -63,7 +64,7 @@ template <bool MAX> __device__ __forceinline__ float over_group(float x, float* 
 
 // MODE 1: the loss; 2: the gradient, from the statistics of an earlier call; 3: both.  TWO: the sums at T and at 1 are different ones and both
 // are wanted: for T = 2 and 4 the exponential at 1 is the square, or its square, of that at T (one or two products for an instruction of four times a product's
-// time), with 1 it is made.  C runs of 16 bytes a lane hold the row; C = 0: it is read again where it is needed.
+// time; 8192 x 32768 bf16 270 us, with both made, as for T = 1.5, 287), with 1 it is made.  C runs of 16 bytes a lane hold the row; C = 0: it is read again where it is needed.
 template <typename T, typename S, int MODE, int TWO, int C>
 __global__ __launch_bounds__(1024, C <= 4 ? 8 : 4) void distill_kernel(DistillArgs a) {
   constexpr int N = 16 / sizeof(T), HELD = C ? C : 1;
@@ -210,7 +211,9 @@ __global__ __launch_bounds__(1024, C <= 4 ? 8 : 4) void distill_kernel(DistillAr
       values(c, x);
 #pragma unroll
       for (int e = 0; e < N; ++e) x[e] = dense(x[e]);
-      if (V - j >= N) store_run_past(dz + j, x);  // (270 us of passes in a row, with stores that stay in the caches 278)
+      // (passes in a row 270 us, with stores that stay in the caches 279; with the two products that read dz behind it, bf16 rows of 32768: 8192 1080 and 1095 us, 2048 456 and 461, 1024,
+      // whose dz the last cache would hold, 251 and 233; in z's place, whose lines are there, 222 both)
+      if (V - j >= N) store_run_past(dz + j, x);
       else store_some<N>(dz + j, V - j, x);
     });
   } else {

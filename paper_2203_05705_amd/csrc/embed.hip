@@ -11,7 +11,7 @@
 // Summing: a row's team of lanes walks its tokens, kInFlight at a time.  Frequent tokens would leave one team behind: a row of more than
 // kLong tokens is summed in pieces of kPiece sorted positions each by a launch before, and its team adds the pieces up.
 //
-// Measured, passes in a row with the forward pass: 8192 tokens, bf16 rows of 1024, an fp32 table of 32768 66 us (launches of 7 + 7 + 15 + 40 us, 2.8 TB/s); 131072 tokens, a table of
+// Measured, passes in a row with the forward pass: 8192 tokens, bf16 rows of 1024, an fp32 table of 32768 69 us (launches of 7 + 7 + 15 + 40 us, 2.7 TB/s); 131072 tokens, a table of
 // 50000 added to 371 us (96 + 51 + 74 + 152).  Pieces of 128 and two loads of ids ahead took 179 and 489 us in the gradient's launches, these 62 and 277.
 // One generation step, 64 tokens: 2.6 us.
 #include "rows.hpp"
@@ -19,7 +19,9 @@
 namespace ard {
 
 constexpr int kSortWaves = 16;     // wavefronts of a sorting workgroup
-constexpr int kMaxSpan = 1024;     // ids that one may own: counts of span x wavefronts in LDS
+// workgroups that a table is shared out to, one a compute unit (131072 tokens, 50000 rows of 1024: the gradient's launches 241 us; 64 shares 257, 128 247, 512 254, 1024 286)
+constexpr int kShares = 256;
+constexpr int kMaxSpan = 1024;     // ids that one may own: counts of span x wavefronts in LDS, 64 KB
 constexpr int kPiece = 32;         // sorted positions whose sum is a piece of a long row
 constexpr int kLong = 32;          // tokens beyond which a row is summed in pieces (no fewer than kPiece: a piece meets two long rows at most)
 constexpr int kAhead = 8;          // loads of ids asked for together
@@ -191,7 +193,9 @@ __global__ __launch_bounds__(256) void embed_bwd_kernel(int V, int D, const int3
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[j] = ADD ? fmaf(scale, sum[j], old[j]) : s == e ? 0.0f : scale * sum[j];  // (+0.0 without a token, whatever the scale)
-      if (!ADD && D - c >= 8) store_run_past(dE + v * lde + c, sum);  // (32768 x 1024, 8192 tokens, passes in a row: 67 us, with stores that stay in the caches 107)
+      // (32768 x 1024, 8192 tokens, passes in a row 69 us, with stores that stay in the caches 107; with the AdamW step that reads the gradient behind it, passes of the gradient
+      // and the step: 50000 rows of 1024 349 and 353, 32768 237 and 239, 8192 61 and 59, 4096 of 512 22.4 and 24.2)
+      if (!ADD && D - c >= 8) store_run_past(dE + v * lde + c, sum);
       else store_some<8>(dE + v * lde + c, D - c, sum);
     }
   }
@@ -263,7 +267,7 @@ extern "C" int32_t ard_embed_bwd(int32_t dtype, int32_t wdtype, int32_t R, int32
   int32_t *start = (int32_t*)((char*)ws + sp.start), *sorted = (int32_t*)((char*)ws + sp.sorted);
   float* pieces = (float*)((char*)ws + sp.pieces);
   hipStream_t st = (hipStream_t)stream;
-  const int span = imin(kMaxSpan, imax(1, ceil_div(V, 256)));
+  const int span = imin(kMaxSpan, imax(1, ceil_div(V, kShares)));
   ARD_LAUNCH(embed_sort_kernel, dim3(ceil_div(V, span)), dim3(64 * kSortWaves), 0, st, R, V, span, d_ids, start, sorted);
   ARD_LAUNCH_CHECK("embed_sort_kernel");
   const Team t = team_of(D);

@@ -152,7 +152,7 @@ template <int N, int LD> __device__ __forceinline__ Parts<N> col_parts(const uin
 // A workgroup of four wavefronts makes the operands of a chunk and a key head, then of its heads, or a share of them, in turn; wavefront w has rows 16 w .. 16 w + 15.  Phases of few
 // instructions with barriers between them bound it, more than its stores do (2.5 TB/s), so three workgroups share a compute unit, which takes keys and
 // queries as stored (not as fp32) in LDS; the gates' sums are made where their wavefront has least else to do.  Measured, bf16, forward / backward: 4096 x 4 x 16 heads of
-// 64 x 64 77 / 88 us, 16384 x 1 x 8 of 128 x 128 66; two workgroups, diagonal blocks inverted by way of LDS: 91 / 102, 77.  Without its loads, its stores, the inverses or
+// 64 x 64 74 / 84 us, 16384 x 1 x 8 of 128 x 128 61; two workgroups, diagonal blocks inverted by way of LDS: 91 / 102, 77.  Without its loads, its stores, the inverses or
 // the products each it would take 0.75 to 0.95 of its time: no one of them.
 template <typename T, int DK, bool BWD> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 3 : 2) void gdr_prep_kernel(GdrArgs a, int splits) {
   constexpr int IN = kInput<T>, KB = DK / 32;
@@ -470,8 +470,8 @@ template <int IN, int DK> __device__ __forceinline__ void add_outer(const u32x4*
 // P lies there as values, which become parts where they are used: so the operands of heads of 128 take 80 KB, and two workgroups share a compute unit where nothing is kept
 // (bf16, 512 x 32 x 16 heads of 128 x 128: 262 us with the operands' launch, one workgroup, or P in parts, 300).
 // KEEP: the states before the chunks are stored, in ckpt.
-// A chunk is a chain of products that wait for each other: 3.8 us with one workgroup of a head on the chip, 5 with 256.  Measured, bf16: 8 x 1024 x 8 heads of 128 x 128 78 us;
-// 16384 x 1 x 8 of 128 x 128 in 16 segments 89 + 44 + 83, at once 965; 4096 x 4 x 16 of 64 x 64 in 4 segments 58 + 6 + 74, at once 216.
+// A chunk is a chain of products that wait for each other: 4.3 us with few workgroups on the chip, 5.2 with 128 that keep their states.  Measured, bf16: 8 x 1024 x 8 heads of
+// 128 x 128 83 us; 16384 x 1 x 8 of 128 x 128 in 16 segments 75 + 41 + 80, at once 1108; 4096 x 4 x 16 of 64 x 64 in 4 segments 53 + 6 + 77, at once 221.
 //
 // Few heads leave most of the chip idle, and their chunks follow one another.  So a long sequence is cut into segments.  A segment is linear in the
 // state before it: S' = F S + Z.  SUM walks all but the last segment at once, for Z (from a state of zeros) and F (DK more columns, from the
@@ -696,7 +696,7 @@ template <typename T, int DK, bool NEAR> __global__ __launch_bounds__(256) void 
   store_tiles(StateWindow(a.u + hu * kChunk * a.dvp, a.dvp, kChunk, a.dvp, at.first), u);
 }
 
-// SUM: as forward, of segments from the last on.  Measured, bf16: 8 x 1024 x 8 heads of 128 x 128 91 us; 4096 x 4 x 16 of 64 x 64 in 4 segments 88 + 6 + 82, at once 239.
+// SUM: as forward, of segments from the last on.  Measured, bf16: 8 x 1024 x 8 heads of 128 x 128 88 us; 4096 x 4 x 16 of 64 x 64 in 4 segments 82 + 6 + 79, at once 240.
 template <typename T, int DK, bool NEAR, int MODE>
 __global__ __launch_bounds__(256) void gdr_back_kernel(GdrArgs a, ard_steps d_o, const float* dST, ard_steps dv, float* dS0, int groups) {
   constexpr int IN = kInput<T>, KB = DK / 32, KF = 4 * KB * IN, KTF = DK / 8 * IN, MF = 6 * 3;
@@ -889,9 +889,9 @@ template <> struct Four<uint16_t> {
 // rows of Dk or half of them.  U, dX and dO go around through LDS, each tile the right hand operand of its own wavefronts and the left hand one of the others; S and dS' follow there in
 // pieces of 32 columns, a tile of rows from each wavefront, one stored while the one before it is multiplied.  Operands are read from LDS where they are used, for all of a wavefront's
 // rows at once: its registers hold sums, not operands (with those of its own steps in registers too, 256 were not enough, and what was spilled took most of the time).  They are parts, made
-// once; where LDS does not hold all of them so, dX, then U, then dO are values there (bf16, heads of 128 x 128: whole states and all three as values 246 us, so 190).
+// once; where LDS does not hold all of them so, dX, then U, then dO are values there (bf16, heads of 128 x 128: whole states and all three as values 240 us, so 184).
 // What later and earlier steps give is made apart, each before its own products, so that the operands of one are gone when the other's come.
-// Measured, bf16: 8 x 1024 x 8 heads of 128 x 128 190 us, 4096 x 4 x 16 of 64 x 64 with 8 key heads 234; matrix and vector instructions follow one another in
+// Measured, bf16: 8 x 1024 x 8 heads of 128 x 128 184 us, 4096 x 4 x 16 of 64 x 64 with 8 key heads 219; matrix and vector instructions follow one another in
 // the same phases, and one workgroup a compute unit (LDS, registers) cannot fill the waits between them.
 template <typename T, int DK, int DV, bool QUICK>
 __global__ __launch_bounds__(DK * 4) void gdr_grads_kernel(GdrArgs a, ard_steps d_o, const float* ckpt, ard_steps dq, ard_steps dk, ard_steps df, ard_steps db) {
@@ -1295,9 +1295,9 @@ static GdrPlan gdr_plan(int32_t dtype, int T, int B, int Hk, int H, int Dk, int 
   return p;
 }
 
-// Up to this many steps go one by one, as a chunk costs as much with few steps as with 64.  Measured, one by one against a chunk, 8 steps, us: bf16 16.1 and 17.6
-// (8 sequences x 8 heads of 64 x 64), 16.9 and 25.7 (32 x 16 of 64 x 64), 19.4 and 19.6 (1 x 8 of 128 x 128), 57 and 73 (128 x 8 of 128 x 128); 12 steps 22.4 and 17.6,
-// 22.9 and 25.7, 27.4 and 19.6, 76 and 74.  fp32 gains until 12 to 32.
+// Up to this many steps go one by one, as a chunk costs as much with few steps as with 64.  Measured, one by one against a chunk, 8 steps, us: bf16 16.1 and 18.2
+// (8 sequences x 8 heads of 64 x 64), 17.2 and 27.0 (32 x 16 of 64 x 64), 19.4 and 19.8 (1 x 8 of 128 x 128), 59 and 77 (128 x 8 of 128 x 128); 12 steps 22.5 and 18.2,
+// 23.1 and 27.3, 27.3 and 20.0, 77 and 77.  fp32 gains until 12 to 32.
 constexpr int kFewSteps = 8;
 
 static int32_t gdr_check(int32_t dtype, int32_t T, int32_t B, int32_t Hk, int32_t H, int32_t Dk, int32_t Dv) {
@@ -1325,8 +1325,8 @@ static int32_t gdr_numbers(float scale, float eps) {
 }
 
 // Workgroups of the operands of a chunk and a key head: more than one, each with a share of its heads, where one each would not fill the chip (keys' and
-// queries' products are made by each of them).  Measured, shared out against one each, forward / backward of 64 steps x 16 x 8 heads of 128 x 128, 2 key heads, bf16: 24 / 120 and
-// 42 / 139 us; 2048 x 1 x 32 of 64 x 64, 4 key heads: 68 / 159 and 101 / 195; 256 x 8 x 24 of 64 x 64, 12 key heads (384 workgroups): 37 / 93 and 40 / 99.
+// queries' products are made by each of them).  Measured, shared out against one each, forward / backward of 64 steps x 16 x 8 heads of 128 x 128, 2 key heads, bf16: 26 / 154 and
+// 45 / 172 us; 2048 x 1 x 32 of 64 x 64, 4 key heads: 72 / 169 and 104 / 204; 256 x 8 x 24 of 64 x 64, 12 key heads (384 workgroups): 41 / 99 and 43 / 105.
 static int prep_splits(const GdrArgs& a) {
   const int64_t units = (int64_t)a.chunks * a.B * a.Hk;
   return units * 2 <= 768 ? (int)std::min<int64_t>(a.group, 768 / units) : 1;

@@ -66,7 +66,7 @@ template <int N> __device__ __forceinline__ void store_run(uint16_t* p, const fl
     *reinterpret_cast<typename Run<uint16_t, N>::V*>(p) = v;
   }
 }
-// the same past the caches' order of use, for what nothing reads again soon
+// the same past the caches' order of use: for what is written once and does better so with what reads it next, as measured where it is used
 template <int N> __device__ __forceinline__ void store_run_past(float* p, const float (&x)[N]) {
   if constexpr (N == 1) {
     __builtin_nontemporal_store(x[0], p);
