@@ -539,7 +539,8 @@ int32_t ard_glr_bwd(int32_t dtype, int32_t T, int32_t B, int32_t H, const void* 
  * backward pass needs.  States, sums and gates are fp32, sums of log(a) fp64; results are rounded once.
  * Backward: d_o and dST (fp32, NULL: zeros) are the gradients of o and ST; grads[5] those of q, k, v, f, b (the heads that share a query or key
  * added up), every element written, +0.0 behind a sequence's end; dS0 (fp32, may be NULL) that of S0, which may be dST.
- * |q|^2 and |k|^2 are sums in fp32; eps is at least 2^-100.
+ * |q|^2 and |k|^2 are sums in fp32; eps is at least 2^-100.  Where many steps' keys are one direction (as all are of one element), fp32 results may be off by 3e-5 of
+ * their size, df by 3e-4; elsewhere by some 1e-6.
  * in, grads: five ard_steps on the host, in the order q, k, v, f, b.  Otherwise no output may overlap an input or another output.
  * Dk and Dv are at most ARD_GDR_MAX (else ARD_EUNSUPPORTED).
  */
